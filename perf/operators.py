@@ -1,7 +1,9 @@
-"""Calls of the attention sublayer's operators, in the sizes and layouts in which they occur.
+"""Calls of the token mixers that stand beside the scan, in the sizes and layouts in which they occur.
 
 The encoders that the scan belongs to keep some attention sublayers between the
-propagation ones.  Their operators, in the order in which a sublayer calls them:
+propagation ones, and the scan's counterpart over a sequence of tokens is a
+linear recurrence with a matrix state.  Their operators, in the order in which a
+sublayer calls them:
 
 * norm_fwd / norm_bwd: the RMS norm of every query and key head, with the position
   rotation in the same pass, and its gradient.  q and k are slices of one fused
@@ -11,6 +13,10 @@ propagation ones.  Their operators, in the order in which a sublayer calls them:
   lower bound hides.  v is still the projection's slice.
 * attn_train: the same and its gradient, one step of training.
 * decode: one token (or a few) at the end of each sequence against its cache.
+* delta_fwd: the gated delta rule, S_t = exp(g_t) (I - beta_t k_t k_t^T) S_{t-1} + beta_t k_t v_t^T
+  with o_t = S_t^T q_t / sqrt(Dk), from a state and to one (fp32 [B][H][Dk][Dv]);
+  one token a sequence is its serving form.
+* delta_train: the same and its gradient.
 
 `plain` forms are in 32 bits, rounded once at the end; `exact` is each operator's
 definition in 64 bits.
@@ -33,14 +39,8 @@ def listed():
         dict(name="norm_fwd-74x74", op="norm_fwd", B=32, T=5476, Hq=18, Hkv=18, D=64, R=64, pairs="half", dtype="bf16"),
         # the 64 x 64 training workload of 768 channels, batch 8
         dict(name="norm_bwd-64x64", op="norm_bwd", B=8, T=4096, Hq=12, Hkv=12, D=64, R=64, pairs="half", dtype="bf16"),
-        # 37 x 37 tokens in fp32, heads of 72 of which 48 are rotated, shared keys, adjacent pairs
-        dict(name="norm_bwd-37x37-f32", op="norm_bwd", B=3, T=1369, Hq=16, Hkv=4, D=72, R=48, pairs="adjacent", dtype="f32"),
-        # 14 x 14 tokens and 4 register tokens of 384 channels, batch 32: every token sees every token
-        dict(name="attn_fwd-14x14", op="attn_fwd", B=32, T=200, Hq=6, Hkv=6, D=64, left=-1, right=-1, sinks=0, ragged=False, dtype="bf16"),
         # 185 x 185 tokens behind 4 register tokens of 1152 channels: 6 image rows either side
         dict(name="attn_fwd-185x185", op="attn_fwd", B=1, T=34229, Hq=18, Hkv=18, D=64, left=1110, right=1110, sinks=4, ragged=False, dtype="bf16"),
-        # a ragged causal batch in fp32 with shared keys
-        dict(name="attn_fwd-ragged-f32", op="attn_fwd", B=4, T=1001, Hq=8, Hkv=2, D=80, left=255, right=0, sinks=5, ragged=True, dtype="f32"),
         # the 64 x 64 training workload behind 4 register tokens: 7 image rows either side
         dict(name="attn_train-64x64", op="attn_train", B=8, T=4100, Hq=12, Hkv=12, D=64, left=448, right=448, sinks=4, ragged=False, dtype="bf16"),
         # causal training on long sequences, four query heads to a key head, ragged lengths
@@ -51,6 +51,12 @@ def listed():
         dict(name="decode-one", op="decode", B=1, T=1, Tk=32768, Hq=16, Hkv=4, D=128, left=4095, sinks=4, ragged=True, dtype="bf16"),
         # one token each of 64 sequences, the whole of ragged caches of up to 8192
         dict(name="decode-64", op="decode", B=64, T=1, Tk=8192, Hq=16, Hkv=4, D=128, left=-1, sinks=0, ragged=True, dtype="bf16"),
+        # the 64 x 64 training workload as a sequence, 12 heads of 64
+        dict(name="delta_train-64x64", op="delta_train", B=8, T=4096, Hq=12, Hv=12, D=64, Dv=64, ragged=False, dtype="bf16"),
+        # long ragged sequences continued from a state, four value heads to a key head
+        dict(name="delta_fwd-8191", op="delta_fwd", B=2, T=8191, Hq=4, Hv=16, D=128, Dv=128, ragged=True, dtype="bf16"),
+        # one token each of 64 sequences
+        dict(name="delta_fwd-token", op="delta_fwd", B=64, T=1, Hq=4, Hv=16, D=128, Dv=128, ragged=False, dtype="bf16"),
     ]
 
 
@@ -61,7 +67,7 @@ def _log(rng, lo, hi):
 
 def draw(rng):
     top = max(_cost(c) for c in listed())
-    op = rng.choice(["norm_fwd", "norm_bwd", "attn_fwd", "attn_fwd", "attn_train", "attn_train", "decode", "decode"])
+    op = rng.choice(["norm_fwd", "norm_bwd", "attn_fwd", "attn_fwd", "attn_train", "attn_train", "decode", "decode", "delta_fwd", "delta_fwd", "delta_train"])
     while True:
         dtype = rng.choice(["bf16", "bf16", "bf16", "f32"])
         Hkv = rng.choice([1, 2, 3, 4, 6, 8, 12, 16, 18])
@@ -75,10 +81,16 @@ def draw(rng):
         elif op == "decode":
             c.update(T=rng.choice([1, 1, 1, 2, 5]), Tk=_log(rng, 16, 65536), sinks=rng.choice([0, 1, 4, 16]), ragged=True)
             c.update(left=rng.choice([-1, _log(rng, 16, 8192)]))
+        elif op.startswith("delta"):
+            c.update(B=_log(rng, 1, 16), T=min(c["T"], 8192), Hq=Hkv, Hv=Hq, D=rng.choice([32, 64, 96, 128]), Dv=rng.choice([32, 64, 96, 128]))
+            c.update(T=1 if op == "delta_fwd" and rng.random() < 0.4 else c["T"], ragged=rng.choice([False, True]))
+            c.pop("Hkv")
         else:
             c.update(left=rng.choice([-1, _log(rng, 16, 2048), _log(rng, 16, 2048)]), right=rng.choice([0, 0, -1, _log(rng, 16, 2048)]))
             c.update(sinks=rng.choice([0, 1, 4, 16]), ragged=rng.choice([False, True]))
-        if dtype == "f32" and not op.startswith("norm") and _cost(c) > top / 16:
+        if dtype == "f32" and op.startswith("attn") and _cost(c) > top / 16:
+            continue
+        if op.startswith("delta") and c["B"] * c["T"] * c["Hv"] * c["D"] * c["Dv"] > 8 * 4096 * 12 * 64 * 64:
             continue
         if op.startswith("attn") and 4 * c["B"] * Hq * c["T"] * _span(c) > 12e9:   # what the plain form's scores take
             continue
@@ -121,7 +133,14 @@ def _visible(c):
 
 def work(case):
     c, s = case, 2 if case["dtype"] == "bf16" else 4
-    B, T, Hq, Hkv, D = c["B"], c["T"], c["Hq"], c["Hkv"], c["D"]
+    B, T, Hq, D = c["B"], c["T"], c["Hq"], c["D"]
+    if c["op"].startswith("delta"):
+        Hv, Dv = c["Hv"], c["Dv"]
+        state, tokens = 8 * B * Hv * D * Dv, B * T * (2 * Hq * D + 2 * Hv * Dv + 2 * Hv) * s
+        if c["op"] == "delta_fwd":
+            return {"bytes": state + tokens, "flops": 6 * B * T * Hv * D * Dv}
+        return {"bytes": 2 * state + 2 * tokens, "flops": 18 * B * T * Hv * D * Dv}
+    Hkv = c["Hkv"]
     if c["op"].startswith("norm"):
         n = B * T * (Hq + Hkv) * D
         table = T * c["R"] * 4 + 2 * D * s
@@ -155,7 +174,7 @@ def _table(T, R):
 
 def prepare(case, seed):
     c, dt = case, _dtype(case)
-    B, T, Hq, Hkv, D = c["B"], c["T"], c["Hq"], c["Hkv"], c["D"]
+    B, T, Hq, D = c["B"], c["T"], c["Hq"], c["D"]
     g = torch.Generator(device=DEV)
     g.manual_seed(seed)
 
@@ -165,6 +184,19 @@ def prepare(case, seed):
     st = {"case": c}
     lens = _lens(c)
     st["lens"] = torch.tensor(lens, dtype=torch.int32, device=DEV) if lens else None
+    if c["op"].startswith("delta"):
+        Hv, Dv = c["Hv"], c["Dv"]
+        unit = torch.nn.functional.normalize
+        st.update(q=unit(rand(B, T, Hq, D).float(), dim=-1).to(dt), k=unit(rand(B, T, Hq, D).float(), dim=-1).to(dt), v=rand(B, T, Hv, Dv))
+        # decays whose memory is some ten to a thousand tokens, and how much of a value is written
+        st["g"] = (-torch.exp(rand(B, T, Hv).float() - 4)).to(dt)
+        st["beta"] = torch.sigmoid(rand(B, T, Hv).float()).to(dt)
+        st["state"] = 0.1 * torch.randn(B, Hv, D, Dv, device=DEV, generator=g)
+        if c["op"] == "delta_train":
+            st["do"] = rand(B, T, Hv, Dv)
+            st["dstate"] = 0.1 * torch.randn(B, Hv, D, Dv, device=DEV, generator=g)
+        return st
+    Hkv = c["Hkv"]
     if c["op"] == "decode":
         st.update(q=rand(B, T, Hq, D), k=rand(B, c["Tk"], Hkv, D), v=rand(B, c["Tk"], Hkv, D))
         return st
@@ -199,6 +231,12 @@ def _run_own(c, s):
         return gspn.qk_norm_rotate_bwd(s["q"], s["k"], s["wq"], s["wk"], s["dyq"], s["dyk"], s["cos"], s["sin"], eps=EPS, pairs=c["pairs"])
     if c["op"] == "decode":
         return gspn.window_attn_decode(s["q"], s["k"], s["v"], s["lens"], left=c["left"], sinks=c["sinks"])
+    if c["op"] == "delta_fwd":
+        return gspn.delta_rule_fwd(s["q"], s["k"], s["v"], s["g"], s["beta"], state=s["state"], lens=s["lens"])
+    if c["op"] == "delta_train":
+        x = (s["q"], s["k"], s["v"], s["g"], s["beta"])
+        o, end, reserve = gspn.delta_rule_fwd_train(*x, state=s["state"], lens=s["lens"])
+        return (o, end, *gspn.delta_rule_bwd_reserve(*x, s["do"], reserve, dstate=s["dstate"], state=s["state"], lens=s["lens"]))
     mask = dict(left=c["left"], right=c["right"], sinks=c["sinks"], lens=s["lens"])
     o, lse = gspn.window_attn_fwd(s["q"], s["k"], s["v"], **mask)
     if c["op"] == "attn_fwd":
@@ -214,6 +252,13 @@ def _run_plain(c, s):
         return dq, dk, dwq, dwk
     if c["op"] == "decode":
         return _decode(c, s)
+    if c["op"] == "delta_fwd":
+        return _delta(c, s, *(s[x].float() for x in ("q", "k", "v", "g", "beta", "state")))
+    if c["op"] == "delta_train":
+        x = [s[n].float().requires_grad_() for n in ("q", "k", "v", "g", "beta", "state")]
+        o, end = _delta(c, s, *x)
+        grads = torch.autograd.grad((o, end), x, (s["do"], s["dstate"]))
+        return (o.detach(), end.detach(), *(d.to(s[n].dtype) for d, n in zip(grads, ("q", "k", "v", "g", "beta", "state"))))
     return _attn(c, s)
 
 
@@ -335,6 +380,50 @@ def _decode(c, s):
     return o.view(B, Hkv, Hq // Hkv, T, D).permute(0, 3, 1, 2, 4).reshape(B, T, Hq, D).to(s["q"].dtype)
 
 
+def _delta(c, s, q, k, v, g, beta, state):
+    """The chunked form: within a chunk of n tokens U = (I + L)^-1 beta (V - exp(G) K S), L strictly lower
+    triangular, and the state S once a chunk; (I + L)^-1 as a product of (I + (-L)^(2^i))."""
+    B, T, Hv, Dv = v.shape
+    D, rep = c["D"], Hv // c["Hq"]
+    n = min(64, T)
+    nc = -(-T // n)
+    live = None
+    if s["lens"] is not None:   # tokens past a sequence's end write nothing and decay nothing
+        live = (torch.arange(T, device=DEV) < s["lens"][:, None])[:, :, None]
+        g, beta = g * live, beta * live
+
+    def chunks(x):   # [B][T][H]... as [B][H][nc][n]...
+        x = torch.nn.functional.pad(x, (0, 0) * (x.dim() - 2) + (0, nc * n - T)).unflatten(1, (nc, n))
+        return x.movedim(3, 1)
+
+    q, k = (chunks(x).repeat_interleave(rep, 1) for x in (q, k))
+    v, g, beta = chunks(v), chunks(g), chunks(beta)
+    G = g.cumsum(-1)
+    lower = torch.ones(n, n, device=DEV, dtype=torch.bool).tril()
+    decay = torch.exp((G[..., :, None] - G[..., None, :]).masked_fill(~lower, -math.inf))
+    m = -(k @ k.transpose(-1, -2)) * decay * beta[..., None]
+    m = m.tril(-1)
+    inv = torch.eye(n, device=DEV) + m
+    for _ in range(max(0, (n - 1).bit_length() - 1)):
+        m = m @ m
+        inv = inv + inv @ m
+    u0 = inv @ (beta[..., None] * v)
+    w = inv @ ((beta * G.exp())[..., None] * k)
+    a = (q @ k.transpose(-1, -2)) * decay / math.sqrt(D)
+    qd = q * (G.exp() / math.sqrt(D))[..., None]
+    kd = (k * (G[..., -1:] - G).exp()[..., None]).transpose(-1, -2)
+    end = G[..., -1].exp()
+    out = []
+    for i in range(nc):
+        u = u0[:, :, i] - w[:, :, i] @ state
+        out.append(qd[:, :, i] @ state + a[:, :, i] @ u)
+        state = end[:, :, i, None, None] * state + kd[:, :, i] @ u
+    o = torch.stack(out, 2).flatten(2, 3)[:, :, :T].transpose(1, 2)
+    if live is not None:
+        o = o * live[..., None]
+    return o.to(s["v"].dtype), state
+
+
 # ---------------------------------------------------------------------------
 # the definitions in 64 bits
 # ---------------------------------------------------------------------------
@@ -346,7 +435,57 @@ def exact(case, seed):
     if c["op"] == "norm_bwd":
         a, b = _exact_norm(c, s, "q"), _exact_norm(c, s, "k")
         return a[1], b[1], a[2], b[2]
+    if c["op"].startswith("delta"):
+        return _exact_delta(c, s)
     return _exact_attn(c, s)
+
+
+def _exact_delta(c, s):
+    """Token by token, and for the gradient back again over the states that were kept."""
+    B, T, Hv, Dv = s["v"].shape
+    D, rep, train = c["D"], Hv // c["Hq"], c["op"] == "delta_train"
+    if train and 8 * B * Hv * D * Dv * T > 60e9:
+        return None
+    q, k = (s[x].double().repeat_interleave(rep, 2) for x in "qk")
+    v, g, beta, S = (s[x].double() for x in ("v", "g", "beta", "state"))
+    live = torch.ones(B, T, device=DEV, dtype=torch.float64)
+    if s["lens"] is not None:
+        live = (torch.arange(T, device=DEV) < s["lens"][:, None]).double()
+    a = torch.exp(g * live[..., None])
+    beta = beta * live[..., None]
+    q = q * live[..., None, None] / math.sqrt(D)
+    o = torch.zeros(B, T, Hv, Dv, device=DEV, dtype=torch.float64)
+    kept = []
+    for t in range(T):
+        kept.append(S) if train else None
+        S = a[:, t, :, None, None] * S
+        u = beta[:, t, :, None] * (v[:, t] - (S * k[:, t, :, :, None]).sum(2))
+        S = S + k[:, t, :, :, None] * u[:, :, None]
+        o[:, t] = (S * q[:, t, :, :, None]).sum(2)
+    if not train:
+        return o, S
+    end, dS, do = S, s["dstate"].double(), s["do"].double()
+    dq, dk, dv, dg, db = (torch.zeros_like(x) for x in (q, k, v, g, beta))
+    for t in reversed(range(T)):
+        kt = k[:, t, :, :, None]
+        before = a[:, t, :, None, None] * kept[t]
+        z = v[:, t] - (before * kt).sum(2)
+        u = beta[:, t, :, None] * z
+        S = before + kt * u[:, :, None]
+        dq[:, t] = (S * do[:, t, :, None]).sum(-1)
+        dS = dS + q[:, t, :, :, None] * do[:, t, :, None]
+        du = (dS * kt).sum(2)
+        dk[:, t] = (dS * u[:, :, None]).sum(-1)
+        db[:, t] = (du * z).sum(-1)
+        dz = beta[:, t, :, None] * du
+        dv[:, t] = dz
+        dk[:, t] -= (before * dz[:, :, None]).sum(-1)
+        dS = dS - kt * dz[:, :, None]
+        dg[:, t] = (dS * before).sum((-1, -2))
+        dS = a[:, t, :, None, None] * dS
+    dq = dq * live[..., None, None] / math.sqrt(D)
+    dq, dk = (x.unflatten(2, (c["Hq"], rep)).sum(3) for x in (dq, dk))
+    return o, end, dq, dk, dv, dg * live[..., None], db * live[..., None], dS
 
 
 def _exact_norm(c, s, which):
