@@ -379,6 +379,101 @@ int gspn_latent_params(const void *xc, const void *l_u, const void *l_lam,
                        const void *l_w, void *u, void *lam, void *w,
                        int direction, int B, int Cc, int H, int W, int dtype,
                        void *stream);
+
+/*
+ * Token mixers beside the scan.  The encoders that the scan belongs to keep
+ * some attention sublayers; these are the operators of such a sublayer.
+ *
+ * Layouts.  A "heads" tensor is [B][T][H][D] with D contiguous; `strides`, a
+ * host array of three int64 per heads tensor in argument order (batch, token
+ * and head strides in elements; NULL: all contiguous), lets it be a slice of a
+ * fused projection or of a cache.  Strides of dimensions of size 1 are not
+ * read.  Heads tensors have one storage type (fp32 or bf16), base pointers and
+ * strides that are multiples of 16 bytes, and D a multiple of 8
+ * (GSPN_ERR_ALIGN, GSPN_ERR_UNSUPPORTED).  int32 and fp32 arrays (lens, lse,
+ * positions) are contiguous and need their own alignment only.  Outputs may be
+ * slices of one buffer's tokens (dq, dk and dv of one fused gradient); they
+ * must not overlap anything otherwise (GSPN_ERR_ALIAS).  Arithmetic is fp32;
+ * with bf16 storage the operands of matrix products are bf16 (softmax weights
+ * and their gradients are rounded to nearest even for the products that take
+ * them, their sums are not).  The rest is as for the scan: asynchronous on
+ * `stream`, no allocation, results that repeat bit for bit.
+ *
+ * Norm of query and key heads with the position rotation:
+ *   n = x / sqrt(mean(x^2) + eps),  z = w n,  y = z with its first R entries
+ *   turned in pairs (a, b) -> (a cos - b sin, a sin + b cos)
+ * q, yq [B][T][Hq][D]; k, yk [B][T][Hk][D]; wq, wk [D] in the storage type, or
+ * NULL for ones; cos_t, sin_t fp32 [table_rows][R/2]; a token's row is
+ * positions[b][t] (int32, limited to the table) or, without positions,
+ * first + t, which must lie in the table.  pairs: GSPN_PAIRS_HALF turns entry
+ * i with R/2 + i, GSPN_PAIRS_ADJACENT 2i with 2i + 1.  R even, 0 to D (0: no
+ * rotation; the tables may be NULL).  D up to 256.  yq may be q and yk k, with
+ * the same strides.
+ * The backward takes q and k as the forward did and the gradients of yq, yk;
+ * it writes dq, dk and, for each weight given, dwq or dwk [D].
+ * strides: forward q, k, yq, yk; backward q, k, dyq, dyk, dq, dk.
+ */
+#define GSPN_PAIRS_HALF 0
+#define GSPN_PAIRS_ADJACENT 1
+int gspn_qk_norm_rotate_fwd(const void *q, const void *k, const void *wq, const void *wk,
+                            const float *cos_t, const float *sin_t, const int32_t *positions,
+                            void *yq, void *yk, const int64_t *strides, int B, int T, int Hq,
+                            int Hk, int D, int R, int table_rows, int first, int pairs,
+                            float eps, int dtype, void *stream);
+int gspn_qk_norm_rotate_workspace_size(int B, int T, int Hq, int Hk, int D, int R, int pairs,
+                                       int dtype, int64_t *bytes);
+int gspn_qk_norm_rotate_bwd(const void *q, const void *k, const void *wq, const void *wk,
+                            const float *cos_t, const float *sin_t, const int32_t *positions,
+                            const void *dyq, const void *dyk, void *dq, void *dk, void *dwq,
+                            void *dwk, const int64_t *strides, int B, int T, int Hq, int Hk,
+                            int D, int R, int table_rows, int first, int pairs, float eps,
+                            int dtype, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Attention with a sliding window and sinks.  Query t of sequence b stands at
+ * position p = t + offset among the keys and sees key j when
+ *   j < len and p < len                   len = lens[b] (limited to 0..Tk), or Tk without lens
+ *   j <= p + right                        (right < 0: no such bound)
+ *   j >= p - left  or  j < sinks          (left < 0: no such bound)
+ * right = 0 is causal; the first `sinks` tokens are hidden by no lower bound.
+ *   o = sum_j softmax_j(scale q k_j) v_j,  lse = log sum_j exp(scale q k_j)
+ * A query that sees no key has o = 0, lse = -infinity and no part in any
+ * gradient.  Keys, values and queries at and past len may hold anything, NaN
+ * included; those before it must be finite.
+ * q, o [B][Tq][Hq][D]; k, v [B][Tk][Hkv][D], Hq a multiple of Hkv: query head h
+ * reads key head h / (Hq / Hkv); D up to 128; lse fp32 [B][Hq][Tq] (NULL: not
+ * wanted, forward only); scale > 0.
+ * gspn_window_attn_bwd takes the forward's inputs, o and lse, and the gradient
+ * dout of o.  gspn_window_attn_decode is the form for the last Tq tokens of
+ * each sequence over a cache of Tk: p = len - Tq + t, causal, no lse; its time
+ * goes by the keys seen.  A cache that holds only the sinks and the window (in
+ * any order) is read with left = -1, all its tokens being visible.
+ * strides: forward and decode q, k, v, o; backward q, k, v, o, dout, dq, dk, dv.
+ * gspn_window_attn_workspace_size: op one of GSPN_ATTN_*; right and offset are
+ * not read for GSPN_ATTN_DECODE.
+ */
+#define GSPN_ATTN_FWD 0
+#define GSPN_ATTN_BWD 1
+#define GSPN_ATTN_DECODE 2
+int gspn_window_attn_workspace_size(int op, int B, int Tq, int Tk, int Hq, int Hkv, int D,
+                                    int left, int right, int sinks, int offset, int dtype,
+                                    int64_t *bytes);
+int gspn_window_attn_fwd(const void *q, const void *k, const void *v, const int32_t *lens,
+                         void *o, float *lse, const int64_t *strides, int B, int Tq, int Tk,
+                         int Hq, int Hkv, int D, int left, int right, int sinks, int offset,
+                         float scale, int dtype, void *workspace, int64_t workspace_bytes,
+                         void *stream);
+int gspn_window_attn_bwd(const void *q, const void *k, const void *v, const void *o,
+                         const float *lse, const void *dout, const int32_t *lens, void *dq,
+                         void *dk, void *dv, const int64_t *strides, int B, int Tq, int Tk,
+                         int Hq, int Hkv, int D, int left, int right, int sinks, int offset,
+                         float scale, int dtype, void *workspace, int64_t workspace_bytes,
+                         void *stream);
+int gspn_window_attn_decode(const void *q, const void *k, const void *v, const int32_t *lens,
+                            void *o, const int64_t *strides, int B, int Tq, int Tk, int Hq,
+                            int Hkv, int D, int left, int sinks, float scale, int dtype,
+                            void *workspace, int64_t workspace_bytes, void *stream);
+
 /* Static description of a status code (never NULL). */
 const char *gspn_strerror(int status);
 

@@ -1,0 +1,245 @@
+"""Torch front end of the token mixers beside the scan (argument marshalling only).
+
+The norm of query and key heads with the position rotation
+(``qk_norm_rotate_*``) and windowed attention (``window_attn_*``), see
+``include/gspn.h`` for the formulas.  Tensors are [B, T, H, D] with D
+contiguous and any other strides (slices of a fused projection or of a cache);
+every call runs on the current stream of its tensors' device unless one is
+given, and takes the workspace it needs from torch unless it is handed one.
+"""
+from __future__ import annotations
+
+import ctypes
+import functools
+import math
+
+from ._native import (_check_raise, _current_device, _dtype_code, _stream_handle, load)
+
+PAIRS = {"half": 0, "adjacent": 1}
+ATTN_FWD, ATTN_BWD, ATTN_DECODE = 0, 1, 2
+
+
+def _heads(named):
+    """Every tensor of `named` ({name: (tensor, shape)}) is on one GPU, of one
+    dtype, of its shape and contiguous in its last dimension."""
+    first = None
+    for name, (t, shape) in named.items():
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
+        if not t.is_cuda:
+            raise ValueError("tensors must be on a GPU")
+        if t.stride(-1) != 1 and t.shape[-1] > 1:
+            raise ValueError(f"{name} must be contiguous in its last dimension")
+        if first is None:
+            first = t
+        elif t.dtype != first.dtype:
+            raise ValueError(f"{name} must have dtype {first.dtype}, not {t.dtype}")
+        elif t.get_device() != first.get_device():
+            raise ValueError(f"{name} must be on {first.device}")
+
+
+def _strides(*tensors):
+    """Batch, token and head strides of every tensor, in order."""
+    out = []
+    for t in tensors:
+        out += t.stride()[:3]
+    return (ctypes.c_int64 * len(out))(*out)
+
+
+def _plain(name, t, shape, dtype, like):
+    """An optional contiguous tensor's pointer (None: none)."""
+    if t is None:
+        return None
+    if (tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous()
+            or t.get_device() != like.get_device()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {like.device}")
+    return t.data_ptr()
+
+
+def _take(nbytes, given, device):
+    """The buffer a call works in: `given` where it is large enough, else a new one."""
+    if nbytes == 0:
+        return None, 0
+    import torch
+    if given is not None:
+        if given.device != device or given.dtype != torch.uint8 or not given.is_contiguous():
+            raise ValueError("workspace must be a contiguous uint8 tensor on the inputs' device")
+        if given.numel() >= nbytes:
+            return given.data_ptr(), given.numel()
+    buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return buf.data_ptr(), nbytes
+
+
+@functools.lru_cache(maxsize=256)
+def _sized(name, args, device):
+    """A size query's answer, asked once per sizes and current device."""
+    n = ctypes.c_int64(0)
+    _check_raise(getattr(load(), name)(*args, ctypes.byref(n)))
+    return n.value
+
+
+# ---------------------------------------------------------------------------
+# norm of query and key heads, with the position rotation
+# ---------------------------------------------------------------------------
+
+def _norm_sizes(q, k, wq, wk, cos, sin, positions, pairs):
+    import torch
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q and k must be [B, T, H, D]")
+    if pairs not in PAIRS:
+        raise ValueError(f"pairs must be one of {list(PAIRS)}")
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin go together")
+    B, T, Hq, D = q.shape
+    Hk = k.shape[2]
+    rows, half = (0, 0) if cos is None else (cos.shape[0], cos.shape[-1])
+    ptrs = (_plain("wq", wq, (D,), q.dtype, q), _plain("wk", wk, (D,), q.dtype, q),
+            _plain("cos", cos, (rows, half), torch.float32, q),
+            _plain("sin", sin, (rows, half), torch.float32, q),
+            _plain("positions", positions, (B, T), torch.int32, q))
+    return B, T, Hq, Hk, D, 2 * half, rows, ptrs
+
+
+def qk_norm_rotate_fwd(q, k, wq=None, wk=None, cos=None, sin=None, eps: float = 1e-6,
+                       positions=None, first: int = 0, pairs: str = "half", out=None,
+                       stream=None):
+    """(yq, yk): every head of q [B, T, Hq, D] and k [B, T, Hk, D] divided by
+    its root mean square, times wq or wk [D] (None: ones), its first
+    2 * cos.shape[1] entries turned by the angles of its token's row of cos and
+    sin (fp32 [rows, R / 2]; None: no rotation): row positions[b, t] (int32), or
+    first + t.  pairs: "half" turns entry i with R / 2 + i, "adjacent" 2i with
+    2i + 1.  `out`: (yq, yk), which may be (q, k)."""
+    import torch
+    B, T, Hq, Hk, D, R, rows, ptrs = _norm_sizes(q, k, wq, wk, cos, sin, positions, pairs)
+    if out is None:
+        out = (torch.empty((B, T, Hq, D), dtype=q.dtype, device=q.device),
+               torch.empty((B, T, Hk, D), dtype=q.dtype, device=q.device))
+    yq, yk = out
+    _heads({"q": (q, (B, T, Hq, D)), "k": (k, (B, T, Hk, D)), "yq": (yq, (B, T, Hq, D)),
+            "yk": (yk, (B, T, Hk, D))})
+    _check_raise(load().gspn_qk_norm_rotate_fwd(
+        q.data_ptr(), k.data_ptr(), *ptrs, yq.data_ptr(), yk.data_ptr(),
+        _strides(q, k, yq, yk), B, T, Hq, Hk, D, R, rows, first, PAIRS[pairs], eps,
+        _dtype_code(q), _stream_handle(q, stream)))
+    return yq, yk
+
+
+def qk_norm_rotate_bwd(q, k, wq, wk, dyq, dyk, cos=None, sin=None, eps: float = 1e-6,
+                       positions=None, first: int = 0, pairs: str = "half", out=None,
+                       stream=None, workspace=None):
+    """(dq, dk, dwq, dwk) of qk_norm_rotate_fwd's q, k and weights, from the
+    gradients dyq, dyk of its outputs (dwq, dwk None where the weight is)."""
+    import torch
+    B, T, Hq, Hk, D, R, rows, ptrs = _norm_sizes(q, k, wq, wk, cos, sin, positions, pairs)
+    if out is None:
+        kw = dict(dtype=q.dtype, device=q.device)
+        out = (torch.empty((B, T, Hq, D), **kw), torch.empty((B, T, Hk, D), **kw),
+               None if wq is None else torch.empty(D, **kw),
+               None if wk is None else torch.empty(D, **kw))
+    dq, dk, dwq, dwk = out
+    _heads({"q": (q, (B, T, Hq, D)), "k": (k, (B, T, Hk, D)), "dyq": (dyq, (B, T, Hq, D)),
+            "dyk": (dyk, (B, T, Hk, D)), "dq": (dq, (B, T, Hq, D)), "dk": (dk, (B, T, Hk, D))})
+    dt = _dtype_code(q)
+    n = _sized("gspn_qk_norm_rotate_workspace_size", (B, T, Hq, Hk, D, R, PAIRS[pairs], dt),
+               _current_device())
+    ws, nbytes = _take(n, workspace, q.device)
+    _check_raise(load().gspn_qk_norm_rotate_bwd(
+        q.data_ptr(), k.data_ptr(), *ptrs, dyq.data_ptr(), dyk.data_ptr(), dq.data_ptr(),
+        dk.data_ptr(), _plain("dwq", dwq, (D,), q.dtype, q), _plain("dwk", dwk, (D,), q.dtype, q),
+        _strides(q, k, dyq, dyk, dq, dk), B, T, Hq, Hk, D, R, rows, first, PAIRS[pairs], eps, dt,
+        ws, nbytes, _stream_handle(q, stream)))
+    return out
+
+
+# ---------------------------------------------------------------------------
+# attention with a sliding window and sinks
+# ---------------------------------------------------------------------------
+
+def _attn_sizes(q, k, v, lens):
+    import torch
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q, k and v must be [B, T, H, D]")
+    B, Tq, Hq, D = q.shape
+    Tk, Hkv = k.shape[1], k.shape[2]
+    return B, Tq, Tk, Hq, Hkv, D, _plain("lens", lens, (B,), torch.int32, q)
+
+
+def _attn_workspace(op, sizes, left, right, sinks, offset, dt, given, device):
+    n = _sized("gspn_window_attn_workspace_size",
+               (op, *sizes, left, right, sinks, offset, dt), _current_device())
+    return _take(n, given, device)
+
+
+def window_attn_fwd(q, k, v, left: int = -1, right: int = -1, sinks: int = 0, lens=None,
+                    offset: int = 0, scale=None, o=None, lse=None, stream=None, workspace=None):
+    """(o, lse): attention of q [B, Tq, Hq, D] over k, v [B, Tk, Hkv, D], where
+    the query at position p = t + offset sees the keys p - left .. p + right
+    (-1: no bound) and, up to p + right, the first `sinks` tokens; lens (int32
+    [B]): the sequences' lengths, past which nothing is seen and sees nothing.
+    scale: 1 / sqrt(D) unless given.  lse: fp32 [B, Hq, Tq], for the backward."""
+    import torch
+    B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens)
+    if o is None:
+        o = torch.empty((B, Tq, Hq, D), dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty((B, Hq, Tq), dtype=torch.float32, device=q.device)
+    _heads({"q": (q, (B, Tq, Hq, D)), "k": (k, (B, Tk, Hkv, D)), "v": (v, (B, Tk, Hkv, D)),
+            "o": (o, (B, Tq, Hq, D))})
+    dt = _dtype_code(q)
+    ws, nbytes = _attn_workspace(ATTN_FWD, (B, Tq, Tk, Hq, Hkv, D), left, right, sinks, offset, dt,
+                                 workspace, q.device)
+    _check_raise(load().gspn_window_attn_fwd(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), lens_p, o.data_ptr(),
+        _plain("lse", lse, (B, Hq, Tq), torch.float32, q), _strides(q, k, v, o), B, Tq, Tk, Hq,
+        Hkv, D, left, right, sinks, offset, 1 / math.sqrt(D) if scale is None else scale, dt, ws,
+        nbytes, _stream_handle(q, stream)))
+    return o, lse
+
+
+def window_attn_bwd(q, k, v, o, lse, do, left: int = -1, right: int = -1, sinks: int = 0,
+                    lens=None, offset: int = 0, scale=None, out=None, stream=None,
+                    workspace=None):
+    """(dq, dk, dv) from the gradient `do` of window_attn_fwd's o; o and lse are
+    the forward's, the other arguments those it was called with."""
+    import torch
+    B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens)
+    if out is None:
+        kw = dict(dtype=q.dtype, device=q.device)
+        out = (torch.empty((B, Tq, Hq, D), **kw), torch.empty((B, Tk, Hkv, D), **kw),
+               torch.empty((B, Tk, Hkv, D), **kw))
+    dq, dk, dv = out
+    qs, ks = (B, Tq, Hq, D), (B, Tk, Hkv, D)
+    _heads({"q": (q, qs), "k": (k, ks), "v": (v, ks), "o": (o, qs), "do": (do, qs), "dq": (dq, qs),
+            "dk": (dk, ks), "dv": (dv, ks)})
+    dt = _dtype_code(q)
+    ws, nbytes = _attn_workspace(ATTN_BWD, (B, Tq, Tk, Hq, Hkv, D), left, right, sinks, offset, dt,
+                                 workspace, q.device)
+    _check_raise(load().gspn_window_attn_bwd(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+        _plain("lse", lse, (B, Hq, Tq), torch.float32, q), do.data_ptr(), lens_p, dq.data_ptr(),
+        dk.data_ptr(), dv.data_ptr(), _strides(q, k, v, o, do, dq, dk, dv), B, Tq, Tk, Hq, Hkv, D,
+        left, right, sinks, offset, 1 / math.sqrt(D) if scale is None else scale, dt, ws, nbytes,
+        _stream_handle(q, stream)))
+    return dq, dk, dv
+
+
+def window_attn_decode(q, k, v, lens=None, left: int = -1, sinks: int = 0, scale=None, o=None,
+                       stream=None, workspace=None):
+    """o for the last Tq tokens of each sequence, q [B, Tq, Hq, D], over a cache
+    k, v [B, Tk, Hkv, D] of which lens[b] tokens (None: all) are there, the
+    queries' own among them: query t stands at position lens[b] - Tq + t and
+    sees the `left` keys before it (-1: all), itself and the first `sinks`."""
+    import torch
+    B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens)
+    if o is None:
+        o = torch.empty((B, Tq, Hq, D), dtype=q.dtype, device=q.device)
+    _heads({"q": (q, (B, Tq, Hq, D)), "k": (k, (B, Tk, Hkv, D)), "v": (v, (B, Tk, Hkv, D)),
+            "o": (o, (B, Tq, Hq, D))})
+    dt = _dtype_code(q)
+    ws, nbytes = _attn_workspace(ATTN_DECODE, (B, Tq, Tk, Hq, Hkv, D), left, 0, sinks, 0, dt,
+                                 workspace, q.device)
+    _check_raise(load().gspn_window_attn_decode(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), lens_p, o.data_ptr(), _strides(q, k, v, o), B,
+        Tq, Tk, Hq, Hkv, D, left, sinks, 1 / math.sqrt(D) if scale is None else scale, dt, ws,
+        nbytes, _stream_handle(q, stream)))
+    return o

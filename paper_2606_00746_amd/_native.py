@@ -35,6 +35,9 @@ EXPORTED = ("gspn_workspace_size", "gspn_scan_fwd", "gspn_scan_bwd", "gspn_scan_
             "gspn_reserve_size_norm", "gspn_scan_fwd_norm_train", "gspn_scan_bwd_norm_reserve",
             "gspn_project",
             "gspn_latent_params", "gspn_latent_workspace_size", "gspn_latent_fwd",
+            "gspn_qk_norm_rotate_fwd", "gspn_qk_norm_rotate_workspace_size",
+            "gspn_qk_norm_rotate_bwd", "gspn_window_attn_workspace_size", "gspn_window_attn_fwd",
+            "gspn_window_attn_bwd", "gspn_window_attn_decode",
             "gspn_strerror", "gspn_last_hip_error", "gspn_version")
 
 _lib = None
@@ -81,6 +84,14 @@ def load() -> ctypes.CDLL:
         lib.gspn_latent_params.argtypes = [vp] * 7 + [i] * 6 + [vp]
         lib.gspn_latent_workspace_size.argtypes = [i] * 7 + [pi64]
         lib.gspn_latent_fwd.argtypes = [vp] * 7 + [i] * 7 + ws
+        f = ctypes.c_float
+        lib.gspn_qk_norm_rotate_fwd.argtypes = [vp] * 10 + [i] * 9 + [f, i, vp]
+        lib.gspn_qk_norm_rotate_workspace_size.argtypes = [i] * 8 + [pi64]
+        lib.gspn_qk_norm_rotate_bwd.argtypes = [vp] * 14 + [i] * 9 + [f, i] + ws
+        lib.gspn_window_attn_workspace_size.argtypes = [i] * 12 + [pi64]
+        lib.gspn_window_attn_fwd.argtypes = [vp] * 7 + [i] * 10 + [f, i] + ws
+        lib.gspn_window_attn_bwd.argtypes = [vp] * 11 + [i] * 10 + [f, i] + ws
+        lib.gspn_window_attn_decode.argtypes = [vp] * 6 + [i] * 8 + [f, i] + ws
         for name in EXPORTED:
             getattr(lib, name).restype = i
         lib.gspn_strerror.argtypes = [i]

@@ -65,6 +65,8 @@ int check_buffers(const Buf *bufs, int n)
     return GSPN_OK;
 }
 
+}  // namespace
+
 int hip_status(hipError_t e)
 {
     if (e == hipSuccess)
@@ -72,10 +74,6 @@ int hip_status(hipError_t e)
     g_last_hip_error = (int)e;
     return GSPN_ERR_HIP;
 }
-
-}  // namespace
-
-
 
 }  // namespace gspn
 

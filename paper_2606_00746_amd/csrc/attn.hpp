@@ -1,0 +1,336 @@
+// Attention with a sliding window and sinks: the problem, and the tiles and
+// matrix-core fragments that its kernels share (internal).
+//
+// Every product runs on 32 x 32 (decode: 16 x 16) matrix instructions in the
+// orientation that leaves a softmax row in one lane: the scores are formed
+// transposed, S^T = K Q^T, so that lane l of a wave holds query l % 32 and, in
+// the registers r = 0..15 of a 32-key block, the keys 8 (r / 4) + 4 (l / 32) +
+// r % 4.  The second product, O^T = V^T P^T, takes P^T as its B operand
+// straight from those registers: a contraction may run over the keys in any
+// order that both operands share, so V^T is read in the order that P^T has.
+// bf16: V's tile lies in LDS as rows of keys, and ds_read_b64_tr_b16 turns four
+// rows of 16 columns around on the way out.  fp32: one ds_read_b32 a step.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "cdna.hpp"
+#include "device.hpp"
+#include "launch.hpp"
+
+namespace gspn {
+
+// A [B][T][H][D] tensor: base and strides of b, t, h in elements; D is contiguous.
+struct Heads {
+    void *p = nullptr;
+    int64_t sb = 0, st = 0, sh = 0;
+};
+
+struct AttnProblem {
+    Heads q, k, v, o, dout, dq, dk, dv;
+    float *lse;              // [B][Hq][Tq]
+    const int32_t *lens;     // [B], or null: Tk
+    int B, Tq, Tk, Hq, Hkv, D;
+    int left, right;         // < 0: no bound
+    int sinks, offset;       // query t stands at position t + offset
+    bool tail;               // query t stands at lens[b] - Tq + t instead
+    float scale;
+    int dtype;
+    Workspace *ws;
+};
+
+hipError_t launch_attn_fwd(const AttnProblem &p, hipStream_t s);
+hipError_t launch_attn_bwd(const AttnProblem &p, hipStream_t s);
+hipError_t launch_attn_split(const AttnProblem &p, hipStream_t s);
+bool attn_split_preferred(const AttnProblem &p);
+
+constexpr int kAttnMaxHead = 128;
+
+#ifdef __HIPCC__
+
+namespace attn {
+
+using namespace cdna;
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kRows = 64;        // rows of a staged tile
+constexpr int kThreads = 256;    // 4 waves
+
+// v of this lane's row in both halves of the wave.
+__device__ __forceinline__ float half_max(float v)
+{
+    const uint32_t b = __float_as_uint(v);
+    const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float v)
+{
+    const uint32_t b = __float_as_uint(v);
+    const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// 16-byte pieces of a tile of DP columns in LDS.  Rows are S pieces apart, a
+// power of two, and piece c of row r lies at c ^ swizzle(r): 16 consecutive
+// rows of one piece (a row-wise fragment) and 4 consecutive rows of four
+// adjacent pieces (a turned-around one) then fall in different banks, both
+// measured at the rate of linear addresses.
+template <typename T, int DP>
+struct Tile {
+    static constexpr int kPer = 16 / (int)sizeof(T);     // elements of a piece
+    static constexpr int kPieces = DP / kPer;
+    static constexpr int kS = kPieces <= 4 ? 4 : kPieces <= 8 ? 8 : kPieces <= 16 ? 16 : 32;
+    static constexpr int kBytes = kRows * kS * 16;
+    static constexpr int kLoads = kRows * kPieces / kThreads;
+    static_assert(kRows * kPieces % kThreads == 0, "a tile is whole pieces per thread");
+
+    __device__ static __forceinline__ int swizzle(int r)
+    {
+        if (kS == 4)
+            return (r >> 2) & 3;
+        if (kS == 8)
+            return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
+        return (r & 3) << 2 | ((r >> 2) & 3);
+    }
+    __device__ static __forceinline__ int at(int r, int c) { return (r * kS + (c ^ swizzle(r))) * 16; }
+
+    uint4 reg[kLoads];
+
+    // Rows row0 .. row0 + 63 of a tensor with row stride st into registers;
+    // rows from `rows` on and columns from D on read as zero.
+    __device__ __forceinline__ void load(const T *base, int64_t st, int row0, int rows, int D)
+    {
+        const T *p = base + (int64_t)row0 * st;
+        const int n = rows - row0;
+        if (n >= kRows && D == DP) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int x = threadIdx.x + i * kThreads, r = x / kPieces, c = x % kPieces;
+                reg[i] = *reinterpret_cast<const uint4 *>(p + r * st + c * kPer);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int x = threadIdx.x + i * kThreads, r = x / kPieces, c = x % kPieces;
+                reg[i] = make_uint4(0, 0, 0, 0);
+                if (r < n && c * kPer < D)
+                    reg[i] = *reinterpret_cast<const uint4 *>(p + r * st + c * kPer);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(char *lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int x = threadIdx.x + i * kThreads, r = x / kPieces, c = x % kPieces;
+            *reinterpret_cast<uint4 *>(lds + at(r, c)) = reg[i];
+        }
+    }
+};
+
+// A row-wise fragment: 16 bytes of a row, the columns 2 s + l / 32 pieces in.
+template <typename T>
+struct Frag;
+template <>
+struct Frag<bf16_t> {
+    bf16x8_t v;
+};
+template <>
+struct Frag<float> {
+    f32x4_t v;
+};
+
+template <typename T, int DP>
+__device__ __forceinline__ Frag<T> tile_frag(const char *lds, int row, int piece)
+{
+    return *reinterpret_cast<const Frag<T> *>(lds + Tile<T, DP>::at(row, piece));
+}
+
+// The same from global memory (columns from D on as zero).
+template <typename T>
+__device__ __forceinline__ Frag<T> row_frag(const T *row, int piece, int D)
+{
+    constexpr int kPer = 16 / (int)sizeof(T);
+    Frag<T> f;
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (piece * kPer < D)
+        u = *reinterpret_cast<const uint4 *>(row + piece * kPer);
+    f.v = __builtin_bit_cast(decltype(f.v), u);
+    return f;
+}
+
+// acc += A B^T over the columns of one pair of pieces (bf16: 16, fp32: 8).
+__device__ __forceinline__ f32x16_t mma(Frag<bf16_t> a, Frag<bf16_t> b, f32x16_t acc)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16_t mma(Frag<float> a, Frag<float> b, f32x16_t acc)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], acc, 0, 0, 0);
+    return acc;
+}
+
+// The B operand of the second product, from the 16 registers of a 32 x 32
+// block: bf16 rounds to nearest even (the products that follow take 8
+// significant bits; sums of the unrounded values stay in fp32), fp32 takes
+// them as they are.
+template <typename T>
+struct Probs;
+template <>
+struct Probs<bf16_t> {
+    bf16x8_t v[2];
+    __device__ __forceinline__ explicit Probs(const f32x16_t &p)
+    {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint4 u = make_uint4(pack2(p[8 * t], p[8 * t + 1]), pack2(p[8 * t + 2], p[8 * t + 3]),
+                                       pack2(p[8 * t + 4], p[8 * t + 5]), pack2(p[8 * t + 6], p[8 * t + 7]));
+            v[t] = __builtin_bit_cast(bf16x8_t, u);
+        }
+    }
+};
+template <>
+struct Probs<float> {
+    f32x16_t v;
+    __device__ __forceinline__ explicit Probs(const f32x16_t &p) : v(p) {}
+};
+
+__device__ __forceinline__ s16x4_t read_turned(const char *lds)
+{
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s16x4_t *)(lds));
+}
+
+// acc[db] += X^T P over the 32 rows row0.. of the tile X (columns 32 db ..).
+template <int DP>
+__device__ __forceinline__ void mma_turned(const char *lds, int row0, const Probs<bf16_t> &p,
+                                           f32x16_t (&acc)[DP / 32])
+{
+    using X = Tile<bf16_t, DP>;
+    const int l = threadIdx.x % 64, h = l / 32, i = l % 16, r = 4 * h + (i >> 2);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db) {
+            const int c = 4 * db + 2 * (l % 32 / 16) + ((i & 3) >> 1), in = 8 * (i & 1);
+            const s16x4_t a0 = read_turned(lds + X::at(row0 + 16 * t + r, c) + in);
+            const s16x4_t a1 = read_turned(lds + X::at(row0 + 16 * t + 8 + r, c) + in);
+            struct {
+                s16x4_t a, b;
+            } both = {a0, a1};
+            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, both),
+                                                              p.v[t], acc[db], 0, 0, 0);
+        }
+}
+template <int DP>
+__device__ __forceinline__ void mma_turned(const char *lds, int row0, const Probs<float> &p,
+                                           f32x16_t (&acc)[DP / 32])
+{
+    using X = Tile<float, DP>;
+    const int l = threadIdx.x % 64, h = l / 32, d = l % 32;
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db) {
+            const float a = *reinterpret_cast<const float *>(
+                lds + X::at(row0 + 8 * (r / 4) + 4 * h + r % 4, 8 * db + d / 4) + 4 * (d % 4));
+            acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p.v[r], acc[db], 0, 0, 0);
+        }
+}
+
+// Stores a column (4 consecutive rows of a 32 x 32 result a register quad:
+// entries d .. d + 3 of one token) scaled by f.
+__device__ __forceinline__ void store4(bf16_t *p, float a, float b, float c, float d)
+{
+    const u32x2 v = {pack2(a, b), pack2(c, d)};
+    *reinterpret_cast<u32x2 *>(p) = v;
+}
+__device__ __forceinline__ void store4(float *p, float a, float b, float c, float d)
+{
+    const u32x4 v = {__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)};
+    *reinterpret_cast<u32x4 *>(p) = v;
+    // a wide store reads its registers after issue: they stay as they are past it
+    asm volatile("s_nop 7\n\ts_nop 7" : : "v"(v) : "memory");
+}
+template <typename T, int DP>
+__device__ __forceinline__ void store_column(T *row, const f32x16_t (&acc)[DP / 32], float f, int D)
+{
+    const int h = threadIdx.x % 64 / 32;
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = 32 * db + 8 * g + 4 * h;
+            if (d < D)
+                store4(row + d, acc[db][4 * g] * f, acc[db][4 * g + 1] * f, acc[db][4 * g + 2] * f,
+                       acc[db][4 * g + 3] * f);
+        }
+}
+
+__device__ __forceinline__ int seq_len(const AttnProblem &p, int b)
+{
+    return p.lens ? min(max(p.lens[b], 0), p.Tk) : p.Tk;
+}
+
+// The keys that the query at position p sees: j <= hi, and j >= lo or j < sinks.
+__device__ __forceinline__ void key_bounds(const AttnProblem &a, int len, int p, int &lo, int &hi)
+{
+    hi = p < 0 || p >= len ? -1 : a.right < 0 ? len - 1 : min(len - 1, p + a.right);
+    lo = a.left < 0 ? 0 : max(0, p - a.left);
+}
+
+// The tiles of kRows keys that the queries t0 .. t0 + nt - 1 see: those that
+// hold sinks ahead of the window, then the window's.
+struct KeyTiles {
+    int ns, first, n;
+    __device__ __forceinline__ KeyTiles(const AttnProblem &a, int len, int t0, int nt)
+    {
+        const int p0 = t0 + a.offset, p1 = p0 + nt - 1;
+        const int hi = p0 >= len ? -1 : a.right < 0 ? len - 1 : min(len - 1, p1 + a.right);
+        const int lo = a.left < 0 ? 0 : max(0, p0 - a.left);
+        ns = (min(a.sinks, lo) + kRows - 1) / kRows;
+        first = max(ns, lo / kRows);
+        n = hi < 0 ? 0 : ns + max(0, hi / kRows + 1 - first);
+    }
+    __device__ __forceinline__ int row(int it) const
+    {
+        return (it < ns ? it : first + it - ns) * kRows;
+    }
+};
+
+// Whether some, or all, of the queries t0 .. t0 + nt - 1 see keys of the tile
+// at k0 (all: every key of it).
+struct KeyRange {
+    int lo_some, hi_some, lo_all, hi_all, sinks;
+    __device__ __forceinline__ KeyRange(const AttnProblem &a, int len, int t0, int nt)
+    {
+        const int p0 = t0 + a.offset, p1 = p0 + nt - 1;
+        hi_some = p0 >= len ? -1 : a.right < 0 ? len - 1 : min(len - 1, p1 + a.right);
+        hi_all = p1 >= len ? -1 : a.right < 0 ? len - 1 : min(len - 1, p0 + a.right);
+        lo_some = a.left < 0 ? 0 : p0 - a.left;
+        lo_all = a.left < 0 ? 0 : p1 - a.left;
+        sinks = a.sinks;
+    }
+    __device__ __forceinline__ bool some(int k0) const
+    {
+        return k0 <= hi_some && (k0 + kRows > lo_some || k0 < sinks);
+    }
+    __device__ __forceinline__ bool all(int k0) const
+    {
+        return k0 + kRows - 1 <= hi_all && (k0 >= lo_all || k0 + kRows <= sinks);
+    }
+};
+
+}  // namespace attn
+
+#endif
+
+}  // namespace gspn

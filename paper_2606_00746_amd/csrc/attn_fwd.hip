@@ -1,0 +1,213 @@
+// Forward of windowed attention (gspn_window_attn_fwd).
+//
+//   o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i k_j - lse_i),
+//   lse_i = log sum_j exp(scale q_i k_j)     over the keys j that query i sees
+//
+// One pass over the keys with a running maximum and sum.  A workgroup owns
+// 4 x 32 QB queries of one head, a wave 32 QB of them; tiles of 64 keys and
+// values are staged in LDS for all four waves, double buffered: the loads of
+// the next tile are in flight, in registers, while one is multiplied.  The
+// tiles are those of the sinks, then those of the window; a wave passes over
+// tiles that none of its queries sees and masks only those that not all see.
+#include <algorithm>
+
+#include "attn.hpp"
+
+namespace gspn {
+namespace {
+
+using namespace attn;
+
+// How far (in powers of two) a row's scores may exceed the maximum that its
+// sums are kept against before they are scaled to a new one: the exponentials
+// stay below 2^8, their bf16 roundings are relative, and few tiles rescale.
+constexpr float kSlack = 8.f;
+
+template <typename T, int DP, int QB>
+__global__ __launch_bounds__(kThreads, (DP * sizeof(T) * QB <= 256 ? 2 : 1))
+void attn_fwd_kernel(AttnProblem a)
+{
+    using X = Tile<T, DP>;
+    constexpr int kSlices = X::kPieces / 2, kTQ = 4 * 32 * QB;
+    __shared__ __attribute__((aligned(16))) char lds[2][2][X::kBytes];
+
+    const int G = a.Hq / a.Hkv, nqt = (a.Tq + kTQ - 1) / kTQ;
+    int id = xcd_remap(blockIdx.x, gridDim.x);
+    const int g = id % G;
+    id /= G;
+    const int qt = id % nqt;
+    id /= nqt;
+    const int hk = id % a.Hkv, b = id / a.Hkv, hq = hk * G + g;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x % 64;
+    const int c = l % 32, h = l / 32;
+    const int len = seq_len(a, b);
+
+    const T *qp = static_cast<const T *>(a.q.p) + b * a.q.sb + hq * a.q.sh;
+    const T *kp = static_cast<const T *>(a.k.p) + b * a.k.sb + hk * a.k.sh;
+    const T *vp = static_cast<const T *>(a.v.p) + b * a.v.sb + hk * a.v.sh;
+
+    const int t0 = qt * kTQ, tw = t0 + w * 32 * QB;
+    const KeyTiles wg(a, len, t0, min(kTQ, a.Tq - t0));
+    const KeyRange wave(a, len, tw, 32 * QB);
+
+    Frag<T> qf[QB][kSlices];
+    int lo[QB], hi[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const int t = tw + 32 * qb + c;
+        const T *row = qp + (int64_t)min(t, a.Tq - 1) * a.q.st;
+#pragma unroll
+        for (int s = 0; s < kSlices; ++s)
+            qf[qb][s] = row_frag(row, 2 * s + h, a.D);
+        key_bounds(a, len, t + a.offset, lo[qb], hi[qb]);
+    }
+
+    f32x16_t acc[QB][DP / 32];
+    float m[QB], sum[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        m[qb] = -__builtin_inff();
+        sum[qb] = 0.f;
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                acc[qb][db][r] = 0.f;
+    }
+    const float s2 = a.scale * kLog2e, slack = kSlack / s2;
+
+    X kt, vt;
+    const int n = wg.n;
+    if (n > 0) {
+        kt.load(kp, a.k.st, wg.row(0), len, a.D);
+        vt.load(vp, a.v.st, wg.row(0), len, a.D);
+        kt.store(lds[0][0]);
+        vt.store(lds[0][1]);
+    }
+    lds_barrier();
+
+    for (int it = 0; it < n; ++it) {
+        const int k0 = wg.row(it);
+        const char *kl = lds[it & 1][0], *vl = lds[it & 1][1];
+        if (it + 1 < n) {
+            kt.load(kp, a.k.st, wg.row(it + 1), len, a.D);
+            vt.load(vp, a.v.st, wg.row(it + 1), len, a.D);
+        }
+        if (wave.some(k0)) {
+            const bool all = wave.all(k0);
+            f32x16_t s[QB][2];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        s[qb][kb][r] = 0.f;
+#pragma unroll
+                for (int sl = 0; sl < kSlices; ++sl) {
+                    const Frag<T> kf = tile_frag<T, DP>(kl, 32 * kb + c, 2 * sl + h);
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb)
+                        s[qb][kb] = mma(kf, qf[qb][sl], s[qb][kb]);
+                }
+            }
+            if (!all) {
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int j = k0 + 32 * kb + 8 * (r / 4) + 4 * h + r % 4;
+                            const bool see = j <= hi[qb] && (j >= lo[qb] || j < a.sinks);
+                            s[qb][kb][r] = see ? s[qb][kb][r] : -__builtin_inff();
+                        }
+            }
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+                float mx = -__builtin_inff();
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        mx = fmaxf(mx, s[qb][kb][r]);
+                mx = half_max(mx);
+                if (__any(mx > m[qb] + slack)) {
+                    const float mn = fmaxf(m[qb], mx);
+                    const float f = m[qb] == -__builtin_inff()
+                                        ? 0.f
+                                        : __builtin_amdgcn_exp2f((m[qb] - mn) * s2);
+                    m[qb] = mn;
+                    sum[qb] *= f;
+#pragma unroll
+                    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            acc[qb][db][r] *= f;
+                }
+                const float base = m[qb] == -__builtin_inff() ? 0.f : m[qb] * s2;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    float part = 0.f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        s[qb][kb][r] = __builtin_amdgcn_exp2f(fmaf(s[qb][kb][r], s2, -base));
+                        part += s[qb][kb][r];
+                    }
+                    sum[qb] += part;
+                    mma_turned<DP>(vl, 32 * kb, Probs<T>(s[qb][kb]), acc[qb]);
+                }
+            }
+        }
+        if (it + 1 < n) {
+            kt.store(lds[(it + 1) & 1][0]);
+            vt.store(lds[(it + 1) & 1][1]);
+        }
+        lds_barrier();
+    }
+
+    T *op = static_cast<T *>(a.o.p) + b * a.o.sb + hq * a.o.sh;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const int t = tw + 32 * qb + c;
+        const float z = half_sum(sum[qb]);
+        if (t < a.Tq) {
+            store_column<T, DP>(op + t * a.o.st, acc[qb], z > 0.f ? 1.f / z : 0.f, a.D);
+            if (a.lse && h == 0)
+                a.lse[((int64_t)b * a.Hq + hq) * a.Tq + t] =
+                    z > 0.f ? fmaf(m[qb], s2, __builtin_amdgcn_logf(z)) * kLn2 : -__builtin_inff();
+        }
+    }
+}
+
+template <typename T, int DP, int QB>
+hipError_t run(const AttnProblem &p, hipStream_t s)
+{
+    const int64_t tiles = (p.Tq + 128 * QB - 1) / (128 * QB), blocks = tiles * p.B * p.Hq;
+    if (blocks * kThreads > kMaxThreads)
+        return hipErrorInvalidConfiguration;
+    if (p.ws->counting)
+        return hipSuccess;
+    attn_fwd_kernel<T, DP, QB><<<dim3((unsigned)blocks), kThreads, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run(const AttnProblem &p, hipStream_t s)
+{
+    return p.D <= 32   ? run<T, 32, 1>(p, s)
+           : p.D <= 64 ? run<T, 64, 1>(p, s)
+           : p.D <= 96 ? run<T, 96, 1>(p, s)
+                       : run<T, 128, 1>(p, s);
+}
+
+}  // namespace
+
+hipError_t launch_attn_fwd(const AttnProblem &p, hipStream_t s)
+{
+    if (attn_split_preferred(p))
+        return launch_attn_split(p, s);
+    return p.dtype == 0 ? run<float>(p, s) : run<bf16_t>(p, s);
+}
+
+}  // namespace gspn

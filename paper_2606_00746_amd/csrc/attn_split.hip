@@ -1,0 +1,387 @@
+// Windowed attention of few queries a sequence (gspn_window_attn_decode, and
+// forwards of few queries): the keys split over waves and workgroups.
+//
+// What counts is one pass over the keys and values that the queries see.  The
+// G query heads that share a key head, times the Tq queries, are the rows of
+// one problem, 16 of them a workgroup, so that shared keys are read once.  A
+// wave takes blocks of 32 keys in turn: K straight into registers as the A
+// operand of S^T = K Q^T (16 x 16 matrix instructions, lane l: key l % 16, 16
+// bytes of it), V through a piece of LDS of the wave's own, where it is turned
+// around for O^T = V^T P^T.  The next block's loads are in flight meanwhile.
+// Each wave keeps its running maximum, sum and output; the workgroup's four are
+// joined in LDS, and those of several workgroups by attn_join_kernel, in order.
+#include <algorithm>
+
+#include "attn.hpp"
+
+namespace gspn {
+namespace {
+
+using namespace attn;
+
+constexpr int kCol = 16;     // query rows of a workgroup
+constexpr int kBlock = 32;   // keys of a block
+
+// v over the four lanes l % 16 + 16 u of a row.
+__device__ __forceinline__ float quad_max(float v)
+{
+    v = half_max(v);
+    const uint32_t b = __float_as_uint(v);
+    const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float quad_sum(float v)
+{
+    v = half_sum(v);
+    const uint32_t b = __float_as_uint(v);
+    const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ f32x4_t mma16(Frag<bf16_t> a, Frag<bf16_t> b, f32x4_t acc)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4_t mma16(Frag<float> a, Frag<float> b, f32x4_t acc)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e], b.v[e], acc, 0, 0, 0);
+    return acc;
+}
+
+// acc[db] += V^T P over the wave's block of 32 keys; p[t]: keys 16 t + 4 u + 0..3.
+template <int DP>
+__device__ __forceinline__ void mma16_turned(const char *lds, const f32x4_t (&p)[2],
+                                             f32x4_t (&acc)[DP / 16], const bf16_t *)
+{
+    using X = Tile<bf16_t, DP>;
+    const int l = threadIdx.x % 64, u = l / 16, i = l % 16, r = 4 * u + (i >> 2);
+    const uint4 w = make_uint4(pack2(p[0][0], p[0][1]), pack2(p[0][2], p[0][3]),
+                               pack2(p[1][0], p[1][1]), pack2(p[1][2], p[1][3]));
+    const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, w);
+#pragma unroll
+    for (int db = 0; db < DP / 16; ++db) {
+        const int c = 2 * db + ((i & 3) >> 1), in = 8 * (i & 1);
+        struct {
+            s16x4_t a, b;
+        } both = {read_turned(lds + X::at(r, c) + in), read_turned(lds + X::at(16 + r, c) + in)};
+        acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, both), pb,
+                                                          acc[db], 0, 0, 0);
+    }
+}
+template <int DP>
+__device__ __forceinline__ void mma16_turned(const char *lds, const f32x4_t (&p)[2],
+                                             f32x4_t (&acc)[DP / 16], const float *)
+{
+    using X = Tile<float, DP>;
+    const int l = threadIdx.x % 64, u = l / 16, d = l % 16;
+#pragma unroll
+    for (int db = 0; db < DP / 16; ++db)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const float a = *reinterpret_cast<const float *>(
+                lds + X::at(16 * (r / 4) + 4 * u + r % 4, 4 * db + d / 4) + 4 * (d % 4));
+            acc[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p[r / 4][r % 4], acc[db], 0, 0, 0);
+        }
+}
+
+// One block's K and V in registers: pieces past the last key or column are zero.
+template <typename T, int DP>
+struct Block {
+    using X = Tile<T, DP>;
+    static constexpr int kSlices = X::kPieces / 4, kLoads = kBlock * X::kPieces / 64;
+    Frag<T> k[2][kSlices];
+    uint4 v[kLoads];
+    __device__ __forceinline__ void load(const T *kp, int64_t ks, const T *vp, int64_t vs, int j0, int end,
+                                         int D)
+    {
+        const int l = threadIdx.x % 64;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int j = j0 + 16 * t + l % 16;
+#pragma unroll
+            for (int s = 0; s < kSlices; ++s) {
+                k[t][s].v = decltype(k[t][s].v){};
+                if (j < end)
+                    k[t][s] = row_frag(kp + j * ks, 4 * s + l / 16, D);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int x = l + 64 * i, r = x / X::kPieces, c = x % X::kPieces;
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (j0 + r < end && c * X::kPer < D)
+                v[i] = *reinterpret_cast<const uint4 *>(vp + (j0 + r) * vs + c * X::kPer);
+        }
+    }
+    __device__ __forceinline__ void store_v(char *lds) const
+    {
+        const int l = threadIdx.x % 64;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int x = l + 64 * i;
+            *reinterpret_cast<uint4 *>(lds + X::at(x / X::kPieces, x % X::kPieces)) = v[i];
+        }
+    }
+};
+
+// Each workgroup's share of a row: its maximum, its sum and the output over its keys.
+struct Shares {
+    float *out;      // [tile][split][16][DP]
+    float *stat;     // [tile][split][16][2]
+    int splits;
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(kThreads, 1) void attn_split_kernel(AttnProblem a, Shares sh)
+{
+    using X = Tile<T, DP>;
+    constexpr int kSlices = X::kPieces / 4, kPitch = DP + 4;
+    constexpr int kV = kBlock * X::kS * 16, kO = kCol * kPitch * 4, kWave = kV > kO ? kV : kO;
+    __shared__ __attribute__((aligned(16))) char lds[4][kWave];
+    __shared__ float stats[4][kCol][2];
+
+    const int G = a.Hq / a.Hkv, rows = a.Tq * G, nt = (rows + kCol - 1) / kCol;
+    int id = blockIdx.x;
+    const int split = id % sh.splits;
+    id /= sh.splits;
+    const int tile = id, rt = id % nt;
+    id /= nt;
+    const int hk = id % a.Hkv, b = id / a.Hkv;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x % 64;
+    const int c = l % 16, u = l / 16;
+    const int len = seq_len(a, b), off = a.tail ? len - a.Tq : a.offset;
+
+    // the keys that the tile's rows see, in blocks: the sinks ahead of the window, then the window
+    const int ta = rt * kCol / G, tb = min(rows - 1, rt * kCol + kCol - 1) / G;
+    int lo_t, hi_t, lo_b, hi_b;
+    key_bounds(a, len, max(0, ta + off), lo_t, hi_t);
+    key_bounds(a, len, tb + off, lo_b, hi_b);
+    const int top = min(len - 1, a.right < 0 ? len - 1 : tb + off + a.right);
+    const bool none = tb + off < 0 || max(0, ta + off) >= len;
+    const int sunk = min(min(a.sinks, lo_t), top + 1), ns = (sunk + kBlock - 1) / kBlock;
+    const int n = none ? 0 : ns + (top < lo_t ? 0 : (top - lo_t) / kBlock + 1);
+    const int i0 = (int)((int64_t)n * split / sh.splits), i1 = (int)((int64_t)n * (split + 1) / sh.splits);
+    const auto key_of = [&](int i) { return i < ns ? i * kBlock : lo_t + (i - ns) * kBlock; };
+    const auto end_of = [&](int i) { return i < ns ? sunk : top + 1; };
+
+    const int row = rt * kCol + c, t = min(row, rows - 1) / G, hq = hk * G + min(row, rows - 1) % G;
+    int lo, hi;
+    key_bounds(a, len, t + off, lo, hi);
+    const T *qr = static_cast<const T *>(a.q.p) + b * a.q.sb + t * a.q.st + hq * a.q.sh;
+    const T *kp = static_cast<const T *>(a.k.p) + b * a.k.sb + hk * a.k.sh;
+    const T *vp = static_cast<const T *>(a.v.p) + b * a.v.sb + hk * a.v.sh;
+    Frag<T> qf[kSlices];
+#pragma unroll
+    for (int s = 0; s < kSlices; ++s)
+        qf[s] = row_frag(qr, 4 * s + u, a.D);
+
+    f32x4_t acc[DP / 16];
+#pragma unroll
+    for (int db = 0; db < DP / 16; ++db)
+        acc[db] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m = -__builtin_inff(), sum = 0.f;
+    const float s2 = a.scale * kLog2e;
+
+    Block<T, DP> x;
+    if (i0 + w < i1)
+        x.load(kp, a.k.st, vp, a.v.st, key_of(i0 + w), end_of(i0 + w), a.D);
+    for (int i = i0 + w; i < i1; i += 4) {
+        const int k0 = key_of(i), end = end_of(i);
+        f32x4_t s[2];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            s[kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int sl = 0; sl < kSlices; ++sl)
+                s[kt] = mma16(x.k[kt][sl], qf[sl], s[kt]);
+        }
+        x.store_v(lds[w]);
+        __builtin_amdgcn_wave_barrier();
+        if (i + 4 < i1)
+            x.load(kp, a.k.st, vp, a.v.st, key_of(i + 4), end_of(i + 4), a.D);
+        float mx = -__builtin_inff();
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = k0 + 16 * kt + 4 * u + e;
+                const bool see = j < end && j <= hi && (j >= lo || j < a.sinks);
+                s[kt][e] = see ? s[kt][e] : -__builtin_inff();
+                mx = fmaxf(mx, s[kt][e]);
+            }
+        mx = quad_max(mx);
+        if (__any(mx > m)) {
+            const float mn = fmaxf(m, mx);
+            const float f = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m - mn) * s2);
+            m = mn;
+            sum *= f;
+#pragma unroll
+            for (int db = 0; db < DP / 16; ++db)
+                acc[db] *= f;
+        }
+        const float base = m == -__builtin_inff() ? 0.f : m * s2;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[kt][e] = __builtin_amdgcn_exp2f(fmaf(s[kt][e], s2, -base));
+                sum += s[kt][e];
+            }
+        mma16_turned<DP>(lds[w], s, acc, static_cast<const T *>(nullptr));
+        __builtin_amdgcn_wave_barrier();
+    }
+    sum = quad_sum(sum);
+
+    // the four waves' shares, joined
+    lds_barrier();
+    float *mine = reinterpret_cast<float *>(lds[w]);
+#pragma unroll
+    for (int db = 0; db < DP / 16; ++db)
+        *reinterpret_cast<f32x4_t *>(mine + c * kPitch + 16 * db + 4 * u) = acc[db];
+    if (u == 0) {
+        stats[w][c][0] = m * s2;
+        stats[w][c][1] = sum;
+    }
+    lds_barrier();
+    for (int x4 = threadIdx.x; x4 < kCol * (DP / 4); x4 += kThreads) {
+        const int r = x4 / (DP / 4), d = x4 % (DP / 4) * 4;
+        float top2 = -__builtin_inff();
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            top2 = fmaxf(top2, stats[v][r][0]);
+        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+        float z = 0.f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const float mv = stats[v][r][0];
+            const float f = mv == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(mv - top2);
+            z = fmaf(f, stats[v][r][1], z);
+            o += f * *reinterpret_cast<const f32x4_t *>(reinterpret_cast<const float *>(lds[v]) + r * kPitch + d);
+        }
+        if (sh.splits > 1) {
+            const int64_t at = ((int64_t)tile * sh.splits + split) * kCol + r;
+            store4(sh.out + at * DP + d, o[0], o[1], o[2], o[3]);
+            if (d == 0) {
+                sh.stat[2 * at] = top2;
+                sh.stat[2 * at + 1] = z;
+            }
+        } else if (rt * kCol + r < rows) {
+            const int tt = (rt * kCol + r) / G, hh = hk * G + (rt * kCol + r) % G;
+            const float f = z > 0.f ? 1.f / z : 0.f;
+            if (d < a.D)
+                store4(static_cast<T *>(a.o.p) + b * a.o.sb + tt * a.o.st + hh * a.o.sh + d, o[0] * f,
+                       o[1] * f, o[2] * f, o[3] * f);
+            if (d == 0 && a.lse)
+                a.lse[((int64_t)b * a.Hq + hh) * a.Tq + tt] =
+                    z > 0.f ? (top2 + __builtin_amdgcn_logf(z)) * kLn2 : -__builtin_inff();
+        }
+    }
+}
+
+// Joins the splits' shares of a row: four entries a thread.
+template <typename T, int DP>
+__global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnProblem a, Shares sh)
+{
+    constexpr int kQuads = DP / 4;
+    const int G = a.Hq / a.Hkv, rows = a.Tq * G, nt = (rows + kCol - 1) / kCol;
+    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, all = (int64_t)a.B * a.Hkv * rows;
+    const int64_t item = id / kQuads;
+    const int d = (int)(id % kQuads) * 4;
+    if (item >= all || d >= a.D)
+        return;
+    const int row = (int)(item % rows), hk = (int)(item / rows % a.Hkv), b = (int)(item / rows / a.Hkv);
+    const int64_t at = (((int64_t)b * a.Hkv + hk) * nt + row / kCol) * sh.splits * kCol + row % kCol;
+    float top2 = -__builtin_inff();
+    for (int i = 0; i < sh.splits; ++i)
+        top2 = fmaxf(top2, sh.stat[2 * (at + i * kCol)]);
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    float z = 0.f;
+    for (int i = 0; i < sh.splits; ++i) {
+        const float m = sh.stat[2 * (at + i * kCol)];
+        const float f = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - top2);
+        z = fmaf(f, sh.stat[2 * (at + i * kCol) + 1], z);
+        o += f * *reinterpret_cast<const f32x4_t *>(sh.out + (at + i * kCol) * DP + d);
+    }
+    const int t = row / G, hq = hk * G + row % G;
+    const float f = z > 0.f ? 1.f / z : 0.f;
+    store4(static_cast<T *>(a.o.p) + b * a.o.sb + t * a.o.st + hq * a.o.sh + d, o[0] * f, o[1] * f,
+           o[2] * f, o[3] * f);
+    if (d == 0 && a.lse)
+        a.lse[((int64_t)b * a.Hq + hq) * a.Tq + t] =
+            z > 0.f ? (top2 + __builtin_amdgcn_logf(z)) * kLn2 : -__builtin_inff();
+}
+
+int64_t tiles_of(const AttnProblem &p)
+{
+    return (int64_t)p.B * p.Hkv * (((int64_t)p.Tq * (p.Hq / p.Hkv) + kCol - 1) / kCol);
+}
+
+// Keys that one tile's rows see at most.
+int64_t keys_of(const AttnProblem &p)
+{
+    const int G = p.Hq / p.Hkv;
+    const int64_t span = std::min<int64_t>(p.Tq, (kCol - 1) / G + 2);
+    if (p.left < 0 || p.right < 0)
+        return p.Tk;
+    return std::min<int64_t>(p.Tk, (int64_t)p.left + p.right + span + p.sinks);
+}
+
+// Workgroups wanted at least, and blocks of keys that a wave of one has at least.
+constexpr int kWanted = 1024, kLeast = 2;
+
+template <typename T, int DP>
+hipError_t run(const AttnProblem &p, hipStream_t s)
+{
+    const int64_t tiles = tiles_of(p), blocks = keys_of(p) / kBlock + 2;
+    Shares sh{};
+    sh.splits = (int)std::max<int64_t>(1, std::min((kWanted + tiles - 1) / tiles, blocks / (4 * kLeast)));
+    if (sh.splits > 1) {
+        void *out = nullptr, *stat = nullptr;
+        hipError_t e = p.ws->take(&out, (size_t)tiles * sh.splits * kCol * DP * 4);
+        if (e == hipSuccess)
+            e = p.ws->take(&stat, (size_t)tiles * sh.splits * kCol * 2 * 4);
+        if (e != hipSuccess)
+            return e;
+        sh.out = static_cast<float *>(out);
+        sh.stat = static_cast<float *>(stat);
+    }
+    const int64_t n = tiles * sh.splits;
+    if (n * kThreads > kMaxThreads)
+        return hipErrorInvalidConfiguration;
+    if (p.ws->counting)
+        return hipSuccess;
+    attn_split_kernel<T, DP><<<dim3((unsigned)n), kThreads, 0, s>>>(p, sh);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || sh.splits == 1)
+        return e;
+    const int64_t m = (int64_t)p.B * p.Tq * p.Hq * (DP / 4);
+    attn_join_kernel<T, DP><<<dim3((unsigned)((m + kThreads - 1) / kThreads)), kThreads, 0, s>>>(p, sh);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run(const AttnProblem &p, hipStream_t s)
+{
+    return p.D <= 32   ? run<T, 32>(p, s)
+           : p.D <= 64 ? run<T, 64>(p, s)
+           : p.D <= 96 ? run<T, 96>(p, s)
+                       : run<T, 128>(p, s);
+}
+
+}  // namespace
+
+// Forwards whose queries of one key head fill at most two of these tiles: the
+// forward proper would read the keys once for every query head, and split none.
+bool attn_split_preferred(const AttnProblem &p)
+{
+    return (int64_t)p.Tq * (p.Hq / p.Hkv) <= 2 * kCol;
+}
+
+hipError_t launch_attn_split(const AttnProblem &p, hipStream_t s)
+{
+    return p.dtype == 0 ? run<float>(p, s) : run<bf16_t>(p, s);
+}
+
+}  // namespace gspn

@@ -95,6 +95,9 @@ inline hipError_t take_reserve(const Problem &p, ReserveParts *r)
     return e;
 }
 
+// The status of a HIP call's result; a failure is kept for gspn_last_hip_error.
+int hip_status(hipError_t e);
+
 // Planes whose sides are both <= kSmallSide run on the register-resident path.
 constexpr int kSmallSide = 64;
 
