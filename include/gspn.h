@@ -382,7 +382,8 @@ int gspn_latent_params(const void *xc, const void *l_u, const void *l_lam,
 
 /*
  * Token mixers beside the scan.  The encoders that the scan belongs to keep
- * some attention sublayers; these are the operators of such a sublayer.
+ * some attention sublayers; these are the operators of such a sublayer, and a
+ * linear recurrence over a sequence of tokens, the scan's counterpart.
  *
  * Layouts.  A "heads" tensor is [B][T][H][D] with D contiguous; `strides`, a
  * host array of three int64 per heads tensor in argument order (batch, token
@@ -473,6 +474,55 @@ int gspn_window_attn_decode(const void *q, const void *k, const void *v, const i
                             void *o, const int64_t *strides, int B, int Tq, int Tk, int Hq,
                             int Hkv, int D, int left, int sinks, float scale, int dtype,
                             void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * The gated delta rule: a recurrence over the tokens of a sequence with a
+ * Dk x Dv state for each value head,
+ *   S_t = exp(g_t) (I - beta_t k_t k_t^T) S_{t-1} + beta_t k_t v_t^T
+ *   o_t = scale S_t^T q_t
+ * q, k [B][T][Hq][Dk]; v, o [B][T][Hv][Dv], Hv a multiple of Hq: value head h
+ * reads query and key head h / (Hv / Hq); g, beta [B][T][Hv], contiguous, in the
+ * storage type, finite, g <= 0 (values below -100 count as -100, where exp(g)
+ * is 0 to fp32) and keys of a length of about 1 (|I - beta k k^T| <= 1, or the
+ * recurrence itself grows).  state, state_out: fp32 [B][Hv][Dk][Dv], the state
+ * ahead of the first token (NULL: zeros) and behind the last (NULL: not wanted);
+ * they may be the same buffer.  Dk and Dv up to 128.  lens as for the
+ * attention: tokens at and past it write nothing, leave the state as it is, may
+ * hold anything, and have o = 0 and gradients 0.  States and what they are
+ * formed from are fp32 for either storage type.
+ * Up to 8 tokens run the recurrence itself, more run in chunks of 64 (results
+ * agree within the rounding of fp32).
+ * Training: gspn_delta_rule_fwd_train also fills a caller buffer, the reserve
+ * (gspn_delta_rule_reserve_size bytes), with the states and inverses of its
+ * chunks, which gspn_delta_rule_bwd_reserve reads.  dstate_out (NULL: zeros) is
+ * the gradient of state_out, dstate (NULL: not wanted) that of state.
+ * strides: forward q, k, v, o; backward q, k, v, dout, dq, dk, dv.
+ */
+#define GSPN_DELTA_FWD 0
+#define GSPN_DELTA_FWD_TRAIN 1
+#define GSPN_DELTA_BWD_RESERVE 2
+int gspn_delta_rule_workspace_size(int op, int B, int T, int Hq, int Hv, int Dk, int Dv,
+                                   int dtype, int64_t *bytes);
+int gspn_delta_rule_reserve_size(int B, int T, int Hq, int Hv, int Dk, int Dv, int dtype,
+                                 int64_t *bytes);
+int gspn_delta_rule_fwd(const void *q, const void *k, const void *v, const void *g,
+                        const void *beta, const float *state, const int32_t *lens, void *o,
+                        float *state_out, const int64_t *strides, int B, int T, int Hq, int Hv,
+                        int Dk, int Dv, float scale, int dtype, void *workspace,
+                        int64_t workspace_bytes, void *stream);
+int gspn_delta_rule_fwd_train(const void *q, const void *k, const void *v, const void *g,
+                              const void *beta, const float *state, const int32_t *lens, void *o,
+                              float *state_out, const int64_t *strides, int B, int T, int Hq,
+                              int Hv, int Dk, int Dv, float scale, int dtype, void *reserve,
+                              int64_t reserve_bytes, void *workspace, int64_t workspace_bytes,
+                              void *stream);
+int gspn_delta_rule_bwd_reserve(const void *q, const void *k, const void *v, const void *g,
+                                const void *beta, const void *dout, const float *dstate_out,
+                                const int32_t *lens, void *dq, void *dk, void *dv, void *dg,
+                                void *dbeta, float *dstate, const int64_t *strides, int B, int T,
+                                int Hq, int Hv, int Dk, int Dv, float scale, int dtype,
+                                void *reserve, int64_t reserve_bytes, void *workspace,
+                                int64_t workspace_bytes, void *stream);
 
 /* Static description of a status code (never NULL). */
 const char *gspn_strerror(int status);

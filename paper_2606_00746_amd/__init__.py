@@ -6,9 +6,11 @@ scan directions, forward and backward, as hand-written HIP kernels for gfx950
 behind a C ABI (``include/gspn.h``).  This package is the ctypes binding.
 
 Beside the scan: the operators of an attention sublayer (norm of query and key
-heads with the position rotation, attention with a sliding window and sinks).
+heads with the position rotation, attention with a sliding window and sinks),
+and the gated delta rule, a recurrence over a sequence of tokens.
 """
-from ._mixers import (qk_norm_rotate_bwd, qk_norm_rotate_fwd, window_attn_bwd, window_attn_decode,
+from ._mixers import (delta_reserve_size, delta_rule_bwd_reserve, delta_rule_fwd,
+                      delta_rule_fwd_train, qk_norm_rotate_bwd, qk_norm_rotate_fwd, window_attn_bwd, window_attn_decode,
                       window_attn_fwd)
 from ._native import (ALL, B2T, BF16, BLOCKED, F32, L2R, LIB_PATH, OP_BWD, OP_BWD_BLOCKED,
                       OP_BWD_NORM, OP_BWD_NORM_RESERVE, OP_BWD_RESERVE, OP_FWD, OP_FWD_BLOCKED,
@@ -33,6 +35,7 @@ __all__ = ["ALL", "B2T", "BF16", "BLOCKED", "F32", "L2R", "LIB_PATH", "OP_BWD", 
            "gspn_scan_fwd", "gspn_scan_fwd_blocked", "gspn_scan_fwd_norm", "gspn_scan_fwd_norm_train",
            "gspn_scan_fwd_train",
            "gspn_strerror", "gspn_version", "gspn_workspace_size", "gspn_workspace_size_slots",
+           "delta_reserve_size", "delta_rule_bwd_reserve", "delta_rule_fwd", "delta_rule_fwd_train",
            "latent_fwd", "latent_params", "load", "project", "qk_norm_rotate_bwd", "qk_norm_rotate_fwd",
            "reserve_size", "scan_bwd",
            "scan_bwd_norm", "scan_bwd_norm_reserve", "scan_bwd_reserve", "scan_fwd",

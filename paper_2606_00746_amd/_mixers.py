@@ -1,8 +1,8 @@
 """Torch front end of the token mixers beside the scan (argument marshalling only).
 
 The norm of query and key heads with the position rotation
-(``qk_norm_rotate_*``) and windowed attention (``window_attn_*``), see
-``include/gspn.h`` for the formulas.  Tensors are [B, T, H, D] with D
+(``qk_norm_rotate_*``), windowed attention (``window_attn_*``) and the gated
+delta rule (``delta_rule_*``), see ``include/gspn.h`` for the formulas.  Tensors are [B, T, H, D] with D
 contiguous and any other strides (slices of a fused projection or of a cache);
 every call runs on the current stream of its tensors' device unless one is
 given, and takes the workspace it needs from torch unless it is handed one.
@@ -17,6 +17,7 @@ from ._native import (_check_raise, _current_device, _dtype_code, _stream_handle
 
 PAIRS = {"half": 0, "adjacent": 1}
 ATTN_FWD, ATTN_BWD, ATTN_DECODE = 0, 1, 2
+DELTA_FWD, DELTA_FWD_TRAIN, DELTA_BWD_RESERVE = 0, 1, 2
 
 
 def _heads(named):
@@ -243,3 +244,116 @@ def window_attn_decode(q, k, v, lens=None, left: int = -1, sinks: int = 0, scale
         Tq, Tk, Hq, Hkv, D, left, sinks, 1 / math.sqrt(D) if scale is None else scale, dt, ws,
         nbytes, _stream_handle(q, stream)))
     return o
+
+
+# ---------------------------------------------------------------------------
+# the gated delta rule
+# ---------------------------------------------------------------------------
+
+def _delta_sizes(q, k, v, g, beta, lens):
+    import torch
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError("q, k and v must be [B, T, H, D]")
+    B, T, Hq, Dk = q.shape
+    Hv, Dv = v.shape[2], v.shape[3]
+    gates = (_plain("g", g, (B, T, Hv), q.dtype, q), _plain("beta", beta, (B, T, Hv), q.dtype, q))
+    return (B, T, Hq, Hv, Dk, Dv), gates, _plain("lens", lens, (B,), torch.int32, q)
+
+
+def _reserve(reserve, n, device):
+    """The reserve's pointer and bytes."""
+    import torch
+    if (reserve.dtype != torch.uint8 or not reserve.is_contiguous() or not reserve.is_cuda
+            or reserve.device != device):
+        raise ValueError("reserve must be a contiguous uint8 tensor on the inputs' device")
+    if reserve.numel() < n:
+        raise ValueError(f"reserve of {reserve.numel()} bytes, smaller than the {n} bytes "
+                         "these tensors take")
+    return reserve.data_ptr(), reserve.numel()
+
+
+def delta_reserve_size(q, v) -> int:
+    """Bytes of the reserve of the delta rule's training pair for these tensors."""
+    B, T, Hq, Dk = q.shape
+    return _sized("gspn_delta_rule_reserve_size",
+                  (B, T, Hq, v.shape[2], Dk, v.shape[3], _dtype_code(q)), _current_device())
+
+
+def _delta_fwd(op, q, k, v, g, beta, state, lens, scale, o, state_out, reserve, stream, workspace):
+    import torch
+    sizes, gates, lens_p = _delta_sizes(q, k, v, g, beta, lens)
+    B, T, Hq, Hv, Dk, Dv = sizes
+    if o is None:
+        o = torch.empty((B, T, Hv, Dv), dtype=q.dtype, device=q.device)
+    if state_out is None:
+        state_out = torch.empty((B, Hv, Dk, Dv), dtype=torch.float32, device=q.device)
+    _heads({"q": (q, (B, T, Hq, Dk)), "k": (k, (B, T, Hq, Dk)), "v": (v, (B, T, Hv, Dv)),
+            "o": (o, (B, T, Hv, Dv))})
+    dt = _dtype_code(q)
+    n = _sized("gspn_delta_rule_workspace_size", (op, *sizes, dt), _current_device())
+    ws = _take(n, workspace, q.device)
+    args = (q.data_ptr(), k.data_ptr(), v.data_ptr(), *gates,
+            _plain("state", state, (B, Hv, Dk, Dv), torch.float32, q), lens_p, o.data_ptr(),
+            _plain("state_out", state_out, (B, Hv, Dk, Dv), torch.float32, q),
+            _strides(q, k, v, o), *sizes, 1 / math.sqrt(Dk) if scale is None else scale, dt)
+    if op == DELTA_FWD:
+        _check_raise(load().gspn_delta_rule_fwd(*args, *ws, _stream_handle(q, stream)))
+        return o, state_out
+    n = delta_reserve_size(q, v)
+    if reserve is None:
+        reserve = torch.empty(n, dtype=torch.uint8, device=q.device)
+    _check_raise(load().gspn_delta_rule_fwd_train(*args, *_reserve(reserve, n, q.device), *ws,
+                                                  _stream_handle(q, stream)))
+    return o, state_out, reserve
+
+
+def delta_rule_fwd(q, k, v, g, beta, state=None, lens=None, scale=None, o=None, state_out=None,
+                   stream=None, workspace=None):
+    """(o, state_out): S_t = exp(g_t) (I - beta_t k_t k_t^T) S_{t-1} + beta_t k_t v_t^T
+    and o_t = scale S_t^T q_t for q, k [B, T, Hq, Dk], v [B, T, Hv, Dv] and g,
+    beta [B, T, Hv], from `state` (fp32 [B, Hv, Dk, Dv]; None: zeros).  lens
+    (int32 [B]): the sequences' lengths.  scale: 1 / sqrt(Dk) unless given.
+    state_out may be state.  A token at a time is its serving form."""
+    return _delta_fwd(DELTA_FWD, q, k, v, g, beta, state, lens, scale, o, state_out, None, stream,
+                      workspace)
+
+
+def delta_rule_fwd_train(q, k, v, g, beta, state=None, lens=None, scale=None, o=None,
+                         state_out=None, reserve=None, stream=None, workspace=None):
+    """delta_rule_fwd that also fills the reserve that delta_rule_bwd_reserve
+    reads (a uint8 device tensor of delta_reserve_size bytes, or None for a new
+    one).  Returns (o, state_out, reserve)."""
+    return _delta_fwd(DELTA_FWD_TRAIN, q, k, v, g, beta, state, lens, scale, o, state_out, reserve,
+                      stream, workspace)
+
+
+def delta_rule_bwd_reserve(q, k, v, g, beta, do, reserve, dstate=None, state=None, lens=None,
+                           scale=None, out=None, stream=None, workspace=None):
+    """(dq, dk, dv, dg, dbeta, dstate_in) from the gradients `do` of o and
+    `dstate` of state_out (None: zeros); the other arguments are those of
+    delta_rule_fwd_train, which filled `reserve`.  dstate_in is the gradient of
+    `state`, None where the forward began from zeros."""
+    import torch
+    sizes, gates, lens_p = _delta_sizes(q, k, v, g, beta, lens)
+    B, T, Hq, Hv, Dk, Dv = sizes
+    qs, vs, gs, ss = (B, T, Hq, Dk), (B, T, Hv, Dv), (B, T, Hv), (B, Hv, Dk, Dv)
+    if out is None:
+        kw = dict(dtype=q.dtype, device=q.device)
+        out = (torch.empty(qs, **kw), torch.empty(qs, **kw), torch.empty(vs, **kw),
+               torch.empty(gs, **kw), torch.empty(gs, **kw),
+               None if state is None else torch.empty(ss, dtype=torch.float32, device=q.device))
+    dq, dk, dv, dg, dbeta, din = out
+    _heads({"q": (q, qs), "k": (k, qs), "v": (v, vs), "do": (do, vs), "dq": (dq, qs),
+            "dk": (dk, qs), "dv": (dv, vs)})
+    dt = _dtype_code(q)
+    n = _sized("gspn_delta_rule_workspace_size", (DELTA_BWD_RESERVE, *sizes, dt),
+               _current_device())
+    ws = _take(n, workspace, q.device)
+    _check_raise(load().gspn_delta_rule_bwd_reserve(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), *gates, do.data_ptr(),
+        _plain("dstate", dstate, ss, torch.float32, q), lens_p, dq.data_ptr(), dk.data_ptr(),
+        dv.data_ptr(), _plain("dg", dg, gs, q.dtype, q), _plain("dbeta", dbeta, gs, q.dtype, q),
+        _plain("dstate_in", din, ss, torch.float32, q), _strides(q, k, v, do, dq, dk, dv), *sizes,
+        1 / math.sqrt(Dk) if scale is None else scale, dt,
+        *_reserve(reserve, delta_reserve_size(q, v), q.device), *ws, _stream_handle(q, stream)))
+    return out

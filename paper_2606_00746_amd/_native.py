@@ -38,6 +38,8 @@ EXPORTED = ("gspn_workspace_size", "gspn_scan_fwd", "gspn_scan_bwd", "gspn_scan_
             "gspn_qk_norm_rotate_fwd", "gspn_qk_norm_rotate_workspace_size",
             "gspn_qk_norm_rotate_bwd", "gspn_window_attn_workspace_size", "gspn_window_attn_fwd",
             "gspn_window_attn_bwd", "gspn_window_attn_decode",
+            "gspn_delta_rule_workspace_size", "gspn_delta_rule_reserve_size",
+            "gspn_delta_rule_fwd", "gspn_delta_rule_fwd_train", "gspn_delta_rule_bwd_reserve",
             "gspn_strerror", "gspn_last_hip_error", "gspn_version")
 
 _lib = None
@@ -92,6 +94,11 @@ def load() -> ctypes.CDLL:
         lib.gspn_window_attn_fwd.argtypes = [vp] * 7 + [i] * 10 + [f, i] + ws
         lib.gspn_window_attn_bwd.argtypes = [vp] * 11 + [i] * 10 + [f, i] + ws
         lib.gspn_window_attn_decode.argtypes = [vp] * 6 + [i] * 8 + [f, i] + ws
+        lib.gspn_delta_rule_workspace_size.argtypes = [i] * 8 + [pi64]
+        lib.gspn_delta_rule_reserve_size.argtypes = [i] * 7 + [pi64]
+        lib.gspn_delta_rule_fwd.argtypes = [vp] * 10 + [i] * 6 + [f, i] + ws
+        lib.gspn_delta_rule_fwd_train.argtypes = [vp] * 10 + [i] * 6 + [f, i, vp, i64] + ws
+        lib.gspn_delta_rule_bwd_reserve.argtypes = [vp] * 15 + [i] * 6 + [f, i, vp, i64] + ws
         for name in EXPORTED:
             getattr(lib, name).restype = i
         lib.gspn_strerror.argtypes = [i]

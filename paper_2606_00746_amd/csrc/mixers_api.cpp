@@ -1,15 +1,17 @@
 // C ABI of the token mixers beside the scan: the norm of query and key heads
-// with the position rotation, and windowed attention.  Argument checks (host
-// only, before any HIP call), workspaces, launches.
+// with the position rotation, windowed attention, and the gated delta rule.
+// Argument checks (host only, before any HIP call), workspaces, launches.
 #include <hip/hip_runtime.h>
 
 #include <math.h>
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/gspn.h"
 #include "attn.hpp"
+#include "delta.hpp"
 #include "launch.hpp"
 #include "qk_norm.hpp"
 
@@ -129,6 +131,11 @@ struct Buffers {
     }
 };
 
+template <typename P>
+struct requires_reserve : std::false_type {};
+template <>
+struct requires_reserve<DeltaProblem> : std::true_type {};
+
 // Runs `launch` in counting mode for the bytes it takes, checks the caller's
 // workspace against them and the other buffers, and launches.
 template <typename P>
@@ -150,6 +157,9 @@ int run(P &p, hipError_t (*launch)(const P &, hipStream_t), Buffers &bufs, void 
         if (bufs.status != GSPN_OK)
             return bufs.status;
     }
+    if constexpr (requires_reserve<P>::value)
+        if (p.rs)
+            p.rs->used = 0;
     ws = Workspace{};
     ws.base = static_cast<char *>(workspace);
     ws.size = (size_t)std::max<int64_t>(0, bytes);
@@ -232,6 +242,78 @@ int make_norm(NormProblem &p, int B, int T, int Hq, int Hk, int D, int R, int ro
     p.eps = eps;
     p.dtype = dtype;
     return GSPN_OK;
+}
+
+int make_delta(DeltaProblem &p, int B, int T, int Hq, int Hv, int Dk, int Dv, float scale, int dtype)
+{
+    int st = check_sizes(B, T, 1, Hq, Hv, Dk, kDeltaMaxHead, dtype);
+    if (st == GSPN_OK)
+        st = check_sizes(B, T, 1, Hv, Hq, Dv, kDeltaMaxHead, dtype);
+    if (st != GSPN_OK)
+        return st;
+    if (Hv % Hq != 0 || !isfinite(scale))
+        return GSPN_ERR_DIM;
+    p = DeltaProblem{};
+    p.B = B, p.T = T, p.Hq = Hq, p.Hv = Hv, p.Dk = Dk, p.Dv = Dv;
+    p.scale = scale;
+    p.dtype = dtype;
+    return GSPN_OK;
+}
+
+// Bytes of the training pair's reserve.
+int64_t delta_reserve(const DeltaProblem &p)
+{
+    Workspace rs;
+    rs.counting = true;
+    DeltaKept kept;
+    take_delta_kept(p, &rs, &kept);
+    return (int64_t)rs.used;
+}
+
+// The inputs that both passes of the delta rule read.
+void delta_inputs(DeltaProblem &p, Buffers &bufs, const void *q, const void *k, const void *v, const void *g,
+                  const void *beta, const int32_t *lens, const int64_t *strides)
+{
+    const int64_t gates = (int64_t)p.B * p.T * p.Hv * storage(p.dtype);
+    p.q = bufs.heads(q, at(strides, 0), p.B, p.T, p.Hq, p.Dk, p.dtype, false);
+    p.k = bufs.heads(k, at(strides, 1), p.B, p.T, p.Hq, p.Dk, p.dtype, false);
+    p.v = bufs.heads(v, at(strides, 2), p.B, p.T, p.Hv, p.Dv, p.dtype, false);
+    bufs.buffer(g, gates, (int)storage(p.dtype), false);
+    bufs.buffer(beta, gates, (int)storage(p.dtype), false);
+    bufs.buffer(lens, (int64_t)p.B * 4, 4, false, true);
+    p.g = g, p.beta = beta, p.lens = lens;
+}
+
+int delta_fwd(const void *q, const void *k, const void *v, const void *g, const void *beta, const float *state,
+              const int32_t *lens, void *o, float *state_out, const int64_t *strides, int B, int T, int Hq, int Hv, int Dk,
+              int Dv, float scale, int dtype, void *reserve, int64_t reserve_bytes, bool train, void *workspace,
+              int64_t workspace_bytes, void *stream)
+{
+    DeltaProblem p;
+    const int st = make_delta(p, B, T, Hq, Hv, Dk, Dv, scale, dtype);
+    if (st != GSPN_OK)
+        return st;
+    Buffers bufs;
+    delta_inputs(p, bufs, q, k, v, g, beta, lens, strides);
+    const int64_t states = (int64_t)B * Hv * Dk * Dv * 4;
+    if (state != state_out)   // a state may be continued in place
+        bufs.buffer(state, states, 16, false, true);
+    p.o = bufs.heads(o, at(strides, 3), B, T, Hv, Dv, dtype, true);
+    bufs.buffer(state_out, states, 16, true, true);
+    p.state = state, p.state_out = state_out;
+    Workspace rs;
+    if (train) {
+        const int64_t need = delta_reserve(p);
+        if (bufs.status == GSPN_OK && (reserve == nullptr || reserve_bytes < need))
+            return GSPN_ERR_WORKSPACE;
+        bufs.buffer(reserve, need, 16, true);
+        rs.base = static_cast<char *>(reserve);
+        rs.size = (size_t)need;
+        p.rs = &rs;
+    }
+    if (bufs.status != GSPN_OK)
+        return bufs.status;
+    return run(p, launch_delta_fwd, bufs, workspace, workspace_bytes, stream);
 }
 
 // The weights and tables that both passes of the norm read.
@@ -406,4 +488,90 @@ extern "C" int gspn_window_attn_decode(const void *q, const void *k, const void 
     p.lens = lens;
     p.tail = true;
     return run(p, launch_attn_split, bufs, workspace, workspace_bytes, stream);
+}
+
+extern "C" int gspn_delta_rule_reserve_size(int B, int T, int Hq, int Hv, int Dk, int Dv, int dtype, int64_t *bytes)
+{
+    if (bytes == nullptr)
+        return GSPN_ERR_NULL;
+    *bytes = 0;
+    DeltaProblem p;
+    const int st = make_delta(p, B, T, Hq, Hv, Dk, Dv, 1.f, dtype);
+    if (st == GSPN_OK)
+        *bytes = delta_reserve(p);
+    return st;
+}
+
+extern "C" int gspn_delta_rule_workspace_size(int op, int B, int T, int Hq, int Hv, int Dk, int Dv, int dtype,
+                                              int64_t *bytes)
+{
+    if (bytes == nullptr)
+        return GSPN_ERR_NULL;
+    *bytes = 0;
+    if (op != GSPN_DELTA_FWD && op != GSPN_DELTA_FWD_TRAIN && op != GSPN_DELTA_BWD_RESERVE)
+        return GSPN_ERR_UNSUPPORTED;
+    DeltaProblem p;
+    const int st = make_delta(p, B, T, Hq, Hv, Dk, Dv, 1.f, dtype);
+    if (st != GSPN_OK)
+        return st;
+    Workspace rs;
+    rs.counting = true;
+    if (op != GSPN_DELTA_FWD)
+        p.rs = &rs;
+    return count(p, op == GSPN_DELTA_BWD_RESERVE ? launch_delta_bwd : launch_delta_fwd, bytes);
+}
+
+extern "C" int gspn_delta_rule_fwd(const void *q, const void *k, const void *v, const void *g, const void *beta,
+                                   const float *state, const int32_t *lens, void *o, float *state_out,
+                                   const int64_t *strides, int B, int T, int Hq, int Hv, int Dk, int Dv, float scale,
+                                   int dtype, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    return delta_fwd(q, k, v, g, beta, state, lens, o, state_out, strides, B, T, Hq, Hv, Dk, Dv, scale, dtype, nullptr, 0,
+                     false, workspace, workspace_bytes, stream);
+}
+
+extern "C" int gspn_delta_rule_fwd_train(const void *q, const void *k, const void *v, const void *g, const void *beta,
+                                         const float *state, const int32_t *lens, void *o, float *state_out,
+                                         const int64_t *strides, int B, int T, int Hq, int Hv, int Dk, int Dv, float scale,
+                                         int dtype, void *reserve, int64_t reserve_bytes, void *workspace,
+                                         int64_t workspace_bytes, void *stream)
+{
+    return delta_fwd(q, k, v, g, beta, state, lens, o, state_out, strides, B, T, Hq, Hv, Dk, Dv, scale, dtype, reserve,
+                     reserve_bytes, true, workspace, workspace_bytes, stream);
+}
+
+extern "C" int gspn_delta_rule_bwd_reserve(const void *q, const void *k, const void *v, const void *g, const void *beta,
+                                           const void *dout, const float *dstate_out, const int32_t *lens, void *dq,
+                                           void *dk, void *dv, void *dg, void *dbeta, float *dstate, const int64_t *strides,
+                                           int B, int T, int Hq, int Hv, int Dk, int Dv, float scale, int dtype,
+                                           void *reserve, int64_t reserve_bytes, void *workspace, int64_t workspace_bytes,
+                                           void *stream)
+{
+    DeltaProblem p;
+    const int st = make_delta(p, B, T, Hq, Hv, Dk, Dv, scale, dtype);
+    if (st != GSPN_OK)
+        return st;
+    Buffers bufs;
+    delta_inputs(p, bufs, q, k, v, g, beta, lens, strides);
+    const int64_t states = (int64_t)B * Hv * Dk * Dv * 4, gates = (int64_t)B * T * Hv * storage(dtype);
+    p.dout = bufs.heads(dout, at(strides, 3), B, T, Hv, Dv, dtype, false);
+    bufs.buffer(dstate_out, states, 16, false, true);
+    p.dq = bufs.heads(dq, at(strides, 4), B, T, Hq, Dk, dtype, true);
+    p.dk = bufs.heads(dk, at(strides, 5), B, T, Hq, Dk, dtype, true);
+    p.dv = bufs.heads(dv, at(strides, 6), B, T, Hv, Dv, dtype, true);
+    bufs.buffer(dg, gates, (int)storage(dtype), true);
+    bufs.buffer(dbeta, gates, (int)storage(dtype), true);
+    bufs.buffer(dstate, states, 16, true, true);
+    p.dg = dg, p.dbeta = dbeta, p.dstate = dstate_out, p.dstate_in = dstate;
+    const int64_t need = delta_reserve(p);
+    if (bufs.status == GSPN_OK && (reserve == nullptr || reserve_bytes < need))
+        return GSPN_ERR_WORKSPACE;
+    bufs.buffer(reserve, need, 16, false);
+    if (bufs.status != GSPN_OK)
+        return bufs.status;
+    Workspace rs;
+    rs.base = static_cast<char *>(reserve);
+    rs.size = (size_t)need;
+    p.rs = &rs;
+    return run(p, launch_delta_bwd, bufs, workspace, workspace_bytes, stream);
 }

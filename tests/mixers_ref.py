@@ -83,3 +83,34 @@ def attention(q, k, v, see, scale, do=None):
                mag_dk=scale * (np.abs(ds) + p * mag_d).T @ np.abs(q),
                wide_dq=scale * (p * mag_dp) @ np.abs(k), wide_dk=scale * (p * mag_dp).T @ np.abs(q))
     return out
+
+
+def delta_rule(q, k, v, g, beta, S, scale, do=None, dS=None):
+    """One head, token by token: q, k [T][Dk], v [T][Dv], g, beta [T], S [Dk][Dv].
+    A dict of o, state and, with do and dS, the gradients."""
+    T = len(g)
+    a, o, kept = np.exp(g), np.zeros_like(v), []
+    for t in range(T):
+        kept.append(S)
+        S = a[t] * S
+        S = S + np.outer(k[t], beta[t] * (v[t] - S.T @ k[t]))
+        o[t] = scale * S.T @ q[t]
+    out = dict(o=o, state=S)
+    if do is None:
+        return out
+    dq, dk, dv, dg, db = (np.zeros_like(x) for x in (q, k, v, g, beta))
+    for t in reversed(range(T)):
+        before = a[t] * kept[t]
+        z = v[t] - before.T @ k[t]
+        S = before + np.outer(k[t], beta[t] * z)
+        dq[t] = scale * S @ do[t]
+        dS = dS + scale * np.outer(q[t], do[t])
+        du = dS.T @ k[t]
+        db[t] = du @ z
+        dk[t] = dS @ (beta[t] * z) - before @ (beta[t] * du)
+        dv[t] = beta[t] * du
+        dS = dS - np.outer(k[t], beta[t] * du)
+        dg[t] = (dS * before).sum()
+        dS = a[t] * dS
+    out.update(dq=dq, dk=dk, dv=dv, dg=dg, dbeta=db, dstate=dS)
+    return out
