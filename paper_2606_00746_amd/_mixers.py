@@ -58,17 +58,18 @@ def _plain(name, t, shape, dtype, like):
 
 
 def _take(nbytes, given, device):
-    """The buffer a call works in: `given` where it is large enough, else a new one."""
+    """The buffer a call works in: `given` where it is large enough, else a new one,
+    as (pointer, bytes) and the tensor, which has to outlive the call."""
     if nbytes == 0:
-        return None, 0
+        return (None, 0), None
     import torch
     if given is not None:
         if given.device != device or given.dtype != torch.uint8 or not given.is_contiguous():
             raise ValueError("workspace must be a contiguous uint8 tensor on the inputs' device")
         if given.numel() >= nbytes:
-            return given.data_ptr(), given.numel()
+            return (given.data_ptr(), given.numel()), given
     buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    return buf.data_ptr(), nbytes
+    return (buf.data_ptr(), nbytes), buf
 
 
 @functools.lru_cache(maxsize=256)
@@ -143,12 +144,12 @@ def qk_norm_rotate_bwd(q, k, wq, wk, dyq, dyk, cos=None, sin=None, eps: float = 
     dt = _dtype_code(q)
     n = _sized("gspn_qk_norm_rotate_workspace_size", (B, T, Hq, Hk, D, R, PAIRS[pairs], dt),
                _current_device())
-    ws, nbytes = _take(n, workspace, q.device)
+    ws, held = _take(n, workspace, q.device)
     _check_raise(load().gspn_qk_norm_rotate_bwd(
         q.data_ptr(), k.data_ptr(), *ptrs, dyq.data_ptr(), dyk.data_ptr(), dq.data_ptr(),
         dk.data_ptr(), _plain("dwq", dwq, (D,), q.dtype, q), _plain("dwk", dwk, (D,), q.dtype, q),
         _strides(q, k, dyq, dyk, dq, dk), B, T, Hq, Hk, D, R, rows, first, PAIRS[pairs], eps, dt,
-        ws, nbytes, _stream_handle(q, stream)))
+        *ws, _stream_handle(q, stream)))
     return out
 
 
@@ -187,13 +188,13 @@ def window_attn_fwd(q, k, v, left: int = -1, right: int = -1, sinks: int = 0, le
     _heads({"q": (q, (B, Tq, Hq, D)), "k": (k, (B, Tk, Hkv, D)), "v": (v, (B, Tk, Hkv, D)),
             "o": (o, (B, Tq, Hq, D))})
     dt = _dtype_code(q)
-    ws, nbytes = _attn_workspace(ATTN_FWD, (B, Tq, Tk, Hq, Hkv, D), left, right, sinks, offset, dt,
-                                 workspace, q.device)
+    ws, held = _attn_workspace(ATTN_FWD, (B, Tq, Tk, Hq, Hkv, D), left, right, sinks, offset, dt,
+                               workspace, q.device)
     _check_raise(load().gspn_window_attn_fwd(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), lens_p, o.data_ptr(),
         _plain("lse", lse, (B, Hq, Tq), torch.float32, q), _strides(q, k, v, o), B, Tq, Tk, Hq,
-        Hkv, D, left, right, sinks, offset, 1 / math.sqrt(D) if scale is None else scale, dt, ws,
-        nbytes, _stream_handle(q, stream)))
+        Hkv, D, left, right, sinks, offset, 1 / math.sqrt(D) if scale is None else scale, dt, *ws,
+        _stream_handle(q, stream)))
     return o, lse
 
 
@@ -213,13 +214,13 @@ def window_attn_bwd(q, k, v, o, lse, do, left: int = -1, right: int = -1, sinks:
     _heads({"q": (q, qs), "k": (k, ks), "v": (v, ks), "o": (o, qs), "do": (do, qs), "dq": (dq, qs),
             "dk": (dk, ks), "dv": (dv, ks)})
     dt = _dtype_code(q)
-    ws, nbytes = _attn_workspace(ATTN_BWD, (B, Tq, Tk, Hq, Hkv, D), left, right, sinks, offset, dt,
-                                 workspace, q.device)
+    ws, held = _attn_workspace(ATTN_BWD, (B, Tq, Tk, Hq, Hkv, D), left, right, sinks, offset, dt,
+                               workspace, q.device)
     _check_raise(load().gspn_window_attn_bwd(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
         _plain("lse", lse, (B, Hq, Tq), torch.float32, q), do.data_ptr(), lens_p, dq.data_ptr(),
         dk.data_ptr(), dv.data_ptr(), _strides(q, k, v, o, do, dq, dk, dv), B, Tq, Tk, Hq, Hkv, D,
-        left, right, sinks, offset, 1 / math.sqrt(D) if scale is None else scale, dt, ws, nbytes,
+        left, right, sinks, offset, 1 / math.sqrt(D) if scale is None else scale, dt, *ws,
         _stream_handle(q, stream)))
     return dq, dk, dv
 
@@ -237,12 +238,12 @@ def window_attn_decode(q, k, v, lens=None, left: int = -1, sinks: int = 0, scale
     _heads({"q": (q, (B, Tq, Hq, D)), "k": (k, (B, Tk, Hkv, D)), "v": (v, (B, Tk, Hkv, D)),
             "o": (o, (B, Tq, Hq, D))})
     dt = _dtype_code(q)
-    ws, nbytes = _attn_workspace(ATTN_DECODE, (B, Tq, Tk, Hq, Hkv, D), left, 0, sinks, 0, dt,
-                                 workspace, q.device)
+    ws, held = _attn_workspace(ATTN_DECODE, (B, Tq, Tk, Hq, Hkv, D), left, 0, sinks, 0, dt,
+                               workspace, q.device)
     _check_raise(load().gspn_window_attn_decode(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), lens_p, o.data_ptr(), _strides(q, k, v, o), B,
-        Tq, Tk, Hq, Hkv, D, left, sinks, 1 / math.sqrt(D) if scale is None else scale, dt, ws,
-        nbytes, _stream_handle(q, stream)))
+        Tq, Tk, Hq, Hkv, D, left, sinks, 1 / math.sqrt(D) if scale is None else scale, dt, *ws,
+        _stream_handle(q, stream)))
     return o
 
 
@@ -291,7 +292,7 @@ def _delta_fwd(op, q, k, v, g, beta, state, lens, scale, o, state_out, reserve, 
             "o": (o, (B, T, Hv, Dv))})
     dt = _dtype_code(q)
     n = _sized("gspn_delta_rule_workspace_size", (op, *sizes, dt), _current_device())
-    ws = _take(n, workspace, q.device)
+    ws, held = _take(n, workspace, q.device)
     args = (q.data_ptr(), k.data_ptr(), v.data_ptr(), *gates,
             _plain("state", state, (B, Hv, Dk, Dv), torch.float32, q), lens_p, o.data_ptr(),
             _plain("state_out", state_out, (B, Hv, Dk, Dv), torch.float32, q),
@@ -348,7 +349,7 @@ def delta_rule_bwd_reserve(q, k, v, g, beta, do, reserve, dstate=None, state=Non
     dt = _dtype_code(q)
     n = _sized("gspn_delta_rule_workspace_size", (DELTA_BWD_RESERVE, *sizes, dt),
                _current_device())
-    ws = _take(n, workspace, q.device)
+    ws, held = _take(n, workspace, q.device)
     _check_raise(load().gspn_delta_rule_bwd_reserve(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), *gates, do.data_ptr(),
         _plain("dstate", dstate, ss, torch.float32, q), lens_p, dq.data_ptr(), dk.data_ptr(),
