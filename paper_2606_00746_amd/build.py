@@ -14,7 +14,7 @@ SOURCES = ["api.cpp", "scan_tiny.hip", "scan_small.hip", "scan_med_64.hip", "sca
            "scan_med_48.hip", "scan_med_40_32_24.hip", "scan_med.hip", "scan_pm.hip",
            "scan_wide.hip", "scan_norm.hip", "scan_plane.hip", "scan_line.hip", "scan_general.hip", "latent.hip",
            "mixers_api.cpp", "qk_norm.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_split.hip",
-           "delta_fwd.hip", "delta_bwd.hip"]
+           "delta_fwd.hip", "delta_bwd.hip", "delta_bf16.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

@@ -47,6 +47,10 @@ struct DeltaProblem {
 
 hipError_t launch_delta_fwd(const DeltaProblem &p, hipStream_t s);
 hipError_t launch_delta_bwd(const DeltaProblem &p, hipStream_t s);
+// bf16 storage (delta_bf16.hip), and what its training forward takes from p.rs.
+hipError_t launch_delta16_fwd(const DeltaProblem &p, hipStream_t s);
+hipError_t launch_delta16_bwd(const DeltaProblem &p, hipStream_t s);
+hipError_t delta16_reserve(const DeltaProblem &p);
 
 constexpr int kDeltaMaxHead = 128;
 constexpr int kChunk = 64;

@@ -542,17 +542,13 @@ hipError_t run(const DeltaProblem &p, hipStream_t s)
     return hipGetLastError();
 }
 
-template <typename T>
-hipError_t pick(const DeltaProblem &p, hipStream_t s)
-{
-    return p.Dk <= 64 ? run<T, 64>(p, s) : run<T, 128>(p, s);
-}
-
 }  // namespace
 
 hipError_t launch_delta_bwd(const DeltaProblem &p, hipStream_t s)
 {
-    return p.dtype == 0 ? pick<float>(p, s) : pick<bf16_t>(p, s);
+    if (p.dtype != 0)
+        return launch_delta16_bwd(p, s);
+    return p.Dk <= 64 ? run<float, 64>(p, s) : run<float, 128>(p, s);
 }
 
 }  // namespace gspn

@@ -445,18 +445,20 @@ hipError_t step(const DeltaProblem &p, hipStream_t s)
 constexpr int kFewTokens = 8;
 
 template <typename T>
-hipError_t pick(const DeltaProblem &p, hipStream_t s)
+hipError_t few(const DeltaProblem &p, hipStream_t s)
 {
-    if (!p.rs && p.T <= kFewTokens)
-        return p.Dk <= 64 ? step<T, 64>(p, s) : step<T, 128>(p, s);
-    return p.Dk <= 64 ? run<T, 64>(p, s) : run<T, 128>(p, s);
+    return p.Dk <= 64 ? step<T, 64>(p, s) : step<T, 128>(p, s);
 }
 
 }  // namespace
 
 hipError_t launch_delta_fwd(const DeltaProblem &p, hipStream_t s)
 {
-    return p.dtype == 0 ? pick<float>(p, s) : pick<bf16_t>(p, s);
+    if (!p.rs && p.T <= kFewTokens)
+        return p.dtype == 0 ? few<float>(p, s) : few<bf16_t>(p, s);
+    if (p.dtype != 0)
+        return launch_delta16_fwd(p, s);
+    return p.Dk <= 64 ? run<float, 64>(p, s) : run<float, 128>(p, s);
 }
 
 }  // namespace gspn

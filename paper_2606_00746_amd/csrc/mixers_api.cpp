@@ -266,7 +266,12 @@ int64_t delta_reserve(const DeltaProblem &p)
     Workspace rs;
     rs.counting = true;
     DeltaKept kept;
-    take_delta_kept(p, &rs, &kept);
+    DeltaProblem q = p;
+    q.rs = &rs;
+    if (p.dtype == GSPN_F32)
+        take_delta_kept(q, &rs, &kept);
+    else
+        delta16_reserve(q);
     return (int64_t)rs.used;
 }
 
