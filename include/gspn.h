@@ -390,8 +390,8 @@ int gspn_latent_params(const void *xc, const void *l_u, const void *l_lam,
  * and head strides in elements; NULL: all contiguous), lets it be a slice of a
  * fused projection or of a cache.  Strides of dimensions of size 1 are not
  * read.  Heads tensors have one storage type (fp32 or bf16), base pointers and
- * strides that are multiples of 16 bytes, and D a multiple of 8
- * (GSPN_ERR_ALIGN, GSPN_ERR_UNSUPPORTED).  int32 and fp32 arrays (lens, lse,
+ * strides that are multiples of 16 bytes, token strides up to 2^23, and D a
+ * multiple of 8 (GSPN_ERR_ALIGN, GSPN_ERR_UNSUPPORTED).  int32 and fp32 arrays (lens, lse,
  * positions) are contiguous and need their own alignment only.  Outputs may be
  * slices of one buffer's tokens (dq, dk and dv of one fused gradient); they
  * must not overlap anything otherwise (GSPN_ERR_ALIAS).  Arithmetic is fp32;

@@ -246,6 +246,13 @@ __device__ __forceinline__ void mma_turned(const char *lds, int row0, const Prob
         }
 }
 
+// A wide store reads its registers after issue: an asm behind it keeps them as they are.
+__device__ __forceinline__ void put16(void *p, u32x4 v)
+{
+    *reinterpret_cast<u32x4 *>(p) = v;
+    asm volatile("s_nop 7\n\ts_nop 7" : : "v"(v) : "memory");
+}
+
 // Stores a column (4 consecutive rows of a 32 x 32 result a register quad:
 // entries d .. d + 3 of one token) scaled by f.
 __device__ __forceinline__ void store4(bf16_t *p, float a, float b, float c, float d)
@@ -255,10 +262,7 @@ __device__ __forceinline__ void store4(bf16_t *p, float a, float b, float c, flo
 }
 __device__ __forceinline__ void store4(float *p, float a, float b, float c, float d)
 {
-    const u32x4 v = {__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)};
-    *reinterpret_cast<u32x4 *>(p) = v;
-    // a wide store reads its registers after issue: they stay as they are past it
-    asm volatile("s_nop 7\n\ts_nop 7" : : "v"(v) : "memory");
+    put16(p, u32x4{__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)});
 }
 template <typename T, int DP>
 __device__ __forceinline__ void store_column(T *row, const f32x16_t (&acc)[DP / 32], float f, int D)

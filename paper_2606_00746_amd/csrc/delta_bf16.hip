@@ -10,15 +10,14 @@
 // has three terms and its results differ from fp32 products' in the last bits;
 // what only goes into a bf16 output has two.
 //
-// The chunks of one head are a chain: X from S, U from X, S' from U.  A wave
-// holds 16 columns of the state and goes through the chain by itself, in
-// registers: the rows of a 16 x 16 result stand for the indexes
+// The chunks of one head are a chain: X from S, U from X, S' from U.  A workgroup
+// takes 16 columns of a state through it, each of its waves 32 rows of the state
+// and a share of the tokens.  The rows of a 16 x 16 result stand for the indexes
 //   32 g + 8 u + 4 blk + i    (register i of lane 16 u + c, blocks blk = 0, 1)
 // so that a pair of blocks holds 8 consecutive indexes in a lane, which is the B
 // operand of a product that contracts over them, and the 16-byte pieces of rows
-// are its A operands.  There is no LDS round trip and no barrier in the chain;
-// a wave's own piece of LDS turns K around for the last product.  The chain
-// leaves its states and U behind as such operands, 1 KB a wave and term.
+// are its A operands.  The chain leaves its states and U behind as such operands,
+// 1 KB a wave and term.
 #include <algorithm>
 
 #include "delta.hpp"
@@ -81,7 +80,7 @@ __device__ __forceinline__ void store_terms(uint4 *p, int64_t unit, int l, const
 {
 #pragma unroll
     for (int n = 0; n < N; ++n)
-        gst128(p + (unit * N + n) * 64 + l, __builtin_bit_cast(uint4, t.v[n]));
+        put16(p + (unit * N + n) * 64 + l, __builtin_bit_cast(u32x4, t.v[n]));
 }
 
 constexpr int kGateRows = 5;   // beta, beta exp(G), exp(G_63 - G), exp(G), G
@@ -190,162 +189,216 @@ __global__ __launch_bounds__(kThreads) void delta16_inverse_kernel(DeltaProblem 
         }
 }
 
-// A chunk's 64 rows of K (or Q) as A operands of products over Dk, and turned
-// around in LDS for products over the tokens.
-template <int DKP>
-struct KeyRows {
-    static constexpr int NG = DKP / 32;
-    using X = Tile<bf16_t, DKP>;
-    uint4 r[4][NG];
-    __device__ __forceinline__ void load(const bf16_t *k, int64_t st, int n, int Dk, int l)
+// A chunk's 64 rows of 32 columns of K (or Q), a wave's share: as A operands of
+// products over those columns, and in LDS, turned around, of products over the
+// tokens.  Rows past the sequence's end read as its last: what they are multiplied
+// with is 0.
+struct KeyShare {
+    using X = Tile<bf16_t, 32>;
+    uint4 r[4];
+    // base: the chunk's first row (uniform); st: row stride in elements; col: this
+    // lane's first column (read only where `in`: r starts as zeros)
+    __device__ __forceinline__ void load(const bf16_t *base, int64_t st, int n, int col, bool in, int l)
     {
-        const int c = l % 16, u = l / 16;
+        const int t0 = 8 * (l % 16 / 4) + l % 4;
+        if (!in)
+            return;
+        if (n >= kChunk) {
+            const uint32_t off = (uint32_t)(t0 * (int)st + col) * 2;
 #pragma unroll
-        for (int tb = 0; tb < 4; ++tb) {
-            const int t = index_of(tb, c);
+            for (int tb = 0; tb < 4; ++tb)
+                r[tb] = ld16(reinterpret_cast<const char *>(base + (32 * (tb / 2) + 4 * (tb & 1)) * st) + off);
+        } else {
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                r[tb][g] = make_uint4(0, 0, 0, 0);
-                if (t < n && 32 * g + 8 * u < Dk)
-                    r[tb][g] = ld16(k + t * st + 32 * g + 8 * u);
-            }
+            for (int tb = 0; tb < 4; ++tb)
+                r[tb] = ld16(base + min(32 * (tb / 2) + 4 * (tb & 1) + t0, n - 1) * st + col);
         }
     }
     __device__ __forceinline__ void store(char *lds, int l) const
     {
 #pragma unroll
         for (int tb = 0; tb < 4; ++tb)
-#pragma unroll
-            for (int g = 0; g < NG; ++g)
-                *reinterpret_cast<uint4 *>(lds + X::at(index_of(tb, l % 16), 4 * g + l / 16)) = r[tb][g];
+            *reinterpret_cast<uint4 *>(lds + X::at(index_of(tb, l % 16), l / 16)) = r[tb];
     }
-    // rows kb (indexes of Dk as index_of) of the transpose, tokens 32 g .. 32 g + 31
-    __device__ static __forceinline__ Terms<1> turned(const char *lds, int kb, int g, int l)
+    // block blk (of 16 of the 32 columns) of the transpose, tokens 32 g .. 32 g + 31
+    __device__ static __forceinline__ Terms<1> turned(const char *lds, int blk, int g, int l)
     {
-        const int i = l % 16, u = l / 16, piece = 4 * (kb / 2) + (i & 3), in = 8 * (kb & 1);
-        const int row = 32 * g + 8 * u + (i >> 2);
+        const int i = l % 16, row = 32 * g + 8 * (l / 16) + (i >> 2);
         struct {
             s16x4_t a, b;
-        } v = {read_turned(lds + X::at(row, piece) + in), read_turned(lds + X::at(row + 4, piece) + in)};
+        } v = {read_turned(lds + X::at(row, i & 3) + 8 * blk), read_turned(lds + X::at(row + 4, i & 3) + 8 * blk)};
         return Terms<1>{{__builtin_bit_cast(bf16x8_t, v)}};
     }
 };
 
-// U and the states: one wave, 16 columns, all chunks in turn.
-template <int DKP>
-__global__ __launch_bounds__(64, 1) void delta16_state_kernel(DeltaProblem p, Kept16 kept, int nc, int nv)
+// A chunk's results by blocks of 16 tokens, exchanged between the waves as B
+// operands of three terms: [group of 32 tokens][term][lane] of 16 bytes, of which
+// a block fills half.
+struct Exchange {
+    __attribute__((aligned(16))) char b[2 * 3 * 1024];
+    __device__ __forceinline__ void put(int tb, int l, f32x4_t v)
+    {
+        const Terms<3> t = split<3>(v, f32x4_t{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+        for (int n = 0; n < 3; ++n) {
+            const uint4 w = __builtin_bit_cast(uint4, t.v[n]);
+            *reinterpret_cast<uint2 *>(b + ((tb / 2 * 3 + n) * 64 + l) * 16 + 8 * (tb & 1)) = make_uint2(w.x, w.y);
+        }
+    }
+    __device__ __forceinline__ Terms<3> get(int g, int l) const
+    {
+        Terms<3> t;
+#pragma unroll
+        for (int n = 0; n < 3; ++n)
+            t.v[n] = __builtin_bit_cast(bf16x8_t, ld16(b + ((g * 3 + n) * 64 + l) * 16));
+        return t;
+    }
+};
+// The half of an operand of two terms that a block of tokens fills, to memory.
+__device__ __forceinline__ void store_half(uint4 *p, int64_t unit, int tb, int l, f32x4_t v)
 {
-    constexpr int NG = DKP / 32;
-    __shared__ __attribute__((aligned(16))) char lds[Tile<bf16_t, DKP>::kBytes];
+    const Terms<kKeep> t = split<kKeep>(v, f32x4_t{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+    for (int n = 0; n < kKeep; ++n) {
+        const uint4 w = __builtin_bit_cast(uint4, t.v[n]);
+        reinterpret_cast<uint2 *>(p + (unit * kKeep + n) * 64 + l)[tb & 1] = make_uint2(w.x, w.y);
+    }
+}
+
+// The chain's own tokens: the blocks that wave w of NW takes through the inverse,
+// paired so that the triangle's work is even.
+template <int NW>
+__device__ __forceinline__ int own_block(int w, int j)
+{
+    return j == 0 ? w : 3 - w;
+}
+
+// U and the states of 16 columns, all chunks in turn.  Wave w holds the rows
+// 32 w .. 32 w + 31 of the state, forms their share of K S, and takes the
+// blocks own_block of the tokens through X and U: the three exchanges are the
+// chain's length, its work is shared.
+template <int DKP>
+__global__ __launch_bounds__(DKP * 2) void delta16_state_kernel(DeltaProblem p, Kept16 kept, int nc, int nv)
+{
+    constexpr int NW = DKP / 32, NT = 4 / NW;
+    __shared__ __attribute__((aligned(16))) char kl[NW][KeyShare::X::kBytes];
+    __shared__ __attribute__((aligned(16))) f32x4_t part[NW][4][64];
+    __shared__ Exchange xl, ul;
     int id = xcd_remap(blockIdx.x, gridDim.x);
     const int sl = id % nv;
     id /= nv;
     const int hv = id % p.Hv, b = id / p.Hv;
-    const int l = threadIdx.x, c = l % 16, u = l / 16, col = 16 * sl + c;
-    const int len = delta_len(p, b);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x % 64, c = l % 16, u = l / 16;
+    const int col = 16 * sl + c, len = delta_len(p, b), live = (len + kChunk - 1) / kChunk;
     const bf16_t *k = static_cast<const bf16_t *>(p.k.p) + b * p.k.sb + (hv / (p.Hv / p.Hq)) * p.k.sh;
-    const bf16_t *v = static_cast<const bf16_t *>(p.v.p) + b * p.v.sb + hv * p.v.sh + col;
-    const bool in = col < p.Dv;
+    const bf16_t *v = static_cast<const bf16_t *>(p.v.p) + b * p.v.sb + hv * p.v.sh;
+    const bool in = col < p.Dv, kin = 32 * w + 8 * u < p.Dk;
     const int64_t head = (int64_t)b * p.Hv + hv;
 
-    f32x4_t S[2 * NG];
+    f32x4_t S[2];
 #pragma unroll
-    for (int kb = 0; kb < 2 * NG; ++kb)
+    for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = 32 * (kb / 2) + 8 * u + 4 * (kb & 1) + i;
-            S[kb][i] = p.state && r < p.Dk && in ? p.state[(head * p.Dk + r) * p.Dv + col] : 0.f;
+            const int r = 32 * w + 8 * u + 4 * blk + i;
+            S[blk][i] = p.state && r < p.Dk && in ? p.state[(head * p.Dk + r) * p.Dv + col] : 0.f;
         }
 
-    KeyRows<DKP> kr;
-    Terms<3> inv[kInvUnits];
-    uint32_t vr[4][4];
-    f32x4_t gb[4], ge[4], gl[4];
+    KeyShare kr{};
+    Terms<3> inv[NT][2];
+    uint32_t vr[NT][4] = {};
+    f32x4_t gb[NT], ge[NT], gl[NT];
+    float gk = 0.f;
+    int lane0 = 0;   // 0, but not to the compiler: a scalar load would be waited for with LDS
+    asm("" : "+v"(lane0));
     const auto fetch_k = [&](int ch) {
-        kr.load(k + (int64_t)ch * kChunk * p.k.st, p.k.st, len - ch * kChunk, p.Dk, l);
+        kr.load(k + (int64_t)ch * kChunk * p.k.st, p.k.st, len - ch * kChunk, 32 * w + 8 * u, kin, l);
     };
-    const auto fetch_v = [&](int ch) {
+    const auto fetch_rest = [&](int ch) {
         const float *g = kept.gates + (head * nc + ch) * kGateRows * kChunk;
+        const uint4 *m = kept.inv + (head * nc + ch) * (kInvUnits * 3 * 64);
+        gk = g[4 * kChunk - 1 + lane0];
 #pragma unroll
-        for (int tb = 0; tb < 4; ++tb) {
-            const int t = 32 * (tb / 2) + 8 * u + 4 * (tb & 1);
-            gb[tb] = load4(g + t);
-            ge[tb] = load4(g + kChunk + t);
-            gl[tb] = load4(g + 2 * kChunk + t);
+        for (int j = 0; j < NT; ++j) {
+            const int tb = own_block<NW>(w, j), t = 32 * (tb / 2) + 8 * u + 4 * (tb & 1);
+            gb[j] = load4(g + t);
+            ge[j] = load4(g + kChunk + t);
+            gl[j] = load4(g + 2 * kChunk + t);
+            inv[j][0] = load_terms<3>(m, inv_unit(tb, 0), l);
+            if (tb >= 2)
+                inv[j][1] = load_terms<3>(m, inv_unit(tb, 1), l);
+            if (in)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                vr[tb][i] = 0;
-                if (in && ch * kChunk + t + i < len)
-                    vr[tb][i] = v[(int64_t)(ch * kChunk + t + i) * p.v.st];
-            }
+                for (int i = 0; i < 4; ++i)
+                    vr[j][i] = v[(int64_t)min(ch * kChunk + t + i, len - 1) * p.v.st + col];
         }
     };
-    const auto fetch_inv = [&](int ch) {
-#pragma unroll
-        for (int i = 0; i < kInvUnits; ++i)
-            inv[i] = load_terms<3>(kept.inv + (head * nc + ch) * (kInvUnits * 3 * 64), i, l);
-    };
-    fetch_k(0);
-    fetch_v(0);
-    fetch_inv(0);
-    for (int ch = 0; ch < nc; ++ch) {
+    if (live > 0) {
+        fetch_k(0);
+        fetch_rest(0);
+    }
+    for (int ch = 0; ch < live; ++ch) {
         const int64_t at = head * nc + ch;
-        const float keep = kept.gates[at * kGateRows * kChunk + 3 * kChunk + kChunk - 1];
-        kr.store(lds, l);
-        f32x4_t x[4];
-#pragma unroll
-        for (int tb = 0; tb < 4; ++tb)
-            x[tb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            const Terms<3> s = split<3>(S[2 * g], S[2 * g + 1]);
-            store_terms<kKeep>(kept.s, (at * nv + sl) * NG + g, l, s);
+        const float keep = gk;
+        kr.store(kl[w], l);
+        {
+            const Terms<3> s = split<3>(S[0], S[1]);
+            store_terms<kKeep>(kept.s, (at * nv + sl) * NW + w, l, s);
 #pragma unroll
             for (int tb = 0; tb < 4; ++tb)
-                x[tb] = mma(one(kr.r[tb][g]), s, x[tb]);
+                part[w][tb][l] = mma(one(kr.r[tb]), s, f32x4_t{0.f, 0.f, 0.f, 0.f});
         }
-        if (ch + 1 < nc)
+        if (ch + 1 < live)
             fetch_k(ch + 1);
+        lds_barrier();
 #pragma unroll
-        for (int tb = 0; tb < 4; ++tb)
+        for (int j = 0; j < NT; ++j) {
+            const int tb = own_block<NW>(w, j);
+            f32x4_t x = part[0][tb][l];
+#pragma unroll
+            for (int n = 1; n < NW; ++n)
+                x += part[n][tb][l];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                x[tb][i] = gb[tb][i] * bf_lo(vr[tb][i]) - ge[tb][i] * x[tb][i];
-        f32x4_t scaled[4];
-        const Terms<3> x0 = split<3>(x[0], x[1]), x1 = split<3>(x[2], x[3]);
+                x[i] = gb[j][i] * bf_lo(vr[j][i]) - ge[j][i] * x[i];
+            xl.put(tb, l, x);
+        }
+        lds_barrier();
+        f32x4_t y[NT];
+        const Terms<3> x0 = xl.get(0, l), x1 = xl.get(1, l);
 #pragma unroll
-        for (int tb = 0; tb < 4; ++tb) {
-            f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-            y = mma(inv[inv_unit(tb, 0)], x0, y);
+        for (int j = 0; j < NT; ++j) {
+            const int tb = own_block<NW>(w, j);
+            y[j] = mma(inv[j][0], x0, f32x4_t{0.f, 0.f, 0.f, 0.f});
             if (tb >= 2)
-                y = mma(inv[inv_unit(tb, 1)], x1, y);
-            x[tb] = y;
-            scaled[tb] = gl[tb] * y;
+                y[j] = mma(inv[j][1], x1, y[j]);
+            ul.put(tb, l, gl[j] * y[j]);
         }
-        if (ch + 1 < nc) {
-            fetch_v(ch + 1);
-            fetch_inv(ch + 1);
+        if (ch + 1 < live)
+            fetch_rest(ch + 1);
+        lds_barrier();
+        const Terms<3> u0 = ul.get(0, l), u1 = ul.get(1, l);
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+            S[blk] *= keep;
+            S[blk] = mma(KeyShare::turned(kl[w], blk, 0, l), u0, S[blk]);
+            S[blk] = mma(KeyShare::turned(kl[w], blk, 1, l), u1, S[blk]);
         }
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
-            store_terms<kKeep>(kept.u, (at * nv + sl) * 2 + g, l, split<kKeep>(x[2 * g], x[2 * g + 1]));
-        const Terms<3> u0 = split<3>(scaled[0], scaled[1]), u1 = split<3>(scaled[2], scaled[3]);
-#pragma unroll
-        for (int kb = 0; kb < 2 * NG; ++kb) {
-            S[kb] *= keep;
-            S[kb] = mma(KeyRows<DKP>::turned(lds, kb, 0, l), u0, S[kb]);
-            S[kb] = mma(KeyRows<DKP>::turned(lds, kb, 1, l), u1, S[kb]);
+        for (int j = 0; j < NT; ++j) {
+            const int tb = own_block<NW>(w, j);
+            store_half(kept.u, (at * nv + sl) * 2 + tb / 2, tb, l, y[j]);
         }
         __builtin_amdgcn_wave_barrier();
     }
     if (p.state_out && in)
 #pragma unroll
-        for (int kb = 0; kb < 2 * NG; ++kb)
+        for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int r = 32 * (kb / 2) + 8 * u + 4 * (kb & 1) + i;
+                const int r = 32 * w + 8 * u + 4 * blk + i;
                 if (r < p.Dk)
-                    p.state_out[(head * p.Dk + r) * p.Dv + col] = S[kb][i];
+                    p.state_out[(head * p.Dk + r) * p.Dv + col] = S[blk][i];
             }
 }
 
@@ -400,6 +453,14 @@ __global__ __launch_bounds__(kThreads) void delta16_out_kernel(DeltaProblem p, K
     const int64_t at = ((int64_t)b * p.Hv + hv) * nc + ch;
     const float *gates = kept.gates + at * kGateRows * kChunk;
 
+    if (n == 0) {   // past the sequence's end: nothing was left for it
+        for (int x = threadIdx.x; x < kChunk * p.Dv / 4; x += kThreads) {
+            const int t = x / (p.Dv / 4), d = x % (p.Dv / 4) * 4;
+            if (t0 + t < p.T)
+                store4(o + t * p.o.st + d, 0.f, 0.f, 0.f, 0.f);
+        }
+        return;
+    }
     uint4 qr[4][NG];
 #pragma unroll
     for (int tb = 0; tb < 4; ++tb)
@@ -488,6 +549,8 @@ __global__ __launch_bounds__(kThreads) void delta16_du_kernel(DeltaProblem p, Ke
     const int64_t at = ((int64_t)b * p.Hv + hv) * nc + ch;
     const float *gates = kept.gates + at * kGateRows * kChunk;
 
+    if (n == 0)
+        return;
     X x;
     x.load(d, p.dout.st, 0, n, p.Dv);
     {   // P[t][s] as rows of s, for the 16 columns s of block w
@@ -537,139 +600,162 @@ __global__ __launch_bounds__(kThreads) void delta16_du_kernel(DeltaProblem p, Ke
     }
 }
 
-// R, dV and the gradients of the states: one wave, 16 columns, the chunks from
-// the last on.
+// R, dV and the gradients of the states of 16 columns, the chunks from the last
+// on; shared among the waves like delta16_state_kernel.
 template <int DKP>
-__global__ __launch_bounds__(64, 1) void delta16_dstate_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv)
+__global__ __launch_bounds__(DKP * 2) void delta16_dstate_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv)
 {
-    constexpr int NG = DKP / 32;
-    using X = Tile<bf16_t, DKP>;
-    __shared__ __attribute__((aligned(16))) char kl[X::kBytes], ql[X::kBytes];
+    constexpr int NW = DKP / 32, NT = 4 / NW;
+    __shared__ __attribute__((aligned(16))) char kl[NW][KeyShare::X::kBytes], ql[NW][KeyShare::X::kBytes];
+    __shared__ __attribute__((aligned(16))) f32x4_t part[NW][4][64];
+    __shared__ Exchange xl, zl, yl;
     int id = xcd_remap(blockIdx.x, gridDim.x);
     const int sl = id % nv;
     id /= nv;
     const int hv = id % p.Hv, b = id / p.Hv, hq = hv / (p.Hv / p.Hq);
-    const int l = threadIdx.x, c = l % 16, u = l / 16, col = 16 * sl + c;
-    const int len = delta_len(p, b);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x % 64, c = l % 16, u = l / 16;
+    const int col = 16 * sl + c, len = delta_len(p, b), live = (len + kChunk - 1) / kChunk;
     const bf16_t *q = static_cast<const bf16_t *>(p.q.p) + b * p.q.sb + hq * p.q.sh;
     const bf16_t *k = static_cast<const bf16_t *>(p.k.p) + b * p.k.sb + hq * p.k.sh;
-    const bf16_t *d = static_cast<const bf16_t *>(p.dout.p) + b * p.dout.sb + hv * p.dout.sh + col;
+    const bf16_t *d = static_cast<const bf16_t *>(p.dout.p) + b * p.dout.sb + hv * p.dout.sh;
     bf16_t *dv = static_cast<bf16_t *>(p.dv.p) + b * p.dv.sb + hv * p.dv.sh + col;
-    const bool in = col < p.Dv;
+    const bool in = col < p.Dv, kin = 32 * w + 8 * u < p.Dk;
     const int64_t head = (int64_t)b * p.Hv + hv;
 
-    f32x4_t S[2 * NG];
+    f32x4_t S[2];
 #pragma unroll
-    for (int kb = 0; kb < 2 * NG; ++kb)
+    for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = 32 * (kb / 2) + 8 * u + 4 * (kb & 1) + i;
-            S[kb][i] = p.dstate && r < p.Dk && in ? p.dstate[(head * p.Dk + r) * p.Dv + col] : 0.f;
+            const int r = 32 * w + 8 * u + 4 * blk + i;
+            S[blk][i] = p.dstate && r < p.Dk && in ? p.dstate[(head * p.Dk + r) * p.Dv + col] : 0.f;
         }
 
-    KeyRows<DKP> kr, qr;
-    Terms<3> inv[kInvUnits];
-    uint32_t dr[4][4];
-    f32x4_t gb[4], ge[4], gl[4], gq[4], du[4];
+    KeyShare kr{}, qr{};
+    Terms<3> inv[NT][2];
+    uint32_t dr[NT][4] = {};
+    f32x4_t gb[NT], ge[NT], gl[NT], gq[NT], du[NT];
+    float gk = 0.f;
+    int lane0 = 0;   // as in delta16_state_kernel
+    asm("" : "+v"(lane0));
     const auto fetch_k = [&](int ch) {
-        kr.load(k + (int64_t)ch * kChunk * p.k.st, p.k.st, len - ch * kChunk, p.Dk, l);
-        qr.load(q + (int64_t)ch * kChunk * p.q.st, p.q.st, len - ch * kChunk, p.Dk, l);
+        const int n = len - ch * kChunk;
+        kr.load(k + (int64_t)ch * kChunk * p.k.st, p.k.st, n, 32 * w + 8 * u, kin, l);
+        qr.load(q + (int64_t)ch * kChunk * p.q.st, p.q.st, n, 32 * w + 8 * u, kin, l);
     };
-    const auto fetch_d = [&](int ch) {
+    const auto fetch_rest = [&](int ch) {
         const int64_t at = head * nc + ch;
         const float *g = kept.gates + at * kGateRows * kChunk;
+        const uint4 *m = kept.turned + at * (kInvUnits * 3 * 64);
+        gk = g[4 * kChunk - 1 + lane0];
 #pragma unroll
-        for (int tb = 0; tb < 4; ++tb) {
-            const int t = 32 * (tb / 2) + 8 * u + 4 * (tb & 1);
-            gb[tb] = load4(g + t);
-            ge[tb] = load4(g + kChunk + t);
-            gl[tb] = load4(g + 2 * kChunk + t);
-            gq[tb] = load4(g + 3 * kChunk + t);
-            du[tb] = load4(gr.du + (((at * nv + sl) * 4 + tb) * 64 + l) * 4);
+        for (int j = 0; j < NT; ++j) {
+            const int tb = own_block<NW>(w, j), t = 32 * (tb / 2) + 8 * u + 4 * (tb & 1);
+            gb[j] = load4(g + t);
+            ge[j] = load4(g + kChunk + t);
+            gl[j] = load4(g + 2 * kChunk + t);
+            gq[j] = load4(g + 3 * kChunk + t);
+            du[j] = load4(gr.du + (((at * nv + sl) * 4 + tb) * 64 + l) * 4);
+            if (tb < 2)
+                inv[j][0] = load_terms<3>(m, turned_unit(tb, 0), l);
+            inv[j][1] = load_terms<3>(m, turned_unit(tb, 1), l);
+            if (in)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                dr[tb][i] = 0;
-                if (in && ch * kChunk + t + i < len)
-                    dr[tb][i] = d[(int64_t)(ch * kChunk + t + i) * p.dout.st];
-            }
+                for (int i = 0; i < 4; ++i)
+                    dr[j][i] = d[(int64_t)min(ch * kChunk + t + i, len - 1) * p.dout.st + col];
         }
     };
-    const auto fetch_inv = [&](int ch) {
-#pragma unroll
-        for (int i = 0; i < kInvUnits; ++i)
-            inv[i] = load_terms<3>(kept.turned + (head * nc + ch) * (kInvUnits * 3 * 64), i, l);
-    };
-    fetch_k(nc - 1);
-    fetch_d(nc - 1);
-    fetch_inv(nc - 1);
-    for (int ch = nc - 1; ch >= 0; --ch) {
+    if (live > 0) {
+        fetch_k(live - 1);
+        fetch_rest(live - 1);
+    }
+    for (int ch = live - 1; ch >= 0; --ch) {
         const int64_t at = head * nc + ch;
-        const float keep = kept.gates[at * kGateRows * kChunk + 3 * kChunk + kChunk - 1];
-        kr.store(kl, l);
-        qr.store(ql, l);
-        f32x4_t x[4];
-#pragma unroll
-        for (int tb = 0; tb < 4; ++tb)
-            x[tb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            const Terms<3> s = split<3>(S[2 * g], S[2 * g + 1]);
-            store_terms<kKeep>(gr.ds, (at * nv + sl) * NG + g, l, s);
+        const int n = len - ch * kChunk;
+        const float keep = gk;
+        kr.store(kl[w], l);
+        qr.store(ql[w], l);
+        {
+            const Terms<3> s = split<3>(S[0], S[1]);
+            store_terms<kKeep>(gr.ds, (at * nv + sl) * NW + w, l, s);
 #pragma unroll
             for (int tb = 0; tb < 4; ++tb)
-                x[tb] = mma(one(kr.r[tb][g]), s, x[tb]);
+                part[w][tb][l] = mma(one(kr.r[tb]), s, f32x4_t{0.f, 0.f, 0.f, 0.f});
         }
         if (ch > 0)
             fetch_k(ch - 1);
+        // dO's share of the states' gradient needs nothing from the chain
 #pragma unroll
-        for (int tb = 0; tb < 4; ++tb)
-            x[tb] = du[tb] + gl[tb] * x[tb];
-        f32x4_t z[4], y[4];
-        const Terms<3> x0 = split<3>(x[0], x[1]), x1 = split<3>(x[2], x[3]);
+        for (int j = 0; j < NT; ++j) {
+            const int tb = own_block<NW>(w, j), t = 32 * (tb / 2) + 8 * u + 4 * (tb & 1);
+            f32x4_t y;
 #pragma unroll
-        for (int tb = 0; tb < 4; ++tb) {
-            f32x4_t a = {0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < 4; ++i)
+                y[i] = t + i < n ? p.scale * gq[j][i] * bf_lo(dr[j][i]) : 0.f;
+            yl.put(tb, l, y);
+        }
+        lds_barrier();
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int tb = own_block<NW>(w, j), t = 32 * (tb / 2) + 8 * u + 4 * (tb & 1);
+            f32x4_t x = part[0][tb][l];
+#pragma unroll
+            for (int m = 1; m < NW; ++m)
+                x += part[m][tb][l];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                x[i] = t + i < n ? du[j][i] + gl[j][i] * x[i] : 0.f;
+            xl.put(tb, l, x);
+        }
+        lds_barrier();
+        f32x4_t r[NT];
+        const Terms<3> x0 = xl.get(0, l), x1 = xl.get(1, l);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int tb = own_block<NW>(w, j), t = 32 * (tb / 2) + 8 * u + 4 * (tb & 1);
+            r[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             if (tb < 2)
-                a = mma(inv[turned_unit(tb, 0)], x0, a);
-            a = mma(inv[turned_unit(tb, 1)], x1, a);
-            x[tb] = a;
-            const int t = ch * kChunk + 32 * (tb / 2) + 8 * u + 4 * (tb & 1);
+                r[j] = mma(inv[j][0], x0, r[j]);
+            r[j] = mma(inv[j][1], x1, r[j]);
+            zl.put(tb, l, -(ge[j] * r[j]));
+            if (in)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (in && t + i < p.T)
-                    store_f(dv + (int64_t)(t + i) * p.dv.st, gb[tb][i] * a[i]);
-                y[tb][i] = p.scale * gq[tb][i] * bf_lo(dr[tb][i]);
-            }
-            z[tb] = -(ge[tb] * a);
+                for (int i = 0; i < 4; ++i)
+                    if (t + i < n)
+                        store_f(dv + (int64_t)(ch * kChunk + t + i) * p.dv.st, gb[j][i] * r[j][i]);
         }
-        if (ch > 0) {
-            fetch_d(ch - 1);
-            fetch_inv(ch - 1);
+        if (ch > 0)
+            fetch_rest(ch - 1);
+        lds_barrier();
+        const Terms<3> z0 = zl.get(0, l), z1 = zl.get(1, l), y0 = yl.get(0, l), y1 = yl.get(1, l);
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+            S[blk] *= keep;
+            S[blk] = mma(KeyShare::turned(ql[w], blk, 0, l), y0, S[blk]);
+            S[blk] = mma(KeyShare::turned(ql[w], blk, 1, l), y1, S[blk]);
+            S[blk] = mma(KeyShare::turned(kl[w], blk, 0, l), z0, S[blk]);
+            S[blk] = mma(KeyShare::turned(kl[w], blk, 1, l), z1, S[blk]);
         }
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
-            store_terms<kKeep>(gr.r, (at * nv + sl) * 2 + g, l, split<kKeep>(x[2 * g], x[2 * g + 1]));
-        const Terms<3> z0 = split<3>(z[0], z[1]), z1 = split<3>(z[2], z[3]);
-        const Terms<3> y0 = split<3>(y[0], y[1]), y1 = split<3>(y[2], y[3]);
-#pragma unroll
-        for (int kb = 0; kb < 2 * NG; ++kb) {
-            S[kb] *= keep;
-            S[kb] = mma(KeyRows<DKP>::turned(kl, kb, 0, l), z0, S[kb]);
-            S[kb] = mma(KeyRows<DKP>::turned(kl, kb, 1, l), z1, S[kb]);
-            S[kb] = mma(KeyRows<DKP>::turned(ql, kb, 0, l), y0, S[kb]);
-            S[kb] = mma(KeyRows<DKP>::turned(ql, kb, 1, l), y1, S[kb]);
+        for (int j = 0; j < NT; ++j) {
+            const int tb = own_block<NW>(w, j);
+            store_half(gr.r, (at * nv + sl) * 2 + tb / 2, tb, l, r[j]);
         }
-        __builtin_amdgcn_wave_barrier();
+        lds_barrier();   // yl is written ahead of the next chunk's first exchange
     }
     if (p.dstate_in && in)
 #pragma unroll
-        for (int kb = 0; kb < 2 * NG; ++kb)
+        for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int r = 32 * (kb / 2) + 8 * u + 4 * (kb & 1) + i;
-                if (r < p.Dk)
-                    p.dstate_in[(head * p.Dk + r) * p.Dv + col] = S[kb][i];
+                const int rr = 32 * w + 8 * u + 4 * blk + i;
+                if (rr < p.Dk)
+                    p.dstate_in[(head * p.Dk + rr) * p.Dv + col] = S[blk][i];
             }
+    // tokens that no chunk above has
+    for (int64_t t = len + threadIdx.x / 16; t < p.T; t += DKP * 2 / 16)
+        if (in)
+            store_f(dv + t * p.dv.st, 0.f);
 }
 
 __device__ __forceinline__ float over_c(float v)   // over the 16 lanes of one u
@@ -740,6 +826,24 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
     const int t0 = ch * kChunk, n = max(0, min(kChunk, delta_len(p, b) - t0));
     const bf16_t *q = static_cast<const bf16_t *>(p.q.p) + b * p.q.sb + hq * p.q.sh + (int64_t)t0 * p.q.st;
     const bf16_t *k = static_cast<const bf16_t *>(p.k.p) + b * p.k.sb + hq * p.k.sh + (int64_t)t0 * p.k.st;
+    bf16_t *dqo = static_cast<bf16_t *>(p.dq.p) + b * p.dq.sb + hq * p.dq.sh + (int64_t)t0 * p.dq.st;
+    bf16_t *dko = static_cast<bf16_t *>(p.dk.p) + b * p.dk.sb + hq * p.dk.sh + (int64_t)t0 * p.dk.st;
+    if (n == 0) {   // past the sequence's end
+        for (int x = threadIdx.x; x < kChunk * p.Dk / 4; x += kThreads) {
+            const int t = x / (p.Dk / 4), m = x % (p.Dk / 4) * 4;
+            if (t0 + t < p.T) {
+                store4(dqo + t * p.dq.st + m, 0.f, 0.f, 0.f, 0.f);
+                store4(dko + t * p.dk.st + m, 0.f, 0.f, 0.f, 0.f);
+            }
+        }
+        for (int x = threadIdx.x; x < kChunk * rep; x += kThreads)
+            if (t0 + x / rep < p.T) {
+                const int64_t to = ((int64_t)b * p.T + t0 + x / rep) * p.Hv + hq * rep + x % rep;
+                store_f(static_cast<bf16_t *>(p.dg) + to, 0.f);
+                store_f(static_cast<bf16_t *>(p.dbeta) + to, 0.f);
+            }
+        return;
+    }
     {
         X a, e;
         a.load(q, p.q.st, 0, n, p.Dk);
@@ -991,8 +1095,6 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
                 }
             }
     }
-    bf16_t *dqo = static_cast<bf16_t *>(p.dq.p) + b * p.dq.sb + hq * p.dq.sh + (int64_t)t0 * p.dq.st;
-    bf16_t *dko = static_cast<bf16_t *>(p.dk.p) + b * p.dk.sb + hq * p.dk.sh + (int64_t)t0 * p.dk.st;
 #pragma unroll
     for (int j = 0; j < NB; ++j)
 #pragma unroll
@@ -1036,7 +1138,7 @@ hipError_t fwd(const DeltaProblem &p, hipStream_t s)
     if (e == hipSuccess)
         e = p.ws->take(&inv, (size_t)(heads * nc * kInvUnits * 3 * 1024));
     kept.inv = static_cast<uint4 *>(inv);
-    if (heads * nc * kThreads > kMaxThreads || heads * nv * 64 > kMaxThreads)
+    if (heads * nc * kThreads > kMaxThreads || heads * nv * DKP * 2 > kMaxThreads)
         return hipErrorInvalidConfiguration;
     if (e != hipSuccess || p.ws->counting)
         return e;
@@ -1044,7 +1146,7 @@ hipError_t fwd(const DeltaProblem &p, hipStream_t s)
     e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    delta16_state_kernel<DKP><<<dim3((unsigned)(heads * nv)), 64, 0, s>>>(p, kept, nc, nv);
+    delta16_state_kernel<DKP><<<dim3((unsigned)(heads * nv)), DKP * 2, 0, s>>>(p, kept, nc, nv);
     e = hipGetLastError();
     if (e != hipSuccess)
         return e;
@@ -1066,7 +1168,7 @@ hipError_t bwd(const DeltaProblem &p, hipStream_t s)
         e = p.ws->take(&r, (size_t)(n * nv * 2 * kKeep * 1024));
     if (e == hipSuccess)
         e = p.ws->take(&ds, (size_t)(n * nv * (DKP / 32) * kKeep * 1024));
-    if (n * kThreads > kMaxThreads || heads * nv * 64 > kMaxThreads)
+    if (n * kThreads > kMaxThreads || heads * nv * DKP * 2 > kMaxThreads)
         return hipErrorInvalidConfiguration;
     if (e != hipSuccess || p.ws->counting)
         return e;
@@ -1078,7 +1180,7 @@ hipError_t bwd(const DeltaProblem &p, hipStream_t s)
     e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    delta16_dstate_kernel<DKP><<<dim3((unsigned)(heads * nv)), 64, 0, s>>>(p, kept, g, nc, nv);
+    delta16_dstate_kernel<DKP><<<dim3((unsigned)(heads * nv)), DKP * 2, 0, s>>>(p, kept, g, nc, nv);
     e = hipGetLastError();
     if (e != hipSuccess)
         return e;

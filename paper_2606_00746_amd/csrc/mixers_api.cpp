@@ -88,9 +88,10 @@ struct Buffers {
             fail(GSPN_ERR_NULL);
             return h;
         }
-        constexpr int64_t kMost = (int64_t)1 << 44;
+        // token strides: 64 rows of any tile are within 32-bit offsets of its first
+        constexpr int64_t kMost = (int64_t)1 << 44, kMostStep = (int64_t)1 << 23;
         if (h.sh < 0 || h.st < 0 || h.sb < 0 || h.sh > kMost || h.st > kMost || h.sb > kMost / std::max<int64_t>(1, B) ||
-            h.st > kMost / T) {
+            h.st > kMostStep) {
             fail(GSPN_ERR_UNSUPPORTED);
             return h;
         }
