@@ -265,6 +265,25 @@ __device__ __forceinline__ void store_half(uint4 *p, int64_t unit, int tb, int l
     }
 }
 
+// This lane's column of four consecutive tokens 8 u + t .. of a chunk (t uniform);
+// tokens past the sequence's end read as its last.
+__device__ __forceinline__ void load_column(uint32_t (&r)[4], const bf16_t *base, int64_t st, int t, int n, int col,
+                                            bool in, int u)
+{
+    if (!in)
+        return;
+    if (n >= kChunk) {
+        const uint32_t off = (uint32_t)(8 * u * (int)st + col) * 2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            r[i] = *reinterpret_cast<const bf16_t *>(reinterpret_cast<const char *>(base + (t + i) * st) + off);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            r[i] = base[(int64_t)min(8 * u + t + i, n - 1) * st + col];
+    }
+}
+
 // The chain's own tokens: the blocks that wave w of NW takes through the inverse,
 // paired so that the triangle's work is even.
 template <int NW>
@@ -304,52 +323,46 @@ __global__ __launch_bounds__(DKP * 2) void delta16_state_kernel(DeltaProblem p, 
             S[blk][i] = p.state && r < p.Dk && in ? p.state[(head * p.Dk + r) * p.Dv + col] : 0.f;
         }
 
-    KeyShare kr{};
-    Terms<3> inv[NT][2];
-    uint32_t vr[NT][4] = {};
-    f32x4_t gb[NT], ge[NT], gl[NT];
-    float gk = 0.f;
+    // what a chunk reads beside the state: loaded a chunk ahead of its use
+    struct Ahead {
+        KeyShare kr;
+        Terms<3> inv[NT][2];
+        uint32_t vr[NT][4];
+        f32x4_t gb[NT], ge[NT], gl[NT];
+        float gk;
+    } even{}, odd{};
     int lane0 = 0;   // 0, but not to the compiler: a scalar load would be waited for with LDS
     asm("" : "+v"(lane0));
-    const auto fetch_k = [&](int ch) {
-        kr.load(k + (int64_t)ch * kChunk * p.k.st, p.k.st, len - ch * kChunk, 32 * w + 8 * u, kin, l);
-    };
-    const auto fetch_rest = [&](int ch) {
+    const auto fetch = [&](int ch, Ahead &x) {
+        const int n = len - ch * kChunk;
         const float *g = kept.gates + (head * nc + ch) * kGateRows * kChunk;
         const uint4 *m = kept.inv + (head * nc + ch) * (kInvUnits * 3 * 64);
-        gk = g[4 * kChunk - 1 + lane0];
+        x.kr.load(k + (int64_t)ch * kChunk * p.k.st, p.k.st, n, 32 * w + 8 * u, kin, l);
+        x.gk = g[4 * kChunk - 1 + lane0];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const int tb = own_block<NW>(w, j), t = 32 * (tb / 2) + 8 * u + 4 * (tb & 1);
-            gb[j] = load4(g + t);
-            ge[j] = load4(g + kChunk + t);
-            gl[j] = load4(g + 2 * kChunk + t);
-            inv[j][0] = load_terms<3>(m, inv_unit(tb, 0), l);
+            const int tb = own_block<NW>(w, j), t = 32 * (tb / 2) + 4 * (tb & 1);
+            load_column(x.vr[j], v + (int64_t)ch * kChunk * p.v.st, p.v.st, t, n, col, in, u);
+            x.gb[j] = load4(g + t + 8 * u);
+            x.ge[j] = load4(g + kChunk + t + 8 * u);
+            x.gl[j] = load4(g + 2 * kChunk + t + 8 * u);
+            x.inv[j][0] = load_terms<3>(m, inv_unit(tb, 0), l);
             if (tb >= 2)
-                inv[j][1] = load_terms<3>(m, inv_unit(tb, 1), l);
-            if (in)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    vr[j][i] = v[(int64_t)min(ch * kChunk + t + i, len - 1) * p.v.st + col];
+                x.inv[j][1] = load_terms<3>(m, inv_unit(tb, 1), l);
         }
     };
-    if (live > 0) {
-        fetch_k(0);
-        fetch_rest(0);
-    }
-    for (int ch = 0; ch < live; ++ch) {
+    const auto chunk = [&](int ch, Ahead &now, Ahead &next) {
         const int64_t at = head * nc + ch;
-        const float keep = gk;
-        kr.store(kl[w], l);
+        if (ch + 1 < live)
+            fetch(ch + 1, next);
+        now.kr.store(kl[w], l);
         {
             const Terms<3> s = split<3>(S[0], S[1]);
-            store_terms<kKeep>(kept.s, (at * nv + sl) * NW + w, l, s);
 #pragma unroll
             for (int tb = 0; tb < 4; ++tb)
-                part[w][tb][l] = mma(one(kr.r[tb]), s, f32x4_t{0.f, 0.f, 0.f, 0.f});
+                part[w][tb][l] = mma(one(now.kr.r[tb]), s, f32x4_t{0.f, 0.f, 0.f, 0.f});
+            store_terms<kKeep>(kept.s, (at * nv + sl) * NW + w, l, s);
         }
-        if (ch + 1 < live)
-            fetch_k(ch + 1);
         lds_barrier();
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
@@ -360,7 +373,7 @@ __global__ __launch_bounds__(DKP * 2) void delta16_state_kernel(DeltaProblem p, 
                 x += part[n][tb][l];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                x[i] = gb[j][i] * bf_lo(vr[j][i]) - ge[j][i] * x[i];
+                x[i] = now.gb[j][i] * bf_lo(now.vr[j][i]) - now.ge[j][i] * x[i];
             xl.put(tb, l, x);
         }
         lds_barrier();
@@ -369,18 +382,16 @@ __global__ __launch_bounds__(DKP * 2) void delta16_state_kernel(DeltaProblem p, 
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             const int tb = own_block<NW>(w, j);
-            y[j] = mma(inv[j][0], x0, f32x4_t{0.f, 0.f, 0.f, 0.f});
+            y[j] = mma(now.inv[j][0], x0, f32x4_t{0.f, 0.f, 0.f, 0.f});
             if (tb >= 2)
-                y[j] = mma(inv[j][1], x1, y[j]);
-            ul.put(tb, l, gl[j] * y[j]);
+                y[j] = mma(now.inv[j][1], x1, y[j]);
+            ul.put(tb, l, now.gl[j] * y[j]);
         }
-        if (ch + 1 < live)
-            fetch_rest(ch + 1);
         lds_barrier();
         const Terms<3> u0 = ul.get(0, l), u1 = ul.get(1, l);
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk) {
-            S[blk] *= keep;
+            S[blk] *= now.gk;
             S[blk] = mma(KeyShare::turned(kl[w], blk, 0, l), u0, S[blk]);
             S[blk] = mma(KeyShare::turned(kl[w], blk, 1, l), u1, S[blk]);
         }
@@ -390,6 +401,13 @@ __global__ __launch_bounds__(DKP * 2) void delta16_state_kernel(DeltaProblem p, 
             store_half(kept.u, (at * nv + sl) * 2 + tb / 2, tb, l, y[j]);
         }
         __builtin_amdgcn_wave_barrier();
+    };
+    if (live > 0)
+        fetch(0, even);
+    for (int ch = 0; ch < live; ch += 2) {
+        chunk(ch, even, odd);
+        if (ch + 1 < live)
+            chunk(ch + 1, odd, even);
     }
     if (p.state_out && in)
 #pragma unroll
@@ -631,59 +649,51 @@ __global__ __launch_bounds__(DKP * 2) void delta16_dstate_kernel(DeltaProblem p,
             S[blk][i] = p.dstate && r < p.Dk && in ? p.dstate[(head * p.Dk + r) * p.Dv + col] : 0.f;
         }
 
-    KeyShare kr{}, qr{};
-    Terms<3> inv[NT][2];
-    uint32_t dr[NT][4] = {};
-    f32x4_t gb[NT], ge[NT], gl[NT], gq[NT], du[NT];
-    float gk = 0.f;
-    int lane0 = 0;   // as in delta16_state_kernel
+    struct Ahead {   // as in delta16_state_kernel
+        KeyShare kr, qr;
+        Terms<3> inv[NT][2];
+        uint32_t dr[NT][4];
+        f32x4_t gb[NT], ge[NT], gl[NT], gq[NT], du[NT];
+        float gk;
+    } even{}, odd{};
+    int lane0 = 0;
     asm("" : "+v"(lane0));
-    const auto fetch_k = [&](int ch) {
-        const int n = len - ch * kChunk;
-        kr.load(k + (int64_t)ch * kChunk * p.k.st, p.k.st, n, 32 * w + 8 * u, kin, l);
-        qr.load(q + (int64_t)ch * kChunk * p.q.st, p.q.st, n, 32 * w + 8 * u, kin, l);
-    };
-    const auto fetch_rest = [&](int ch) {
+    const auto fetch = [&](int ch, Ahead &x) {
         const int64_t at = head * nc + ch;
+        const int n = len - ch * kChunk;
         const float *g = kept.gates + at * kGateRows * kChunk;
         const uint4 *m = kept.turned + at * (kInvUnits * 3 * 64);
-        gk = g[4 * kChunk - 1 + lane0];
+        x.kr.load(k + (int64_t)ch * kChunk * p.k.st, p.k.st, n, 32 * w + 8 * u, kin, l);
+        x.qr.load(q + (int64_t)ch * kChunk * p.q.st, p.q.st, n, 32 * w + 8 * u, kin, l);
+        x.gk = g[4 * kChunk - 1 + lane0];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const int tb = own_block<NW>(w, j), t = 32 * (tb / 2) + 8 * u + 4 * (tb & 1);
-            gb[j] = load4(g + t);
-            ge[j] = load4(g + kChunk + t);
-            gl[j] = load4(g + 2 * kChunk + t);
-            gq[j] = load4(g + 3 * kChunk + t);
-            du[j] = load4(gr.du + (((at * nv + sl) * 4 + tb) * 64 + l) * 4);
+            const int tb = own_block<NW>(w, j), t = 32 * (tb / 2) + 4 * (tb & 1);
+            load_column(x.dr[j], d + (int64_t)ch * kChunk * p.dout.st, p.dout.st, t, n, col, in, u);
+            x.gb[j] = load4(g + t + 8 * u);
+            x.ge[j] = load4(g + kChunk + t + 8 * u);
+            x.gl[j] = load4(g + 2 * kChunk + t + 8 * u);
+            x.gq[j] = load4(g + 3 * kChunk + t + 8 * u);
+            x.du[j] = load4(gr.du + (((at * nv + sl) * 4 + tb) * 64 + l) * 4);
             if (tb < 2)
-                inv[j][0] = load_terms<3>(m, turned_unit(tb, 0), l);
-            inv[j][1] = load_terms<3>(m, turned_unit(tb, 1), l);
-            if (in)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    dr[j][i] = d[(int64_t)min(ch * kChunk + t + i, len - 1) * p.dout.st + col];
+                x.inv[j][0] = load_terms<3>(m, turned_unit(tb, 0), l);
+            x.inv[j][1] = load_terms<3>(m, turned_unit(tb, 1), l);
         }
     };
-    if (live > 0) {
-        fetch_k(live - 1);
-        fetch_rest(live - 1);
-    }
-    for (int ch = live - 1; ch >= 0; --ch) {
+    const auto chunk = [&](int ch, Ahead &now, Ahead &next) {
         const int64_t at = head * nc + ch;
         const int n = len - ch * kChunk;
-        const float keep = gk;
-        kr.store(kl[w], l);
-        qr.store(ql[w], l);
+        if (ch > 0)
+            fetch(ch - 1, next);
+        now.kr.store(kl[w], l);
+        now.qr.store(ql[w], l);
         {
             const Terms<3> s = split<3>(S[0], S[1]);
-            store_terms<kKeep>(gr.ds, (at * nv + sl) * NW + w, l, s);
 #pragma unroll
             for (int tb = 0; tb < 4; ++tb)
-                part[w][tb][l] = mma(one(kr.r[tb]), s, f32x4_t{0.f, 0.f, 0.f, 0.f});
+                part[w][tb][l] = mma(one(now.kr.r[tb]), s, f32x4_t{0.f, 0.f, 0.f, 0.f});
+            store_terms<kKeep>(gr.ds, (at * nv + sl) * NW + w, l, s);
         }
-        if (ch > 0)
-            fetch_k(ch - 1);
         // dO's share of the states' gradient needs nothing from the chain
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
@@ -691,7 +701,7 @@ __global__ __launch_bounds__(DKP * 2) void delta16_dstate_kernel(DeltaProblem p,
             f32x4_t y;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                y[i] = t + i < n ? p.scale * gq[j][i] * bf_lo(dr[j][i]) : 0.f;
+                y[i] = t + i < n ? p.scale * now.gq[j][i] * bf_lo(now.dr[j][i]) : 0.f;
             yl.put(tb, l, y);
         }
         lds_barrier();
@@ -704,7 +714,7 @@ __global__ __launch_bounds__(DKP * 2) void delta16_dstate_kernel(DeltaProblem p,
                 x += part[m][tb][l];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                x[i] = t + i < n ? du[j][i] + gl[j][i] * x[i] : 0.f;
+                x[i] = t + i < n ? now.du[j][i] + now.gl[j][i] * x[i] : 0.f;
             xl.put(tb, l, x);
         }
         lds_barrier();
@@ -712,25 +722,18 @@ __global__ __launch_bounds__(DKP * 2) void delta16_dstate_kernel(DeltaProblem p,
         const Terms<3> x0 = xl.get(0, l), x1 = xl.get(1, l);
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const int tb = own_block<NW>(w, j), t = 32 * (tb / 2) + 8 * u + 4 * (tb & 1);
+            const int tb = own_block<NW>(w, j);
             r[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             if (tb < 2)
-                r[j] = mma(inv[j][0], x0, r[j]);
-            r[j] = mma(inv[j][1], x1, r[j]);
-            zl.put(tb, l, -(ge[j] * r[j]));
-            if (in)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (t + i < n)
-                        store_f(dv + (int64_t)(ch * kChunk + t + i) * p.dv.st, gb[j][i] * r[j][i]);
+                r[j] = mma(now.inv[j][0], x0, r[j]);
+            r[j] = mma(now.inv[j][1], x1, r[j]);
+            zl.put(tb, l, -(now.ge[j] * r[j]));
         }
-        if (ch > 0)
-            fetch_rest(ch - 1);
         lds_barrier();
         const Terms<3> z0 = zl.get(0, l), z1 = zl.get(1, l), y0 = yl.get(0, l), y1 = yl.get(1, l);
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk) {
-            S[blk] *= keep;
+            S[blk] *= now.gk;
             S[blk] = mma(KeyShare::turned(ql[w], blk, 0, l), y0, S[blk]);
             S[blk] = mma(KeyShare::turned(ql[w], blk, 1, l), y1, S[blk]);
             S[blk] = mma(KeyShare::turned(kl[w], blk, 0, l), z0, S[blk]);
@@ -738,10 +741,22 @@ __global__ __launch_bounds__(DKP * 2) void delta16_dstate_kernel(DeltaProblem p,
         }
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const int tb = own_block<NW>(w, j);
+            const int tb = own_block<NW>(w, j), t = 32 * (tb / 2) + 8 * u + 4 * (tb & 1);
             store_half(gr.r, (at * nv + sl) * 2 + tb / 2, tb, l, r[j]);
+            if (in)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (t + i < n)
+                        store_f(dv + (int64_t)(ch * kChunk + t + i) * p.dv.st, now.gb[j][i] * r[j][i]);
         }
         lds_barrier();   // yl is written ahead of the next chunk's first exchange
+    };
+    if (live > 0)
+        fetch(live - 1, even);
+    for (int ch = live - 1; ch >= 0; ch -= 2) {
+        chunk(ch, even, odd);
+        if (ch > 0)
+            chunk(ch - 1, odd, even);
     }
     if (p.dstate_in && in)
 #pragma unroll
