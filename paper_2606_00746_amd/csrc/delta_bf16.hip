@@ -103,6 +103,7 @@ __device__ __forceinline__ constexpr int turned_unit(int tb, int g) { return tb 
 __device__ __forceinline__ int index_of(int tb, int m) { return 32 * (tb / 2) + 8 * (m / 4) + 4 * (tb & 1) + m % 4; }
 
 // Gates, and (I + b M)^-1 by forward substitution, a wave a chunk, a lane a column.
+template <int DKP>
 __global__ __launch_bounds__(kThreads) void delta16_inverse_kernel(DeltaProblem p, Kept16 kept, int nc)
 {
     __shared__ __attribute__((aligned(16))) float lds[4][kChunk * kPitch];
@@ -129,15 +130,20 @@ __global__ __launch_bounds__(kThreads) void delta16_inverse_kernel(DeltaProblem 
 #pragma unroll
         for (int r = 0; r < 16; ++r)
             kk[i][r] = 0.f;
-    for (int s = 0; s * 16 < p.Dk; ++s) {
-        Frag<bf16_t> a = {}, d = {};
+    Frag<bf16_t> ka[DKP / 16], kd[DKP / 16];
+#pragma unroll
+    for (int s = 0; s < DKP / 16; ++s) {
+        ka[s] = kd[s] = Frag<bf16_t>{};
         if (c < n)
-            a = row_frag(k + c * p.k.st, 2 * s + h, p.Dk);
+            ka[s] = row_frag(k + c * p.k.st, 2 * s + h, p.Dk);
         if (32 + c < n)
-            d = row_frag(k + (32 + c) * p.k.st, 2 * s + h, p.Dk);
-        kk[0] = attn::mma(a, a, kk[0]);
-        kk[1] = attn::mma(d, a, kk[1]);
-        kk[2] = attn::mma(d, d, kk[2]);
+            kd[s] = row_frag(k + (32 + c) * p.k.st, 2 * s + h, p.Dk);
+    }
+#pragma unroll
+    for (int s = 0; s < DKP / 16; ++s) {
+        kk[0] = attn::mma(ka[s], ka[s], kk[0]);
+        kk[1] = attn::mma(kd[s], ka[s], kk[1]);
+        kk[2] = attn::mma(kd[s], kd[s], kk[2]);
     }
     float *m = lds[w];
 #pragma unroll
@@ -485,6 +491,18 @@ __global__ __launch_bounds__(kThreads) void delta16_out_kernel(DeltaProblem p, K
 #pragma unroll
         for (int g = 0; g < NG; ++g)
             qr[tb][g] = piece_of(q, p.q.st, 16 * tb + c, n, 32 * g + 8 * u, p.Dk);
+    // the wave's first slice of the state and U is in flight while P is formed
+    Terms<kKeep> sf[NG], uf[2];
+    const auto fetch = [&](int sl) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+            sf[g] = load_terms<kKeep>(kept.s, (at * nv + sl) * NG + g, l);
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+            uf[g] = load_terms<kKeep>(kept.u, (at * nv + sl) * 2 + g, l);
+    };
+    if (w < nv)
+        fetch(w);
     {   // P[t][s] for the 16 tokens t of block w
         const float gt = gates[4 * kChunk + 16 * w + c];
         uint4 mine[NG], kr[4][NG];
@@ -518,15 +536,14 @@ __global__ __launch_bounds__(kThreads) void delta16_out_kernel(DeltaProblem p, K
 #pragma unroll
         for (int tb = 0; tb < 4; ++tb)
             acc[tb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        const Terms<kKeep> u0 = load_terms<kKeep>(kept.u, (at * nv + sl) * 2, l);
-        const Terms<kKeep> u1 = load_terms<kKeep>(kept.u, (at * nv + sl) * 2 + 1, l);
+        const Terms<kKeep> u0 = uf[0], u1 = uf[1];
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            const Terms<kKeep> s = load_terms<kKeep>(kept.s, (at * nv + sl) * NG + g, l);
+        for (int g = 0; g < NG; ++g)
 #pragma unroll
             for (int tb = 0; tb < 4; ++tb)
-                acc[tb] = mma(s, one(qr[tb][g]), acc[tb]);
-        }
+                acc[tb] = mma(sf[g], one(qr[tb][g]), acc[tb]);
+        if (sl + 4 < nv)
+            fetch(sl + 4);
 #pragma unroll
         for (int tb = 0; tb < 4; ++tb) {
             acc[tb] *= p.scale * gates[3 * kChunk + 16 * tb + c];
@@ -550,7 +567,7 @@ struct Grads16 {
 };
 
 // scale A^T dO of a chunk.
-template <int DVP>
+template <int DKP, int DVP>
 __global__ __launch_bounds__(kThreads) void delta16_du_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv)
 {
     using X = Tile<bf16_t, DVP>;
@@ -577,13 +594,21 @@ __global__ __launch_bounds__(kThreads) void delta16_du_kernel(DeltaProblem p, Ke
 #pragma unroll
         for (int tb = 0; tb < 4; ++tb)
             a[tb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        for (int e = 8 * u; e < p.Dk + 8 * u; e += 32) {
-            const Terms<1> kf = one(piece_of(k, p.k.st, 16 * w + c, n, e, p.Dk));
+        uint4 kf[DKP / 32], qf[4][DKP / 32];
+#pragma unroll
+        for (int g = 0; g < DKP / 32; ++g) {
+            kf[g] = piece_of(k, p.k.st, 16 * w + c, n, 32 * g + 8 * u, p.Dk);
 #pragma unroll
             for (int tb = 0; tb < 4; ++tb)
                 if (tb >= w)
-                    a[tb] = mma(one(piece_of(q, p.q.st, 16 * tb + c, n, e, p.Dk)), kf, a[tb]);
+                    qf[tb][g] = piece_of(q, p.q.st, 16 * tb + c, n, 32 * g + 8 * u, p.Dk);
         }
+#pragma unroll
+        for (int tb = 0; tb < 4; ++tb)
+            if (tb >= w)
+#pragma unroll
+                for (int g = 0; g < DKP / 32; ++g)
+                    a[tb] = mma(one(qf[tb][g]), one(kf[g]), a[tb]);
 #pragma unroll
         for (int tb = 0; tb < 4; ++tb)
             if (tb >= (w & 2)) {
@@ -791,17 +816,31 @@ __device__ __forceinline__ float over_u(float v)   // over the four u of one lan
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Operands that were left as [unit of 16 columns][32 rows in pieces of 8] put
-// into LDS as rows of 64 entries, one row a column: piece 4 g + u of row 16 sl + c.
-__device__ __forceinline__ void unpack(char *lds, const uint4 *units, int64_t first, int stride, int g0, int nv, int rows)
-{
-    // one 16-byte piece a thread: nv slices x 2 groups x 2 terms x 64 lanes
-    for (int x = threadIdx.x; x < nv * 2 * kKeep * 64; x += kThreads) {
-        const int l = x % 64, n = x / 64 % kKeep, g = x / 64 / kKeep % 2, sl = x / 64 / kKeep / 2;
-        const uint4 v = units[((first + (int64_t)sl * stride + g0 + g) * kKeep + n) * 64 + l];
-        *reinterpret_cast<uint4 *>(lds + n * rows * 128 + Square16::at(16 * sl + l % 16, 4 * g + l / 16)) = v;
+// Operands that were left as [unit of 16 columns][32 rows in pieces of 8] on
+// their way into LDS as rows of 64 entries, one row a column: piece 4 g + u of
+// row 16 sl + c.  A 16-byte piece a thread and step; columns that no slice has
+// are zero.
+template <int DVP>
+struct Unpacked {
+    uint4 r[DVP / 16];
+    __device__ __forceinline__ void load(const uint4 *units, int64_t first, int stride, int g0, int nv)
+    {
+#pragma unroll
+        for (int i = 0; i < DVP / 16; ++i) {
+            const int l = threadIdx.x % 64, n = threadIdx.x / 64 % kKeep, g = threadIdx.x / 128;
+            r[i] = make_uint4(0, 0, 0, 0);
+            if (i < nv)
+                r[i] = units[((first + (int64_t)i * stride + g0 + g) * kKeep + n) * 64 + l];
+        }
     }
-}
+    __device__ __forceinline__ void store(char *lds) const
+    {
+        const int l = threadIdx.x % 64, n = threadIdx.x / 64 % kKeep, g = threadIdx.x / 128;
+#pragma unroll
+        for (int i = 0; i < DVP / 16; ++i)
+            *reinterpret_cast<uint4 *>(lds + n * DVP * 128 + Square16::at(16 * i + l % 16, 4 * g + l / 16)) = r[i];
+    }
+};
 // A or B operand from such rows: entries 16 blk + c (of 64), rows 32 g + 8 u ..
 __device__ __forceinline__ Terms<kKeep> turned_terms(const char *lds, int blk, int g, int l, int rows)
 {
@@ -879,6 +918,10 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
         const float *gates = kept.gates + at * kGateRows * kChunk;
         const bf16_t *d = static_cast<const bf16_t *>(p.dout.p) + b * p.dout.sb + hv * p.dout.sh + (int64_t)t0 * p.dout.st;
         const bf16_t *v = static_cast<const bf16_t *>(p.v.p) + b * p.v.sb + hv * p.v.sh + (int64_t)t0 * p.v.st;
+        Unpacked<DVP> iu, ir, is;
+        iu.load(kept.u, at * nv * 2, 2, 0, nv);
+        ir.load(gr.r, at * nv * 2, 2, 0, nv);
+        is.load(kept.s, at * nv * NG, NG, 0, nv);
         // dO by tokens, entries 32 g + 8 u .. of token 16 tb + c
         uint4 df[4][NE];
 #pragma unroll
@@ -887,17 +930,11 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
             for (int g = 0; g < NE; ++g)
                 df[tb][g] = piece_of(d, p.dout.st, 16 * tb + c, n, 32 * g + 8 * u, p.Dv);
         lds_barrier();   // the waves are done with the last head's P and N
-        unpack(ul, kept.u, at * nv * 2, 2, 0, nv, DVP);
-        unpack(rl, gr.r, at * nv * 2, 2, 0, nv, DVP);
-        unpack(sd, kept.s, at * nv * NG, NG, 0, nv, DVP);
-        if (nv * 16 < DVP)   // rows that no slice has
-            for (int x = threadIdx.x; x < kKeep * (DVP - nv * 16) * 8; x += kThreads) {
-                const int at16 = (x / 8 / (DVP - nv * 16)) * kMat + Square16::at(nv * 16 + x / 8 % (DVP - nv * 16), x % 8);
-                *reinterpret_cast<uint4 *>(ul + at16) = make_uint4(0, 0, 0, 0);
-                *reinterpret_cast<uint4 *>(rl + at16) = make_uint4(0, 0, 0, 0);
-                *reinterpret_cast<uint4 *>(sd + at16) = make_uint4(0, 0, 0, 0);
-            }
+        iu.store(ul);
+        ir.store(rl);
+        is.store(sd);
         lds_barrier();
+        is.load(gr.ds, at * nv * NG, NG, 0, nv);
 
         const int t = 16 * w + c;   // this lane's token of the 64 x 64 matrices
         const float bt = gates[t], gt = gates[4 * kChunk + t];
@@ -969,8 +1006,9 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
             const int m0 = 64 * j + 16 * w + 4 * u;
             if (j > 0) {
                 lds_barrier();
-                unpack(sd, kept.s, at * nv * NG, NG, 2 * j, nv, DVP);
+                is.store(sd);
                 lds_barrier();
+                is.load(gr.ds, at * nv * NG, NG, 2 * j, nv);
             }
             f32x4_t y1[4], y2[4];
 #pragma unroll
@@ -1003,8 +1041,10 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
                 }
             }
             lds_barrier();
-            unpack(sd, gr.ds, at * nv * NG, NG, 2 * j, nv, DVP);
+            is.store(sd);
             lds_barrier();
+            if (j + 1 < NB)
+                is.load(kept.s, at * nv * NG, NG, 2 * j + 2, nv);
             f32x4_t y3[4];
 #pragma unroll
             for (int tb = 0; tb < 4; ++tb)
@@ -1157,7 +1197,7 @@ hipError_t fwd(const DeltaProblem &p, hipStream_t s)
         return hipErrorInvalidConfiguration;
     if (e != hipSuccess || p.ws->counting)
         return e;
-    delta16_inverse_kernel<<<dim3((unsigned)((heads * nc + 3) / 4)), kThreads, 0, s>>>(p, kept, nc);
+    delta16_inverse_kernel<DKP><<<dim3((unsigned)((heads * nc + 3) / 4)), kThreads, 0, s>>>(p, kept, nc);
     e = hipGetLastError();
     if (e != hipSuccess)
         return e;
@@ -1191,7 +1231,7 @@ hipError_t bwd(const DeltaProblem &p, hipStream_t s)
     g.du = static_cast<float *>(du);
     g.r = static_cast<uint4 *>(r);
     g.ds = static_cast<uint4 *>(ds);
-    delta16_du_kernel<DVP><<<dim3((unsigned)n), kThreads, 0, s>>>(p, kept, g, nc, nv);
+    delta16_du_kernel<DKP, DVP><<<dim3((unsigned)n), kThreads, 0, s>>>(p, kept, g, nc, nv);
     e = hipGetLastError();
     if (e != hipSuccess)
         return e;
