@@ -101,28 +101,28 @@ struct Tile {
     __device__ static __forceinline__ int at(int r, int c) { return (r * kS + (c ^ swizzle(r))) * 16; }
 
     uint4 reg[kLoads];
+    uint32_t off[kLoads];   // of this thread's pieces in a tile of the tensor
 
-    // Rows row0 .. row0 + 63 of a tensor with row stride st into registers;
-    // rows from `rows` on and columns from D on read as zero.
+    // Before the first load: a tensor with row stride st, columns from D on read as zero.
+    __device__ __forceinline__ void start(int64_t st, int D)
+    {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int x = threadIdx.x + i * kThreads, r = x / kPieces, c = x % kPieces;
+            off[i] = c * kPer < D ? (uint32_t)(r * (int)st * (int)sizeof(T) + c * 16) : 0x80000000u;
+        }
+    }
+    // Rows row0 .. row0 + 63 into registers; rows from `rows` on read as zero.  The
+    // buffer's range does both: a tile is below 2^31 bytes (token strides are below
+    // 2^23), pieces that count as absent lie beyond.
     __device__ __forceinline__ void load(const T *base, int64_t st, int row0, int rows, int D)
     {
-        const T *p = base + (int64_t)row0 * st;
-        const int n = rows - row0;
-        if (n >= kRows && D == DP) {
+        const int n = min(rows - row0, kRows);
+        const uint32_t bytes = n <= 0 ? 0u : (uint32_t)((n - 1) * (int)st + D) * (uint32_t)sizeof(T);
+        const rsrc_t r = make_rsrc(base + (int64_t)row0 * st, bytes);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int x = threadIdx.x + i * kThreads, r = x / kPieces, c = x % kPieces;
-                reg[i] = *reinterpret_cast<const uint4 *>(p + r * st + c * kPer);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int x = threadIdx.x + i * kThreads, r = x / kPieces, c = x % kPieces;
-                reg[i] = make_uint4(0, 0, 0, 0);
-                if (r < n && c * kPer < D)
-                    reg[i] = *reinterpret_cast<const uint4 *>(p + r * st + c * kPer);
-            }
-        }
+        for (int i = 0; i < kLoads; ++i)
+            reg[i] = ld128(r, off[i], 0);
     }
     __device__ __forceinline__ void store(char *lds) const
     {
@@ -163,6 +163,16 @@ __device__ __forceinline__ Frag<T> row_frag(const T *row, int piece, int D)
         u = *reinterpret_cast<const uint4 *>(row + piece * kPer);
     f.v = __builtin_bit_cast(decltype(f.v), u);
     return f;
+}
+
+// The loads that filled these are waited for here, once, and not again where a
+// loop that follows first uses them.
+template <typename T, int N>
+__device__ __forceinline__ void arrived(Frag<T> (&f)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        asm volatile("" : "+v"(f[i].v));
 }
 
 // acc += A B^T over the columns of one pair of pieces (bf16: 16, fp32: 8).

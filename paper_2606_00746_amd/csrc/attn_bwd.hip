@@ -89,6 +89,8 @@ void attn_dq_kernel(AttnProblem a, float *delta)
             acc[db][r] = 0.f;
 
     X kt, vt;
+    kt.start(a.k.st, a.D);
+    vt.start(a.v.st, a.D);
     const int n = wg.n;
     if (n > 0) {
         kt.load(kp, a.k.st, wg.row(0), len, a.D);
@@ -96,6 +98,8 @@ void attn_dq_kernel(AttnProblem a, float *delta)
         kt.store(lds[0][0]);
         vt.store(lds[0][1]);
     }
+    arrived(qf);
+    arrived(df);
     lds_barrier();
     for (int it = 0; it < n; ++it) {
         const int k0 = wg.row(it);
@@ -221,6 +225,8 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
     const float s2 = a.scale * kLog2e;
 
     X qt, dt;
+    qt.start(a.q.st, a.D);
+    dt.start(a.dout.st, a.D);
     float stat = 0.f;
     // queries from qrows on stand past the sequence's end: they count as zero rows
     const int qrows = max(0, min(a.Tq, len - a.offset));
@@ -246,6 +252,8 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
         fetch(i0);
         put(0);
     }
+    arrived(kf);
+    arrived(vf);
     lds_barrier();
     for (int i = i0; i < i1; ++i) {
         const int buf = (i - i0) & 1, t0 = (first + i % nt) * kRows;

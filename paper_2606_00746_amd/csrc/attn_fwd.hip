@@ -77,6 +77,8 @@ void attn_fwd_kernel(AttnProblem a)
     const float s2 = a.scale * kLog2e, slack = kSlack / s2;
 
     X kt, vt;
+    kt.start(a.k.st, a.D);
+    vt.start(a.v.st, a.D);
     const int n = wg.n;
     if (n > 0) {
         kt.load(kp, a.k.st, wg.row(0), len, a.D);
@@ -84,6 +86,9 @@ void attn_fwd_kernel(AttnProblem a)
         kt.store(lds[0][0]);
         vt.store(lds[0][1]);
     }
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+        arrived(qf[qb]);
     lds_barrier();
 
     for (int it = 0; it < n; ++it) {

@@ -587,6 +587,7 @@ __global__ __launch_bounds__(kThreads) void delta16_du_kernel(DeltaProblem p, Ke
     if (n == 0)
         return;
     X x;
+    x.start(p.dout.st, p.Dv);
     x.load(d, p.dout.st, 0, n, p.Dv);
     {   // P[t][s] as rows of s, for the 16 columns s of block w
         const float gs = gates[4 * kChunk + 16 * w + c];
@@ -900,6 +901,8 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
     }
     {
         X a, e;
+        a.start(p.q.st, p.Dk);
+        e.start(p.k.st, p.Dk);
         a.load(q, p.q.st, 0, n, p.Dk);
         e.load(k, p.k.st, 0, n, p.Dk);
         a.store(ql);
