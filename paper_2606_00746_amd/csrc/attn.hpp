@@ -219,30 +219,47 @@ __device__ __forceinline__ s16x4_t read_turned(const char *lds)
         (__attribute__((address_space(3))) s16x4_t *)(lds));
 }
 
-// acc[db] += X^T P over the 32 rows row0.. of the tile X (columns 32 db ..).
+// The A operands of X^T P over the 32 rows row0.. of a tile X, read ahead of P.
+template <typename T, int DP>
+struct Turned;
 template <int DP>
-__device__ __forceinline__ void mma_turned(const char *lds, int row0, const Probs<bf16_t> &p,
-                                           f32x16_t (&acc)[DP / 32])
+struct Turned<bf16_t, DP> {
+    bf16x8_t v[2][DP / 32];
+    __device__ __forceinline__ void load(const char *lds, int row0)
+    {
+        using X = Tile<bf16_t, DP>;
+        const int l = threadIdx.x % 64, h = l / 32, i = l % 16, r = row0 + 4 * h + (i >> 2);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db) {
+                const int c = 4 * db + 2 * (l % 32 / 16) + ((i & 3) >> 1), in = 8 * (i & 1);
+                struct {
+                    s16x4_t a, b;
+                } both = {read_turned(lds + X::at(16 * t + r, c) + in), read_turned(lds + X::at(16 * t + 8 + r, c) + in)};
+                v[t][db] = __builtin_bit_cast(bf16x8_t, both);
+            }
+    }
+};
+template <int DP>
+struct Turned<float, DP> {   // read where they are used: 16 products take their time
+    const char *lds;
+    int row0;
+    __device__ __forceinline__ void load(const char *tile, int row) { lds = tile, row0 = row; }
+};
+
+// acc[db] += X^T P (columns 32 db .. of X).
+template <int DP>
+__device__ __forceinline__ void mma_turned(const Turned<bf16_t, DP> &x, const Probs<bf16_t> &p, f32x16_t (&acc)[DP / 32])
 {
-    using X = Tile<bf16_t, DP>;
-    const int l = threadIdx.x % 64, h = l / 32, i = l % 16, r = 4 * h + (i >> 2);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int db = 0; db < DP / 32; ++db) {
-            const int c = 4 * db + 2 * (l % 32 / 16) + ((i & 3) >> 1), in = 8 * (i & 1);
-            const s16x4_t a0 = read_turned(lds + X::at(row0 + 16 * t + r, c) + in);
-            const s16x4_t a1 = read_turned(lds + X::at(row0 + 16 * t + 8 + r, c) + in);
-            struct {
-                s16x4_t a, b;
-            } both = {a0, a1};
-            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, both),
-                                                              p.v[t], acc[db], 0, 0, 0);
-        }
+        for (int db = 0; db < DP / 32; ++db)
+            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.v[t][db], p.v[t], acc[db], 0, 0, 0);
 }
 template <int DP>
-__device__ __forceinline__ void mma_turned(const char *lds, int row0, const Probs<float> &p,
-                                           f32x16_t (&acc)[DP / 32])
+__device__ __forceinline__ void mma_turned(const Turned<float, DP> &x, const Probs<float> &p, f32x16_t (&acc)[DP / 32])
 {
     using X = Tile<float, DP>;
     const int l = threadIdx.x % 64, h = l / 32, d = l % 32;
@@ -251,9 +268,45 @@ __device__ __forceinline__ void mma_turned(const char *lds, int row0, const Prob
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db) {
             const float a = *reinterpret_cast<const float *>(
-                lds + X::at(row0 + 8 * (r / 4) + 4 * h + r % 4, 8 * db + d / 4) + 4 * (d % 4));
+                x.lds + X::at(x.row0 + 8 * (r / 4) + 4 * h + r % 4, 8 * db + d / 4) + 4 * (d % 4));
             acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p.v[r], acc[db], 0, 0, 0);
         }
+}
+
+// This lane's row of a tile as row-wise fragments; bf16: all read at once.
+template <typename T, int DP>
+struct RowFrags;
+template <int DP>
+struct RowFrags<bf16_t, DP> {
+    static constexpr int kSlices = Tile<bf16_t, DP>::kPieces / 2;
+    Frag<bf16_t> f[kSlices];
+    __device__ __forceinline__ void load(const char *lds, int row)
+    {
+        const int h = threadIdx.x % 64 / 32;
+#pragma unroll
+        for (int s = 0; s < kSlices; ++s)
+            f[s] = tile_frag<bf16_t, DP>(lds, row, 2 * s + h);
+    }
+    __device__ __forceinline__ Frag<bf16_t> at(int s) const { return f[s]; }
+};
+template <int DP>
+struct RowFrags<float, DP> {
+    const char *lds;
+    int row;
+    __device__ __forceinline__ void load(const char *tile, int r) { lds = tile, row = r; }
+    __device__ __forceinline__ Frag<float> at(int s) const
+    {
+        return tile_frag<float, DP>(lds, row, 2 * s + (int)(threadIdx.x % 64 / 32));
+    }
+};
+
+// bf16: reads of LDS stay ahead of the products they are for, as written (the
+// compiler otherwise puts each read next to its use and waits for it).
+template <typename T>
+__device__ __forceinline__ void reads_first()
+{
+    if (sizeof(T) == 2)
+        step_fence();
 }
 
 // A wide store reads its registers after issue: an asm behind it keeps them as they are.
@@ -299,6 +352,13 @@ __device__ __forceinline__ void key_bounds(const AttnProblem &a, int len, int p,
 {
     hi = p < 0 || p >= len ? -1 : a.right < 0 ? len - 1 : min(len - 1, p + a.right);
     lo = a.left < 0 ? 0 : max(0, p - a.left);
+}
+
+// Whether a query that sees lo .. hi, and sinks up to hi, sees key j; sunk: whether
+// the tile of j holds sinks.
+__device__ __forceinline__ bool sees(int j, int lo, int hi, int sinks, bool sunk)
+{
+    return sunk ? j <= hi && (j >= lo || j < sinks) : (uint32_t)(j - lo) <= (uint32_t)(hi - lo) && hi >= lo;
 }
 
 // The tiles of kRows keys that the queries t0 .. t0 + nt - 1 see: those that

@@ -116,23 +116,30 @@ void attn_dq_kernel(AttnProblem a, float *delta)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     s[r] = dp[r] = 0.f;
+                RowFrags<T, DP> kf, vf;
+                Turned<T, DP> kx;
+                kf.load(kl, 32 * kb + c);
+                vf.load(vl, 32 * kb + c);
+                reads_first<T>();
 #pragma unroll
                 for (int sl = 0; sl < kSlices; ++sl) {
-                    s = mma(tile_frag<T, DP>(kl, 32 * kb + c, 2 * sl + h), qf[sl], s);
-                    dp = mma(tile_frag<T, DP>(vl, 32 * kb + c, 2 * sl + h), df[sl], dp);
+                    s = mma(kf.at(sl), qf[sl], s);
+                    dp = mma(vf.at(sl), df[sl], dp);
                 }
+                kx.load(kl, 32 * kb);
+                reads_first<T>();
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], s2, -lse2)) * (dp[r] - d);
                 if (!all) {
+                    const bool sunk = k0 < a.sinks;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int j = k0 + 32 * kb + 8 * (r / 4) + 4 * h + r % 4;
-                        const bool see = j <= hi && (j >= lo || j < a.sinks);
-                        s[r] = see ? s[r] : 0.f;
+                        s[r] = sees(j, lo, hi, a.sinks, sunk) ? s[r] : 0.f;
                     }
                 }
-                mma_turned<DP>(kl, 32 * kb, Probs<T>(s), acc);
+                mma_turned<DP>(kx, Probs<T>(s), acc);
             }
         }
         if (it + 1 < n) {
@@ -268,31 +275,41 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     s[r] = dp[r] = 0.f;
+                RowFrags<T, DP> qf, df;
+                Turned<T, DP> qx, dx;
+                qf.load(ql, 32 * qb + c);
+                df.load(dl, 32 * qb + c);
+                reads_first<T>();
 #pragma unroll
                 for (int sl = 0; sl < kSlices; ++sl) {
-                    s = mma(tile_frag<T, DP>(ql, 32 * qb + c, 2 * sl + h), kf[sl], s);
-                    dp = mma(tile_frag<T, DP>(dl, 32 * qb + c, 2 * sl + h), vf[sl], dp);
+                    s = mma(qf.at(sl), kf[sl], s);
+                    dp = mma(df.at(sl), vf[sl], dp);
                 }
+                f32x4_t ls[4], de[4];
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int row = 32 * qb + 8 * g + 4 * h;
-                    const f32x4_t ls = *reinterpret_cast<const f32x4_t *>(&stats[buf][0][row]);
-                    const f32x4_t de = *reinterpret_cast<const f32x4_t *>(&stats[buf][1][row]);
+                    ls[g] = *reinterpret_cast<const f32x4_t *>(&stats[buf][0][32 * qb + 8 * g + 4 * h]);
+                    de[g] = *reinterpret_cast<const f32x4_t *>(&stats[buf][1][32 * qb + 8 * g + 4 * h]);
+                }
+                dx.load(dl, 32 * qb);
+                qx.load(ql, 32 * qb);
+                reads_first<T>();
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int r = 4 * g + e;
-                        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], s2, -ls[e]));
-                        dp[r] = s[r] * (dp[r] - de[e]);
-                        if (!all) {
-                            const int t = t0 + row + e;
-                            const bool see = t >= lane_a && t <= lane_b;
-                            s[r] = see ? s[r] : 0.f;
-                            dp[r] = see ? dp[r] : 0.f;
-                        }
+                for (int r = 0; r < 16; ++r) {
+                    s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], s2, -ls[r / 4][r % 4]));
+                    dp[r] = s[r] * (dp[r] - de[r / 4][r % 4]);
+                }
+                if (!all) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int t = t0 + 32 * qb + 8 * (r / 4) + 4 * h + r % 4;
+                        const bool see = (uint32_t)(t - lane_a) <= (uint32_t)(lane_b - lane_a) && lane_b >= lane_a;
+                        s[r] = see ? s[r] : 0.f;
+                        dp[r] = see ? dp[r] : 0.f;
                     }
                 }
-                mma_turned<DP>(dl, 32 * qb, Probs<T>(s), dv);
-                mma_turned<DP>(ql, 32 * qb, Probs<T>(dp), dk);
+                mma_turned<DP>(dx, Probs<T>(s), dv);
+                mma_turned<DP>(qx, Probs<T>(dp), dk);
             }
         }
         if (i + 1 < i1)

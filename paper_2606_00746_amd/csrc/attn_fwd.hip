@@ -24,7 +24,7 @@ using namespace attn;
 constexpr float kSlack = 8.f;
 
 template <typename T, int DP, int QB>
-__global__ __launch_bounds__(kThreads, (DP * sizeof(T) * QB <= 256 ? 2 : 1))
+__global__ __launch_bounds__(kThreads, (DP * sizeof(T) * QB <= 128 ? 3 : DP * sizeof(T) * QB <= 256 ? 2 : 1))
 void attn_fwd_kernel(AttnProblem a)
 {
     using X = Tile<T, DP>;
@@ -101,22 +101,26 @@ void attn_fwd_kernel(AttnProblem a)
         if (wave.some(k0)) {
             const bool all = wave.all(k0);
             f32x16_t s[QB][2];
+            RowFrags<T, DP> kf;
+            Turned<T, DP> vf;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
+                kf.load(kl, 32 * kb + c);
+                reads_first<T>();
 #pragma unroll
-                for (int qb = 0; qb < QB; ++qb)
+                for (int qb = 0; qb < QB; ++qb) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
                         s[qb][kb][r] = 0.f;
 #pragma unroll
-                for (int sl = 0; sl < kSlices; ++sl) {
-                    const Frag<T> kf = tile_frag<T, DP>(kl, 32 * kb + c, 2 * sl + h);
-#pragma unroll
-                    for (int qb = 0; qb < QB; ++qb)
-                        s[qb][kb] = mma(kf, qf[qb][sl], s[qb][kb]);
+                    for (int sl = 0; sl < kSlices; ++sl)
+                        s[qb][kb] = mma(kf.at(sl), qf[qb][sl], s[qb][kb]);
                 }
             }
+            vf.load(vl, 0);
+            reads_first<T>();
             if (!all) {
+                const bool sunk = k0 < a.sinks;
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
@@ -124,10 +128,10 @@ void attn_fwd_kernel(AttnProblem a)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
                             const int j = k0 + 32 * kb + 8 * (r / 4) + 4 * h + r % 4;
-                            const bool see = j <= hi[qb] && (j >= lo[qb] || j < a.sinks);
-                            s[qb][kb][r] = see ? s[qb][kb][r] : -__builtin_inff();
+                            s[qb][kb][r] = sees(j, lo[qb], hi[qb], a.sinks, sunk) ? s[qb][kb][r] : -__builtin_inff();
                         }
             }
+            float base[QB];
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
                 float mx = -__builtin_inff();
@@ -150,17 +154,24 @@ void attn_fwd_kernel(AttnProblem a)
                         for (int r = 0; r < 16; ++r)
                             acc[qb][db][r] *= f;
                 }
-                const float base = m[qb] == -__builtin_inff() ? 0.f : m[qb] * s2;
+                base[qb] = m[qb] == -__builtin_inff() ? 0.f : m[qb] * s2;
+            }
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
+            for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) {
                     float part = 0.f;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        s[qb][kb][r] = __builtin_amdgcn_exp2f(fmaf(s[qb][kb][r], s2, -base));
+                        s[qb][kb][r] = __builtin_amdgcn_exp2f(fmaf(s[qb][kb][r], s2, -base[qb]));
                         part += s[qb][kb][r];
                     }
                     sum[qb] += part;
-                    mma_turned<DP>(vl, 32 * kb, Probs<T>(s[qb][kb]), acc[qb]);
+                    mma_turned<DP>(vf, Probs<T>(s[qb][kb]), acc[qb]);
+                }
+                if (kb == 0) {
+                    vf.load(vl, 32);
+                    reads_first<T>();
                 }
             }
         }
