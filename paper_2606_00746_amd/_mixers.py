@@ -20,38 +20,53 @@ ATTN_FWD, ATTN_BWD, ATTN_DECODE = 0, 1, 2
 DELTA_FWD, DELTA_FWD_TRAIN, DELTA_BWD_RESERVE = 0, 1, 2
 
 
-def _heads(named):
-    """Every tensor of `named` ({name: (tensor, shape)}) is on one GPU, of one
-    dtype, of its shape and contiguous in its last dimension."""
-    first = None
-    for name, (t, shape) in named.items():
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
-        if not t.is_cuda:
-            raise ValueError("tensors must be on a GPU")
-        if t.stride(-1) != 1 and t.shape[-1] > 1:
-            raise ValueError(f"{name} must be contiguous in its last dimension")
-        if first is None:
-            first = t
-        elif t.dtype != first.dtype:
-            raise ValueError(f"{name} must have dtype {first.dtype}, not {t.dtype}")
-        elif t.get_device() != first.get_device():
-            raise ValueError(f"{name} must be on {first.device}")
+# A small call's time is this binding's: its checks are attribute reads in one
+# expression a tensor, and only a failed one is gone into.
+
+def _heads(first, *tensors):
+    """(tensor, shape, name) each: on first's GPU, of its dtype, of that shape and
+    contiguous in its last dimension."""
+    dtype, dev = first.dtype, first.get_device()
+    for t, shape, name in tensors:
+        if t.shape != shape or t.dtype != dtype or t.get_device() != dev or t.stride(-1) != 1:
+            _name_fault(first, t, shape, name)
+    if dev < 0:
+        raise ValueError("tensors must be on a GPU")
+
+
+def _name_fault(first, t, shape, name):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
+    if t.dtype != first.dtype:
+        raise ValueError(f"{name} must have dtype {first.dtype}, not {t.dtype}")
+    if t.device != first.device:
+        raise ValueError(f"{name} must be on {first.device}")
+    if t.shape[-1] > 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+
+
+_Strides = {n: ctypes.c_int64 * (3 * n) for n in (4, 6, 7, 8)}
 
 
 def _strides(*tensors):
-    """Batch, token and head strides of every tensor, in order."""
+    """Batch, token and head strides of every tensor, in order; None where all are
+    contiguous."""
+    for t in tensors:
+        if not t.is_contiguous():
+            break
+    else:
+        return None
     out = []
     for t in tensors:
         out += t.stride()[:3]
-    return (ctypes.c_int64 * len(out))(*out)
+    return _Strides[len(tensors)](*out)
 
 
 def _plain(name, t, shape, dtype, like):
     """An optional contiguous tensor's pointer (None: none)."""
     if t is None:
         return None
-    if (tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous()
+    if (t.shape != shape or t.dtype != dtype or not t.is_contiguous()
             or t.get_device() != like.get_device()):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {like.device}")
     return t.data_ptr()
@@ -114,11 +129,10 @@ def qk_norm_rotate_fwd(q, k, wq=None, wk=None, cos=None, sin=None, eps: float = 
     import torch
     B, T, Hq, Hk, D, R, rows, ptrs = _norm_sizes(q, k, wq, wk, cos, sin, positions, pairs)
     if out is None:
-        out = (torch.empty((B, T, Hq, D), dtype=q.dtype, device=q.device),
-               torch.empty((B, T, Hk, D), dtype=q.dtype, device=q.device))
+        out = q.new_empty((B, T, Hq, D)), q.new_empty((B, T, Hk, D))
     yq, yk = out
-    _heads({"q": (q, (B, T, Hq, D)), "k": (k, (B, T, Hk, D)), "yq": (yq, (B, T, Hq, D)),
-            "yk": (yk, (B, T, Hk, D))})
+    _heads(q, (q, (B, T, Hq, D), "q"), (k, (B, T, Hk, D), "k"), (yq, (B, T, Hq, D), "yq"),
+           (yk, (B, T, Hk, D), "yk"))
     _check_raise(load().gspn_qk_norm_rotate_fwd(
         q.data_ptr(), k.data_ptr(), *ptrs, yq.data_ptr(), yk.data_ptr(),
         _strides(q, k, yq, yk), B, T, Hq, Hk, D, R, rows, first, PAIRS[pairs], eps,
@@ -139,8 +153,8 @@ def qk_norm_rotate_bwd(q, k, wq, wk, dyq, dyk, cos=None, sin=None, eps: float = 
                None if wq is None else torch.empty(D, **kw),
                None if wk is None else torch.empty(D, **kw))
     dq, dk, dwq, dwk = out
-    _heads({"q": (q, (B, T, Hq, D)), "k": (k, (B, T, Hk, D)), "dyq": (dyq, (B, T, Hq, D)),
-            "dyk": (dyk, (B, T, Hk, D)), "dq": (dq, (B, T, Hq, D)), "dk": (dk, (B, T, Hk, D))})
+    _heads(q, (q, (B, T, Hq, D), "q"), (k, (B, T, Hk, D), "k"), (dyq, (B, T, Hq, D), "dyq"),
+           (dyk, (B, T, Hk, D), "dyk"), (dq, (B, T, Hq, D), "dq"), (dk, (B, T, Hk, D), "dk"))
     dt = _dtype_code(q)
     n = _sized("gspn_qk_norm_rotate_workspace_size", (B, T, Hq, Hk, D, R, PAIRS[pairs], dt),
                _current_device())
@@ -182,11 +196,11 @@ def window_attn_fwd(q, k, v, left: int = -1, right: int = -1, sinks: int = 0, le
     import torch
     B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens)
     if o is None:
-        o = torch.empty((B, Tq, Hq, D), dtype=q.dtype, device=q.device)
+        o = q.new_empty((B, Tq, Hq, D))
     if lse is None:
         lse = torch.empty((B, Hq, Tq), dtype=torch.float32, device=q.device)
-    _heads({"q": (q, (B, Tq, Hq, D)), "k": (k, (B, Tk, Hkv, D)), "v": (v, (B, Tk, Hkv, D)),
-            "o": (o, (B, Tq, Hq, D))})
+    _heads(q, (q, (B, Tq, Hq, D), "q"), (k, (B, Tk, Hkv, D), "k"), (v, (B, Tk, Hkv, D), "v"),
+           (o, (B, Tq, Hq, D), "o"))
     dt = _dtype_code(q)
     ws, held = _attn_workspace(ATTN_FWD, (B, Tq, Tk, Hq, Hkv, D), left, right, sinks, offset, dt,
                                workspace, q.device)
@@ -211,8 +225,8 @@ def window_attn_bwd(q, k, v, o, lse, do, left: int = -1, right: int = -1, sinks:
                torch.empty((B, Tk, Hkv, D), **kw))
     dq, dk, dv = out
     qs, ks = (B, Tq, Hq, D), (B, Tk, Hkv, D)
-    _heads({"q": (q, qs), "k": (k, ks), "v": (v, ks), "o": (o, qs), "do": (do, qs), "dq": (dq, qs),
-            "dk": (dk, ks), "dv": (dv, ks)})
+    _heads(q, (q, qs, "q"), (k, ks, "k"), (v, ks, "v"), (o, qs, "o"), (do, qs, "do"),
+           (dq, qs, "dq"), (dk, ks, "dk"), (dv, ks, "dv"))
     dt = _dtype_code(q)
     ws, held = _attn_workspace(ATTN_BWD, (B, Tq, Tk, Hq, Hkv, D), left, right, sinks, offset, dt,
                                workspace, q.device)
@@ -234,9 +248,9 @@ def window_attn_decode(q, k, v, lens=None, left: int = -1, sinks: int = 0, scale
     import torch
     B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens)
     if o is None:
-        o = torch.empty((B, Tq, Hq, D), dtype=q.dtype, device=q.device)
-    _heads({"q": (q, (B, Tq, Hq, D)), "k": (k, (B, Tk, Hkv, D)), "v": (v, (B, Tk, Hkv, D)),
-            "o": (o, (B, Tq, Hq, D))})
+        o = q.new_empty((B, Tq, Hq, D))
+    _heads(q, (q, (B, Tq, Hq, D), "q"), (k, (B, Tk, Hkv, D), "k"), (v, (B, Tk, Hkv, D), "v"),
+           (o, (B, Tq, Hq, D), "o"))
     dt = _dtype_code(q)
     ws, held = _attn_workspace(ATTN_DECODE, (B, Tq, Tk, Hq, Hkv, D), left, 0, sinks, 0, dt,
                                workspace, q.device)
@@ -285,11 +299,11 @@ def _delta_fwd(op, q, k, v, g, beta, state, lens, scale, o, state_out, reserve, 
     sizes, gates, lens_p = _delta_sizes(q, k, v, g, beta, lens)
     B, T, Hq, Hv, Dk, Dv = sizes
     if o is None:
-        o = torch.empty((B, T, Hv, Dv), dtype=q.dtype, device=q.device)
+        o = q.new_empty((B, T, Hv, Dv))
     if state_out is None:
         state_out = torch.empty((B, Hv, Dk, Dv), dtype=torch.float32, device=q.device)
-    _heads({"q": (q, (B, T, Hq, Dk)), "k": (k, (B, T, Hq, Dk)), "v": (v, (B, T, Hv, Dv)),
-            "o": (o, (B, T, Hv, Dv))})
+    _heads(q, (q, (B, T, Hq, Dk), "q"), (k, (B, T, Hq, Dk), "k"), (v, (B, T, Hv, Dv), "v"),
+           (o, (B, T, Hv, Dv), "o"))
     dt = _dtype_code(q)
     n = _sized("gspn_delta_rule_workspace_size", (op, *sizes, dt), _current_device())
     ws, held = _take(n, workspace, q.device)
@@ -344,8 +358,8 @@ def delta_rule_bwd_reserve(q, k, v, g, beta, do, reserve, dstate=None, state=Non
                torch.empty(gs, **kw), torch.empty(gs, **kw),
                None if state is None else torch.empty(ss, dtype=torch.float32, device=q.device))
     dq, dk, dv, dg, dbeta, din = out
-    _heads({"q": (q, qs), "k": (k, qs), "v": (v, vs), "do": (do, vs), "dq": (dq, qs),
-            "dk": (dk, qs), "dv": (dv, vs)})
+    _heads(q, (q, qs, "q"), (k, qs, "k"), (v, vs, "v"), (do, vs, "do"), (dq, qs, "dq"),
+           (dk, qs, "dk"), (dv, vs, "dv"))
     dt = _dtype_code(q)
     n = _sized("gspn_delta_rule_workspace_size", (DELTA_BWD_RESERVE, *sizes, dt),
                _current_device())

@@ -47,6 +47,14 @@ bool attn_split_preferred(const AttnProblem &p);
 
 constexpr int kAttnMaxHead = 128;
 
+// Whether pairs of waves share their rows of a kernel that would otherwise have
+// `blocks` workgroups: twice as many then, of half the rows, where they would
+// leave CUs without one.
+inline bool attn_pairs(const AttnProblem &, int64_t blocks)
+{
+    return blocks < 256;
+}
+
 #ifdef __HIPCC__
 
 namespace attn {
@@ -101,13 +109,17 @@ struct Tile {
     __device__ static __forceinline__ int at(int r, int c) { return (r * kS + (c ^ swizzle(r))) * 16; }
 
     uint4 reg[kLoads];
-    uint32_t off[kLoads];   // of this thread's pieces in a tile of the tensor
+    // where the threads' pieces repeat every kStep rows, one offset and a uniform
+    // step stand for all of a thread's
+    static constexpr bool kEven = kThreads % kPieces == 0;
+    static constexpr int kStep = kThreads / kPieces;
+    uint32_t off[kEven ? 1 : kLoads];   // of this thread's pieces in a tile of the tensor
 
     // Before the first load: a tensor with row stride st, columns from D on read as zero.
     __device__ __forceinline__ void start(int64_t st, int D)
     {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
+        for (int i = 0; i < (kEven ? 1 : kLoads); ++i) {
             const int x = threadIdx.x + i * kThreads, r = x / kPieces, c = x % kPieces;
             off[i] = c * kPer < D ? (uint32_t)(r * (int)st * (int)sizeof(T) + c * 16) : 0x80000000u;
         }
@@ -122,7 +134,7 @@ struct Tile {
         const rsrc_t r = make_rsrc(base + (int64_t)row0 * st, bytes);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            reg[i] = ld128(r, off[i], 0);
+            reg[i] = kEven ? ld128(r, off[0], i * kStep * (int)st * (int)sizeof(T)) : ld128(r, off[i], 0);
     }
     __device__ __forceinline__ void store(char *lds) const
     {

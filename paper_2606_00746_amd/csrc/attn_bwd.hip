@@ -24,7 +24,27 @@ namespace {
 
 using namespace attn;
 
-constexpr int kKeys = 128;   // keys of a workgroup of attn_dkv_kernel
+// KW: waves that share their rows, each with its part of a tile (1, or 2 with 32
+// rows of it each): the odd wave's sums are added to its neighbour's at the end.
+template <int N>
+__device__ __forceinline__ void join_pair(float *lds, f32x16_t (&acc)[N], int w, int l)
+{
+    float *mine = lds + w / 2 * (64 * 16 * N);
+    lds_barrier();
+    if (w & 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                mine[(16 * i + r) * 64 + l] = acc[i][r];
+    lds_barrier();
+    if (!(w & 1))
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                acc[i][r] += mine[(16 * i + r) * 64 + l];
+}
 
 template <typename T>
 __device__ __forceinline__ float dot(Frag<T> a, Frag<T> b)
@@ -37,12 +57,12 @@ __device__ __forceinline__ float dot(Frag<T> a, Frag<T> b)
     return s;
 }
 
-template <typename T, int DP>
+template <typename T, int DP, int KW>
 __global__ __launch_bounds__(kThreads, (DP * sizeof(T) <= 128 ? 2 : 1))
 void attn_dq_kernel(AttnProblem a, float *delta)
 {
     using X = Tile<T, DP>;
-    constexpr int kSlices = X::kPieces / 2, kTQ = 128;
+    constexpr int kSlices = X::kPieces / 2, kTQ = 128 / KW;
     __shared__ __attribute__((aligned(16))) char lds[2][2][X::kBytes];
 
     const int G = a.Hq / a.Hkv, nqt = (a.Tq + kTQ - 1) / kTQ;
@@ -58,7 +78,8 @@ void attn_dq_kernel(AttnProblem a, float *delta)
 
     const T *kp = static_cast<const T *>(a.k.p) + b * a.k.sb + hk * a.k.sh;
     const T *vp = static_cast<const T *>(a.v.p) + b * a.v.sb + hk * a.v.sh;
-    const int t0 = qt * kTQ, tw = t0 + w * 32, t = tw + c, tr = min(t, a.Tq - 1);
+    const int t0 = qt * kTQ, tw = t0 + w / KW * 32, t = tw + c, tr = min(t, a.Tq - 1);
+    const int kb0 = KW == 2 ? w % 2 : 0;
     const KeyTiles wg(a, len, t0, min(kTQ, a.Tq - t0));
     const KeyRange wave(a, len, tw, 32);
     int lo, hi;
@@ -111,7 +132,7 @@ void attn_dq_kernel(AttnProblem a, float *delta)
         if (wave.some(k0)) {
             const bool all = wave.all(k0);
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
+            for (int kb = kb0; kb < kb0 + 2 / KW; ++kb) {
                 f32x16_t s, dp;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
@@ -148,7 +169,9 @@ void attn_dq_kernel(AttnProblem a, float *delta)
         }
         lds_barrier();
     }
-    if (t < a.Tq)
+    if (KW == 2)
+        join_pair(reinterpret_cast<float *>(lds), acc, w, l);
+    if (t < a.Tq && (KW == 1 || !(w & 1)))
         store_column<T, DP>(static_cast<T *>(a.dq.p) + b * a.dq.sb + hq * a.dq.sh + t * a.dq.st, acc,
                             a.scale, a.D);
 }
@@ -172,12 +195,12 @@ struct KeySplit {
     }
 };
 
-template <typename T, int DP>
+template <typename T, int DP, int KW>
 __global__ __launch_bounds__(kThreads, (DP * sizeof(T) <= 128 ? 2 : 1))
 void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shares)
 {
     using X = Tile<T, DP>;
-    constexpr int kSlices = X::kPieces / 2;
+    constexpr int kSlices = X::kPieces / 2, kKeys = 128 / KW;
     __shared__ __attribute__((aligned(16))) char lds[2][2][X::kBytes];
     __shared__ __attribute__((aligned(16))) float stats[2][2][kRows];
 
@@ -196,7 +219,7 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x % 64;
     const int c = l % 32, h = l / 32;
     const int len = seq_len(a, b);
-    const int k0 = tile * kKeys, kw = k0 + 32 * w, j = kw + c;
+    const int k0 = tile * kKeys, kw = k0 + 32 * (w / KW), j = kw + c, qb0 = KW == 2 ? w % 2 : 0;
 
     // queries t that see some key of the workgroup, of the wave (some, all), of the lane
     const auto after = [&](int key) { return a.right < 0 ? 0 : max(0, key - a.right - a.offset); };
@@ -270,7 +293,7 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
         if (t0 <= some_b && t0 + kRows > some_a) {
             const bool all = t0 >= all_a && t0 + kRows - 1 <= all_b;
 #pragma unroll
-            for (int qb = 0; qb < 2; ++qb) {
+            for (int qb = qb0; qb < qb0 + 2 / KW; ++qb) {
                 f32x16_t s, dp;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
@@ -292,7 +315,6 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
                     de[g] = *reinterpret_cast<const f32x4_t *>(&stats[buf][1][32 * qb + 8 * g + 4 * h]);
                 }
                 dx.load(dl, 32 * qb);
-                qx.load(ql, 32 * qb);
                 reads_first<T>();
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
@@ -309,6 +331,7 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
                     }
                 }
                 mma_turned<DP>(dx, Probs<T>(s), dv);
+                qx.load(ql, 32 * qb);
                 mma_turned<DP>(qx, Probs<T>(dp), dk);
             }
         }
@@ -317,9 +340,15 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
         lds_barrier();
     }
 
+    if (KW == 2) {
+        join_pair(reinterpret_cast<float *>(lds), dk, w, l);
+        join_pair(reinterpret_cast<float *>(lds), dv, w, l);
+        if (w & 1)
+            return;
+    }
     if (parts > 1) {
         float *out = shares + ((int64_t)(b * a.Hkv + hk) * ks.shares() + ks.share(tile, part)) *
-                                  (2 * kKeys * DP) + (32 * w + c) * DP;
+                                  (2 * kKeys * DP) + (32 * (w / KW) + c) * DP;
         store_column<float, DP>(out, dk, 1.f, DP);
         store_column<float, DP>(out + kKeys * DP, dv, 1.f, DP);
     } else if (j < a.Tk) {
@@ -332,7 +361,7 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
 
 // Adds up the shares of the tiles first .. first + count - 1 (of `parts` each),
 // four entries of a key a thread.
-template <typename T, int DP>
+template <typename T, int DP, int kKeys>
 __global__ __launch_bounds__(kThreads) void attn_dkv_sum_kernel(AttnProblem a, KeySplit ks, int first,
                                                                 int count, int parts,
                                                                 const float *shares)
@@ -365,7 +394,7 @@ constexpr int kWanted = 512, kLeast = 4;
 // Workgroups that keys with sinks are split over at most.
 constexpr int64_t kMostShares = 4096;
 
-KeySplit key_split(const AttnProblem &p)
+KeySplit key_split(const AttnProblem &p, int kKeys)
 {
     KeySplit k;
     const int G = p.Hq / p.Hkv;
@@ -385,37 +414,61 @@ KeySplit key_split(const AttnProblem &p)
     return k;
 }
 
-template <typename T, int DP>
-hipError_t run(const AttnProblem &p, hipStream_t s)
+// The keys' gradients, in tiles of 128 / KW keys, from delta.
+template <typename T, int DP, int KW>
+hipError_t run_dkv(const AttnProblem &p, const float *delta, hipStream_t s)
 {
-    const KeySplit ks = key_split(p);
-    void *delta = nullptr, *shares = nullptr;
-    hipError_t e = p.ws->take(&delta, (size_t)p.B * p.Hq * p.Tq * 4);
-    if (e == hipSuccess && ks.slots > 0)
+    constexpr int kKeys = 128 / KW;
+    const KeySplit ks = key_split(p, kKeys);
+    void *shares = nullptr;
+    hipError_t e = hipSuccess;
+    if (ks.slots > 0)
         e = p.ws->take(&shares, (size_t)ks.slots * 2 * kKeys * DP * 4);
-    const int64_t nq = (int64_t)p.B * p.Hq * ((p.Tq + 127) / 128), nk = (int64_t)p.B * p.Hkv * ks.blocks();
-    if (nq * kThreads > kMaxThreads || nk * kThreads > kMaxThreads)
+    const int64_t nk = (int64_t)p.B * p.Hkv * ks.blocks();
+    if (nk * kThreads > kMaxThreads)
         return hipErrorInvalidConfiguration;
     if (e != hipSuccess || p.ws->counting)
         return e;
-    attn_dq_kernel<T, DP><<<dim3((unsigned)nq), kThreads, 0, s>>>(p, static_cast<float *>(delta));
-    e = hipGetLastError();
-    if (e != hipSuccess)
-        return e;
-    attn_dkv_kernel<T, DP><<<dim3((unsigned)nk), kThreads, 0, s>>>(p, static_cast<const float *>(delta), ks,
-                                                                   static_cast<float *>(shares));
+    attn_dkv_kernel<T, DP, KW><<<dim3((unsigned)nk), kThreads, 0, s>>>(p, delta, ks, static_cast<float *>(shares));
     e = hipGetLastError();
     const auto sum = [&](int first, int count, int parts) {
         if (e != hipSuccess || count == 0 || parts == 1)
             return;
         const int64_t n = (int64_t)p.B * p.Hkv * count * (2 * kKeys * DP / 4);
-        attn_dkv_sum_kernel<T, DP><<<dim3((unsigned)((n + kThreads - 1) / kThreads)), kThreads, 0, s>>>(
+        attn_dkv_sum_kernel<T, DP, kKeys><<<dim3((unsigned)((n + kThreads - 1) / kThreads)), kThreads, 0, s>>>(
             p, ks, first, count, parts, static_cast<const float *>(shares));
         e = hipGetLastError();
     };
     sum(0, ks.sunk, ks.sparts);
     sum(ks.sunk, ks.tiles - ks.sunk, ks.parts);
     return e;
+}
+
+template <typename T, int DP, int KW>
+hipError_t run_dq(const AttnProblem &p, float *delta, hipStream_t s)
+{
+    const int64_t n = (int64_t)p.B * p.Hq * ((p.Tq + 128 / KW - 1) / (128 / KW));
+    if (n * kThreads > kMaxThreads)
+        return hipErrorInvalidConfiguration;
+    if (p.ws->counting)
+        return hipSuccess;
+    attn_dq_kernel<T, DP, KW><<<dim3((unsigned)n), kThreads, 0, s>>>(p, delta);
+    return hipGetLastError();
+}
+
+template <typename T, int DP>
+hipError_t run(const AttnProblem &p, hipStream_t s)
+{
+    void *delta = nullptr;
+    hipError_t e = p.ws->take(&delta, (size_t)p.B * p.Hq * p.Tq * 4);
+    if (e != hipSuccess)
+        return e;
+    float *d = static_cast<float *>(delta);
+    e = attn_pairs(p, (int64_t)p.B * p.Hq * ((p.Tq + 127) / 128)) ? run_dq<T, DP, 2>(p, d, s) : run_dq<T, DP, 1>(p, d, s);
+    if (e != hipSuccess)
+        return e;
+    return attn_pairs(p, (int64_t)p.B * p.Hkv * ((p.Tk + 127) / 128)) ? run_dkv<T, DP, 2>(p, d, s)
+                                                                      : run_dkv<T, DP, 1>(p, d, s);
 }
 
 template <typename T>

@@ -23,12 +23,14 @@ using namespace attn;
 // stay below 2^8, their bf16 roundings are relative, and few tiles rescale.
 constexpr float kSlack = 8.f;
 
-template <typename T, int DP, int QB>
+// KW: waves that share their queries, each with its part of every tile's keys
+// (1, or 2 of 32 keys each); their shares are joined at the end.
+template <typename T, int DP, int QB, int KW>
 __global__ __launch_bounds__(kThreads, (DP * sizeof(T) * QB <= 128 ? 3 : DP * sizeof(T) * QB <= 256 ? 2 : 1))
 void attn_fwd_kernel(AttnProblem a)
 {
     using X = Tile<T, DP>;
-    constexpr int kSlices = X::kPieces / 2, kTQ = 4 * 32 * QB;
+    constexpr int kSlices = X::kPieces / 2, kTQ = 4 / KW * 32 * QB, NK = 2 / KW;
     __shared__ __attribute__((aligned(16))) char lds[2][2][X::kBytes];
 
     const int G = a.Hq / a.Hkv, nqt = (a.Tq + kTQ - 1) / kTQ;
@@ -46,7 +48,7 @@ void attn_fwd_kernel(AttnProblem a)
     const T *kp = static_cast<const T *>(a.k.p) + b * a.k.sb + hk * a.k.sh;
     const T *vp = static_cast<const T *>(a.v.p) + b * a.v.sb + hk * a.v.sh;
 
-    const int t0 = qt * kTQ, tw = t0 + w * 32 * QB;
+    const int t0 = qt * kTQ, tw = t0 + w / KW * 32 * QB, kb0 = KW == 2 ? w % 2 : 0;
     const KeyTiles wg(a, len, t0, min(kTQ, a.Tq - t0));
     const KeyRange wave(a, len, tw, 32 * QB);
 
@@ -100,12 +102,12 @@ void attn_fwd_kernel(AttnProblem a)
         }
         if (wave.some(k0)) {
             const bool all = wave.all(k0);
-            f32x16_t s[QB][2];
+            f32x16_t s[QB][NK];
             RowFrags<T, DP> kf;
             Turned<T, DP> vf;
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                kf.load(kl, 32 * kb + c);
+            for (int kb = 0; kb < NK; ++kb) {
+                kf.load(kl, 32 * (kb0 + kb) + c);
                 reads_first<T>();
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) {
@@ -117,17 +119,17 @@ void attn_fwd_kernel(AttnProblem a)
                         s[qb][kb] = mma(kf.at(sl), qf[qb][sl], s[qb][kb]);
                 }
             }
-            vf.load(vl, 0);
+            vf.load(vl, 32 * kb0);
             reads_first<T>();
             if (!all) {
                 const bool sunk = k0 < a.sinks;
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
+                    for (int kb = 0; kb < NK; ++kb)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
-                            const int j = k0 + 32 * kb + 8 * (r / 4) + 4 * h + r % 4;
+                            const int j = k0 + 32 * (kb0 + kb) + 8 * (r / 4) + 4 * h + r % 4;
                             s[qb][kb][r] = sees(j, lo[qb], hi[qb], a.sinks, sunk) ? s[qb][kb][r] : -__builtin_inff();
                         }
             }
@@ -136,7 +138,7 @@ void attn_fwd_kernel(AttnProblem a)
             for (int qb = 0; qb < QB; ++qb) {
                 float mx = -__builtin_inff();
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
+                for (int kb = 0; kb < NK; ++kb)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
                         mx = fmaxf(mx, s[qb][kb][r]);
@@ -157,7 +159,7 @@ void attn_fwd_kernel(AttnProblem a)
                 base[qb] = m[qb] == -__builtin_inff() ? 0.f : m[qb] * s2;
             }
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
+            for (int kb = 0; kb < NK; ++kb) {
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) {
                     float part = 0.f;
@@ -169,7 +171,7 @@ void attn_fwd_kernel(AttnProblem a)
                     sum[qb] += part;
                     mma_turned<DP>(vf, Probs<T>(s[qb][kb]), acc[qb]);
                 }
-                if (kb == 0) {
+                if (kb + 1 < NK) {
                     vf.load(vl, 32);
                     reads_first<T>();
                 }
@@ -182,6 +184,32 @@ void attn_fwd_kernel(AttnProblem a)
         lds_barrier();
     }
 
+    if (KW == 2) {   // the odd wave's share to its neighbour, scaled to a common maximum
+        static_assert(QB == 1 || KW == 1, "one block of queries a pair of waves");
+        float *mine = reinterpret_cast<float *>(lds) + w / 2 * (64 * (DP / 2 + 2));
+        if (w & 1) {
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    mine[(16 * db + r) * 64 + l] = acc[0][db][r];
+            mine[DP / 2 * 64 + l] = m[0];
+            mine[(DP / 2 + 1) * 64 + l] = sum[0];
+        }
+        lds_barrier();
+        if (w & 1)
+            return;
+        const float mo = mine[DP / 2 * 64 + l], mn = fmaxf(m[0], mo);
+        const float f = m[0] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m[0] - mn) * s2);
+        const float fo = mo == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((mo - mn) * s2);
+        m[0] = mn;
+        sum[0] = f * sum[0] + fo * mine[(DP / 2 + 1) * 64 + l];
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                acc[0][db][r] = f * acc[0][db][r] + fo * mine[(16 * db + r) * 64 + l];
+    }
     T *op = static_cast<T *>(a.o.p) + b * a.o.sb + hq * a.o.sh;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
@@ -196,25 +224,32 @@ void attn_fwd_kernel(AttnProblem a)
     }
 }
 
-template <typename T, int DP, int QB>
+template <typename T, int DP, int QB, int KW>
 hipError_t run(const AttnProblem &p, hipStream_t s)
 {
-    const int64_t tiles = (p.Tq + 128 * QB - 1) / (128 * QB), blocks = tiles * p.B * p.Hq;
+    constexpr int kTQ = 4 / KW * 32 * QB;
+    const int64_t tiles = (p.Tq + kTQ - 1) / kTQ, blocks = tiles * p.B * p.Hq;
     if (blocks * kThreads > kMaxThreads)
         return hipErrorInvalidConfiguration;
     if (p.ws->counting)
         return hipSuccess;
-    attn_fwd_kernel<T, DP, QB><<<dim3((unsigned)blocks), kThreads, 0, s>>>(p);
+    attn_fwd_kernel<T, DP, QB, KW><<<dim3((unsigned)blocks), kThreads, 0, s>>>(p);
     return hipGetLastError();
+}
+
+template <typename T, int DP>
+hipError_t pick(const AttnProblem &p, hipStream_t s)
+{
+    return attn_pairs(p, (int64_t)p.B * p.Hq * ((p.Tq + 127) / 128)) ? run<T, DP, 1, 2>(p, s) : run<T, DP, 1, 1>(p, s);
 }
 
 template <typename T>
 hipError_t run(const AttnProblem &p, hipStream_t s)
 {
-    return p.D <= 32   ? run<T, 32, 1>(p, s)
-           : p.D <= 64 ? run<T, 64, 1>(p, s)
-           : p.D <= 96 ? run<T, 96, 1>(p, s)
-                       : run<T, 128, 1>(p, s);
+    return p.D <= 32   ? pick<T, 32>(p, s)
+           : p.D <= 64 ? pick<T, 64>(p, s)
+           : p.D <= 96 ? pick<T, 96>(p, s)
+                       : pick<T, 128>(p, s);
 }
 
 }  // namespace
