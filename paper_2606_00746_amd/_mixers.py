@@ -101,20 +101,22 @@ def _sized(name, args, device):
 
 def _norm_sizes(q, k, wq, wk, cos, sin, positions, pairs):
     import torch
-    if q.dim() != 4 or k.dim() != 4:
-        raise ValueError("q and k must be [B, T, H, D]")
     if pairs not in PAIRS:
         raise ValueError(f"pairs must be one of {list(PAIRS)}")
-    if (cos is None) != (sin is None):
-        raise ValueError("cos and sin go together")
     B, T, Hq, D = q.shape
-    Hk = k.shape[2]
-    rows, half = (0, 0) if cos is None else (cos.shape[0], cos.shape[-1])
-    ptrs = (_plain("wq", wq, (D,), q.dtype, q), _plain("wk", wk, (D,), q.dtype, q),
-            _plain("cos", cos, (rows, half), torch.float32, q),
-            _plain("sin", sin, (rows, half), torch.float32, q),
-            _plain("positions", positions, (B, T), torch.int32, q))
-    return B, T, Hq, Hk, D, 2 * half, rows, ptrs
+    rows = half = 0
+    c = s = p = None
+    if cos is not None and sin is not None:
+        rows, half = cos.shape
+        c = _plain("cos", cos, (rows, half), torch.float32, q)
+        s = _plain("sin", sin, (rows, half), torch.float32, q)
+        if positions is not None:
+            p = _plain("positions", positions, (B, T), torch.int32, q)
+    elif cos is not sin:
+        raise ValueError("cos and sin go together")
+    w = (D,)
+    return (B, T, Hq, k.shape[2], D, 2 * half, rows,
+            (_plain("wq", wq, w, q.dtype, q), _plain("wk", wk, w, q.dtype, q), c, s, p))
 
 
 def qk_norm_rotate_fwd(q, k, wq=None, wk=None, cos=None, sin=None, eps: float = 1e-6,

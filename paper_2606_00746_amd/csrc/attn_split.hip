@@ -293,16 +293,34 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnProblem a, Shar
         return;
     const int row = (int)(item % rows), hk = (int)(item / rows % a.Hkv), b = (int)(item / rows / a.Hkv);
     const int64_t at = (((int64_t)b * a.Hkv + hk) * nt + row / kCol) * sh.splits * kCol + row % kCol;
-    float top2 = -__builtin_inff();
-    for (int i = 0; i < sh.splits; ++i)
-        top2 = fmaxf(top2, sh.stat[2 * (at + i * kCol)]);
+    // eight shares at a time, all in flight together
+    constexpr int kAt = 8;
+    float top2 = -__builtin_inff(), z = 0.f;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    float z = 0.f;
-    for (int i = 0; i < sh.splits; ++i) {
-        const float m = sh.stat[2 * (at + i * kCol)];
-        const float f = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - top2);
-        z = fmaf(f, sh.stat[2 * (at + i * kCol) + 1], z);
-        o += f * *reinterpret_cast<const f32x4_t *>(sh.out + (at + i * kCol) * DP + d);
+    for (int i0 = 0; i0 < sh.splits; i0 += kAt) {
+        float m[kAt], y[kAt];
+        f32x4_t x[kAt];
+#pragma unroll
+        for (int i = 0; i < kAt; ++i) {
+            const int64_t j = at + min(i0 + i, sh.splits - 1) * kCol;
+            m[i] = i0 + i < sh.splits ? sh.stat[2 * j] : -__builtin_inff();
+            y[i] = sh.stat[2 * j + 1];
+            x[i] = *reinterpret_cast<const f32x4_t *>(sh.out + j * DP + d);
+        }
+        float mn = top2;
+#pragma unroll
+        for (int i = 0; i < kAt; ++i)
+            mn = fmaxf(mn, m[i]);
+        const float keep = top2 == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(top2 - mn);
+        z *= keep;
+        o *= keep;
+#pragma unroll
+        for (int i = 0; i < kAt; ++i) {
+            const float f = m[i] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m[i] - mn);
+            z = fmaf(f, y[i], z);
+            o += f * x[i];
+        }
+        top2 = mn;
     }
     const int t = row / G, hq = hk * G + row % G;
     const float f = z > 0.f ? 1.f / z : 0.f;

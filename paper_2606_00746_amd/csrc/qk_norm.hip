@@ -102,13 +102,13 @@ __device__ __forceinline__ void load_angles(Angles &g, const float *cs, const fl
     if (P == kNone)
         return;
     if (P == kHalfRuns) {
-        if (r.a >= 0 && r.a < R / 2) {
-            load8(cs + r.a, g.c[0]);
-            load8(sn + r.a, g.s[0]);
-        } else {
+        const bool on = r.a >= 0 && r.a < R / 2;
+        load8(cs + (on ? r.a : 0), g.c[0]);
+        load8(sn + (on ? r.a : 0), g.s[0]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                g.c[0][e] = 1.f, g.s[0][e] = 0.f;
+        for (int e = 0; e < 8; ++e) {
+            g.c[0][e] = on ? g.c[0][e] : 1.f;
+            g.s[0][e] = on ? g.s[0][e] : 0.f;
         }
         return;
     }
@@ -337,12 +337,13 @@ __global__ __launch_bounds__(kBlk) void norm_bwd_kernel(NormProblem p, int lanes
     }
 }
 
-// dw from the blocks' shares: 16 columns a workgroup, its 16 rows of threads
-// adding every 16th share, then their sums in order.
+// dw from the blocks' shares: 16 columns a workgroup, its 64 rows of threads
+// adding every 64th share, eight in flight, then their sums in order.
+constexpr int kSumRows = 64;
 template <typename T>
-__global__ __launch_bounds__(kBlk) void norm_dw_kernel(NormProblem p, const float *part, int nbq, int nbk)
+__global__ __launch_bounds__(16 * kSumRows) void norm_dw_kernel(NormProblem p, const float *part, int nbq, int nbk)
 {
-    __shared__ float sums[16][17];
+    __shared__ float sums[kSumRows][17];
     const int cols = (p.D + 15) / 16, second = blockIdx.x / cols;
     const int e = blockIdx.x % cols * 16 + threadIdx.x % 16, i0 = threadIdx.x / 16;
     const int n = second ? nbk : nbq;
@@ -352,14 +353,21 @@ __global__ __launch_bounds__(kBlk) void norm_dw_kernel(NormProblem p, const floa
         return;
     float s = 0.f;
     if (e < p.D)
-        for (int i = i0; i < n; i += 16)
-            s += in[(int64_t)i * p.D + e];
+        for (int i = i0; i < n; i += 8 * kSumRows) {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                x[j] = i + j * kSumRows < n ? in[(int64_t)(i + j * kSumRows) * p.D + e] : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                s += x[j];
+        }
     sums[i0][threadIdx.x % 16] = s;
     __syncthreads();
     if (i0 == 0 && e < p.D) {
         float a = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
+        for (int i = 0; i < kSumRows; ++i)
             a += sums[i][threadIdx.x];
         store_f(static_cast<T *>(out) + e, a);
     }
@@ -431,7 +439,7 @@ hipError_t bwd(const NormProblem &p, hipStream_t s)
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !part)
         return e;
-    norm_dw_kernel<T><<<dim3((unsigned)(2 * ((p.D + 15) / 16))), kBlk, 0, s>>>(p, static_cast<const float *>(part), nbq, nbk);
+    norm_dw_kernel<T><<<dim3((unsigned)(2 * ((p.D + 15) / 16))), 16 * kSumRows, 0, s>>>(p, static_cast<const float *>(part), nbq, nbk);
     return hipGetLastError();
 }
 
