@@ -347,7 +347,7 @@ int64_t keys_of(const AttnProblem &p)
 }
 
 // Workgroups wanted at least, and blocks of keys that a wave of one has at least.
-constexpr int kWanted = 1024, kLeast = 2;
+constexpr int kWanted = 2048, kLeast = 2;
 
 template <typename T, int DP>
 hipError_t run(const AttnProblem &p, hipStream_t s)
