@@ -146,6 +146,78 @@ struct Tile {
     }
 };
 
+// The offset of an LDS address, as LDS instructions take it.
+__device__ __forceinline__ uint32_t lds_offset(const void *p)
+{
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)(p);
+}
+
+// bf16 tiles on their way from memory straight into LDS (no registers, several
+// tiles ahead), in Tile's order: a load writes 64 lanes' pieces one after the
+// other, so a lane reads the piece that belongs at its place.  Rows past the last
+// and columns past D read as the last: their products count for nothing (weights
+// of 0, columns that are not stored), and what they read is finite.
+template <int DP>
+struct Flow {
+    using X = Tile<bf16_t, DP>;
+    static constexpr int kLoads = kRows * X::kS / kThreads;   // loads of a wave and tile
+    static constexpr int kStep = kThreads / X::kS;            // rows between a thread's pieces
+    int row, col;      // of this thread's first piece: row of the tile, byte in the row
+    uint32_t off;
+    int64_t st;
+    __device__ __forceinline__ void start(int64_t stride, int D)
+    {
+        st = stride;
+        row = threadIdx.x / X::kS;
+        col = 16 * min((int)(threadIdx.x % X::kS) ^ X::swizzle(row), D / 8 - 1);
+        off = (uint32_t)(row * (int)st * 2 + col);
+    }
+    // Rows row0 .. row0 + 63 (row0 < rows) to lds.
+    __device__ __forceinline__ void load(char *lds, const bf16_t *base, int row0, int rows, int w) const
+    {
+        const rsrc_t r = make_rsrc(base + (int64_t)row0 * st, 0xffffffffu);
+        const int n = rows - row0;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            auto to = (__attribute__((address_space(3))) void *)(lds + i * (kThreads * 16) + w * 1024);
+            if (n >= kRows)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, off, i * kStep * (int)st * 2, 0, 0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, (uint32_t)(min(row + i * kStep, n - 1) * (int)st * 2 + col), 0, 0, 0);
+        }
+    }
+};
+
+// Waits until at most N of the wave's loads are on their way, then for the other waves.
+template <int N>
+__device__ __forceinline__ void landed()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+}
+
+// Reads of such tiles: the compiler would hold every LDS read until all of the
+// loads into LDS have come, so these are its instructions by hand, each group with
+// its wait, into registers of their own.
+template <int N, int O>
+__device__ __forceinline__ void lds_read4(const uint32_t (&a)[N], int at, u32x4 (&v)[N])
+{
+    asm volatile("ds_read_b128 %0, %4 offset:%8\n\tds_read_b128 %1, %5 offset:%8\n\t"
+                 "ds_read_b128 %2, %6 offset:%8\n\tds_read_b128 %3, %7 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(v[at]), "=&v"(v[at + 1]), "=&v"(v[at + 2]), "=&v"(v[at + 3])
+                 : "v"(a[at]), "v"(a[at + 1]), "v"(a[at + 2]), "v"(a[at + 3]), "n"(O)
+                 : "memory");
+}
+template <int N, int O>
+__device__ __forceinline__ void lds_read2(const uint32_t (&a)[N], int at, u32x4 (&v)[N])
+{
+    asm volatile("ds_read_b128 %0, %2 offset:%4\n\tds_read_b128 %1, %3 offset:%4\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(v[at]), "=&v"(v[at + 1])
+                 : "v"(a[at]), "v"(a[at + 1]), "n"(O)
+                 : "memory");
+}
+
 // A row-wise fragment: 16 bytes of a row, the columns 2 s + l / 32 pieces in.
 template <typename T>
 struct Frag;
@@ -311,6 +383,56 @@ struct RowFrags<float, DP> {
         return tile_frag<float, DP>(lds, row, 2 * s + (int)(threadIdx.x % 64 / 32));
     }
 };
+
+// The same from tiles that flowed in: `tile` is their LDS offset.  The piece and
+// the row lie in different bits of an address, so that pieces differ by exclusive
+// ors and 32-row blocks by constants.
+template <int DP, int BLOCK>
+__device__ __forceinline__ void flow_rows(uint32_t tile, Frag<bf16_t> (&f)[DP / 16])
+{
+    using X = Tile<bf16_t, DP>;
+    const int c = threadIdx.x % 32, h = threadIdx.x % 64 / 32;
+    const uint32_t a0 = tile + X::at(c, h);
+    uint32_t a[DP / 16];
+    u32x4 v[DP / 16];
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s)
+        a[s] = a0 ^ (32 * s);
+    constexpr int kAt = BLOCK * 32 * X::kS * 16;
+#pragma unroll
+    for (int s = 0; s + 4 <= DP / 16; s += 4)
+        lds_read4<DP / 16, kAt>(a, s, v);
+    if constexpr (DP / 16 % 4 == 2)
+        lds_read2<DP / 16, kAt>(a, DP / 16 - 2, v);
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s)
+        f[s].v = __builtin_bit_cast(bf16x8_t, v[s]);
+}
+template <int DP, int BLOCK>
+__device__ __forceinline__ void flow_turned(uint32_t tile, Turned<bf16_t, DP> &x)
+{
+    using X = Tile<bf16_t, DP>;
+    const int l = threadIdx.x % 64, h = l / 32, i = l % 16, r = 4 * h + (i >> 2);
+    const uint32_t a0 = tile + X::at(r, 2 * (l % 32 / 16) + ((i & 3) >> 1)) + 8 * (i & 1);
+    constexpr int kAt = BLOCK * 32 * X::kS * 16, kRow = X::kS * 16;
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db) {
+        // rows 8 on: the other exclusive or
+        const uint32_t a = a0 ^ (64 * db), b = a ^ 32;
+        u32x2 v[4];
+        asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %5 offset:%7\n\t"
+                     "ds_read_b64_tr_b16 %2, %4 offset:%8\n\tds_read_b64_tr_b16 %3, %5 offset:%9\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+                     : "v"(a), "v"(b), "n"(kAt), "n"(kAt + 8 * kRow), "n"(kAt + 16 * kRow), "n"(kAt + 24 * kRow)
+                     : "memory");
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const u32x4 w = {v[2 * t][0], v[2 * t][1], v[2 * t + 1][0], v[2 * t + 1][1]};
+            x.v[t][db] = __builtin_bit_cast(bf16x8_t, w);
+        }
+    }
+}
 
 // bf16: reads of LDS stay ahead of the products they are for, as written (the
 // compiler otherwise puts each read next to its use and waits for it).

@@ -31,7 +31,11 @@ void attn_fwd_kernel(AttnProblem a)
 {
     using X = Tile<T, DP>;
     constexpr int kSlices = X::kPieces / 2, kTQ = 4 / KW * 32 * QB, NK = 2 / KW;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][X::kBytes];
+    // bf16 tiles flow straight into LDS, two ahead where three fit beside other
+    // workgroups; fp32 tiles come through registers
+    constexpr bool kFlows = sizeof(T) == 2;
+    constexpr int kSlots = kFlows && DP <= 64 ? 3 : 2, kAhead = kSlots - 1;
+    __shared__ __attribute__((aligned(16))) char lds[kSlots][2][X::kBytes];
 
     const int G = a.Hq / a.Hkv, nqt = (a.Tq + kTQ - 1) / kTQ;
     int id = xcd_remap(blockIdx.x, gridDim.x);
@@ -79,24 +83,46 @@ void attn_fwd_kernel(AttnProblem a)
     const float s2 = a.scale * kLog2e, slack = kSlack / s2;
 
     X kt, vt;
-    kt.start(a.k.st, a.D);
-    vt.start(a.v.st, a.D);
+    Flow<DP> kw, vw;
     const int n = wg.n;
-    if (n > 0) {
-        kt.load(kp, a.k.st, wg.row(0), len, a.D);
-        vt.load(vp, a.v.st, wg.row(0), len, a.D);
-        kt.store(lds[0][0]);
-        vt.store(lds[0][1]);
-    }
+    const auto flow = [&](int it) {
+        if constexpr (kFlows) {
+            kw.load(lds[it % kSlots][0], kp, wg.row(it), len, w);
+            vw.load(lds[it % kSlots][1], vp, wg.row(it), len, w);
+        }
+    };
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
         arrived(qf[qb]);
-    lds_barrier();
+    if constexpr (kFlows) {
+        kw.start(a.k.st, a.D);
+        vw.start(a.v.st, a.D);
+        for (int it = 0; it < min(n, kAhead); ++it)
+            flow(it);
+    } else {
+        kt.start(a.k.st, a.D);
+        vt.start(a.v.st, a.D);
+        if (n > 0) {
+            kt.load(kp, a.k.st, wg.row(0), len, a.D);
+            vt.load(vp, a.v.st, wg.row(0), len, a.D);
+            kt.store(lds[0][0]);
+            vt.store(lds[0][1]);
+        }
+        lds_barrier();
+    }
 
     for (int it = 0; it < n; ++it) {
         const int k0 = wg.row(it);
-        const char *kl = lds[it & 1][0], *vl = lds[it & 1][1];
-        if (it + 1 < n) {
+        const char *kl = lds[it % kSlots][0], *vl = lds[it % kSlots][1];
+        if constexpr (kFlows) {
+            // this tile has come, and every wave is done with the one before it
+            if (kAhead == 2 && it + 1 < n)
+                landed<2 * Flow<DP>::kLoads>();
+            else
+                landed<0>();
+            if (it + kAhead < n)
+                flow(it + kAhead);
+        } else if (it + 1 < n) {
             kt.load(kp, a.k.st, wg.row(it + 1), len, a.D);
             vt.load(vp, a.v.st, wg.row(it + 1), len, a.D);
         }
@@ -107,8 +133,14 @@ void attn_fwd_kernel(AttnProblem a)
             Turned<T, DP> vf;
 #pragma unroll
             for (int kb = 0; kb < NK; ++kb) {
-                kf.load(kl, 32 * (kb0 + kb) + c);
-                reads_first<T>();
+                if constexpr (kFlows) {
+                    if (kb0 + kb == 0)
+                        flow_rows<DP, 0>(lds_offset(kl), kf.f);
+                    else
+                        flow_rows<DP, 1>(lds_offset(kl), kf.f);
+                } else {
+                    kf.load(kl, 32 * (kb0 + kb) + c);
+                }
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) {
 #pragma unroll
@@ -119,8 +151,17 @@ void attn_fwd_kernel(AttnProblem a)
                         s[qb][kb] = mma(kf.at(sl), qf[qb][sl], s[qb][kb]);
                 }
             }
-            vf.load(vl, 32 * kb0);
-            reads_first<T>();
+            const auto turn = [&](int kb) {
+                if constexpr (kFlows) {
+                    if (kb == 0)
+                        flow_turned<DP, 0>(lds_offset(vl), vf);
+                    else
+                        flow_turned<DP, 1>(lds_offset(vl), vf);
+                } else {
+                    vf.load(vl, 32 * kb);
+                }
+            };
+            turn(kb0);
             if (!all) {
                 const bool sunk = k0 < a.sinks;
 #pragma unroll
@@ -171,18 +212,20 @@ void attn_fwd_kernel(AttnProblem a)
                     sum[qb] += part;
                     mma_turned<DP>(vf, Probs<T>(s[qb][kb]), acc[qb]);
                 }
-                if (kb + 1 < NK) {
-                    vf.load(vl, 32);
-                    reads_first<T>();
-                }
+                if (kb + 1 < NK)
+                    turn(1);
             }
         }
-        if (it + 1 < n) {
-            kt.store(lds[(it + 1) & 1][0]);
-            vt.store(lds[(it + 1) & 1][1]);
+        if constexpr (!kFlows) {
+            if (it + 1 < n) {
+                kt.store(lds[(it + 1) & 1][0]);
+                vt.store(lds[(it + 1) & 1][1]);
+            }
+            lds_barrier();
         }
-        lds_barrier();
     }
+    if (kFlows && KW == 2)
+        lds_barrier();
 
     if (KW == 2) {   // the odd wave's share to its neighbour, scaled to a common maximum
         static_assert(QB == 1 || KW == 1, "one block of queries a pair of waves");
