@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libgspn.so")
 SOURCES = ["api.cpp", "scan_tiny.hip", "scan_small.hip", "scan_med_64.hip", "scan_med_56.hip",
            "scan_med_48.hip", "scan_med_40_32_24.hip", "scan_med.hip", "scan_pm.hip",
            "scan_wide.hip", "scan_norm.hip", "scan_plane.hip", "scan_line.hip", "scan_general.hip", "latent.hip",
-           "mixers_api.cpp", "qk_norm.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_split.hip",
+           "mixers_api.cpp", "qk_norm.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_bwd_f32.hip", "attn_split.hip",
            "delta_fwd.hip", "delta_bwd.hip", "delta_bf16.hip"]
 ARCH = "gfx950"
 
@@ -24,7 +24,7 @@ HIPCC_FLAGS = [
     "-I", os.path.join(HERE, "..", "include"),
 ]
 
-# Attention's gradient kernels keep up to 128 accumulator registers a lane beside as
+# Attention's bf16 gradient kernels keep up to 128 accumulator registers a lane beside as
 # many operands: with results of matrix instructions in vector registers the compiler
 # does not copy them between the two register files around every tile (key gradients
 # at heads of 128: 628 -> 398 us).

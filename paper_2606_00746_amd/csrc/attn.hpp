@@ -42,6 +42,7 @@ struct AttnProblem {
 
 hipError_t launch_attn_fwd(const AttnProblem &p, hipStream_t s);
 hipError_t launch_attn_bwd(const AttnProblem &p, hipStream_t s);
+hipError_t launch_attn_bwd_f32(const AttnProblem &p, hipStream_t s);
 hipError_t launch_attn_split(const AttnProblem &p, hipStream_t s);
 bool attn_split_preferred(const AttnProblem &p);
 
@@ -152,8 +153,8 @@ __device__ __forceinline__ uint32_t lds_offset(const void *p)
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)(p);
 }
 
-// bf16 tiles on their way from memory straight into LDS (no registers, several
-// tiles ahead), in Tile's order: a load writes 64 lanes' pieces one after the
+// bf16 tiles on their way from memory straight into LDS, through no registers, in
+// Tile's order: a load writes 64 lanes' pieces one after the
 // other, so a lane reads the piece that belongs at its place.  Rows past the last
 // and columns past D read as the last: their products count for nothing (weights
 // of 0, columns that are not stored), and what they read is finite.
@@ -188,11 +189,10 @@ struct Flow {
     }
 };
 
-// Waits until at most N of the wave's loads are on their way, then for the other waves.
-template <int N>
+// Waits for the wave's loads, then for the other waves'.
 __device__ __forceinline__ void landed()
 {
-    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
 }
@@ -432,6 +432,19 @@ __device__ __forceinline__ void flow_turned(uint32_t tile, Turned<bf16_t, DP> &x
             x.v[t][db] = __builtin_bit_cast(bf16x8_t, w);
         }
     }
+}
+
+// The rows' statistics of a 32 x 32 block as its registers need them: rows 8 g +
+// 4 (l / 32) .. of 64 values at `at`.
+template <int BLOCK>
+__device__ __forceinline__ void flow_stats(uint32_t at, f32x4_t (&v)[4])
+{
+    const uint32_t a = at + 16 * (threadIdx.x % 64 / 32);
+    asm volatile("ds_read_b128 %0, %4 offset:%5\n\tds_read_b128 %1, %4 offset:%6\n\t"
+                 "ds_read_b128 %2, %4 offset:%7\n\tds_read_b128 %3, %4 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+                 : "v"(a), "n"(128 * BLOCK), "n"(128 * BLOCK + 32), "n"(128 * BLOCK + 64), "n"(128 * BLOCK + 96)
+                 : "memory");
 }
 
 // bf16: reads of LDS stay ahead of the products they are for, as written (the

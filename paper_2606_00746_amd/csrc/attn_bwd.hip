@@ -1,490 +1,11 @@
-// Gradient of windowed attention (gspn_window_attn_bwd).
-//
-//   p_ij = exp(scale q_i k_j - lse_i)          (again from q, k and the forward's lse)
-//   d_i  = sum_e do_ie o_ie
-//   ds_ij = p_ij (do_i v_j - d_i)
-//   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i
-//
-// Two kernels, so that no sum crosses workgroups in an order of its own:
-//  * attn_dq_kernel owns 128 queries and runs over their keys as the forward
-//    does; it also forms d_i, which the other kernel reads;
-//  * attn_dkv_kernel owns 128 keys (a wave 32 of them) and runs over the
-//    queries that see them, of every head that shares the keys.
-// The scores are formed twice, which costs 2 of the 7 products; the sums over
-// queries of either kernel are in a fixed order and need no atomics.  Keys that
-// all later queries see (sinks), and calls with few keys, have their
-// queries split over several workgroups, whose fp32 shares are added up, in
-// order, by attn_dkv_sum_kernel.
-#include <algorithm>
-
-#include "attn.hpp"
+// Gradient of windowed attention, bf16 storage.
+#include "attn_bwd.hpp"
 
 namespace gspn {
-namespace {
-
-using namespace attn;
-
-// KW: waves that share their rows, each with its part of a tile (1, or 2 with 32
-// rows of it each): the odd wave's sums are added to its neighbour's at the end.
-template <int N>
-__device__ __forceinline__ void join_pair(float *lds, f32x16_t (&acc)[N], int w, int l)
-{
-    float *mine = lds + w / 2 * (64 * 16 * N);
-    lds_barrier();
-    if (w & 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                mine[(16 * i + r) * 64 + l] = acc[i][r];
-    lds_barrier();
-    if (!(w & 1))
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                acc[i][r] += mine[(16 * i + r) * 64 + l];
-}
-
-template <typename T>
-__device__ __forceinline__ float dot(Frag<T> a, Frag<T> b)
-{
-    constexpr int n = 16 / sizeof(T);
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < n; ++e)
-        s = fmaf((float)a.v[e], (float)b.v[e], s);
-    return s;
-}
-
-template <typename T, int DP, int KW>
-__global__ __launch_bounds__(kThreads, (DP * sizeof(T) <= 128 ? 2 : 1))
-void attn_dq_kernel(AttnProblem a, float *delta)
-{
-    using X = Tile<T, DP>;
-    constexpr int kSlices = X::kPieces / 2, kTQ = 128 / KW;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][X::kBytes];
-
-    const int G = a.Hq / a.Hkv, nqt = (a.Tq + kTQ - 1) / kTQ;
-    int id = xcd_remap(blockIdx.x, gridDim.x);
-    const int g = id % G;
-    id /= G;
-    const int qt = id % nqt;
-    id /= nqt;
-    const int hk = id % a.Hkv, b = id / a.Hkv, hq = hk * G + g;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x % 64;
-    const int c = l % 32, h = l / 32;
-    const int len = seq_len(a, b);
-
-    const T *kp = static_cast<const T *>(a.k.p) + b * a.k.sb + hk * a.k.sh;
-    const T *vp = static_cast<const T *>(a.v.p) + b * a.v.sb + hk * a.v.sh;
-    const int t0 = qt * kTQ, tw = t0 + w / KW * 32, t = tw + c, tr = min(t, a.Tq - 1);
-    const int kb0 = KW == 2 ? w % 2 : 0;
-    const KeyTiles wg(a, len, t0, min(kTQ, a.Tq - t0));
-    const KeyRange wave(a, len, tw, 32);
-    int lo, hi;
-    key_bounds(a, len, t + a.offset, lo, hi);
-
-    Frag<T> qf[kSlices], df[kSlices];
-    const T *qr = static_cast<const T *>(a.q.p) + b * a.q.sb + hq * a.q.sh + tr * a.q.st;
-    const T *dr = static_cast<const T *>(a.dout.p) + b * a.dout.sb + hq * a.dout.sh + tr * a.dout.st;
-    const T *orow = static_cast<const T *>(a.o.p) + b * a.o.sb + hq * a.o.sh + tr * a.o.st;
-    float d = 0.f;
-#pragma unroll
-    for (int s = 0; s < kSlices; ++s) {
-        qf[s] = row_frag(qr, 2 * s + h, a.D);
-        df[s] = row_frag(dr, 2 * s + h, a.D);
-        d += dot(df[s], row_frag(orow, 2 * s + h, a.D));
-    }
-    d = half_sum(d);
-    const int64_t stat = ((int64_t)b * a.Hq + hq) * a.Tq + tr;
-    if (t < a.Tq && h == 0)
-        delta[stat] = d;
-    const float s2 = a.scale * kLog2e, lse2 = a.lse[stat] * kLog2e;
-
-    f32x16_t acc[DP / 32];
-#pragma unroll
-    for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-            acc[db][r] = 0.f;
-
-    X kt, vt;
-    kt.start(a.k.st, a.D);
-    vt.start(a.v.st, a.D);
-    const int n = wg.n;
-    if (n > 0) {
-        kt.load(kp, a.k.st, wg.row(0), len, a.D);
-        vt.load(vp, a.v.st, wg.row(0), len, a.D);
-        kt.store(lds[0][0]);
-        vt.store(lds[0][1]);
-    }
-    arrived(qf);
-    arrived(df);
-    lds_barrier();
-    for (int it = 0; it < n; ++it) {
-        const int k0 = wg.row(it);
-        const char *kl = lds[it & 1][0], *vl = lds[it & 1][1];
-        if (it + 1 < n) {
-            kt.load(kp, a.k.st, wg.row(it + 1), len, a.D);
-            vt.load(vp, a.v.st, wg.row(it + 1), len, a.D);
-        }
-        if (wave.some(k0)) {
-            const bool all = wave.all(k0);
-#pragma unroll
-            for (int kb = kb0; kb < kb0 + 2 / KW; ++kb) {
-                f32x16_t s, dp;
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    s[r] = dp[r] = 0.f;
-                RowFrags<T, DP> kf, vf;
-                Turned<T, DP> kx;
-                kf.load(kl, 32 * kb + c);
-                vf.load(vl, 32 * kb + c);
-                reads_first<T>();
-#pragma unroll
-                for (int sl = 0; sl < kSlices; ++sl) {
-                    s = mma(kf.at(sl), qf[sl], s);
-                    dp = mma(vf.at(sl), df[sl], dp);
-                }
-                kx.load(kl, 32 * kb);
-                reads_first<T>();
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], s2, -lse2)) * (dp[r] - d);
-                if (!all) {
-                    const bool sunk = k0 < a.sinks;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = k0 + 32 * kb + 8 * (r / 4) + 4 * h + r % 4;
-                        s[r] = sees(j, lo, hi, a.sinks, sunk) ? s[r] : 0.f;
-                    }
-                }
-                mma_turned<DP>(kx, Probs<T>(s), acc);
-            }
-        }
-        if (it + 1 < n) {
-            kt.store(lds[(it + 1) & 1][0]);
-            vt.store(lds[(it + 1) & 1][1]);
-        }
-        lds_barrier();
-    }
-    if (KW == 2)
-        join_pair(reinterpret_cast<float *>(lds), acc, w, l);
-    if (t < a.Tq && (KW == 1 || !(w & 1)))
-        store_column<T, DP>(static_cast<T *>(a.dq.p) + b * a.dq.sb + hq * a.dq.sh + t * a.dq.st, acc,
-                            a.scale, a.D);
-}
-
-// How the keys' tiles of one (b, head) go to workgroups: `sunk` tiles that hold
-// sinks, each split over `sparts` of them, then the others over `parts`.
-struct KeySplit {
-    int tiles, sunk, sparts, parts;
-    int64_t slots;           // fp32 shares of a tile, over the batch
-    __host__ __device__ int blocks() const { return sunk * sparts + (tiles - sunk) * parts; }
-    // shares ahead of this (b, head)'s tile: tiles with one part have none
-    __host__ __device__ int shares() const
-    {
-        return (sparts > 1 ? sunk * sparts : 0) + (parts > 1 ? (tiles - sunk) * parts : 0);
-    }
-    __host__ __device__ int share(int tile, int part) const
-    {
-        if (tile < sunk)
-            return tile * sparts + part;
-        return (sparts > 1 ? sunk * sparts : 0) + (tile - sunk) * parts + part;
-    }
-};
-
-template <typename T, int DP, int KW>
-__global__ __launch_bounds__(kThreads, (DP * sizeof(T) <= 128 ? 2 : 1))
-void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shares)
-{
-    using X = Tile<T, DP>;
-    constexpr int kSlices = X::kPieces / 2, kKeys = 128 / KW;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][X::kBytes];
-    __shared__ __attribute__((aligned(16))) float stats[2][2][kRows];
-
-    const int G = a.Hq / a.Hkv, per = ks.blocks();
-    int id = xcd_remap(blockIdx.x, gridDim.x);
-    const int x = id % per;
-    id /= per;
-    const int hk = id % a.Hkv, b = id / a.Hkv;
-    int tile, part, parts;
-    if (x < ks.sunk * ks.sparts) {
-        tile = x / ks.sparts, part = x % ks.sparts, parts = ks.sparts;
-    } else {
-        const int y = x - ks.sunk * ks.sparts;
-        tile = ks.sunk + y / ks.parts, part = y % ks.parts, parts = ks.parts;
-    }
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x % 64;
-    const int c = l % 32, h = l / 32;
-    const int len = seq_len(a, b);
-    const int k0 = tile * kKeys, kw = k0 + 32 * (w / KW), j = kw + c, qb0 = KW == 2 ? w % 2 : 0;
-
-    // queries t that see some key of the workgroup, of the wave (some, all), of the lane
-    const auto after = [&](int key) { return a.right < 0 ? 0 : max(0, key - a.right - a.offset); };
-    const auto until = [&](int key) {
-        const int e = a.left < 0 || key < a.sinks ? len - 1 : min(len - 1, key + a.left);
-        return key >= len ? -1 : min(a.Tq - 1, e - a.offset);
-    };
-    const int ta = after(k0), tb = max(until(k0), until(min(len - 1, k0 + kKeys - 1)));
-    const int some_a = after(kw), some_b = max(until(kw), until(min(len - 1, kw + 31)));
-    const int all_a = after(kw + 31);
-    const int all_b = kw + 31 >= len ? -1 : min(until(kw + 31), until(max(kw, min(a.sinks, kw + 31))));
-    const int lane_a = after(j), lane_b = until(j);
-
-    const int first = ta / kRows, nt = k0 >= len || tb < ta ? 0 : tb / kRows + 1 - first;
-    const int total = nt * G;
-    const int i0 = (int)((int64_t)total * part / parts), i1 = (int)((int64_t)total * (part + 1) / parts);
-
-    Frag<T> kf[kSlices], vf[kSlices];
-    const int jr = max(0, min(j, len - 1));
-    const T *kr = static_cast<const T *>(a.k.p) + b * a.k.sb + hk * a.k.sh + jr * a.k.st;
-    const T *vr = static_cast<const T *>(a.v.p) + b * a.v.sb + hk * a.v.sh + jr * a.v.st;
-#pragma unroll
-    for (int s = 0; s < kSlices; ++s) {
-        kf[s] = row_frag(kr, 2 * s + h, a.D);
-        vf[s] = row_frag(vr, 2 * s + h, a.D);
-    }
-    f32x16_t dk[DP / 32], dv[DP / 32];
-#pragma unroll
-    for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-            dk[db][r] = dv[db][r] = 0.f;
-    const float s2 = a.scale * kLog2e;
-
-    X qt, dt;
-    qt.start(a.q.st, a.D);
-    dt.start(a.dout.st, a.D);
-    float stat = 0.f;
-    // queries from qrows on stand past the sequence's end: they count as zero rows
-    const int qrows = max(0, min(a.Tq, len - a.offset));
-    const auto fetch = [&](int i) {
-        const int hq = hk * G + i / nt, t0 = (first + i % nt) * kRows;
-        qt.load(static_cast<const T *>(a.q.p) + b * a.q.sb + hq * a.q.sh, a.q.st, t0, qrows, a.D);
-        dt.load(static_cast<const T *>(a.dout.p) + b * a.dout.sb + hq * a.dout.sh, a.dout.st, t0, qrows,
-                a.D);
-        if (threadIdx.x < 2 * kRows) {
-            const int t = t0 + threadIdx.x % kRows;
-            const float *src = threadIdx.x < kRows ? a.lse : delta;
-            stat = t < qrows ? src[((int64_t)b * a.Hq + hq) * a.Tq + t] : 0.f;
-        }
-    };
-    const auto put = [&](int buf) {
-        qt.store(lds[buf][0]);
-        dt.store(lds[buf][1]);
-        if (threadIdx.x < 2 * kRows)
-            stats[buf][threadIdx.x / kRows][threadIdx.x % kRows] =
-                threadIdx.x < kRows ? stat * kLog2e : stat;
-    };
-    if (i0 < i1) {
-        fetch(i0);
-        put(0);
-    }
-    arrived(kf);
-    arrived(vf);
-    lds_barrier();
-    for (int i = i0; i < i1; ++i) {
-        const int buf = (i - i0) & 1, t0 = (first + i % nt) * kRows;
-        const char *ql = lds[buf][0], *dl = lds[buf][1];
-        if (i + 1 < i1)
-            fetch(i + 1);
-        if (t0 <= some_b && t0 + kRows > some_a) {
-            const bool all = t0 >= all_a && t0 + kRows - 1 <= all_b;
-#pragma unroll
-            for (int qb = qb0; qb < qb0 + 2 / KW; ++qb) {
-                f32x16_t s, dp;
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    s[r] = dp[r] = 0.f;
-                RowFrags<T, DP> qf, df;
-                Turned<T, DP> qx, dx;
-                qf.load(ql, 32 * qb + c);
-                df.load(dl, 32 * qb + c);
-                reads_first<T>();
-#pragma unroll
-                for (int sl = 0; sl < kSlices; ++sl) {
-                    s = mma(qf.at(sl), kf[sl], s);
-                    dp = mma(df.at(sl), vf[sl], dp);
-                }
-                f32x4_t ls[4], de[4];
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    ls[g] = *reinterpret_cast<const f32x4_t *>(&stats[buf][0][32 * qb + 8 * g + 4 * h]);
-                    de[g] = *reinterpret_cast<const f32x4_t *>(&stats[buf][1][32 * qb + 8 * g + 4 * h]);
-                }
-                dx.load(dl, 32 * qb);
-                reads_first<T>();
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], s2, -ls[r / 4][r % 4]));
-                    dp[r] = s[r] * (dp[r] - de[r / 4][r % 4]);
-                }
-                if (!all) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int t = t0 + 32 * qb + 8 * (r / 4) + 4 * h + r % 4;
-                        const bool see = (uint32_t)(t - lane_a) <= (uint32_t)(lane_b - lane_a) && lane_b >= lane_a;
-                        s[r] = see ? s[r] : 0.f;
-                        dp[r] = see ? dp[r] : 0.f;
-                    }
-                }
-                mma_turned<DP>(dx, Probs<T>(s), dv);
-                qx.load(ql, 32 * qb);
-                mma_turned<DP>(qx, Probs<T>(dp), dk);
-            }
-        }
-        if (i + 1 < i1)
-            put(buf ^ 1);
-        lds_barrier();
-    }
-
-    if (KW == 2) {
-        join_pair(reinterpret_cast<float *>(lds), dk, w, l);
-        join_pair(reinterpret_cast<float *>(lds), dv, w, l);
-        if (w & 1)
-            return;
-    }
-    if (parts > 1) {
-        float *out = shares + ((int64_t)(b * a.Hkv + hk) * ks.shares() + ks.share(tile, part)) *
-                                  (2 * kKeys * DP) + (32 * (w / KW) + c) * DP;
-        store_column<float, DP>(out, dk, 1.f, DP);
-        store_column<float, DP>(out + kKeys * DP, dv, 1.f, DP);
-    } else if (j < a.Tk) {
-        store_column<T, DP>(static_cast<T *>(a.dk.p) + b * a.dk.sb + hk * a.dk.sh + j * a.dk.st, dk,
-                            a.scale, a.D);
-        store_column<T, DP>(static_cast<T *>(a.dv.p) + b * a.dv.sb + hk * a.dv.sh + j * a.dv.st, dv, 1.f,
-                            a.D);
-    }
-}
-
-// Adds up the shares of the tiles first .. first + count - 1 (of `parts` each),
-// four entries of a key a thread.
-template <typename T, int DP, int kKeys>
-__global__ __launch_bounds__(kThreads) void attn_dkv_sum_kernel(AttnProblem a, KeySplit ks, int first,
-                                                                int count, int parts,
-                                                                const float *shares)
-{
-    constexpr int kQuads = DP / 4, kAll = 2 * kKeys * kQuads;
-    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (id >= (int64_t)a.B * a.Hkv * count * kAll)
-        return;
-    const int e = (int)(id % kAll);
-    const int64_t item = id / kAll;
-    const int tile = first + (int)(item % count), hk = (int)(item / count % a.Hkv);
-    const int b = (int)(item / count / a.Hkv);
-    const int which = e / (kKeys * kQuads), key = e / kQuads % kKeys, d = e % kQuads * 4;
-    const int j = tile * kKeys + key;
-    if (j >= a.Tk || d >= a.D)
-        return;
-    const float *in = shares + ((int64_t)(b * a.Hkv + hk) * ks.shares() + ks.share(tile, 0)) *
-                                   (2 * kKeys * DP) + which * kKeys * DP + key * DP + d;
-    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < parts; ++i)
-        sum += *reinterpret_cast<const f32x4_t *>(in + (int64_t)i * (2 * kKeys * DP));
-    const Heads &o = which ? a.dv : a.dk;
-    const float f = which ? 1.f : a.scale;
-    store4(static_cast<T *>(o.p) + b * o.sb + hk * o.sh + j * o.st + d, sum[0] * f, sum[1] * f,
-           sum[2] * f, sum[3] * f);
-}
-
-// Workgroups wanted at least, and query tiles that a part has at least.
-constexpr int kWanted = 512, kLeast = 4;
-// Workgroups that keys with sinks are split over at most.
-constexpr int64_t kMostShares = 4096;
-
-KeySplit key_split(const AttnProblem &p, int kKeys)
-{
-    KeySplit k;
-    const int G = p.Hq / p.Hkv;
-    const int64_t whole = (int64_t)G * ((p.Tq + kRows - 1) / kRows);
-    const int64_t window = p.left < 0 || p.right < 0
-                               ? whole
-                               : std::min<int64_t>(whole, (int64_t)G * (((int64_t)kKeys + p.left + p.right) / kRows + 1));
-    k.tiles = (p.Tk + kKeys - 1) / kKeys;
-    k.sunk = p.left < 0 ? 0 : std::min(k.tiles, (p.sinks + kKeys - 1) / kKeys);
-    const int64_t groups = (int64_t)p.B * p.Hkv * k.tiles;
-    k.parts = (int)std::max<int64_t>(1, std::min((kWanted + groups - 1) / groups, window / kLeast));
-    // sinks: parts about as long as the window's, as long as they do not crowd the card
-    const int64_t each = std::max<int64_t>(kLeast, window / k.parts);
-    const int64_t sunk = (int64_t)p.B * p.Hkv * std::max(1, k.sunk);
-    k.sparts = (int)std::max<int64_t>(1, std::min(whole / each, kMostShares / sunk));
-    k.slots = (int64_t)p.B * p.Hkv * k.shares();
-    return k;
-}
-
-// The keys' gradients, in tiles of 128 / KW keys, from delta.
-template <typename T, int DP, int KW>
-hipError_t run_dkv(const AttnProblem &p, const float *delta, hipStream_t s)
-{
-    constexpr int kKeys = 128 / KW;
-    const KeySplit ks = key_split(p, kKeys);
-    void *shares = nullptr;
-    hipError_t e = hipSuccess;
-    if (ks.slots > 0)
-        e = p.ws->take(&shares, (size_t)ks.slots * 2 * kKeys * DP * 4);
-    const int64_t nk = (int64_t)p.B * p.Hkv * ks.blocks();
-    if (nk * kThreads > kMaxThreads)
-        return hipErrorInvalidConfiguration;
-    if (e != hipSuccess || p.ws->counting)
-        return e;
-    attn_dkv_kernel<T, DP, KW><<<dim3((unsigned)nk), kThreads, 0, s>>>(p, delta, ks, static_cast<float *>(shares));
-    e = hipGetLastError();
-    const auto sum = [&](int first, int count, int parts) {
-        if (e != hipSuccess || count == 0 || parts == 1)
-            return;
-        const int64_t n = (int64_t)p.B * p.Hkv * count * (2 * kKeys * DP / 4);
-        attn_dkv_sum_kernel<T, DP, kKeys><<<dim3((unsigned)((n + kThreads - 1) / kThreads)), kThreads, 0, s>>>(
-            p, ks, first, count, parts, static_cast<const float *>(shares));
-        e = hipGetLastError();
-    };
-    sum(0, ks.sunk, ks.sparts);
-    sum(ks.sunk, ks.tiles - ks.sunk, ks.parts);
-    return e;
-}
-
-template <typename T, int DP, int KW>
-hipError_t run_dq(const AttnProblem &p, float *delta, hipStream_t s)
-{
-    const int64_t n = (int64_t)p.B * p.Hq * ((p.Tq + 128 / KW - 1) / (128 / KW));
-    if (n * kThreads > kMaxThreads)
-        return hipErrorInvalidConfiguration;
-    if (p.ws->counting)
-        return hipSuccess;
-    attn_dq_kernel<T, DP, KW><<<dim3((unsigned)n), kThreads, 0, s>>>(p, delta);
-    return hipGetLastError();
-}
-
-template <typename T, int DP>
-hipError_t run(const AttnProblem &p, hipStream_t s)
-{
-    void *delta = nullptr;
-    hipError_t e = p.ws->take(&delta, (size_t)p.B * p.Hq * p.Tq * 4);
-    if (e != hipSuccess)
-        return e;
-    float *d = static_cast<float *>(delta);
-    e = attn_pairs(p, (int64_t)p.B * p.Hq * ((p.Tq + 127) / 128)) ? run_dq<T, DP, 2>(p, d, s) : run_dq<T, DP, 1>(p, d, s);
-    if (e != hipSuccess)
-        return e;
-    return attn_pairs(p, (int64_t)p.B * p.Hkv * ((p.Tk + 127) / 128)) ? run_dkv<T, DP, 2>(p, d, s)
-                                                                      : run_dkv<T, DP, 1>(p, d, s);
-}
-
-template <typename T>
-hipError_t run(const AttnProblem &p, hipStream_t s)
-{
-    return p.D <= 32   ? run<T, 32>(p, s)
-           : p.D <= 64 ? run<T, 64>(p, s)
-           : p.D <= 96 ? run<T, 96>(p, s)
-                       : run<T, 128>(p, s);
-}
-
-}  // namespace
 
 hipError_t launch_attn_bwd(const AttnProblem &p, hipStream_t s)
 {
-    return p.dtype == 0 ? run<float>(p, s) : run<bf16_t>(p, s);
+    return p.dtype == 0 ? launch_attn_bwd_f32(p, s) : run<bf16_t>(p, s);
 }
 
 }  // namespace gspn

@@ -31,11 +31,9 @@ void attn_fwd_kernel(AttnProblem a)
 {
     using X = Tile<T, DP>;
     constexpr int kSlices = X::kPieces / 2, kTQ = 4 / KW * 32 * QB, NK = 2 / KW;
-    // bf16 tiles flow straight into LDS, two ahead where three fit beside other
-    // workgroups; fp32 tiles come through registers
+    // bf16 tiles flow straight into LDS, fp32 tiles come through registers
     constexpr bool kFlows = sizeof(T) == 2;
-    constexpr int kSlots = kFlows && DP <= 64 ? 3 : 2, kAhead = kSlots - 1;
-    __shared__ __attribute__((aligned(16))) char lds[kSlots][2][X::kBytes];
+    __shared__ __attribute__((aligned(16))) char lds[2][2][X::kBytes];
 
     const int G = a.Hq / a.Hkv, nqt = (a.Tq + kTQ - 1) / kTQ;
     int id = xcd_remap(blockIdx.x, gridDim.x);
@@ -87,8 +85,8 @@ void attn_fwd_kernel(AttnProblem a)
     const int n = wg.n;
     const auto flow = [&](int it) {
         if constexpr (kFlows) {
-            kw.load(lds[it % kSlots][0], kp, wg.row(it), len, w);
-            vw.load(lds[it % kSlots][1], vp, wg.row(it), len, w);
+            kw.load(lds[it & 1][0], kp, wg.row(it), len, w);
+            vw.load(lds[it & 1][1], vp, wg.row(it), len, w);
         }
     };
 #pragma unroll
@@ -97,8 +95,8 @@ void attn_fwd_kernel(AttnProblem a)
     if constexpr (kFlows) {
         kw.start(a.k.st, a.D);
         vw.start(a.v.st, a.D);
-        for (int it = 0; it < min(n, kAhead); ++it)
-            flow(it);
+        if (n > 0)
+            flow(0);
     } else {
         kt.start(a.k.st, a.D);
         vt.start(a.v.st, a.D);
@@ -113,15 +111,12 @@ void attn_fwd_kernel(AttnProblem a)
 
     for (int it = 0; it < n; ++it) {
         const int k0 = wg.row(it);
-        const char *kl = lds[it % kSlots][0], *vl = lds[it % kSlots][1];
+        const char *kl = lds[it & 1][0], *vl = lds[it & 1][1];
         if constexpr (kFlows) {
             // this tile has come, and every wave is done with the one before it
-            if (kAhead == 2 && it + 1 < n)
-                landed<2 * Flow<DP>::kLoads>();
-            else
-                landed<0>();
-            if (it + kAhead < n)
-                flow(it + kAhead);
+            landed();
+            if (it + 1 < n)
+                flow(it + 1);
         } else if (it + 1 < n) {
             kt.load(kp, a.k.st, wg.row(it + 1), len, a.D);
             vt.load(vp, a.v.st, wg.row(it + 1), len, a.D);
