@@ -4,8 +4,9 @@ The norm of query and key heads with the position rotation
 (``qk_norm_rotate_*``), windowed attention (``window_attn_*``) and the gated
 delta rule (``delta_rule_*``), see ``include/gspn.h`` for the formulas.  Tensors are [B, T, H, D] with D
 contiguous and any other strides (slices of a fused projection or of a cache);
-every call runs on the current stream of its tensors' device unless one is
-given, and takes the workspace it needs from torch unless it is handed one.
+every call runs on the current stream of its tensors' device, or on a given one
+(as if that were current: what it allocates belongs to it), and takes the
+workspace it needs from torch unless it is handed one.
 """
 from __future__ import annotations
 
@@ -43,6 +44,17 @@ def _name_fault(first, t, shape, name):
         raise ValueError(f"{name} must be on {first.device}")
     if t.shape[-1] > 1:
         raise ValueError(f"{name} must be contiguous in its last dimension")
+
+
+def _on(call, args):
+    """call(**args) with args["stream"], a torch stream or a handle, as the current one."""
+    import torch
+    s = args.pop("stream")
+    if not hasattr(s, "cuda_stream"):
+        dev = args["q"].device
+        s = torch.cuda.ExternalStream(int(s), device=dev) if s else torch.cuda.default_stream(dev)
+    with torch.cuda.stream(s):
+        return call(**args)
 
 
 _Strides = {n: ctypes.c_int64 * (3 * n) for n in (4, 6, 7, 8)}
@@ -128,6 +140,8 @@ def qk_norm_rotate_fwd(q, k, wq=None, wk=None, cos=None, sin=None, eps: float = 
     sin (fp32 [rows, R / 2]; None: no rotation): row positions[b, t] (int32), or
     first + t.  pairs: "half" turns entry i with R / 2 + i, "adjacent" 2i with
     2i + 1.  `out`: (yq, yk), which may be (q, k)."""
+    if stream is not None:
+        return _on(qk_norm_rotate_fwd, locals())
     import torch
     B, T, Hq, Hk, D, R, rows, ptrs = _norm_sizes(q, k, wq, wk, cos, sin, positions, pairs)
     if out is None:
@@ -138,7 +152,7 @@ def qk_norm_rotate_fwd(q, k, wq=None, wk=None, cos=None, sin=None, eps: float = 
     _check_raise(load().gspn_qk_norm_rotate_fwd(
         q.data_ptr(), k.data_ptr(), *ptrs, yq.data_ptr(), yk.data_ptr(),
         _strides(q, k, yq, yk), B, T, Hq, Hk, D, R, rows, first, PAIRS[pairs], eps,
-        _dtype_code(q), _stream_handle(q, stream)))
+        _dtype_code(q), _stream_handle(q, None)))
     return yq, yk
 
 
@@ -147,6 +161,8 @@ def qk_norm_rotate_bwd(q, k, wq, wk, dyq, dyk, cos=None, sin=None, eps: float = 
                        stream=None, workspace=None):
     """(dq, dk, dwq, dwk) of qk_norm_rotate_fwd's q, k and weights, from the
     gradients dyq, dyk of its outputs (dwq, dwk None where the weight is)."""
+    if stream is not None:
+        return _on(qk_norm_rotate_bwd, locals())
     import torch
     B, T, Hq, Hk, D, R, rows, ptrs = _norm_sizes(q, k, wq, wk, cos, sin, positions, pairs)
     if out is None:
@@ -165,7 +181,7 @@ def qk_norm_rotate_bwd(q, k, wq, wk, dyq, dyk, cos=None, sin=None, eps: float = 
         q.data_ptr(), k.data_ptr(), *ptrs, dyq.data_ptr(), dyk.data_ptr(), dq.data_ptr(),
         dk.data_ptr(), _plain("dwq", dwq, (D,), q.dtype, q), _plain("dwk", dwk, (D,), q.dtype, q),
         _strides(q, k, dyq, dyk, dq, dk), B, T, Hq, Hk, D, R, rows, first, PAIRS[pairs], eps, dt,
-        *ws, _stream_handle(q, stream)))
+        *ws, _stream_handle(q, None)))
     return out
 
 
@@ -195,6 +211,8 @@ def window_attn_fwd(q, k, v, left: int = -1, right: int = -1, sinks: int = 0, le
     (-1: no bound) and, up to p + right, the first `sinks` tokens; lens (int32
     [B]): the sequences' lengths, past which nothing is seen and sees nothing.
     scale: 1 / sqrt(D) unless given.  lse: fp32 [B, Hq, Tq], for the backward."""
+    if stream is not None:
+        return _on(window_attn_fwd, locals())
     import torch
     B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens)
     if o is None:
@@ -210,7 +228,7 @@ def window_attn_fwd(q, k, v, left: int = -1, right: int = -1, sinks: int = 0, le
         q.data_ptr(), k.data_ptr(), v.data_ptr(), lens_p, o.data_ptr(),
         _plain("lse", lse, (B, Hq, Tq), torch.float32, q), _strides(q, k, v, o), B, Tq, Tk, Hq,
         Hkv, D, left, right, sinks, offset, 1 / math.sqrt(D) if scale is None else scale, dt, *ws,
-        _stream_handle(q, stream)))
+        _stream_handle(q, None)))
     return o, lse
 
 
@@ -219,6 +237,8 @@ def window_attn_bwd(q, k, v, o, lse, do, left: int = -1, right: int = -1, sinks:
                     workspace=None):
     """(dq, dk, dv) from the gradient `do` of window_attn_fwd's o; o and lse are
     the forward's, the other arguments those it was called with."""
+    if stream is not None:
+        return _on(window_attn_bwd, locals())
     import torch
     B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens)
     if out is None:
@@ -237,7 +257,7 @@ def window_attn_bwd(q, k, v, o, lse, do, left: int = -1, right: int = -1, sinks:
         _plain("lse", lse, (B, Hq, Tq), torch.float32, q), do.data_ptr(), lens_p, dq.data_ptr(),
         dk.data_ptr(), dv.data_ptr(), _strides(q, k, v, o, do, dq, dk, dv), B, Tq, Tk, Hq, Hkv, D,
         left, right, sinks, offset, 1 / math.sqrt(D) if scale is None else scale, dt, *ws,
-        _stream_handle(q, stream)))
+        _stream_handle(q, None)))
     return dq, dk, dv
 
 
@@ -247,6 +267,8 @@ def window_attn_decode(q, k, v, lens=None, left: int = -1, sinks: int = 0, scale
     k, v [B, Tk, Hkv, D] of which lens[b] tokens (None: all) are there, the
     queries' own among them: query t stands at position lens[b] - Tq + t and
     sees the `left` keys before it (-1: all), itself and the first `sinks`."""
+    if stream is not None:
+        return _on(window_attn_decode, locals())
     import torch
     B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens)
     if o is None:
@@ -259,7 +281,7 @@ def window_attn_decode(q, k, v, lens=None, left: int = -1, sinks: int = 0, scale
     _check_raise(load().gspn_window_attn_decode(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), lens_p, o.data_ptr(), _strides(q, k, v, o), B,
         Tq, Tk, Hq, Hkv, D, left, sinks, 1 / math.sqrt(D) if scale is None else scale, dt, *ws,
-        _stream_handle(q, stream)))
+        _stream_handle(q, None)))
     return o
 
 
@@ -296,7 +318,7 @@ def delta_reserve_size(q, v) -> int:
                   (B, T, Hq, v.shape[2], Dk, v.shape[3], _dtype_code(q)), _current_device())
 
 
-def _delta_fwd(op, q, k, v, g, beta, state, lens, scale, o, state_out, reserve, stream, workspace):
+def _delta_fwd(op, q, k, v, g, beta, state, lens, scale, o, state_out, reserve, workspace):
     import torch
     sizes, gates, lens_p = _delta_sizes(q, k, v, g, beta, lens)
     B, T, Hq, Hv, Dk, Dv = sizes
@@ -314,13 +336,13 @@ def _delta_fwd(op, q, k, v, g, beta, state, lens, scale, o, state_out, reserve, 
             _plain("state_out", state_out, (B, Hv, Dk, Dv), torch.float32, q),
             _strides(q, k, v, o), *sizes, 1 / math.sqrt(Dk) if scale is None else scale, dt)
     if op == DELTA_FWD:
-        _check_raise(load().gspn_delta_rule_fwd(*args, *ws, _stream_handle(q, stream)))
+        _check_raise(load().gspn_delta_rule_fwd(*args, *ws, _stream_handle(q, None)))
         return o, state_out
     n = delta_reserve_size(q, v)
     if reserve is None:
         reserve = torch.empty(n, dtype=torch.uint8, device=q.device)
     _check_raise(load().gspn_delta_rule_fwd_train(*args, *_reserve(reserve, n, q.device), *ws,
-                                                  _stream_handle(q, stream)))
+                                                  _stream_handle(q, None)))
     return o, state_out, reserve
 
 
@@ -331,7 +353,9 @@ def delta_rule_fwd(q, k, v, g, beta, state=None, lens=None, scale=None, o=None, 
     beta [B, T, Hv], from `state` (fp32 [B, Hv, Dk, Dv]; None: zeros).  lens
     (int32 [B]): the sequences' lengths.  scale: 1 / sqrt(Dk) unless given.
     state_out may be state.  A token at a time is its serving form."""
-    return _delta_fwd(DELTA_FWD, q, k, v, g, beta, state, lens, scale, o, state_out, None, stream,
+    if stream is not None:
+        return _on(delta_rule_fwd, locals())
+    return _delta_fwd(DELTA_FWD, q, k, v, g, beta, state, lens, scale, o, state_out, None,
                       workspace)
 
 
@@ -340,8 +364,10 @@ def delta_rule_fwd_train(q, k, v, g, beta, state=None, lens=None, scale=None, o=
     """delta_rule_fwd that also fills the reserve that delta_rule_bwd_reserve
     reads (a uint8 device tensor of delta_reserve_size bytes, or None for a new
     one).  Returns (o, state_out, reserve)."""
+    if stream is not None:
+        return _on(delta_rule_fwd_train, locals())
     return _delta_fwd(DELTA_FWD_TRAIN, q, k, v, g, beta, state, lens, scale, o, state_out, reserve,
-                      stream, workspace)
+                      workspace)
 
 
 def delta_rule_bwd_reserve(q, k, v, g, beta, do, reserve, dstate=None, state=None, lens=None,
@@ -350,6 +376,8 @@ def delta_rule_bwd_reserve(q, k, v, g, beta, do, reserve, dstate=None, state=Non
     `dstate` of state_out (None: zeros); the other arguments are those of
     delta_rule_fwd_train, which filled `reserve`.  dstate_in is the gradient of
     `state`, None where the forward began from zeros."""
+    if stream is not None:
+        return _on(delta_rule_bwd_reserve, locals())
     import torch
     sizes, gates, lens_p = _delta_sizes(q, k, v, g, beta, lens)
     B, T, Hq, Hv, Dk, Dv = sizes
@@ -372,5 +400,5 @@ def delta_rule_bwd_reserve(q, k, v, g, beta, do, reserve, dstate=None, state=Non
         dv.data_ptr(), _plain("dg", dg, gs, q.dtype, q), _plain("dbeta", dbeta, gs, q.dtype, q),
         _plain("dstate_in", din, ss, torch.float32, q), _strides(q, k, v, do, dq, dk, dv), *sizes,
         1 / math.sqrt(Dk) if scale is None else scale, dt,
-        *_reserve(reserve, delta_reserve_size(q, v), q.device), *ws, _stream_handle(q, stream)))
+        *_reserve(reserve, delta_reserve_size(q, v), q.device), *ws, _stream_handle(q, None)))
     return out

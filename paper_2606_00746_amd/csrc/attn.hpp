@@ -51,7 +51,7 @@ constexpr int kAttnMaxHead = 128;
 // Whether pairs of waves share their rows of a kernel that would otherwise have
 // `blocks` workgroups: twice as many then, of half the rows, where they would
 // leave CUs without one.
-inline bool attn_pairs(const AttnProblem &, int64_t blocks)
+inline bool attn_pairs(int64_t blocks)
 {
     return blocks < 256;
 }

@@ -16,6 +16,14 @@
 // all later queries see (sinks), and calls with few keys, have their
 // queries split over several workgroups, whose fp32 shares are added up, in
 // order, by attn_dkv_sum_kernel.
+//
+// bf16: p and ds are rounded to 8 significant bits for their products, and d_i comes
+// from the rounded o_i.  The first costs an error of the size of the results' own
+// rounding.  The second is small beside it where a row has many keys, so that
+// |o_i| << |v_j|, but not where it has few (attn_few_keys): FINE kernels form d_i
+// as sum_j p_ij (do_i v_j), in a pass of its own, and add what rounding p and ds
+// leaves as a second term (relative error of dq and dk at sequences of 16 to 128
+// tokens, against 1.7e-3 for rounded exact results: 2.9e-3 -> 1.7e-3).
 #pragma once
 
 #include <algorithm>
@@ -49,6 +57,20 @@ __device__ __forceinline__ void join_pair(float *lds, f32x16_t (&acc)[N], int w,
                 acc[i][r] += mine[(16 * i + r) * 64 + l];
 }
 
+// acc += X^T p: with FINE, p to 16 significant bits.
+template <int DP, bool FINE, typename T>
+__device__ __forceinline__ void add_turned(const Turned<T, DP> &x, const f32x16_t &p, f32x16_t (&acc)[DP / 32])
+{
+    mma_turned<DP>(x, Probs<T>(p), acc);
+    if constexpr (FINE) {
+        f32x16_t rest;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            rest[r] = p[r] - (float)(__bf16)p[r];
+        mma_turned<DP>(x, Probs<T>(rest), acc);
+    }
+}
+
 template <typename T>
 __device__ __forceinline__ float dot(Frag<T> a, Frag<T> b)
 {
@@ -60,14 +82,16 @@ __device__ __forceinline__ float dot(Frag<T> a, Frag<T> b)
     return s;
 }
 
-template <typename T, int DP, int KW>
+template <typename T, int DP, int KW, bool FINE>
 __global__ __launch_bounds__(kThreads, (DP * sizeof(T) <= 128 ? 2 : 1))
 void attn_dq_kernel(AttnProblem a, float *delta)
 {
     using X = Tile<T, DP>;
     constexpr int kSlices = X::kPieces / 2, kTQ = 128 / KW;
     constexpr bool kFlows = sizeof(T) == 2;   // as in the forward
+    static_assert(!FINE || (kFlows && KW == 2), "");
     __shared__ __attribute__((aligned(16))) char lds[2][2][X::kBytes];
+    __shared__ float sums[kThreads];
 
     const int G = a.Hq / a.Hkv, nqt = (a.Tq + kTQ - 1) / kTQ;
     int id = xcd_remap(blockIdx.x, gridDim.x);
@@ -98,14 +122,25 @@ void attn_dq_kernel(AttnProblem a, float *delta)
     for (int s = 0; s < kSlices; ++s) {
         qf[s] = row_frag(qr, 2 * s + h, a.D);
         df[s] = row_frag(dr, 2 * s + h, a.D);
-        d += dot(df[s], row_frag(orow, 2 * s + h, a.D));
+        if (!FINE)
+            d += dot(df[s], row_frag(orow, 2 * s + h, a.D));
     }
-    d = half_sum(d);
     const int64_t stat = ((int64_t)b * a.Hq + hq) * a.Tq + tr;
     const float s2 = a.scale * kLog2e, lse2 = a.lse[stat] * kLog2e;
-    // for the keys' gradients: d, and lse to the base of 2
-    if (t < a.Tq)
-        delta[(int64_t)h * a.B * a.Hq * a.Tq + stat] = h == 0 ? d : lse2;
+    // d over the lanes (FINE: and waves) that share it; for the keys' gradients: d,
+    // and lse to the base of 2
+    const auto whole = [&] {
+        d = half_sum(d);
+        if constexpr (FINE) {
+            sums[threadIdx.x] = d;
+            lds_barrier();
+            d += sums[threadIdx.x ^ 64];
+        }
+        if (t < a.Tq)
+            delta[(int64_t)h * a.B * a.Hq * a.Tq + stat] = h == 0 ? d : lse2;
+    };
+    if (!FINE)
+        whole();
 
     f32x16_t acc[DP / 32];
 #pragma unroll
@@ -128,8 +163,6 @@ void attn_dq_kernel(AttnProblem a, float *delta)
     if constexpr (kFlows) {
         kw.start(a.k.st, a.D);
         vw.start(a.v.st, a.D);
-        if (n > 0)
-            flow(0);
     } else {
         kt.start(a.k.st, a.D);
         vt.start(a.v.st, a.D);
@@ -141,76 +174,90 @@ void attn_dq_kernel(AttnProblem a, float *delta)
         }
         lds_barrier();
     }
-    for (int it = 0; it < n; ++it) {
-        const int k0 = wg.row(it);
-        const char *kl = lds[it & 1][0], *vl = lds[it & 1][1];
-        if constexpr (kFlows) {
-            landed();
-            if (it + 1 < n)
-                flow(it + 1);
-        } else if (it + 1 < n) {
-            kt.load(kp, a.k.st, wg.row(it + 1), len, a.D);
-            vt.load(vp, a.v.st, wg.row(it + 1), len, a.D);
-        }
-        if (wave.some(k0)) {
-            const bool all = wave.all(k0);
-            // the 32 keys of block `blk`, a constant where it is an address
-            const auto block = [&](auto blk) {
-                constexpr int kb = decltype(blk)::value;
-                f32x16_t s, dp;
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    s[r] = dp[r] = 0.f;
-                RowFrags<T, DP> kf, vf;
-                Turned<T, DP> kx;
-                if constexpr (kFlows) {
-                    flow_rows<DP, kb>(lds_offset(kl), kf.f);
-#pragma unroll
-                    for (int sl = 0; sl < kSlices; ++sl)
-                        s = mma(kf.at(sl), qf[sl], s);
-                    flow_rows<DP, kb>(lds_offset(vl), vf.f);
-#pragma unroll
-                    for (int sl = 0; sl < kSlices; ++sl)
-                        dp = mma(vf.at(sl), df[sl], dp);
-                } else {
-                    kf.load(kl, 32 * kb + c);
-                    vf.load(vl, 32 * kb + c);
-                    reads_first<T>();
-#pragma unroll
-                    for (int sl = 0; sl < kSlices; ++sl) {
-                        s = mma(kf.at(sl), qf[sl], s);
-                        dp = mma(vf.at(sl), df[sl], dp);
-                    }
-                }
-                if constexpr (kFlows)
-                    flow_turned<DP, kb>(lds_offset(kl), kx);
-                else
-                    kx.load(kl, 32 * kb);
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], s2, -lse2)) * (dp[r] - d);
-                if (!all) {
-                    const bool sunk = k0 < a.sinks;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = k0 + 32 * kb + 8 * (r / 4) + 4 * h + r % 4;
-                        s[r] = sees(j, lo, hi, a.sinks, sunk) ? s[r] : 0.f;
-                    }
-                }
-                mma_turned<DP>(kx, Probs<T>(s), acc);
-            };
-            if (KW == 1 || kb0 == 0)
-                block(std::integral_constant<int, 0>{});
-            if (KW == 1 || kb0 == 1)
-                block(std::integral_constant<int, 1>{});
-        }
-        if constexpr (!kFlows) {
-            if (it + 1 < n) {
-                kt.store(lds[(it + 1) & 1][0]);
-                vt.store(lds[(it + 1) & 1][1]);
+    for (int pass = FINE ? 0 : 1; pass < 2; ++pass) {
+        const bool sums_up = FINE && pass == 0;
+        if (kFlows && n > 0)
+            flow(0);
+        for (int it = 0; it < n; ++it) {
+            const int k0 = wg.row(it);
+            const char *kl = lds[it & 1][0], *vl = lds[it & 1][1];
+            if constexpr (kFlows) {
+                landed();
+                if (it + 1 < n)
+                    flow(it + 1);
+            } else if (it + 1 < n) {
+                kt.load(kp, a.k.st, wg.row(it + 1), len, a.D);
+                vt.load(vp, a.v.st, wg.row(it + 1), len, a.D);
             }
-            lds_barrier();
+            if (wave.some(k0)) {
+                const bool all = wave.all(k0);
+                // the 32 keys of block `blk`, a constant where it is an address
+                const auto block = [&](auto blk) {
+                    constexpr int kb = decltype(blk)::value;
+                    f32x16_t s, dp;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        s[r] = dp[r] = 0.f;
+                    RowFrags<T, DP> kf, vf;
+                    Turned<T, DP> kx;
+                    if constexpr (kFlows) {
+                        flow_rows<DP, kb>(lds_offset(kl), kf.f);
+#pragma unroll
+                        for (int sl = 0; sl < kSlices; ++sl)
+                            s = mma(kf.at(sl), qf[sl], s);
+                        flow_rows<DP, kb>(lds_offset(vl), vf.f);
+#pragma unroll
+                        for (int sl = 0; sl < kSlices; ++sl)
+                            dp = mma(vf.at(sl), df[sl], dp);
+                    } else {
+                        kf.load(kl, 32 * kb + c);
+                        vf.load(vl, 32 * kb + c);
+                        reads_first<T>();
+#pragma unroll
+                        for (int sl = 0; sl < kSlices; ++sl) {
+                            s = mma(kf.at(sl), qf[sl], s);
+                            dp = mma(vf.at(sl), df[sl], dp);
+                        }
+                    }
+                    if constexpr (kFlows)
+                        flow_turned<DP, kb>(lds_offset(kl), kx);
+                    else
+                        kx.load(kl, 32 * kb);
+                    const float less = sums_up ? 0.f : d;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], s2, -lse2)) * (dp[r] - less);
+                    if (!all) {
+                        const bool sunk = k0 < a.sinks;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int j = k0 + 32 * kb + 8 * (r / 4) + 4 * h + r % 4;
+                            s[r] = sees(j, lo, hi, a.sinks, sunk) ? s[r] : 0.f;
+                        }
+                    }
+                    if (sums_up) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            d += s[r];
+                    } else {
+                        add_turned<DP, FINE>(kx, s, acc);
+                    }
+                };
+                if (KW == 1 || kb0 == 0)
+                    block(std::integral_constant<int, 0>{});
+                if (KW == 1 || kb0 == 1)
+                    block(std::integral_constant<int, 1>{});
+            }
+            if constexpr (!kFlows) {
+                if (it + 1 < n) {
+                    kt.store(lds[(it + 1) & 1][0]);
+                    vt.store(lds[(it + 1) & 1][1]);
+                }
+                lds_barrier();
+            }
         }
+        if (sums_up)
+            whole();   // (its barrier: the tiles are free)
     }
     if (KW == 2)
         join_pair(reinterpret_cast<float *>(lds), acc, w, l);
@@ -238,7 +285,7 @@ struct KeySplit {
     }
 };
 
-template <typename T, int DP, int KW>
+template <typename T, int DP, int KW, bool FINE>
 __global__ __launch_bounds__(kThreads, (DP * sizeof(T) <= 128 ? 2 : 1))
 void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shares)
 {
@@ -414,12 +461,12 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
                         dp[r] = see ? dp[r] : 0.f;
                     }
                 }
-                mma_turned<DP>(dx, Probs<T>(s), dv);
+                add_turned<DP, FINE>(dx, s, dv);
                 if constexpr (kFlows)
                     flow_turned<DP, qb>(lds_offset(ql), qx);
                 else
                     qx.load(ql, 32 * qb);
-                mma_turned<DP>(qx, Probs<T>(dp), dk);
+                add_turned<DP, FINE>(qx, dp, dk);
             };
             if (KW == 1 || qb0 == 0)
                 block(std::integral_constant<int, 0>{});
@@ -482,6 +529,12 @@ __global__ __launch_bounds__(kThreads) void attn_dkv_sum_kernel(AttnProblem a, K
            sum[2] * f, sum[3] * f);
 }
 
+// Rows with few keys: the sequence is short, or the window narrow.
+bool attn_few_keys(const AttnProblem &p)
+{
+    return p.Tk <= 512 || (p.left >= 0 && p.right >= 0 && (int64_t)p.left + p.right <= 32);
+}
+
 // Workgroups wanted at least, and query tiles that a part has at least.
 constexpr int kWanted = 512, kLeast = 4;
 // Workgroups that keys with sinks are split over at most.
@@ -508,7 +561,7 @@ KeySplit key_split(const AttnProblem &p, int kKeys)
 }
 
 // The keys' gradients, in tiles of 128 / KW keys, from delta.
-template <typename T, int DP, int KW>
+template <typename T, int DP, int KW, bool FINE>
 hipError_t run_dkv(const AttnProblem &p, const float *delta, hipStream_t s)
 {
     constexpr int kKeys = 128 / KW;
@@ -522,7 +575,7 @@ hipError_t run_dkv(const AttnProblem &p, const float *delta, hipStream_t s)
         return hipErrorInvalidConfiguration;
     if (e != hipSuccess || p.ws->counting)
         return e;
-    attn_dkv_kernel<T, DP, KW><<<dim3((unsigned)nk), kThreads, 0, s>>>(p, delta, ks, static_cast<float *>(shares));
+    attn_dkv_kernel<T, DP, KW, FINE><<<dim3((unsigned)nk), kThreads, 0, s>>>(p, delta, ks, static_cast<float *>(shares));
     e = hipGetLastError();
     const auto sum = [&](int first, int count, int parts) {
         if (e != hipSuccess || count == 0 || parts == 1)
@@ -537,7 +590,7 @@ hipError_t run_dkv(const AttnProblem &p, const float *delta, hipStream_t s)
     return e;
 }
 
-template <typename T, int DP, int KW>
+template <typename T, int DP, int KW, bool FINE>
 hipError_t run_dq(const AttnProblem &p, float *delta, hipStream_t s)
 {
     const int64_t n = (int64_t)p.B * p.Hq * ((p.Tq + 128 / KW - 1) / (128 / KW));
@@ -545,7 +598,7 @@ hipError_t run_dq(const AttnProblem &p, float *delta, hipStream_t s)
         return hipErrorInvalidConfiguration;
     if (p.ws->counting)
         return hipSuccess;
-    attn_dq_kernel<T, DP, KW><<<dim3((unsigned)n), kThreads, 0, s>>>(p, delta);
+    attn_dq_kernel<T, DP, KW, FINE><<<dim3((unsigned)n), kThreads, 0, s>>>(p, delta);
     return hipGetLastError();
 }
 
@@ -557,11 +610,18 @@ hipError_t run(const AttnProblem &p, hipStream_t s)
     if (e != hipSuccess)
         return e;
     float *d = static_cast<float *>(delta);
-    e = attn_pairs(p, (int64_t)p.B * p.Hq * ((p.Tq + 127) / 128)) ? run_dq<T, DP, 2>(p, d, s) : run_dq<T, DP, 1>(p, d, s);
+    if constexpr (sizeof(T) == 2) {
+        if (attn_few_keys(p)) {
+            e = run_dq<T, DP, 2, true>(p, d, s);
+            return e == hipSuccess ? run_dkv<T, DP, 2, true>(p, d, s) : e;
+        }
+    }
+    e = attn_pairs((int64_t)p.B * p.Hq * ((p.Tq + 127) / 128)) ? run_dq<T, DP, 2, false>(p, d, s)
+                                                               : run_dq<T, DP, 1, false>(p, d, s);
     if (e != hipSuccess)
         return e;
-    return attn_pairs(p, (int64_t)p.B * p.Hkv * ((p.Tk + 127) / 128)) ? run_dkv<T, DP, 2>(p, d, s)
-                                                                      : run_dkv<T, DP, 1>(p, d, s);
+    return attn_pairs((int64_t)p.B * p.Hkv * ((p.Tk + 127) / 128)) ? run_dkv<T, DP, 2, false>(p, d, s)
+                                                                   : run_dkv<T, DP, 1, false>(p, d, s);
 }
 
 template <typename T>

@@ -3,14 +3,22 @@
 //   o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i k_j - lse_i),
 //   lse_i = log sum_j exp(scale q_i k_j)     over the keys j that query i sees
 //
-// One pass over the keys with a running maximum and sum.  A workgroup owns
-// 4 x 32 QB queries of one head, a wave 32 QB of them; tiles of 64 keys and
-// values are staged in LDS for all four waves, double buffered: the loads of
-// the next tile are in flight, in registers, while one is multiplied.  The
+// One pass over the keys with a running maximum and sum.  A workgroup owns 128
+// queries of one head, a wave 32 of them; tiles of 64 keys and values are staged
+// in LDS for all four waves, double buffered: the next tile is on its way while one
+// is multiplied, bf16 straight into LDS (through registers: 1.40M cycles at the size
+// below, this way 0.98M), fp32 through registers, whose order in LDS differs.  The
 // tiles are those of the sinks, then those of the window; a wave passes over
 // tiles that none of its queries sees and masks only those that not all see.
-#include <algorithm>
-
+// S^T = K Q^T is formed, so that a query's scores are one lane's (and its
+// neighbour's, 32 lanes on) and their exponentials, as they stand in registers, are
+// an operand of O^T += V^T P^T.
+//
+// The bound is the matrix instructions, and the power they draw: 34229 tokens, 18
+// heads of 64, bf16, a window of 1110 to either side and 4 sinks, in 560 us = 630
+// TFLOP/s, at a clock that falls from 2.4 to about 1.7 GHz while it lasts (a large
+// matrix product reaches 1250 on the same card).  64 queries a wave take the LDS
+// reads that a product needs to half, but leave one wave a SIMD: slower.
 #include "attn.hpp"
 
 namespace gspn {
@@ -25,12 +33,12 @@ constexpr float kSlack = 8.f;
 
 // KW: waves that share their queries, each with its part of every tile's keys
 // (1, or 2 of 32 keys each); their shares are joined at the end.
-template <typename T, int DP, int QB, int KW>
-__global__ __launch_bounds__(kThreads, (DP * sizeof(T) * QB <= 128 ? 3 : DP * sizeof(T) * QB <= 256 ? 2 : 1))
+template <typename T, int DP, int KW>
+__global__ __launch_bounds__(kThreads, (DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 256 ? 2 : 1))
 void attn_fwd_kernel(AttnProblem a)
 {
     using X = Tile<T, DP>;
-    constexpr int kSlices = X::kPieces / 2, kTQ = 4 / KW * 32 * QB, NK = 2 / KW;
+    constexpr int kSlices = X::kPieces / 2, kTQ = 128 / KW, NK = 2 / KW;
     // bf16 tiles flow straight into LDS, fp32 tiles come through registers
     constexpr bool kFlows = sizeof(T) == 2;
     __shared__ __attribute__((aligned(16))) char lds[2][2][X::kBytes];
@@ -50,34 +58,26 @@ void attn_fwd_kernel(AttnProblem a)
     const T *kp = static_cast<const T *>(a.k.p) + b * a.k.sb + hk * a.k.sh;
     const T *vp = static_cast<const T *>(a.v.p) + b * a.v.sb + hk * a.v.sh;
 
-    const int t0 = qt * kTQ, tw = t0 + w / KW * 32 * QB, kb0 = KW == 2 ? w % 2 : 0;
+    const int t0 = qt * kTQ, tw = t0 + w / KW * 32, kb0 = KW == 2 ? w % 2 : 0;
     const KeyTiles wg(a, len, t0, min(kTQ, a.Tq - t0));
-    const KeyRange wave(a, len, tw, 32 * QB);
+    const KeyRange wave(a, len, tw, 32);
 
-    Frag<T> qf[QB][kSlices];
-    int lo[QB], hi[QB];
+    Frag<T> qf[kSlices];
+    int lo, hi;
+    const int t = tw + c;
+    const T *row = qp + (int64_t)min(t, a.Tq - 1) * a.q.st;
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const int t = tw + 32 * qb + c;
-        const T *row = qp + (int64_t)min(t, a.Tq - 1) * a.q.st;
-#pragma unroll
-        for (int s = 0; s < kSlices; ++s)
-            qf[qb][s] = row_frag(row, 2 * s + h, a.D);
-        key_bounds(a, len, t + a.offset, lo[qb], hi[qb]);
-    }
+    for (int s = 0; s < kSlices; ++s)
+        qf[s] = row_frag(row, 2 * s + h, a.D);
+    key_bounds(a, len, t + a.offset, lo, hi);
 
-    f32x16_t acc[QB][DP / 32];
-    float m[QB], sum[QB];
+    f32x16_t acc[DP / 32];
+    float m = -__builtin_inff(), sum = 0.f;
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        m[qb] = -__builtin_inff();
-        sum[qb] = 0.f;
+    for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
-        for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                acc[qb][db][r] = 0.f;
-    }
+        for (int r = 0; r < 16; ++r)
+            acc[db][r] = 0.f;
     const float s2 = a.scale * kLog2e, slack = kSlack / s2;
 
     X kt, vt;
@@ -89,9 +89,7 @@ void attn_fwd_kernel(AttnProblem a)
             vw.load(lds[it & 1][1], vp, wg.row(it), len, w);
         }
     };
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
-        arrived(qf[qb]);
+    arrived(qf);
     if constexpr (kFlows) {
         kw.start(a.k.st, a.D);
         vw.start(a.v.st, a.D);
@@ -123,7 +121,7 @@ void attn_fwd_kernel(AttnProblem a)
         }
         if (wave.some(k0)) {
             const bool all = wave.all(k0);
-            f32x16_t s[QB][NK];
+            f32x16_t s[NK];
             RowFrags<T, DP> kf;
             Turned<T, DP> vf;
 #pragma unroll
@@ -137,14 +135,11 @@ void attn_fwd_kernel(AttnProblem a)
                     kf.load(kl, 32 * (kb0 + kb) + c);
                 }
 #pragma unroll
-                for (int qb = 0; qb < QB; ++qb) {
+                for (int r = 0; r < 16; ++r)
+                    s[kb][r] = 0.f;
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        s[qb][kb][r] = 0.f;
-#pragma unroll
-                    for (int sl = 0; sl < kSlices; ++sl)
-                        s[qb][kb] = mma(kf.at(sl), qf[qb][sl], s[qb][kb]);
-                }
+                for (int sl = 0; sl < kSlices; ++sl)
+                    s[kb] = mma(kf.at(sl), qf[sl], s[kb]);
             }
             const auto turn = [&](int kb) {
                 if constexpr (kFlows) {
@@ -160,53 +155,42 @@ void attn_fwd_kernel(AttnProblem a)
             if (!all) {
                 const bool sunk = k0 < a.sinks;
 #pragma unroll
-                for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-                    for (int kb = 0; kb < NK; ++kb)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int j = k0 + 32 * (kb0 + kb) + 8 * (r / 4) + 4 * h + r % 4;
-                            s[qb][kb][r] = sees(j, lo[qb], hi[qb], a.sinks, sunk) ? s[qb][kb][r] : -__builtin_inff();
-                        }
-            }
-            float base[QB];
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) {
-                float mx = -__builtin_inff();
-#pragma unroll
                 for (int kb = 0; kb < NK; ++kb)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        mx = fmaxf(mx, s[qb][kb][r]);
-                mx = half_max(mx);
-                if (__any(mx > m[qb] + slack)) {
-                    const float mn = fmaxf(m[qb], mx);
-                    const float f = m[qb] == -__builtin_inff()
-                                        ? 0.f
-                                        : __builtin_amdgcn_exp2f((m[qb] - mn) * s2);
-                    m[qb] = mn;
-                    sum[qb] *= f;
-#pragma unroll
-                    for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            acc[qb][db][r] *= f;
-                }
-                base[qb] = m[qb] == -__builtin_inff() ? 0.f : m[qb] * s2;
+                    for (int r = 0; r < 16; ++r) {
+                        const int j = k0 + 32 * (kb0 + kb) + 8 * (r / 4) + 4 * h + r % 4;
+                        s[kb][r] = sees(j, lo, hi, a.sinks, sunk) ? s[kb][r] : -__builtin_inff();
+                    }
             }
+            float mx = -__builtin_inff();
+#pragma unroll
+            for (int kb = 0; kb < NK; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    mx = fmaxf(mx, s[kb][r]);
+            mx = half_max(mx);
+            if (__any(mx > m + slack)) {
+                const float mn = fmaxf(m, mx);
+                const float f = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m - mn) * s2);
+                m = mn;
+                sum *= f;
+#pragma unroll
+                for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        acc[db][r] *= f;
+            }
+            const float base = m == -__builtin_inff() ? 0.f : m * s2;
 #pragma unroll
             for (int kb = 0; kb < NK; ++kb) {
+                float part = 0.f;
 #pragma unroll
-                for (int qb = 0; qb < QB; ++qb) {
-                    float part = 0.f;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        s[qb][kb][r] = __builtin_amdgcn_exp2f(fmaf(s[qb][kb][r], s2, -base[qb]));
-                        part += s[qb][kb][r];
-                    }
-                    sum[qb] += part;
-                    mma_turned<DP>(vf, Probs<T>(s[qb][kb]), acc[qb]);
+                for (int r = 0; r < 16; ++r) {
+                    s[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], s2, -base));
+                    part += s[kb][r];
                 }
+                sum += part;
+                mma_turned<DP>(vf, Probs<T>(s[kb]), acc);
                 if (kb + 1 < NK)
                     turn(1);
             }
@@ -219,66 +203,60 @@ void attn_fwd_kernel(AttnProblem a)
             lds_barrier();
         }
     }
-    if (kFlows && KW == 2)
-        lds_barrier();
-
     if (KW == 2) {   // the odd wave's share to its neighbour, scaled to a common maximum
-        static_assert(QB == 1 || KW == 1, "one block of queries a pair of waves");
         float *mine = reinterpret_cast<float *>(lds) + w / 2 * (64 * (DP / 2 + 2));
+        if (kFlows)
+            lds_barrier();
         if (w & 1) {
 #pragma unroll
             for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    mine[(16 * db + r) * 64 + l] = acc[0][db][r];
-            mine[DP / 2 * 64 + l] = m[0];
-            mine[(DP / 2 + 1) * 64 + l] = sum[0];
+                    mine[(16 * db + r) * 64 + l] = acc[db][r];
+            mine[DP / 2 * 64 + l] = m;
+            mine[(DP / 2 + 1) * 64 + l] = sum;
         }
         lds_barrier();
         if (w & 1)
             return;
-        const float mo = mine[DP / 2 * 64 + l], mn = fmaxf(m[0], mo);
-        const float f = m[0] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m[0] - mn) * s2);
+        const float mo = mine[DP / 2 * 64 + l], mn = fmaxf(m, mo);
+        const float f = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((m - mn) * s2);
         const float fo = mo == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((mo - mn) * s2);
-        m[0] = mn;
-        sum[0] = f * sum[0] + fo * mine[(DP / 2 + 1) * 64 + l];
+        m = mn;
+        sum = f * sum + fo * mine[(DP / 2 + 1) * 64 + l];
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                acc[0][db][r] = f * acc[0][db][r] + fo * mine[(16 * db + r) * 64 + l];
+                acc[db][r] = f * acc[db][r] + fo * mine[(16 * db + r) * 64 + l];
     }
     T *op = static_cast<T *>(a.o.p) + b * a.o.sb + hq * a.o.sh;
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const int t = tw + 32 * qb + c;
-        const float z = half_sum(sum[qb]);
-        if (t < a.Tq) {
-            store_column<T, DP>(op + t * a.o.st, acc[qb], z > 0.f ? 1.f / z : 0.f, a.D);
-            if (a.lse && h == 0)
-                a.lse[((int64_t)b * a.Hq + hq) * a.Tq + t] =
-                    z > 0.f ? fmaf(m[qb], s2, __builtin_amdgcn_logf(z)) * kLn2 : -__builtin_inff();
-        }
+    const float z = half_sum(sum);
+    if (t < a.Tq) {
+        store_column<T, DP>(op + t * a.o.st, acc, z > 0.f ? 1.f / z : 0.f, a.D);
+        if (a.lse && h == 0)
+            a.lse[((int64_t)b * a.Hq + hq) * a.Tq + t] =
+                z > 0.f ? fmaf(m, s2, __builtin_amdgcn_logf(z)) * kLn2 : -__builtin_inff();
     }
 }
 
-template <typename T, int DP, int QB, int KW>
+template <typename T, int DP, int KW>
 hipError_t run(const AttnProblem &p, hipStream_t s)
 {
-    constexpr int kTQ = 4 / KW * 32 * QB;
+    constexpr int kTQ = 128 / KW;
     const int64_t tiles = (p.Tq + kTQ - 1) / kTQ, blocks = tiles * p.B * p.Hq;
     if (blocks * kThreads > kMaxThreads)
         return hipErrorInvalidConfiguration;
     if (p.ws->counting)
         return hipSuccess;
-    attn_fwd_kernel<T, DP, QB, KW><<<dim3((unsigned)blocks), kThreads, 0, s>>>(p);
+    attn_fwd_kernel<T, DP, KW><<<dim3((unsigned)blocks), kThreads, 0, s>>>(p);
     return hipGetLastError();
 }
 
 template <typename T, int DP>
 hipError_t pick(const AttnProblem &p, hipStream_t s)
 {
-    return attn_pairs(p, (int64_t)p.B * p.Hq * ((p.Tq + 127) / 128)) ? run<T, DP, 1, 2>(p, s) : run<T, DP, 1, 1>(p, s);
+    return attn_pairs((int64_t)p.B * p.Hq * ((p.Tq + 127) / 128)) ? run<T, DP, 2>(p, s) : run<T, DP, 1>(p, s);
 }
 
 template <typename T>
