@@ -529,7 +529,10 @@ __global__ __launch_bounds__(kThreads) void attn_dkv_sum_kernel(AttnProblem a, K
            sum[2] * f, sum[3] * f);
 }
 
-// Rows with few keys: the sequence is short, or the window narrow.
+// Rows with few keys: the sequence is short, or the window narrow.  What the longer
+// sums cost there, both kernels: 16 x 16 heads of 64, causal, 512 tokens 170 us, 516
+// tokens (without) 110; heads of 128 381 and 203; 8 x 4096 tokens, 12 heads, a window
+// of 33 253 us, of 34 184.
 bool attn_few_keys(const AttnProblem &p)
 {
     return p.Tk <= 512 || (p.left >= 0 && p.right >= 0 && (int64_t)p.left + p.right <= 32);
