@@ -48,14 +48,6 @@ bool attn_split_preferred(const AttnProblem &p);
 
 constexpr int kAttnMaxHead = 128;
 
-// Whether pairs of waves share their rows of a kernel that would otherwise have
-// `blocks` workgroups: twice as many then, of half the rows, where they would
-// leave CUs without one.
-inline bool attn_pairs(int64_t blocks)
-{
-    return blocks < 256;
-}
-
 #ifdef __HIPCC__
 
 namespace attn {

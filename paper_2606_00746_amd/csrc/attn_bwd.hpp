@@ -605,6 +605,11 @@ hipError_t run_dq(const AttnProblem &p, float *delta, hipStream_t s)
     return hipGetLastError();
 }
 
+// Tiles of 128 rows up to which pairs of waves share 32 of them, so that there are
+// twice as many workgroups (us of both kernels, with and without: 42 tiles of heads of
+// 72 21 and 29, 128 of 64 51 and 56, 160 49 and 50, of 128 94 and 80, 512 of 64 71 and 56).
+constexpr int64_t kPairs = 128;
+
 template <typename T, int DP>
 hipError_t run(const AttnProblem &p, hipStream_t s)
 {
@@ -613,18 +618,17 @@ hipError_t run(const AttnProblem &p, hipStream_t s)
     if (e != hipSuccess)
         return e;
     float *d = static_cast<float *>(delta);
+    const auto tiles = [&](int H, int T_) { return (int64_t)p.B * H * ((T_ + 127) / 128); };
     if constexpr (sizeof(T) == 2) {
         if (attn_few_keys(p)) {
             e = run_dq<T, DP, 2, true>(p, d, s);
             return e == hipSuccess ? run_dkv<T, DP, 2, true>(p, d, s) : e;
         }
     }
-    e = attn_pairs((int64_t)p.B * p.Hq * ((p.Tq + 127) / 128)) ? run_dq<T, DP, 2, false>(p, d, s)
-                                                               : run_dq<T, DP, 1, false>(p, d, s);
+    e = tiles(p.Hq, p.Tq) <= kPairs ? run_dq<T, DP, 2, false>(p, d, s) : run_dq<T, DP, 1, false>(p, d, s);
     if (e != hipSuccess)
         return e;
-    return attn_pairs((int64_t)p.B * p.Hkv * ((p.Tk + 127) / 128)) ? run_dkv<T, DP, 2, false>(p, d, s)
-                                                                   : run_dkv<T, DP, 1, false>(p, d, s);
+    return tiles(p.Hkv, p.Tk) <= kPairs ? run_dkv<T, DP, 2, false>(p, d, s) : run_dkv<T, DP, 1, false>(p, d, s);
 }
 
 template <typename T>

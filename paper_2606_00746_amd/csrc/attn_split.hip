@@ -390,11 +390,19 @@ hipError_t run(const AttnProblem &p, hipStream_t s)
 
 }  // namespace
 
-// Forwards whose queries of one key head fill at most two of these tiles: the
-// forward proper would read the keys once for every query head, and split none.
+// Whether a forward is faster here.  The forward proper takes a query tile of 64 rows
+// through its keys one tile after the other, 0.0119 us a key at heads of 64 and 0.0168
+// at heads of 128, for some 512 of its workgroups at a time; this one has a launch more
+// and takes about 2e-8 us a row, key and entry, whatever the rows' number.  Both, bf16
+// (us; here and there): 64 queries of 8 heads of 64, 8192 keys 17 and 97, 512 keys 8.2
+// and 10.2; 512 queries 49 and 97, 1024 queries 84 and 98; 16 x 32 queries, 1024 keys 19
+// and 16; 16 heads of 128 on 4, 256 queries, 8192 keys 94 and 138, 512 queries 162 and 138.
 bool attn_split_preferred(const AttnProblem &p)
 {
-    return (int64_t)p.Tq * (p.Hq / p.Hkv) <= 2 * kCol;
+    const double rows = (double)p.B * p.Hq * p.Tq, keys = (double)keys_of(p);
+    const int64_t blocks = (int64_t)p.B * p.Hq * ((p.Tq + 63) / 64);
+    const double forward = keys * (0.007 + 0.00008 * p.D) * (double)((blocks + 511) / 512);
+    return rows * keys * p.D * 2.5e-8 + 6.0 < forward;
 }
 
 hipError_t launch_attn_split(const AttnProblem &p, hipStream_t s)

@@ -11,8 +11,12 @@
 // lies in a group of up to 16 lanes, 16 entries each as two runs of 8.  Where
 // the rotation pairs entry i with R/2 + i and R/2 is a multiple of 8, a lane
 // owns both runs of its pairs and nothing is exchanged; adjacent pairs lie in
-// one run; other pairings go through LDS.  A group takes several heads of one
-// token, whose rows are in flight together and share the token's angles.
+// one run; other pairings go through LDS.  A group of the forward takes several
+// heads of one token, whose rows are in flight together and share the token's
+// angles (32 x 5476 tokens of 18 + 18 heads of 64, bf16, slices of a fused buffer: 350 to
+// 380 us, 4.3 to 4.6 TB/s, where a large copy reaches 4.9); of the backward one, which
+// leaves registers for more waves (8 x 4096 tokens of 12 + 12 heads of 64: 68 us, 4.5
+// TB/s, and 5 for the weights' shares; two heads at once 80).
 #include <algorithm>
 
 #include "attn.hpp"
@@ -259,15 +263,15 @@ __global__ __launch_bounds__(kBlk) void norm_fwd_kernel(NormProblem p, int lanes
 
 // Blocks 0 .. nbq - 1 take the queries, the others the keys; every block adds
 // up its rows' share of dw in a fixed order and leaves it in part[block].
-template <typename T, int P, int HL>
+template <typename T, int P>
 __global__ __launch_bounds__(kBlk) void norm_bwd_kernel(NormProblem p, int lanes, int nbq, float *part)
 {
     __shared__ float rows[kBlk * 16];
     const int per = kBlk / lanes, grp = threadIdx.x / lanes, lane = threadIdx.x % lanes;
     const bool second = (int)blockIdx.x >= nbq;
     const int blk = second ? blockIdx.x - nbq : blockIdx.x, nblk = second ? gridDim.x - nbq : nbq;
-    const int H = second ? p.Hk : p.Hq, nb = (H + HL - 1) / HL;
-    const int64_t items = (int64_t)p.B * p.T * nb;
+    const int H = second ? p.Hk : p.Hq;
+    const int64_t items = (int64_t)p.B * p.T * H;
     const Heads &xi = second ? p.k : p.q, &yi = second ? p.dyk : p.dyq, &dx = second ? p.dk : p.dq;
     const Runs r = runs_of<P>(lane, p.D, p.R);
     float *row = rows + grp * lanes * 16;
@@ -278,46 +282,38 @@ __global__ __launch_bounds__(kBlk) void norm_bwd_kernel(NormProblem p, int lanes
     for (int e = 0; e < 8; ++e)
         dw[0][e] = dw[1][e] = 0.f;
     for (int64_t item = (int64_t)blk * per + grp; item < items; item += (int64_t)nblk * per) {
-        const int h0 = (int)(item % nb) * HL;
-        const int64_t bt = item / nb;
+        const int h = (int)(item % H);
+        const int64_t bt = item / H;
         const int b = (int)(bt / p.T), t = (int)(bt % p.T);
-        const T *x = static_cast<const T *>(xi.p) + b * xi.sb + t * xi.st + h0 * xi.sh;
-        const T *dy = static_cast<const T *>(yi.p) + b * yi.sb + t * yi.st + h0 * yi.sh;
-        T *out = static_cast<T *>(dx.p) + b * dx.sb + t * dx.st + h0 * dx.sh;
-        float v[HL][2][8], d[HL][2][8];
-#pragma unroll
-        for (int h = 0; h < HL; ++h) {
-            load_row(x + h * xi.sh, h0 + h < H ? r : Runs{-1, -1}, v[h]);
-            load_row(dy + h * yi.sh, h0 + h < H ? r : Runs{-1, -1}, d[h]);
-        }
+        const T *x = static_cast<const T *>(xi.p) + b * xi.sb + t * xi.st + h * xi.sh;
+        const T *dy = static_cast<const T *>(yi.p) + b * yi.sb + t * yi.st + h * yi.sh;
+        T *out = static_cast<T *>(dx.p) + b * dx.sb + t * dx.st + h * dx.sh;
+        float v[2][8], d[2][8];
+        load_row(x, r, v);
+        load_row(dy, r, d);
         Angles g;
         const int64_t at = P == kNone ? 0 : (int64_t)table_row(p, b, t) * (p.R / 2);
         load_angles<P>(g, p.cos + at, p.sin + at, r, p.R);
+        turn<P>(d, g, -1.f, r, p.R, row);
+        float ss = 0.f, sd = 0.f;
 #pragma unroll
-        for (int h = 0; h < HL; ++h) {
-            if (h0 + h >= H)
-                break;
-            turn<P>(d[h], g, -1.f, r, p.R, row);
-            float ss = 0.f, sd = 0.f;
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int e = 0; e < 8; ++e) {
+                ss = fmaf(v[k][e], v[k][e], ss);
+                sd = fmaf(v[k][e], d[k][e] * w[k][e], sd);
+            }
+        ss = group_sum(ss, lanes);
+        sd = group_sum(sd, lanes);
+        const float f = rsqrtf(ss / (float)p.D + p.eps), m = f * f * (sd / (float)p.D);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    ss = fmaf(v[h][k][e], v[h][k][e], ss);
-                    sd = fmaf(v[h][k][e], d[h][k][e] * w[k][e], sd);
-                }
-            ss = group_sum(ss, lanes);
-            sd = group_sum(sd, lanes);
-            const float f = rsqrtf(ss / (float)p.D + p.eps), m = f * f * (sd / (float)p.D);
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    dw[k][e] = fmaf(d[h][k][e], v[h][k][e] * f, dw[k][e]);
-                    d[h][k][e] = f * (d[h][k][e] * w[k][e] - v[h][k][e] * m);
-                }
-            store_row(out + h * dx.sh, r, d[h]);
-        }
+            for (int e = 0; e < 8; ++e) {
+                dw[k][e] = fmaf(d[k][e], v[k][e] * f, dw[k][e]);
+                d[k][e] = f * (d[k][e] * w[k][e] - v[k][e] * m);
+            }
+        store_row(out, r, d);
     }
     if ((second ? p.wk : p.wq) == nullptr)
         return;
@@ -391,8 +387,9 @@ int group_lanes(const NormProblem &p)
     return l;
 }
 
-// Heads that a group of lanes takes together: four, one where that leaves the
-// card with fewer than kFewThreads threads.
+// Heads that a group of lanes of the forward takes together: four, one where that
+// leaves the card with fewer than kFewThreads threads (us, one and four: 4096 tokens of
+// 2 x 12 heads of 64 7.1 and 7.6, 8192 12.7 and 11.4, 65536 90 and 86; 8 tokens 3.5 and 5.5).
 constexpr int64_t kFewThreads = 256 * 1024;
 int heads_each(const NormProblem &p)
 {
@@ -414,17 +411,20 @@ hipError_t fwd(const NormProblem &p, hipStream_t s)
     return hipGetLastError();
 }
 
-// Workgroups of the backward at most (their shares of dw are added up after it).
-constexpr int kBwdBlocks = 2048;
+// Workgroups of the backward at most, and how many there are at least before a group of
+// lanes has kRowsEach rows of its own: each leaves a share of dw to be added up (us at 4096
+// tokens of 2 x 12 heads of 64 15.6 without the latter, 13.8 with it; 4096 tokens of 2 x 16
+// heads of 128 27.4 and 22.8).
+constexpr int kBwdBlocks = 2048, kBwdFew = 512, kRowsEach = 4;
 
-template <typename T, int P, int HL>
+template <typename T, int P>
 hipError_t bwd(const NormProblem &p, hipStream_t s)
 {
     const int lanes = group_lanes(p), per = kBlk / lanes;
     const auto blocks = [&](int H) {
-        const int64_t items = (int64_t)p.B * p.T * ((H + HL - 1) / HL);
-        const int64_t most = std::max(1, (int)((int64_t)kBwdBlocks * H / (p.Hq + p.Hk)));
-        return (int)std::min((items + per - 1) / per, most);
+        const int64_t all = ((int64_t)p.B * p.T * H + per - 1) / per;
+        const auto part = [&](int64_t n) { return std::max<int64_t>(1, n * H / (p.Hq + p.Hk)); };
+        return (int)std::min({all, part(kBwdBlocks), std::max(part(kBwdFew), all / kRowsEach)});
     };
     const int nbq = blocks(p.Hq), nbk = blocks(p.Hk);
     void *part = nullptr;
@@ -435,7 +435,7 @@ hipError_t bwd(const NormProblem &p, hipStream_t s)
     }
     if (p.ws->counting)
         return hipSuccess;
-    norm_bwd_kernel<T, P, HL><<<dim3((unsigned)(nbq + nbk)), kBlk, 0, s>>>(p, lanes, nbq, static_cast<float *>(part));
+    norm_bwd_kernel<T, P><<<dim3((unsigned)(nbq + nbk)), kBlk, 0, s>>>(p, lanes, nbq, static_cast<float *>(part));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !part)
         return e;
@@ -446,11 +446,10 @@ hipError_t bwd(const NormProblem &p, hipStream_t s)
 template <typename T, bool BWD, int P>
 hipError_t pick(const NormProblem &p, hipStream_t s)
 {
-    const bool one = heads_each(p) == 1;
     if constexpr (BWD)
-        return one ? bwd<T, P, 1>(p, s) : bwd<T, P, 2>(p, s);
+        return bwd<T, P>(p, s);
     else
-        return one ? fwd<T, P, 1>(p, s) : fwd<T, P, 4>(p, s);
+        return heads_each(p) == 1 ? fwd<T, P, 1>(p, s) : fwd<T, P, 4>(p, s);
 }
 
 template <typename T, bool BWD>
