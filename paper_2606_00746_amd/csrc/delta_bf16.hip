@@ -867,18 +867,20 @@ __device__ __forceinline__ Terms<kKeep> turned_terms(const char *lds, int blk, i
 
 // dQ, dK, dg and dbeta of a chunk, with the value heads that share its queries
 // and keys in turn.  Wave w holds the rows 64 j + 16 w .. of dQ^T and dK^T.  8 x 4096
-// tokens of 12 heads of 64: 315 us, two workgroups a CU; bound by LDS reads of operands
-// in two terms and by splitting results into terms, behind barriers.
+// tokens of 12 heads of 64: 281 us, two workgroups a CU (with dO in registers instead of
+// LDS and the loads where they are used 315); waits 70% of its time, on LDS reads of operands
+// in two terms and the barriers between its phases.
 template <int DKP, int DVP>
 __global__ __launch_bounds__(kThreads, (DKP + DVP <= 128 ? 2 : 1))
 void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv)
 {
     constexpr int NB = DKP / 64, NG = DKP / 32, NE = DVP / 32;
     using X = Tile<bf16_t, DKP>;
+    using E = Tile<bf16_t, DVP>;
     constexpr int kMat = DVP * 128;                        // one term of [DVP][64]
     constexpr int kPN = 2 * kKeep * Square16::kBytes;      // P and N lie over U and R
     constexpr int kUR = 2 * kKeep * kMat > kPN ? 2 * kKeep * kMat : kPN;
-    __shared__ __attribute__((aligned(16))) char ur[kUR], sd[kKeep * kMat], kl[X::kBytes], ql[X::kBytes];
+    __shared__ __attribute__((aligned(16))) char ur[kUR], sd[kKeep * kMat], kl[X::kBytes], ql[X::kBytes], dl[E::kBytes];
     __shared__ float sums[4][4][kChunk], ss[4];
     char *ul = ur, *rl = ur + kKeep * kMat, *pl = ur, *nl = ur + kKeep * Square16::kBytes;
 
@@ -908,15 +910,11 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
             }
         return;
     }
-    {
-        X a, e;
-        a.start(p.q.st, p.Dk);
-        e.start(p.k.st, p.Dk);
-        a.load(q, p.q.st, 0, n, p.Dk);
-        e.load(k, p.k.st, 0, n, p.Dk);
-        a.store(ql);
-        e.store(kl);
-    }
+    X qt, kt;
+    qt.start(p.q.st, p.Dk);
+    kt.start(p.k.st, p.Dk);
+    qt.load(q, p.q.st, 0, n, p.Dk);
+    kt.load(k, p.k.st, 0, n, p.Dk);
     f32x4_t dq[NB][4], dk[NB][4];   // rows 64 j + 16 w + 4 u + i, token 16 tb + c
 #pragma unroll
     for (int j = 0; j < NB; ++j)
@@ -930,26 +928,42 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
         const float *gates = kept.gates + at * kGateRows * kChunk;
         const bf16_t *d = static_cast<const bf16_t *>(p.dout.p) + b * p.dout.sb + hv * p.dout.sh + (int64_t)t0 * p.dout.st;
         const bf16_t *v = static_cast<const bf16_t *>(p.v.p) + b * p.v.sb + hv * p.v.sh + (int64_t)t0 * p.v.st;
+        // all that a head reads is on its way at once
         Unpacked<DVP> iu, ir, is;
         iu.load(kept.u, at * nv * 2, 2, 0, nv);
         ir.load(gr.r, at * nv * 2, 2, 0, nv);
         is.load(kept.s, at * nv * NG, NG, 0, nv);
-        // dO by tokens, entries 32 g + 8 u .. of token 16 tb + c
-        uint4 df[4][NE];
+        E dt;
+        dt.start(p.dout.st, p.Dv);
+        dt.load(d, p.dout.st, 0, n, p.Dv);
+        const int t = 16 * w + c;   // this lane's token of the 64 x 64 matrices
+        uint4 vp[NE];
 #pragma unroll
-        for (int tb = 0; tb < 4; ++tb)
+        for (int g = 0; g < NE; ++g)
+            vp[g] = piece_of(v, p.v.st, t, n, 32 * g + 8 * u, p.Dv);
+        const float bt = gates[t], gt = gates[4 * kChunk + t];
+        f32x4_t gs[4];
+        float ge[4], gq[4], gl[4];
 #pragma unroll
-            for (int g = 0; g < NE; ++g)
-                df[tb][g] = piece_of(d, p.dout.st, 16 * tb + c, n, 32 * g + 8 * u, p.Dv);
+        for (int tb = 0; tb < 4; ++tb) {
+            gs[tb] = load4(gates + 4 * kChunk + 16 * tb + 4 * u);
+            gq[tb] = gates[3 * kChunk + 16 * tb + c];
+            ge[tb] = gates[kChunk + 16 * tb + c];
+            gl[tb] = gates[2 * kChunk + 16 * tb + c];
+        }
+        step_fence();
         lds_barrier();   // the waves are done with the last head's P and N
+        if (h == 0) {
+            qt.store(ql);
+            kt.store(kl);
+        }
         iu.store(ul);
         ir.store(rl);
         is.store(sd);
+        dt.store(dl);
         lds_barrier();
         is.load(gr.ds, at * nv * NG, NG, 0, nv);
 
-        const int t = 16 * w + c;   // this lane's token of the 64 x 64 matrices
-        const float bt = gates[t], gt = gates[4 * kChunk + t];
         f32x4_t pm[4], nm[4];
         float along = 0.f, db = 0.f, colsum[4][4];
         {
@@ -957,7 +971,7 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
             Terms<kKeep> rf[NE];
 #pragma unroll
             for (int g = 0; g < NE; ++g) {
-                mine[g] = piece_of(d, p.dout.st, t, n, 32 * g + 8 * u, p.Dv);
+                mine[g] = ld16(dl + E::at(t, 4 * g + u));
                 rf[g] = turned_terms(rl, w, g, l, DVP);
             }
 #pragma unroll
@@ -980,11 +994,10 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
                         qk = mma(ks, one(ld16(ql + X::at(t, 4 * g + u))), qk);
                         kk = mma(ks, one(ld16(kl + X::at(t, 4 * g + u))), kk);
                     }
-                    const f32x4_t gs = load4(gates + 4 * kChunk + 16 * sb + 4 * u);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int s = 16 * sb + 4 * u + i;
-                        const float decay = s <= t ? exp_f(gt - gs[i]) : 0.f, strict = s < t ? decay : 0.f;
+                        const float decay = s <= t ? exp_f(gt - gs[sb][i]) : 0.f, strict = s < t ? decay : 0.f;
                         pm[sb][i] = p.scale * decay * c1[i];
                         nm[sb][i] = -bt * strict * c2[i];
                         const float ef = pm[sb][i] * qk[i] + nm[sb][i] * kk[i];
@@ -1006,13 +1019,6 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
         // products with the states: S first, then dS in its place
         float qy[4] = {0.f, 0.f, 0.f, 0.f}, ky[4] = {0.f, 0.f, 0.f, 0.f}, kz[4] = {0.f, 0.f, 0.f, 0.f}, dot = 0.f;
         const float last = gates[4 * kChunk + kChunk - 1];
-        float ge[4], gq[4], gl[4];
-#pragma unroll
-        for (int tb = 0; tb < 4; ++tb) {
-            gq[tb] = gates[3 * kChunk + 16 * tb + c];
-            ge[tb] = gates[kChunk + 16 * tb + c];
-            gl[tb] = gates[2 * kChunk + 16 * tb + c];
-        }
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const int m0 = 64 * j + 16 * w + 4 * u;
@@ -1032,7 +1038,7 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
                 sf[g] = turned_terms(sd, w, g, l, DVP);
 #pragma unroll
                 for (int tb = 0; tb < 4; ++tb) {
-                    y1[tb] = mma(sf[g], one(df[tb][g]), y1[tb]);
+                    y1[tb] = mma(sf[g], one(ld16(dl + E::at(16 * tb + c, 4 * g + u))), y1[tb]);
                     y2[tb] = mma(sf[g], turned_terms(rl, tb, g, l, DVP), y2[tb]);
                 }
             }
@@ -1088,7 +1094,7 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
 #pragma unroll
         for (int g = 0; g < NE; ++g) {
             const Terms<kKeep> rf = turned_terms(rl, w, g, l, DVP);
-            const bf16x8_t vf = one(piece_of(v, p.v.st, t, n, 32 * g + 8 * u, p.Dv)).v[0];
+            const bf16x8_t vf = one(vp[g]).v[0];
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 rv = fmaf((float)rf.v[0][e] + (float)rf.v[1][e], (float)vf[e], rv);
@@ -1148,16 +1154,16 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
                     s16x4_t a, b;
                 } kw = {read_turned(kl + X::at(row, piece) + in), read_turned(kl + X::at(row + 4, piece) + in)},
                   qw = {read_turned(ql + X::at(row, piece) + in), read_turned(ql + X::at(row + 4, piece) + in)};
-                const Terms<1> kt{{__builtin_bit_cast(bf16x8_t, kw)}}, qt{{__builtin_bit_cast(bf16x8_t, qw)}};
+                const Terms<1> kx{{__builtin_bit_cast(bf16x8_t, kw)}}, qx{{__builtin_bit_cast(bf16x8_t, qw)}};
 #pragma unroll
                 for (int tb = 0; tb < 4; ++tb) {
                     if (g <= tb / 2) {   // columns s of group g, rows t = 16 tb + c
-                        dq[j][tb] = mma(kt, row_terms<kKeep>(pl, 16 * tb + c, 4 * g + u), dq[j][tb]);
-                        dk[j][tb] = mma(kt, row_terms<kKeep>(nl, 16 * tb + c, 4 * g + u), dk[j][tb]);
+                        dq[j][tb] = mma(kx, row_terms<kKeep>(pl, 16 * tb + c, 4 * g + u), dq[j][tb]);
+                        dk[j][tb] = mma(kx, row_terms<kKeep>(nl, 16 * tb + c, 4 * g + u), dk[j][tb]);
                     }
                     if (g >= tb / 2) {   // rows t of group g, column s = 16 tb + c
-                        dk[j][tb] = mma(qt, turned_terms(pl, tb, g, l, kChunk), dk[j][tb]);
-                        dk[j][tb] = mma(kt, turned_terms(nl, tb, g, l, kChunk), dk[j][tb]);
+                        dk[j][tb] = mma(qx, turned_terms(pl, tb, g, l, kChunk), dk[j][tb]);
+                        dk[j][tb] = mma(kx, turned_terms(nl, tb, g, l, kChunk), dk[j][tb]);
                     }
                 }
             }
