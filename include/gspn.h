@@ -397,7 +397,8 @@ int gspn_latent_params(const void *xc, const void *l_u, const void *l_lam,
  * must not overlap anything otherwise (GSPN_ERR_ALIAS).  Arithmetic is fp32;
  * with bf16 storage the operands of matrix products are bf16 (softmax weights
  * and their gradients are rounded to nearest even for the products that take
- * them, their sums are not).  The rest is as for the scan: asynchronous on
+ * them, to twice the bits in gradients of short sequences and narrow windows;
+ * their sums are not).  The rest is as for the scan: asynchronous on
  * `stream`, no allocation, results that repeat bit for bit.
  *
  * Norm of query and key heads with the position rotation:

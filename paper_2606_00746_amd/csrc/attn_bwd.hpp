@@ -290,11 +290,13 @@ struct KeySplit {
     }
 };
 
-template <typename T, int DP, int KW, bool FINE>
+// ONLY: of dv (1) or dk (2), 0 both.
+template <typename T, int DP, int KW, bool FINE, int ONLY>
 __global__ __launch_bounds__(kThreads, (DP * sizeof(T) <= 128 ? 2 : 1))
 void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shares)
 {
     using X = Tile<T, DP>;
+    constexpr bool kDv = ONLY != 2, kDk = ONLY != 1;
     constexpr int kSlices = X::kPieces / 2, kKeys = 128 / KW;
     // as in the forward; larger heads leave one wave a SIMD, which reads by hand would
     // stop (heads of 128: 393 us, 481 with them)
@@ -342,7 +344,8 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
 #pragma unroll
     for (int s = 0; s < kSlices; ++s) {
         kf[s] = row_frag(kr, 2 * s + h, a.D);
-        vf[s] = row_frag(vr, 2 * s + h, a.D);
+        if (kDk)
+            vf[s] = row_frag(vr, 2 * s + h, a.D);
     }
     f32x16_t dk[DP / 32], dv[DP / 32];
 #pragma unroll
@@ -430,12 +433,14 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
                         dp = mma(df.at(sl), vf[sl], dp);
                 } else {
                     qf.load(ql, 32 * qb + c);
-                    df.load(dl, 32 * qb + c);
+                    if (kDk)
+                        df.load(dl, 32 * qb + c);
                     reads_first<T>();
 #pragma unroll
                     for (int sl = 0; sl < kSlices; ++sl) {
                         s = mma(qf.at(sl), kf[sl], s);
-                        dp = mma(df.at(sl), vf[sl], dp);
+                        if (kDk)
+                            dp = mma(df.at(sl), vf[sl], dp);
                     }
                 }
                 f32x4_t ls[4], de[4];
@@ -449,7 +454,8 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
                         ls[g] = *reinterpret_cast<const f32x4_t *>(&stats[buf][0][32 * qb + 8 * g + 4 * h]);
                         de[g] = *reinterpret_cast<const f32x4_t *>(&stats[buf][1][32 * qb + 8 * g + 4 * h]);
                     }
-                    dx.load(dl, 32 * qb);
+                    if (kDv)
+                        dx.load(dl, 32 * qb);
                     reads_first<T>();
                 }
 #pragma unroll
@@ -466,7 +472,10 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
                         dp[r] = see ? dp[r] : 0.f;
                     }
                 }
-                add_turned<DP, FINE>(dx, s, dv);
+                if (kDv)
+                    add_turned<DP, FINE>(dx, s, dv);
+                if (!kDk)
+                    return;
                 if constexpr (kFlows)
                     flow_turned<DP, qb>(lds_offset(ql), qx);
                 else
@@ -486,21 +495,27 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
     }
 
     if (KW == 2) {
-        join_pair(reinterpret_cast<float *>(lds), dk, w, l);
-        join_pair(reinterpret_cast<float *>(lds), dv, w, l);
+        if (kDk)
+            join_pair(reinterpret_cast<float *>(lds), dk, w, l);
+        if (kDv)
+            join_pair(reinterpret_cast<float *>(lds), dv, w, l);
         if (w & 1)
             return;
     }
     if (parts > 1) {
         float *out = shares + ((int64_t)(b * a.Hkv + hk) * ks.shares() + ks.share(tile, part)) *
                                   (2 * kKeys * DP) + (32 * (w / KW) + c) * DP;
-        store_column<float, DP>(out, dk, 1.f, DP);
-        store_column<float, DP>(out + kKeys * DP, dv, 1.f, DP);
+        if (kDk)
+            store_column<float, DP>(out, dk, 1.f, DP);
+        if (kDv)
+            store_column<float, DP>(out + kKeys * DP, dv, 1.f, DP);
     } else if (j < a.Tk) {
-        store_column<T, DP>(static_cast<T *>(a.dk.p) + b * a.dk.sb + hk * a.dk.sh + j * a.dk.st, dk,
-                            a.scale, a.D);
-        store_column<T, DP>(static_cast<T *>(a.dv.p) + b * a.dv.sb + hk * a.dv.sh + j * a.dv.st, dv, 1.f,
-                            a.D);
+        if (kDk)
+            store_column<T, DP>(static_cast<T *>(a.dk.p) + b * a.dk.sb + hk * a.dk.sh + j * a.dk.st, dk,
+                                a.scale, a.D);
+        if (kDv)
+            store_column<T, DP>(static_cast<T *>(a.dv.p) + b * a.dv.sb + hk * a.dv.sh + j * a.dv.st, dv, 1.f,
+                                a.D);
     }
 }
 
@@ -585,8 +600,19 @@ hipError_t run_dkv(const AttnProblem &p, const float *delta, hipStream_t s)
         return hipErrorInvalidConfiguration;
     if (e != hipSuccess || p.ws->counting)
         return e;
-    attn_dkv_kernel<T, DP, KW, FINE><<<dim3((unsigned)nk), kThreads, 0, s>>>(p, delta, ks, static_cast<float *>(shares));
+    // fp32 keys, values and both sums at heads of 128 are more than a lane's 512 registers
+    // hold: dv and dk one after the other form the scores twice but spill less (4096 tokens
+    // of 8 heads, a causal window of 1023: 680 us together, 218 and 331 apart)
+    constexpr int kFirst = sizeof(T) == 4 && DP == 128 ? 1 : 0;
+    float *const out = static_cast<float *>(shares);
+    attn_dkv_kernel<T, DP, KW, FINE, kFirst><<<dim3((unsigned)nk), kThreads, 0, s>>>(p, delta, ks, out);
     e = hipGetLastError();
+    if constexpr (kFirst == 1) {
+        if (e == hipSuccess) {
+            attn_dkv_kernel<T, DP, KW, FINE, 2><<<dim3((unsigned)nk), kThreads, 0, s>>>(p, delta, ks, out);
+            e = hipGetLastError();
+        }
+    }
     const auto sum = [&](int first, int count, int parts) {
         if (e != hipSuccess || count == 0 || parts == 1)
             return;
