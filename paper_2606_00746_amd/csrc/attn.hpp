@@ -117,7 +117,8 @@ struct Tile {
             off[i] = c * kPer < D ? (uint32_t)(r * (int)st * (int)sizeof(T) + c * 16) : 0x80000000u;
         }
     }
-    // Rows row0 .. row0 + 63 into registers; rows from `rows` on read as zero.  The
+    // Rows row0 .. row0 + 63 into registers; rows from `rows` on read as zero, where
+    // rows do not overlap (st >= D; else as parts of rows ahead of them).  The
     // buffer's range does both: a tile is below 2^31 bytes (token strides are below
     // 2^23), pieces that count as absent lie beyond.
     __device__ __forceinline__ void load(const T *base, int64_t st, int row0, int rows, int D)
@@ -128,6 +129,18 @@ struct Tile {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
             reg[i] = kEven ? ld128(r, off[0], i * kStep * (int)st * (int)sizeof(T)) : ld128(r, off[i], 0);
+    }
+    // The same where a row that should read as zero counts, whatever its weight:
+    // tokens that share memory (a stride below D, 0 for a view that broadcasts) leave
+    // rows past the last inside the range.
+    __device__ __forceinline__ void load_strict(const T *base, int64_t st, int row0, int rows, int D)
+    {
+        load(base, st, row0, rows, D);
+        if (st < D)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                if (row0 + (int)(threadIdx.x + i * kThreads) / kPieces >= rows)
+                    reg[i] = make_uint4(0, 0, 0, 0);
     }
     __device__ __forceinline__ void store(char *lds) const
     {

@@ -594,7 +594,7 @@ __global__ __launch_bounds__(kThreads) void delta16_du_kernel(DeltaProblem p, Ke
         return;
     X x;
     x.start(p.dout.st, p.Dv);
-    x.load(d, p.dout.st, 0, n, p.Dv);
+    x.load_strict(d, p.dout.st, 0, n, p.Dv);
     {   // P[t][s] as rows of s, for the 16 columns s of block w
         const float gs = gates[4 * kChunk + 16 * w + c];
         f32x4_t a[4];
@@ -913,8 +913,8 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
     X qt, kt;
     qt.start(p.q.st, p.Dk);
     kt.start(p.k.st, p.Dk);
-    qt.load(q, p.q.st, 0, n, p.Dk);
-    kt.load(k, p.k.st, 0, n, p.Dk);
+    qt.load_strict(q, p.q.st, 0, n, p.Dk);
+    kt.load_strict(k, p.k.st, 0, n, p.Dk);
     f32x4_t dq[NB][4], dk[NB][4];   // rows 64 j + 16 w + 4 u + i, token 16 tb + c
 #pragma unroll
     for (int j = 0; j < NB; ++j)
@@ -935,7 +935,7 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
         is.load(kept.s, at * nv * NG, NG, 0, nv);
         E dt;
         dt.start(p.dout.st, p.Dv);
-        dt.load(d, p.dout.st, 0, n, p.Dv);
+        dt.load_strict(d, p.dout.st, 0, n, p.Dv);
         const int t = 16 * w + c;   // this lane's token of the 64 x 64 matrices
         uint4 vp[NE];
 #pragma unroll
