@@ -107,17 +107,19 @@ __device__ __forceinline__ f32x4_t load4(const bf16_t *p)
 }
 
 // The decay of a token: exp(-100) is 0 to fp32 next to anything, and a bound
-// keeps the running sum's digits where one token forgets everything.
+// keeps running sums finite where a token forgets everything.
 constexpr float kLeastGate = -100.f;
 
 // A chunk's gates by lane (token): the running sum of g and beta; tokens from n on
-// decay and write nothing.
+// decay and write nothing.  The sum is G + D, two floats: behind tokens that forget
+// everything G is some hundreds or thousands, whose fp32 steps (2^-12 at 4000) would
+// be errors of the decays exp(G_t - G_s) between the ordinary tokens that follow.
 struct Gates {
-    float G, beta;
+    float G, D, beta;
 };
 __device__ __forceinline__ Gates load_gates(const DeltaProblem &p, int b, int h, int t0, int n, int lane)
 {
-    Gates x{0.f, 0.f};
+    Gates x{0.f, 0.f, 0.f};
     if (lane < n) {
         const int64_t at = ((int64_t)b * p.T + t0 + lane) * p.Hv + h;
         x.G = fmaxf(at_f(p.g, at, p.dtype), kLeastGate);
@@ -129,13 +131,23 @@ __device__ __forceinline__ void sum_gates(Gates &x, int lane)
 {
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-        const float o = __shfl_up(x.G, d);
-        if (lane >= d)
-            x.G += o;
+        const float g = __shfl_up(x.G, d), r = __shfl_up(x.D, d);
+        if (lane >= d) {   // the sum and, exactly, what it leaves
+            const float s = x.G + g, part = s - x.G;
+            const float rest = ((x.G - (s - part)) + (g - part)) + (x.D + r);
+            x.G = s + rest;
+            x.D = rest - (x.G - s);
+        }
     }
 }
 
 __device__ __forceinline__ float exp_f(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// exp(G_t - G_s) from the sums' two floats.
+__device__ __forceinline__ float decay(float gt, float dt, float gs, float ds)
+{
+    return exp_f((gt - gs) + (dt - ds));
+}
 
 __device__ __forceinline__ int delta_len(const DeltaProblem &p, int b)
 {

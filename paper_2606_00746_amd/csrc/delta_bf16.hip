@@ -83,11 +83,11 @@ __device__ __forceinline__ void store_terms(uint4 *p, int64_t unit, int l, const
         put16(p + (unit * N + n) * 64 + l, __builtin_bit_cast(u32x4, t.v[n]));
 }
 
-constexpr int kGateRows = 5;   // beta, beta exp(G), exp(G_63 - G), exp(G), G
+constexpr int kGateRows = 6;   // beta, beta exp(G), exp(G_63 - G), exp(G), and G in its two floats
 constexpr int kInvUnits = 6;   // 16-row blocks x 32-column groups on and below the diagonal
 constexpr int kKeep = 2;       // terms of the states and U that are left behind
 
-// Per (b, value head, chunk): gates [5][64]; the inverse and its transpose as A
+// Per (b, value head, chunk): gates [6][64]; the inverse and its transpose as A
 // operands of three terms; U (units: slice of 16 columns x 2 groups of tokens)
 // and the state ahead of the chunk (slice x groups of Dk) as operands of two.
 struct Kept16 {
@@ -118,13 +118,14 @@ __global__ __launch_bounds__(kThreads) void delta16_inverse_kernel(DeltaProblem 
     const bf16_t *k = static_cast<const bf16_t *>(p.k.p) + b * p.k.sb + (hv / (p.Hv / p.Hq)) * p.k.sh + (int64_t)t0 * p.k.st;
     Gates x = load_gates(p, b, hv, t0, n, l);
     sum_gates(x, l);
-    const float last = __shfl(x.G, kChunk - 1), eg = exp_f(x.G);
+    const float last = __shfl(x.G, kChunk - 1), rest = __shfl(x.D, kChunk - 1), eg = exp_f(x.G);
     float *gates = kept.gates + id * kGateRows * kChunk + l;
     gates[0] = x.beta;
     gates[kChunk] = x.beta * eg;
-    gates[2 * kChunk] = exp_f(last - x.G);
+    gates[2 * kChunk] = decay(last, rest, x.G, x.D);
     gates[3 * kChunk] = eg;
     gates[4 * kChunk] = x.G;
+    gates[5 * kChunk] = x.D;
 
     f32x16_t kk[3];
 #pragma unroll
@@ -154,7 +155,8 @@ __global__ __launch_bounds__(kThreads) void delta16_inverse_kernel(DeltaProblem 
         for (int r = 0; r < 16; ++r) {
             const int t = (i ? 32 : 0) + 8 * (r / 4) + 4 * h + r % 4, s = (i == 2 ? 32 : 0) + c;
             const float gt = __shfl(x.G, t), bt = __shfl(x.beta, t), gs = __shfl(x.G, s);
-            m[t * kPitch + s] = s < t ? bt * exp_f(gt - gs) * kk[i][r] : 0.f;
+            const float dt = __shfl(x.D, t), ds = __shfl(x.D, s);
+            m[t * kPitch + s] = s < t ? bt * decay(gt, dt, gs, ds) * kk[i][r] : 0.f;
         }
     __builtin_amdgcn_wave_barrier();
     float col[kChunk];
@@ -510,7 +512,7 @@ __global__ __launch_bounds__(kThreads) void delta16_out_kernel(DeltaProblem p, K
     if (w < nv)
         fetch(w);
     {   // P[t][s] for the 16 tokens t of block w
-        const float gt = gates[4 * kChunk + 16 * w + c];
+        const float gt = gates[4 * kChunk + 16 * w + c], gd = gates[5 * kChunk + 16 * w + c];
         uint4 mine[NG], kr[4][NG];
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
@@ -529,9 +531,10 @@ __global__ __launch_bounds__(kThreads) void delta16_out_kernel(DeltaProblem p, K
                     for (int g = 0; g < NG; ++g)
                         a = mma(one(kr[sb][g]), one(mine[g]), a);
                     const f32x4_t gs = load4(gates + 4 * kChunk + 16 * sb + 4 * u);
+                    const f32x4_t ds = load4(gates + 5 * kChunk + 16 * sb + 4 * u);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        a[i] = 16 * sb + 4 * u + i <= 16 * w + c ? p.scale * exp_f(gt - gs[i]) * a[i] : 0.f;
+                        a[i] = 16 * sb + 4 * u + i <= 16 * w + c ? p.scale * decay(gt, gd, gs[i], ds[i]) * a[i] : 0.f;
                 }
                 put4<2>(pl, 16 * w + c, 16 * sb + 4 * u, a);
             }
@@ -596,7 +599,7 @@ __global__ __launch_bounds__(kThreads) void delta16_du_kernel(DeltaProblem p, Ke
     x.start(p.dout.st, p.Dv);
     x.load_strict(d, p.dout.st, 0, n, p.Dv);
     {   // P[t][s] as rows of s, for the 16 columns s of block w
-        const float gs = gates[4 * kChunk + 16 * w + c];
+        const float gs = gates[4 * kChunk + 16 * w + c], ds = gates[5 * kChunk + 16 * w + c];
         f32x4_t a[4];
 #pragma unroll
         for (int tb = 0; tb < 4; ++tb)
@@ -620,9 +623,10 @@ __global__ __launch_bounds__(kThreads) void delta16_du_kernel(DeltaProblem p, Ke
         for (int tb = 0; tb < 4; ++tb)
             if (tb >= (w & 2)) {
                 const f32x4_t gt = load4(gates + 4 * kChunk + 16 * tb + 4 * u);
+                const f32x4_t dt = load4(gates + 5 * kChunk + 16 * tb + 4 * u);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    a[tb][i] = 16 * w + c <= 16 * tb + 4 * u + i ? p.scale * exp_f(gt[i] - gs) * a[tb][i] : 0.f;
+                    a[tb][i] = 16 * w + c <= 16 * tb + 4 * u + i ? p.scale * decay(gt[i], dt[i], gs, ds) * a[tb][i] : 0.f;
                 put4<3>(pl, 16 * w + c, 16 * tb + 4 * u, a[tb]);
             }
     }
@@ -941,12 +945,13 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
 #pragma unroll
         for (int g = 0; g < NE; ++g)
             vp[g] = piece_of(v, p.v.st, t, n, 32 * g + 8 * u, p.Dv);
-        const float bt = gates[t], gt = gates[4 * kChunk + t];
-        f32x4_t gs[4];
+        const float bt = gates[t], gt = gates[4 * kChunk + t], gd = gates[5 * kChunk + t];
+        f32x4_t gs[4], ds[4];
         float ge[4], gq[4], gl[4];
 #pragma unroll
         for (int tb = 0; tb < 4; ++tb) {
             gs[tb] = load4(gates + 4 * kChunk + 16 * tb + 4 * u);
+            ds[tb] = load4(gates + 5 * kChunk + 16 * tb + 4 * u);
             gq[tb] = gates[3 * kChunk + 16 * tb + c];
             ge[tb] = gates[kChunk + 16 * tb + c];
             gl[tb] = gates[2 * kChunk + 16 * tb + c];
@@ -997,8 +1002,8 @@ void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int s = 16 * sb + 4 * u + i;
-                        const float decay = s <= t ? exp_f(gt - gs[sb][i]) : 0.f, strict = s < t ? decay : 0.f;
-                        pm[sb][i] = p.scale * decay * c1[i];
+                        const float kept_ts = s <= t ? decay(gt, gd, gs[sb][i], ds[sb][i]) : 0.f, strict = s < t ? kept_ts : 0.f;
+                        pm[sb][i] = p.scale * kept_ts * c1[i];
                         nm[sb][i] = -bt * strict * c2[i];
                         const float ef = pm[sb][i] * qk[i] + nm[sb][i] * kk[i];
                         along += ef;

@@ -50,8 +50,8 @@ __global__ __launch_bounds__(kThreads) void delta_du_kernel(DeltaProblem p, floa
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int t = 32 * rb + 8 * (r / 4) + 4 * h2 + r % 4, s = 32 * cb + c2;
-            const float gt = __shfl(x.G, t), gs = __shfl(x.G, s);
-            al[t * kPitch + s] = s <= t ? p.scale * exp_f(gt - gs) * qk[r] : 0.f;
+            const float gt = __shfl(x.G, t), gs = __shfl(x.G, s), dt = __shfl(x.D, t), ds = __shfl(x.D, s);
+            al[t * kPitch + s] = s <= t ? p.scale * decay(gt, dt, gs, ds) * qk[r] : 0.f;
         }
     }
     lds_barrier();
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kThreads) void delta_dstate_kernel(DeltaProblem p, 
     constexpr int NB = DKP / 64, kKP = DKP + 4, kXP = 20;
     __shared__ __attribute__((aligned(16))) float kl[kChunk * kKP], ql[kChunk * kKP], tl[kChunk * kPitch];
     __shared__ __attribute__((aligned(16))) float part[4][kChunk * kXP], xl[kChunk * kXP], zl[kChunk * kXP];
-    __shared__ float gl[kChunk], bl[kChunk];
+    __shared__ float gl[kChunk], gd[kChunk], bl[kChunk];
 
     const int nv = sv / 16;
     int id = xcd_remap(blockIdx.x, gridDim.x);
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(kThreads) void delta_dstate_kernel(DeltaProblem p, 
 
     Rows<T, DKP> kr, qr;
     Square tr;
-    Gates gt{0.f, 0.f};
+    Gates gt{0.f, 0.f, 0.f};
     f32x4_t dr, ur;
     const auto fetch = [&](int ch) {
         const int t0 = ch * kChunk, n = max(0, min(kChunk, len - t0));
@@ -141,6 +141,7 @@ __global__ __launch_bounds__(kThreads) void delta_dstate_kernel(DeltaProblem p, 
         if (w == 0) {
             sum_gates(gt, l);
             gl[l] = gt.G;
+            gd[l] = gt.D;
             bl[l] = gt.beta;
         }
         const f32x4_t dc = dr, uc = ur;
@@ -171,13 +172,13 @@ __global__ __launch_bounds__(kThreads) void delta_dstate_kernel(DeltaProblem p, 
             for (int i = 0; i < 4; ++i)
                 part[w][(16 * rb + 4 * u + i) * kXP + c] = acc[rb][i];
         lds_barrier();
-        const float last = gl[kChunk - 1];
+        const float last = gl[kChunk - 1], rest = gd[kChunk - 1];
         {
             f32x4_t x = load4(part[0] + xt * kXP + xc);
 #pragma unroll
             for (int y = 1; y < 4; ++y)
                 x += load4(part[y] + xt * kXP + xc);
-            x = uc + exp_f(last - gl[xt]) * x;
+            x = uc + decay(last, rest, gl[xt], gd[xt]) * x;
             *reinterpret_cast<f32x4_t *>(xl + xt * kXP + xc) = x;
         }
         lds_barrier();
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(kThreads, 1) void delta_grad_kernel(DeltaProblem p,
     constexpr int NB = DKP / 64, kKP = DKP + 4;
     __shared__ __attribute__((aligned(16))) float ql[kChunk * kKP], kl[kChunk * kKP];
     __shared__ __attribute__((aligned(16))) float pl[kChunk * kPitch], nl[kChunk * kPitch];
-    __shared__ float gl[kChunk], bl[kChunk], down[4][kChunk], rows[3][kChunk], dots[4][3][kChunk], ss[4];
+    __shared__ float gl[kChunk], gd[kChunk], bl[kChunk], down[4][kChunk], rows[3][kChunk], dots[4][3][kChunk], ss[4];
 
     int id = xcd_remap(blockIdx.x, gridDim.x);
     const int ch = id % nc;
@@ -298,11 +299,12 @@ __global__ __launch_bounds__(kThreads, 1) void delta_grad_kernel(DeltaProblem p,
             Gates g = load_gates(p, b, hv, t0, n, l);
             sum_gates(g, l);
             gl[l] = g.G;
+            gd[l] = g.D;
             bl[l] = g.beta;
         }
         down[w][l] = 0.f;
         lds_barrier();
-        const float last = gl[kChunk - 1];
+        const float last = gl[kChunk - 1], rest = gd[kChunk - 1];
 
         {   // rows 16 w .. of C1, C2, Q K^T, K K^T, up to the diagonal
             f32x4_t c1[4], c2[4], qk[4], kk[4];
@@ -345,9 +347,9 @@ __global__ __launch_bounds__(kThreads, 1) void delta_grad_kernel(DeltaProblem p,
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int t = 16 * w + 4 * u + i, s = 16 * sb + c;
-                        const float decay = s <= t ? exp_f(gl[t] - gl[s]) : 0.f;
-                        const float strict = s < t ? decay : 0.f;
-                        const float pp = p.scale * decay * c1[sb][i], mc = strict * c2[sb][i], nn = -bl[t] * mc;
+                        const float kept_ts = s <= t ? decay(gl[t], gd[t], gl[s], gd[s]) : 0.f;
+                        const float strict = s < t ? kept_ts : 0.f;
+                        const float pp = p.scale * kept_ts * c1[sb][i], mc = strict * c2[sb][i], nn = -bl[t] * mc;
                         pl[t * kPitch + s] = pp;
                         nl[t * kPitch + s] = nn;
                         const float ef = pp * qk[sb][i] + nn * kk[sb][i];
@@ -412,7 +414,7 @@ __global__ __launch_bounds__(kThreads, 1) void delta_grad_kernel(DeltaProblem p,
 #pragma unroll
             for (int tb = 0; tb < 4; ++tb) {
                 const int t = 16 * tb + c;
-                const float eg = exp_f(gl[t]), fq = p.scale * eg, fk = bl[t] * eg, fs = exp_f(last - gl[t]);
+                const float eg = exp_f(gl[t]), fq = p.scale * eg, fk = bl[t] * eg, fs = decay(last, rest, gl[t], gd[t]);
                 const f32x4_t qq = load4(ql + t * kKP + m0 + 4 * u), kx = load4(kl + t * kKP + m0 + 4 * u);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {

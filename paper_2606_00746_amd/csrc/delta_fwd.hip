@@ -49,7 +49,8 @@ __global__ __launch_bounds__(kThreads) void delta_inverse_kernel(DeltaProblem p,
         for (int r = 0; r < 16; ++r) {
             const int t = (i ? 32 : 0) + 8 * (r / 4) + 4 * h + r % 4, s = (i == 2 ? 32 : 0) + c;
             const float gt = __shfl(x.G, t), bt = __shfl(x.beta, t), gs = __shfl(x.G, s);
-            m[t * kPitch + s] = s < t ? bt * exp_f(gt - gs) * kk[i][r] : 0.f;
+            const float dt = __shfl(x.D, t), ds = __shfl(x.D, s);
+            m[t * kPitch + s] = s < t ? bt * decay(gt, dt, gs, ds) * kk[i][r] : 0.f;
         }
     __builtin_amdgcn_wave_barrier();
     float col[kChunk];
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(kThreads) void delta_state_kernel(DeltaProblem p, D
     constexpr int NB = DKP / 64, kKP = DKP + 4, kXP = 20;
     __shared__ __attribute__((aligned(16))) float kl[kChunk * kKP], tl[kChunk * kPitch];
     __shared__ __attribute__((aligned(16))) float part[4][kChunk * kXP], xl[kChunk * kXP], ul[kChunk * kXP];
-    __shared__ float gl[kChunk], bl[kChunk];
+    __shared__ float gl[kChunk], gd[kChunk], bl[kChunk];
 
     const int nv = sv / 16;
     int id = xcd_remap(blockIdx.x, gridDim.x);
@@ -106,7 +107,7 @@ __global__ __launch_bounds__(kThreads) void delta_state_kernel(DeltaProblem p, D
 
     Rows<T, DKP> kr;
     Square tr;
-    Gates gr{0.f, 0.f};
+    Gates gr{0.f, 0.f, 0.f};
     f32x4_t vr;
     const auto fetch = [&](int ch) {
         const int t0 = ch * kChunk, n = max(0, min(kChunk, len - t0));
@@ -125,6 +126,7 @@ __global__ __launch_bounds__(kThreads) void delta_state_kernel(DeltaProblem p, D
         if (w == 0) {
             sum_gates(gr, l);
             gl[l] = gr.G;
+            gd[l] = gr.D;
             bl[l] = gr.beta;
         }
         const f32x4_t vc = vr;
@@ -169,7 +171,7 @@ __global__ __launch_bounds__(kThreads) void delta_state_kernel(DeltaProblem p, D
         }
         lds_barrier();
         // U = inverse (b X), 16 rows a wave
-        const float last = gl[kChunk - 1];
+        const float last = gl[kChunk - 1], rest = gd[kChunk - 1];
         f32x4_t y = {0.f, 0.f, 0.f, 0.f};
         for (int kk = 0; kk <= w; ++kk) {
             const f32x4_t a = load4(tl + (16 * w + c) * kPitch + 16 * kk + 4 * u);
@@ -181,7 +183,7 @@ __global__ __launch_bounds__(kThreads) void delta_state_kernel(DeltaProblem p, D
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * w + 4 * u + i;
             ug[((int64_t)ch * kChunk + t) * sv + c] = y[i];
-            ul[t * kXP + c] = exp_f(last - gl[t]) * y[i];
+            ul[t * kXP + c] = decay(last, rest, gl[t], gd[t]) * y[i];
         }
         const float keep = exp_f(last);
         lds_barrier();
@@ -253,8 +255,8 @@ __global__ __launch_bounds__(kThreads) void delta_out_kernel(DeltaProblem p, Del
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int t = 32 * rb + 8 * (r / 4) + 4 * h2 + r % 4, s = 32 * cb + c2;
-            const float gt = __shfl(x.G, t), gs = __shfl(x.G, s);
-            al[t * kPitch + s] = s <= t ? p.scale * exp_f(gt - gs) * qk[r] : 0.f;
+            const float gt = __shfl(x.G, t), gs = __shfl(x.G, s), dt = __shfl(x.D, t), ds = __shfl(x.D, s);
+            al[t * kPitch + s] = s <= t ? p.scale * decay(gt, dt, gs, ds) * qk[r] : 0.f;
         }
     }
     lds_barrier();
