@@ -109,6 +109,7 @@ __device__ __forceinline__ f32x4_t load4(const bf16_t *p)
 // The decay of a token: exp(-100) is 0 to fp32 next to anything, and a bound
 // keeps running sums finite where a token forgets everything.
 constexpr float kLeastGate = -100.f;
+__device__ __forceinline__ float bounded(float g) { return g < kLeastGate ? kLeastGate : g; }   // (a NaN stays one)
 
 // A chunk's gates by lane (token): the running sum of g and beta; tokens from n on
 // decay and write nothing.  The sum is G + D, two floats: behind tokens that forget
@@ -122,7 +123,7 @@ __device__ __forceinline__ Gates load_gates(const DeltaProblem &p, int b, int h,
     Gates x{0.f, 0.f, 0.f};
     if (lane < n) {
         const int64_t at = ((int64_t)b * p.T + t0 + lane) * p.Hv + h;
-        x.G = fmaxf(at_f(p.g, at, p.dtype), kLeastGate);
+        x.G = bounded(at_f(p.g, at, p.dtype));
         x.beta = at_f(p.beta, at, p.dtype);
     }
     return x;

@@ -349,7 +349,7 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaProblem p)
             continue;
         }
         const int64_t at = ((int64_t)b * p.T + t) * p.Hv + hv;
-        const float a = exp_f(fmaxf(at_f(p.g, at, p.dtype), kLeastGate)), be = at_f(p.beta, at, p.dtype);
+        const float a = exp_f(bounded(at_f(p.g, at, p.dtype))), be = at_f(p.beta, at, p.dtype);
         float kr[NR], qr[NR], kq = 0.f;
         f32x4_t sk = {0.f, 0.f, 0.f, 0.f}, sq = sk;
 #pragma unroll
