@@ -233,10 +233,11 @@ void attn_fwd_kernel(AttnProblem a)
     T *op = static_cast<T *>(a.o.p) + b * a.o.sb + hq * a.o.sh;
     const float z = half_sum(sum);
     if (t < a.Tq) {
-        store_column<T, DP>(op + t * a.o.st, acc, z > 0.f ? 1.f / z : 0.f, a.D);
+        // (a sum of 0: the query sees no key; one that is NaN stays so)
+        store_column<T, DP>(op + t * a.o.st, acc, z == 0.f ? 0.f : 1.f / z, a.D);
         if (a.lse && h == 0)
             a.lse[((int64_t)b * a.Hq + hq) * a.Tq + t] =
-                z > 0.f ? fmaf(m, s2, __builtin_amdgcn_logf(z)) * kLn2 : -__builtin_inff();
+                z == 0.f ? -__builtin_inff() : fmaf(m, s2, __builtin_amdgcn_logf(z)) * kLn2;
     }
 }
 

@@ -273,13 +273,13 @@ __global__ __launch_bounds__(kThreads, 1) void attn_split_kernel(AttnProblem a, 
             }
         } else if (rt * kCol + r < rows) {
             const int tt = (rt * kCol + r) / G, hh = hk * G + (rt * kCol + r) % G;
-            const float f = z > 0.f ? 1.f / z : 0.f;
+            const float f = z == 0.f ? 0.f : 1.f / z;
             if (d < a.D)
                 store4(static_cast<T *>(a.o.p) + b * a.o.sb + tt * a.o.st + hh * a.o.sh + d, o[0] * f,
                        o[1] * f, o[2] * f, o[3] * f);
             if (d == 0 && a.lse)
                 a.lse[((int64_t)b * a.Hq + hh) * a.Tq + tt] =
-                    z > 0.f ? (top2 + __builtin_amdgcn_logf(z)) * kLn2 : -__builtin_inff();
+                    z == 0.f ? -__builtin_inff() : (top2 + __builtin_amdgcn_logf(z)) * kLn2;
         }
     }
 }
@@ -327,12 +327,12 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnProblem a, Shar
         top2 = mn;
     }
     const int t = row / G, hq = hk * G + row % G;
-    const float f = z > 0.f ? 1.f / z : 0.f;
+    const float f = z == 0.f ? 0.f : 1.f / z;
     store4(static_cast<T *>(a.o.p) + b * a.o.sb + t * a.o.st + hq * a.o.sh + d, o[0] * f, o[1] * f,
            o[2] * f, o[3] * f);
     if (d == 0 && a.lse)
         a.lse[((int64_t)b * a.Hq + hq) * a.Tq + t] =
-            z > 0.f ? (top2 + __builtin_amdgcn_logf(z)) * kLn2 : -__builtin_inff();
+            z == 0.f ? -__builtin_inff() : (top2 + __builtin_amdgcn_logf(z)) * kLn2;
 }
 
 int64_t tiles_of(const AttnProblem &p)
