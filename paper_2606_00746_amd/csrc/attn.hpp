@@ -461,19 +461,11 @@ __device__ __forceinline__ void reads_first()
         step_fence();
 }
 
-// A wide store reads its registers after issue: an asm behind it keeps them as they are.
-__device__ __forceinline__ void put16(void *p, u32x4 v)
-{
-    *reinterpret_cast<u32x4 *>(p) = v;
-    asm volatile("s_nop 7\n\ts_nop 7" : : "v"(v) : "memory");
-}
-
 // Stores a column (4 consecutive rows of a 32 x 32 result a register quad:
 // entries d .. d + 3 of one token) scaled by f.
 __device__ __forceinline__ void store4(bf16_t *p, float a, float b, float c, float d)
 {
-    const u32x2 v = {pack2(a, b), pack2(c, d)};
-    *reinterpret_cast<u32x2 *>(p) = v;
+    put8(p, u32x2{pack2(a, b), pack2(c, d)});
 }
 __device__ __forceinline__ void store4(float *p, float a, float b, float c, float d)
 {

@@ -267,10 +267,8 @@ __global__ __launch_bounds__(kThreads, 1) void attn_split_kernel(AttnProblem a, 
         if (sh.splits > 1) {
             const int64_t at = ((int64_t)tile * sh.splits + split) * kCol + r;
             store4(sh.out + at * DP + d, o[0], o[1], o[2], o[3]);
-            if (d == 0) {
-                sh.stat[2 * at] = top2;
-                sh.stat[2 * at + 1] = z;
-            }
+            if (d == 0)
+                put8(sh.stat + 2 * at, u32x2{__float_as_uint(top2), __float_as_uint(z)});
         } else if (rt * kCol + r < rows) {
             const int tt = (rt * kCol + r) / G, hh = hk * G + (rt * kCol + r) % G;
             const float f = z == 0.f ? 0.f : 1.f / z;

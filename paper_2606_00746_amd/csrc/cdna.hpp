@@ -178,6 +178,18 @@ __device__ __forceinline__ void gst128(uint4 *p, uint4 v)
                  : "memory");
 }
 
+// The same through pointers.
+__device__ __forceinline__ void put16(void *p, u32x4 v)
+{
+    *reinterpret_cast<u32x4 *>(p) = v;
+    asm volatile("s_nop 7\n\ts_nop 7" : : "v"(v) : "memory");
+}
+__device__ __forceinline__ void put8(void *p, u32x2 v)
+{
+    *reinterpret_cast<u32x2 *>(p) = v;
+    asm volatile("s_nop 7\n\ts_nop 7" : : "v"(v) : "memory");
+}
+
 // A lane's 16-byte piece of a per-direction plane: the values of storage
 // lines 8q .. 8q+7 at line position j, in line order (two bf16 per dword,
 // the lower line in the low half).  Blocked line-major planes hold it as one

@@ -271,7 +271,7 @@ __device__ __forceinline__ void store_half(uint4 *p, int64_t unit, int tb, int l
 #pragma unroll
     for (int n = 0; n < kKeep; ++n) {
         const uint4 w = __builtin_bit_cast(uint4, t.v[n]);
-        reinterpret_cast<uint2 *>(p + (unit * kKeep + n) * 64 + l)[tb & 1] = make_uint2(w.x, w.y);
+        put8(reinterpret_cast<uint2 *>(p + (unit * kKeep + n) * 64 + l) + (tb & 1), u32x2{w.x, w.y});
     }
 }
 

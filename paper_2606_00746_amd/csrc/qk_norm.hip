@@ -47,7 +47,6 @@ __device__ __forceinline__ void load8(const float *p, float (&f)[8])
     const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
     f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
 }
-using attn::put16;
 __device__ __forceinline__ void store8(bf16_t *p, const float (&f)[8])
 {
     put16(p, u32x4{pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])});

@@ -43,8 +43,8 @@ __device__ __forceinline__ void load8(const bf16_t *p, float (&v)[8])
 }
 __device__ __forceinline__ void store8(float *p, const float (&v)[8])
 {
-    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<float4 *>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    put16(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+    put16(p + 4, u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
 }
 __device__ __forceinline__ void store8(bf16_t *p, const float (&v)[8])
 {
