@@ -87,7 +87,8 @@ struct Tile {
     static constexpr int kPer = 16 / (int)sizeof(T);     // elements of a piece
     static constexpr int kPieces = DP / kPer;
     static constexpr int kS = kPieces <= 4 ? 4 : kPieces <= 8 ? 8 : kPieces <= 16 ? 16 : 32;
-    static constexpr int kBytes = kRows * kS * 16;
+    static constexpr int kRow = kS * 16;                 // bytes of a row
+    static constexpr int kBytes = kRows * kRow;
     static constexpr int kLoads = kRows * kPieces / kThreads;
     static_assert(kRows * kPieces % kThreads == 0, "a tile is whole pieces per thread");
 
@@ -391,7 +392,8 @@ struct RowFrags<float, DP> {
 
 // The same from tiles that flowed in: `tile` is their LDS offset.  The piece and
 // the row lie in different bits of an address, so that pieces differ by exclusive
-// ors and 32-row blocks by constants.
+// ors and 32-row blocks by constants: tiles begin at multiples of a row's bytes
+// (Tile::kRow), which the arrays they lie in are declared with.
 template <int DP, int BLOCK>
 __device__ __forceinline__ void flow_rows(uint32_t tile, Frag<bf16_t> (&f)[DP / 16])
 {

@@ -95,7 +95,7 @@ void attn_dq_kernel(AttnProblem a, float *delta)
     constexpr int kSlices = X::kPieces / 2, kTQ = 128 / KW;
     constexpr bool kFlows = sizeof(T) == 2;   // as in the forward
     static_assert(!FINE || (kFlows && KW == 2), "");
-    __shared__ __attribute__((aligned(16))) char lds[2][2][X::kBytes];
+    __shared__ __attribute__((aligned(X::kRow))) char lds[2][2][X::kBytes];
     __shared__ float sums[kThreads];
 
     const int G = a.Hq / a.Hkv, nqt = (a.Tq + kTQ - 1) / kTQ;
@@ -301,7 +301,7 @@ void attn_dkv_kernel(AttnProblem a, const float *delta, KeySplit ks, float *shar
     // as in the forward; larger heads leave one wave a SIMD, which reads by hand would
     // stop (heads of 128: 393 us, 481 with them)
     constexpr bool kFlows = sizeof(T) == 2 && DP <= 64;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][X::kBytes];
+    __shared__ __attribute__((aligned(X::kRow))) char lds[2][2][X::kBytes];
     __shared__ __attribute__((aligned(16))) float stats[2][2][kRows];
 
     const int G = a.Hq / a.Hkv, per = ks.blocks();

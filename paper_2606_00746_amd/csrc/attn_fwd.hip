@@ -41,7 +41,7 @@ void attn_fwd_kernel(AttnProblem a)
     constexpr int kSlices = X::kPieces / 2, kTQ = 128 / KW, NK = 2 / KW;
     // bf16 tiles flow straight into LDS, fp32 tiles come through registers
     constexpr bool kFlows = sizeof(T) == 2;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][X::kBytes];
+    __shared__ __attribute__((aligned(X::kRow))) char lds[2][2][X::kBytes];
 
     const int G = a.Hq / a.Hkv, nqt = (a.Tq + kTQ - 1) / kTQ;
     int id = xcd_remap(blockIdx.x, gridDim.x);

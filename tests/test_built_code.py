@@ -86,3 +86,24 @@ def test_no_wide_store_loses_its_data(tmp_path):
             found += overwritten(lines)
     assert stores > 1000
     assert not found, found[:5]
+
+
+def shared_tiles(source):
+    """(kernel's mangled name, bytes, alignment) of the [2][2][bytes] arrays of LDS that a
+    source declares, as the compiler's front end has them."""
+    cmd = [lib_build.hipcc(), *lib_build.HIPCC_FLAGS, *lib_build.SOURCE_FLAGS.get(source, []), "-x", "hip",
+           "--offload-device-only", "-Xclang", "-disable-llvm-passes", "-S", "-emit-llvm",
+           os.path.join(lib_build.CSRC, source), "-o", "-"]
+    out = subprocess.run(cmd, check=True, capture_output=True, text=True).stdout
+    found = re.findall(r"^@(\S+) = .*addrspace\(3\) global \[2 x \[2 x \[(\d+) x i8\]\]\] .*align (\d+)", out, re.M)
+    return [(name, int(size), int(align)) for name, size, align in found]
+
+
+def test_tiles_in_lds_begin_at_rows():
+    """Attention's tiles of 64 rows are read at addresses formed by exclusive ors inside a
+    row: an array of them is aligned to a row, not by luck of what lies ahead of it."""
+    with ThreadPoolExecutor(2) as ex:
+        tiles = sum(ex.map(shared_tiles, ("attn_fwd.hip", "attn_bwd.hip")), [])
+    assert len(tiles) >= 8
+    for name, size, align in tiles:
+        assert align % (size // 64) == 0, (name, size, align)
