@@ -82,8 +82,8 @@ struct Buffers {
         Heads h;
         h.p = const_cast<void *>(p);
         h.sh = H > 1 ? (s ? s[2] : D) : D;
-        h.st = T > 1 ? (s ? s[1] : H * D) : (H - 1) * h.sh + D;
-        h.sb = B > 1 ? (s ? s[0] : T * H * D) : (T - 1) * h.st + (H - 1) * h.sh + D;
+        h.st = T > 1 ? (s ? s[1] : H * D) : D;
+        h.sb = B > 1 ? (s ? s[0] : T * H * D) : 0;
         if (p == nullptr) {
             fail(GSPN_ERR_NULL);
             return h;

@@ -89,3 +89,24 @@ def test_norm(kind, dtype, pairs):
         return [*gspn.qk_norm_rotate_fwd(q, k, *w, **kw), *gspn.qk_norm_rotate_bwd(q, k, *w, dyq, dyk, **kw)]
 
     same(both(*x), both(*[t.contiguous() for t in x]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_token_of_heads_outside_tokens(dtype):
+    """One token out of buffers [B, H, T, D], whose heads are a million entries apart."""
+    torch = require_gpu()
+    H, D, tokens = 12, 128, 8192
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x = [(0.1 * torch.randn(1, H, tokens, D, device="cuda", generator=gen)).to(dt)[:, :, 70:71].transpose(1, 2) for _ in range(4)]
+    gates = [(f * torch.rand(1, 1, H, device="cuda", generator=gen)).to(dt) for f in (-0.2, 1.0)]
+    cache = [(torch.randn(1, 300, H, D, device="cuda", generator=gen)).to(dt) for _ in range(2)]
+
+    def all_of(q, k, v, do):
+        o, lse = gspn.window_attn_fwd(q, k, v)
+        r, end, reserve = gspn.delta_rule_fwd_train(q, k, v, *gates)
+        return [*gspn.qk_norm_rotate_fwd(q, k), *gspn.qk_norm_rotate_bwd(q, k, None, None, do, v)[:2],
+                o, lse, *gspn.window_attn_bwd(q, k, v, o, lse, do), gspn.window_attn_decode(q, *cache), r, end,
+                *gspn.delta_rule_bwd_reserve(q, k, v, *gates, do, reserve)[:5], *gspn.delta_rule_fwd(q, k, v, *gates, state=end)]
+
+    same(all_of(*x), all_of(*[t.contiguous() for t in x]))
