@@ -393,8 +393,8 @@ int gspn_latent_params(const void *xc, const void *l_u, const void *l_lam,
  * strides that are multiples of 16 bytes, token strides up to 2^23, and D a
  * multiple of 8 (GSPN_ERR_ALIGN, GSPN_ERR_UNSUPPORTED).  int32 and fp32 arrays (lens, lse,
  * positions) are contiguous and need their own alignment only.  Outputs may be
- * slices of one buffer's tokens (dq, dk and dv of one fused gradient); they
- * must not overlap anything otherwise (GSPN_ERR_ALIAS).  Arithmetic is fp32;
+ * slices of one buffer (dq, dk and dv of one fused gradient), by tokens, by heads
+ * or within heads; they must not overlap anything otherwise (GSPN_ERR_ALIAS).  Arithmetic is fp32;
  * with bf16 storage the operands of matrix products are bf16 (softmax weights
  * and their gradients are rounded to nearest even for the products that take
  * them, to twice the bits in gradients of short sequences and narrow windows;

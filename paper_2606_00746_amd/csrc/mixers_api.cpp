@@ -20,30 +20,68 @@ namespace {
 
 int64_t storage(int dtype) { return dtype == GSPN_F32 ? 4 : 2; }
 
-// A buffer of a call as its checks see it: `rows` tokens of `inner` bytes,
-// `step` bytes apart and `outer` further for every batch entry, over `bytes` in all.
+// A buffer of a call as its checks see it: pieces of `inner` bytes, repeated in
+// up to three dimensions, over `bytes` in all.
 struct Span {
+    struct Dim {
+        int64_t step, n;
+    };
     uintptr_t p = 0;
-    int64_t bytes = 0, inner = 0, step = 0, outer = 0;
+    int64_t bytes = 0, inner = 0;
+    Dim dim[3] = {{0, 1}, {0, 1}, {0, 1}};
     bool output = false;
+
+    // What the dimensions that step by less than s cover, where the others step by
+    // multiples of s and it fits between them; else more than s.
+    int64_t below(int64_t s) const
+    {
+        int64_t ext = inner;
+        for (const Dim &d : dim) {
+            if (d.n <= 1)
+                continue;
+            if (d.step < s)
+                ext += (d.n - 1) * d.step;
+            else if (d.step % s != 0)
+                return s + 1;
+        }
+        return ext;
+    }
+    bool same(const Span &o) const
+    {
+        bool is = p == o.p && bytes == o.bytes && inner == o.inner;
+        for (int i = 0; i < 3; ++i)
+            is = is && dim[i].n == o.dim[i].n && (dim[i].n <= 1 || dim[i].step == o.dim[i].step);
+        return is;
+    }
 };
 
 // A contiguous buffer (aligned to its elements).
 Span flat(const void *p, int64_t bytes, bool output = false)
 {
-    return Span{reinterpret_cast<uintptr_t>(p), bytes, bytes, 0, 0, output};
+    Span x;
+    x.p = reinterpret_cast<uintptr_t>(p);
+    x.bytes = x.inner = bytes;
+    x.output = output;
+    return x;
 }
 
-// Two buffers have no byte in common: their ranges are apart, or they are
-// slices of one buffer's tokens (equal steps, and apart within a step).
+// Two buffers have no byte in common: their ranges are apart, or they are slices
+// of one buffer's tokens, heads or batch entries: some step of theirs repeats both,
+// and what lies within one repetition is apart.
 bool apart(const Span &a, const Span &b)
 {
     if (a.p + (uintptr_t)a.bytes <= b.p || b.p + (uintptr_t)b.bytes <= a.p)
         return true;
-    if (a.step <= 0 || a.step != b.step || a.outer % a.step != 0 || b.outer % b.step != 0)
-        return false;
-    const int64_t d = (int64_t)(b.p - a.p) % a.step, r = d < 0 ? d + a.step : d;
-    return r >= a.inner && r + b.inner <= a.step;
+    for (const Span *x : {&a, &b})
+        for (const Span::Dim &d : x->dim) {
+            const int64_t s = d.step;
+            if (d.n <= 1 || s <= 0)
+                continue;
+            const int64_t ea = a.below(s), eb = b.below(s), off = (int64_t)(b.p - a.p) % s, r = off < 0 ? off + s : off;
+            if (ea <= s && eb <= s && r >= ea && r + eb <= s)
+                return true;
+        }
+    return false;
 }
 
 // The checks of a call's buffers, one after the other.
@@ -101,12 +139,10 @@ struct Buffers {
             return h;
         }
         if (output) {   // no element of an output is written twice
-            struct Dim {
-                int64_t step, n;
-            } dim[3] = {{h.sh, H}, {h.st, T}, {h.sb, B}};
-            std::sort(dim, dim + 3, [](const Dim &x, const Dim &y) { return x.step < y.step; });
+            Span::Dim dim[3] = {{h.sh, H}, {h.st, T}, {h.sb, B}};
+            std::sort(dim, dim + 3, [](const Span::Dim &x, const Span::Dim &y) { return x.step < y.step; });
             int64_t ext = D;
-            for (const Dim &d : dim) {
+            for (const Span::Dim &d : dim) {
                 if (d.n > 1 && d.step < ext)
                     fail(GSPN_ERR_ALIAS);
                 ext += (d.n - 1) * d.step;
@@ -114,13 +150,11 @@ struct Buffers {
         }
         Span x;
         x.p = reinterpret_cast<uintptr_t>(p);
-        x.inner = ((H - 1) * h.sh + D) * es;
-        x.bytes = x.inner + ((T - 1) * h.st + (B - 1) * h.sb) * es;
-        x.step = (T > 1 ? h.st : B > 1 ? h.sb : 0) * es;
-        x.outer = T > 1 && B > 1 ? h.sb * es : 0;
+        x.inner = D * es;
+        x.bytes = x.inner + ((H - 1) * h.sh + (T - 1) * h.st + (B - 1) * h.sb) * es;
+        x.dim[0] = {h.sh * es, H}, x.dim[1] = {h.st * es, T}, x.dim[2] = {h.sb * es, B};
         x.output = output;
-        if (inplace >= 0 && inplace < n && status == GSPN_OK && all[inplace].p == x.p && all[inplace].bytes == x.bytes &&
-            all[inplace].inner == x.inner && all[inplace].step == x.step && all[inplace].outer == x.outer) {
+        if (inplace >= 0 && inplace < n && status == GSPN_OK && all[inplace].same(x)) {
             for (int i = 0; i < n; ++i)
                 if (i != inplace && !apart(all[i], x))
                     fail(GSPN_ERR_ALIAS);

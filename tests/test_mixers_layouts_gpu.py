@@ -110,3 +110,39 @@ def test_one_token_of_heads_outside_tokens(dtype):
                 *gspn.delta_rule_bwd_reserve(q, k, v, *gates, do, reserve)[:5], *gspn.delta_rule_fwd(q, k, v, *gates, state=end)]
 
     same(all_of(*x), all_of(*[t.contiguous() for t in x]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads_first", [False, True])
+def test_fused_buffers_by_heads(heads_first, dtype):
+    """q, k and v beside each other in every head [B][T][H][3][D], and as heads ahead of
+    tokens [B][3 H][T][D]: gradients go into a buffer of that layout, the norm runs in place."""
+    torch = require_gpu()
+    B, T, H, D = 2, 150, 3, 64
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+
+    def rand(*shape):
+        return (0.1 * torch.randn(*shape, device="cuda", generator=gen)).to(dt)
+
+    def slices(f):
+        if heads_first:
+            return [f[:, i * H:(i + 1) * H].transpose(1, 2) for i in range(3)]
+        return [f[:, :, :, i] for i in range(3)]
+
+    fused = rand(B, 3 * H, T, D) if heads_first else rand(B, T, H, 3, D)
+    own = [t.contiguous() for t in slices(fused)]
+    do, gates = rand(B, T, H, D), [(f * torch.rand(B, T, H, device="cuda", generator=gen)).to(dt) for f in (-0.2, 1.0)]
+    o, lse = gspn.window_attn_fwd(*own, left=40, right=8, sinks=2)
+    _, _, reserve = gspn.delta_rule_fwd_train(*own, *gates)
+    want = [gspn.window_attn_bwd(*own, o, lse, do, left=40, right=8, sinks=2),
+            gspn.delta_rule_bwd_reserve(*own, *gates, do, reserve)[:5], gspn.qk_norm_rotate_fwd(*own[:2])]
+    grads = torch.full_like(fused, float("nan"))
+    gspn.window_attn_bwd(*slices(fused), o, lse, do, left=40, right=8, sinks=2, out=slices(grads))
+    same(want[0], slices(grads))
+    dg = [torch.empty_like(g) for g in gates]
+    gspn.delta_rule_bwd_reserve(*slices(fused), *gates, do, reserve, out=(*slices(grads), *dg, None))
+    same(want[1], [*slices(grads), *dg])
+    q, k, v = slices(fused)
+    gspn.qk_norm_rotate_fwd(q, k, out=(q, k))
+    same([*want[2], own[2]], slices(fused))
