@@ -48,6 +48,26 @@ bool attn_split_preferred(const AttnProblem &p);
 
 constexpr int kAttnMaxHead = 128;
 
+// Tiles of 128 rows up to which pairs of waves share 32 rows: twice as many workgroups
+// then, of half the rows.  Forward (us, with and without: 42 tiles 8.8 and 13.1, 224
+// 14.3 and 17.9, 512 20.2 and 22.6, 768 30.4 and 28.3); gradients (both kernels: 42 tiles
+// of heads of 72 21 and 29, 128 of 64 51 and 56, 160 49 and 50, of 128 94 and 80, 512 of
+// 64 71 and 56).
+constexpr int64_t kAttnFwdPairs = 512, kAttnBwdPairs = 128;
+inline int64_t attn_tiles(const AttnProblem &p, int64_t H, int64_t T) { return p.B * H * ((T + 127) / 128); }
+inline bool attn_fwd_pairs(const AttnProblem &p) { return attn_tiles(p, p.Hq, p.Tq) <= kAttnFwdPairs; }
+inline bool attn_dq_pairs(const AttnProblem &p) { return attn_tiles(p, p.Hq, p.Tq) <= kAttnBwdPairs; }
+inline bool attn_dkv_pairs(const AttnProblem &p) { return attn_tiles(p, p.Hkv, p.Tk) <= kAttnBwdPairs; }
+
+// Gradients of bf16 rows with few keys, which take longer sums (attn_bwd.hpp): the
+// sequences' buffer is short, or the window narrow.  What that costs, both kernels: 16 x 16
+// heads of 64, causal, 512 tokens 170 us, 516 tokens (without) 110; heads of 128 381 and
+// 203; 8 x 4096 tokens, 12 heads, a window of 33 253 us, of 34 184.
+inline bool attn_few_keys(const AttnProblem &p)
+{
+    return p.Tk <= 512 || (p.left >= 0 && p.right >= 0 && (int64_t)p.left + p.right <= 32);
+}
+
 #ifdef __HIPCC__
 
 namespace attn {

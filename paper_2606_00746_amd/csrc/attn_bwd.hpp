@@ -549,15 +549,6 @@ __global__ __launch_bounds__(kThreads) void attn_dkv_sum_kernel(AttnProblem a, K
            sum[2] * f, sum[3] * f);
 }
 
-// Rows with few keys: the sequence is short, or the window narrow.  What the longer
-// sums cost there, both kernels: 16 x 16 heads of 64, causal, 512 tokens 170 us, 516
-// tokens (without) 110; heads of 128 381 and 203; 8 x 4096 tokens, 12 heads, a window
-// of 33 253 us, of 34 184.
-bool attn_few_keys(const AttnProblem &p)
-{
-    return p.Tk <= 512 || (p.left >= 0 && p.right >= 0 && (int64_t)p.left + p.right <= 32);
-}
-
 // Workgroups wanted at least, and query tiles that a part has at least: shares of fewer
 // cost more than they save (us of both kernels, 4 tiles and 2: 2 x 777 tokens, 6 heads of
 // 72, a window of 161, bf16 24 and 41, fp32 74 and 90; 1024 tokens, causal, the same).
@@ -638,11 +629,6 @@ hipError_t run_dq(const AttnProblem &p, float *delta, hipStream_t s)
     return hipGetLastError();
 }
 
-// Tiles of 128 rows up to which pairs of waves share 32 of them, so that there are
-// twice as many workgroups (us of both kernels, with and without: 42 tiles of heads of
-// 72 21 and 29, 128 of 64 51 and 56, 160 49 and 50, of 128 94 and 80, 512 of 64 71 and 56).
-constexpr int64_t kPairs = 128;
-
 template <typename T, int DP>
 hipError_t run(const AttnProblem &p, hipStream_t s)
 {
@@ -651,17 +637,16 @@ hipError_t run(const AttnProblem &p, hipStream_t s)
     if (e != hipSuccess)
         return e;
     float *d = static_cast<float *>(delta);
-    const auto tiles = [&](int H, int T_) { return (int64_t)p.B * H * ((T_ + 127) / 128); };
     if constexpr (sizeof(T) == 2) {
         if (attn_few_keys(p)) {
             e = run_dq<T, DP, 2, true>(p, d, s);
             return e == hipSuccess ? run_dkv<T, DP, 2, true>(p, d, s) : e;
         }
     }
-    e = tiles(p.Hq, p.Tq) <= kPairs ? run_dq<T, DP, 2, false>(p, d, s) : run_dq<T, DP, 1, false>(p, d, s);
+    e = attn_dq_pairs(p) ? run_dq<T, DP, 2, false>(p, d, s) : run_dq<T, DP, 1, false>(p, d, s);
     if (e != hipSuccess)
         return e;
-    return tiles(p.Hkv, p.Tk) <= kPairs ? run_dkv<T, DP, 2, false>(p, d, s) : run_dkv<T, DP, 1, false>(p, d, s);
+    return attn_dkv_pairs(p) ? run_dkv<T, DP, 2, false>(p, d, s) : run_dkv<T, DP, 1, false>(p, d, s);
 }
 
 template <typename T>

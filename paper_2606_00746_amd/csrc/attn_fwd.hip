@@ -254,15 +254,10 @@ hipError_t run(const AttnProblem &p, hipStream_t s)
     return hipGetLastError();
 }
 
-// Tiles of 128 queries up to which pairs of waves share 32 queries: twice as many
-// workgroups then, of half the rows (us, with and without: 42 tiles 8.8 and 13.1, 224
-// 14.3 and 17.9, 512 20.2 and 22.6, 768 30.4 and 28.3).
-constexpr int64_t kPairs = 512;
-
 template <typename T, int DP>
 hipError_t pick(const AttnProblem &p, hipStream_t s)
 {
-    return (int64_t)p.B * p.Hq * ((p.Tq + 127) / 128) <= kPairs ? run<T, DP, 2>(p, s) : run<T, DP, 1>(p, s);
+    return attn_fwd_pairs(p) ? run<T, DP, 2>(p, s) : run<T, DP, 1>(p, s);
 }
 
 template <typename T>

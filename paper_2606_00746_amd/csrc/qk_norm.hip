@@ -390,11 +390,6 @@ int group_lanes(const NormProblem &p)
 // leaves the card with fewer than kFewThreads threads (us, one and four: 4096 tokens of
 // 2 x 12 heads of 64 7.1 and 7.6, 8192 12.7 and 11.4, 65536 90 and 86; 8 tokens 3.5 and 5.5).
 constexpr int64_t kFewThreads = 256 * 1024;
-int heads_each(const NormProblem &p)
-{
-    const int64_t n = (int64_t)p.B * p.T * ((p.Hq + 3) / 4 + (p.Hk + 3) / 4) * group_lanes(p);
-    return n < kFewThreads ? 1 : 4;
-}
 
 template <typename T, int P, int HL>
 hipError_t fwd(const NormProblem &p, hipStream_t s)
@@ -448,7 +443,7 @@ hipError_t pick(const NormProblem &p, hipStream_t s)
     if constexpr (BWD)
         return bwd<T, P>(p, s);
     else
-        return heads_each(p) == 1 ? fwd<T, P, 1>(p, s) : fwd<T, P, 4>(p, s);
+        return norm_heads_each(p) == 1 ? fwd<T, P, 1>(p, s) : fwd<T, P, 4>(p, s);
 }
 
 template <typename T, bool BWD>
@@ -463,6 +458,12 @@ hipError_t pick(const NormProblem &p, hipStream_t s)
 }
 
 }  // namespace
+
+int norm_heads_each(const NormProblem &p)
+{
+    const int64_t n = (int64_t)p.B * p.T * ((p.Hq + 3) / 4 + (p.Hk + 3) / 4) * group_lanes(p);
+    return n < kFewThreads ? 1 : 4;
+}
 
 hipError_t launch_norm_rotate_fwd(const NormProblem &p, hipStream_t s)
 {

@@ -22,6 +22,8 @@ struct NormProblem {
 
 constexpr int kNormMaxHead = 256;
 
+// Heads of a token that a group of lanes of the forward takes: 1 or 4.
+int norm_heads_each(const NormProblem &p);
 hipError_t launch_norm_rotate_fwd(const NormProblem &p, hipStream_t s);
 hipError_t launch_norm_rotate_bwd(const NormProblem &p, hipStream_t s);
 
