@@ -397,8 +397,9 @@ int gspn_latent_params(const void *xc, const void *l_u, const void *l_lam,
  * or within heads; they must not overlap anything otherwise (GSPN_ERR_ALIAS).  Arithmetic is fp32;
  * with bf16 storage the operands of matrix products are bf16 (softmax weights
  * and their gradients are rounded to nearest even for the products that take
- * them, to twice the bits in gradients of short sequences and narrow windows;
- * their sums are not).  The rest is as for the scan: asynchronous on
+ * them, to twice the bits in decoding, in forwards that split their keys (few
+ * rows of many keys), and in gradients with Tk up to 512 or a window of at most
+ * 33 keys; their sums are not).  The rest is as for the scan: asynchronous on
  * `stream`, no allocation, results that repeat bit for bit.
  *
  * Norm of query and key heads with the position rotation:

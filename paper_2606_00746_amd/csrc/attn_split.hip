@@ -55,6 +55,8 @@ __device__ __forceinline__ f32x4_t mma16(Frag<float> a, Frag<float> b, f32x4_t a
 }
 
 // acc[db] += V^T P over the wave's block of 32 keys; p[t]: keys 16 t + 4 u + 0..3.
+// bf16: P as a sum of two bf16 terms, 16 bits, so that what is left of an output's error
+// is its own rounding: memory bounds this kernel, and the second product is free.
 template <int DP>
 __device__ __forceinline__ void mma16_turned(const char *lds, const f32x4_t (&p)[2],
                                              f32x4_t (&acc)[DP / 16], const bf16_t *)
@@ -63,15 +65,18 @@ __device__ __forceinline__ void mma16_turned(const char *lds, const f32x4_t (&p)
     const int l = threadIdx.x % 64, u = l / 16, i = l % 16, r = 4 * u + (i >> 2);
     const uint4 w = make_uint4(pack2(p[0][0], p[0][1]), pack2(p[0][2], p[0][3]),
                                pack2(p[1][0], p[1][1]), pack2(p[1][2], p[1][3]));
-    const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, w);
+    const uint4 x = make_uint4(pack2(p[0][0] - bf_lo(w.x), p[0][1] - bf_hi(w.x)), pack2(p[0][2] - bf_lo(w.y), p[0][3] - bf_hi(w.y)),
+                               pack2(p[1][0] - bf_lo(w.z), p[1][1] - bf_hi(w.z)), pack2(p[1][2] - bf_lo(w.w), p[1][3] - bf_hi(w.w)));
+    const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, w), rest = __builtin_bit_cast(bf16x8_t, x);
 #pragma unroll
     for (int db = 0; db < DP / 16; ++db) {
         const int c = 2 * db + ((i & 3) >> 1), in = 8 * (i & 1);
         struct {
             s16x4_t a, b;
         } both = {read_turned(lds + X::at(r, c) + in), read_turned(lds + X::at(16 + r, c) + in)};
-        acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, both), pb,
-                                                          acc[db], 0, 0, 0);
+        const bf16x8_t v = __builtin_bit_cast(bf16x8_t, both);
+        acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, rest, acc[db], 0, 0, 0);
+        acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pb, acc[db], 0, 0, 0);
     }
 }
 template <int DP>
