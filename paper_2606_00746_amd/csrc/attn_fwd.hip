@@ -78,7 +78,7 @@ void attn_fwd_kernel(AttnProblem a)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
             acc[db][r] = 0.f;
-    const float s2 = a.scale * kLog2e, slack = kSlack / s2;
+    const float s2 = a.scale * kLog2e, slack = fminf(kSlack / s2, 3e38f);   // (finite: below, m may be -infinity)
 
     X kt, vt;
     Flow<DP> kw, vw;

@@ -33,3 +33,20 @@ def test_nan_rows(B, Tq, Tk, Hq, Hkv, D, left, dtype):
     see = (p >= j) & ((p - j <= left) | (left < 0))
     G = Hq // Hkv
     assert torch.isnan(o2[0, see, :G]).all() and torch.isnan(lse2[0, :G, see]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [1e-38, 3e-38, 1e-30])
+def test_scales_next_to_nothing(scale, dtype):
+    """Scores of all but 0: lse is the log of the number of keys seen (to the rounding of
+    fp32: 2^-22 of logs below 8), o their values' mean."""
+    torch = require_gpu()
+    q, k, v, do = (dev(a, dtype) for a in make(1, 600, 600, 4, 4, 64, dtype, seed=1))
+    o, lse = gspn.window_attn_fwd(q, k, v, left=-1, right=0, scale=scale)
+    want = torch.arange(1, 601, device="cuda").double().log().float()
+    assert ((lse - want).abs() <= 2.0 ** -22 * 8).all()
+    mean = v.double().cumsum(1) / torch.arange(1, 601, device="cuda").view(1, -1, 1, 1)
+    # a weight and the result are rounded once each (bf16: 2^-8), and summed in fp32
+    u = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -23 * 600
+    bound = u * (v.double().abs().cumsum(1) / torch.arange(1, 601, device="cuda").view(1, -1, 1, 1) + mean.abs()) + 1e-6
+    assert ((o.double() - mean).abs() <= bound).all()
