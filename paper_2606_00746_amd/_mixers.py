@@ -57,6 +57,16 @@ def _on(call, args):
         return call(**args)
 
 
+_MOST = 1 << 30
+
+
+def _ints(**args):
+    """Numbers that the library takes in 32 bits (ctypes would cut them off)."""
+    for name, x in args.items():
+        if not -_MOST <= x <= _MOST:
+            raise ValueError(f"{name} must be between -2**30 and 2**30, not {x}")
+
+
 _Strides = {n: ctypes.c_int64 * (3 * n) for n in (4, 6, 7, 8)}
 
 
@@ -111,8 +121,10 @@ def _sized(name, args, device):
 # norm of query and key heads, with the position rotation
 # ---------------------------------------------------------------------------
 
-def _norm_sizes(q, k, wq, wk, cos, sin, positions, pairs):
+def _norm_sizes(q, k, wq, wk, cos, sin, positions, pairs, first):
     import torch
+    if not 0 <= first <= _MOST:
+        _ints(first=first)
     if pairs not in PAIRS:
         raise ValueError(f"pairs must be one of {list(PAIRS)}")
     B, T, Hq, D = q.shape
@@ -143,7 +155,7 @@ def qk_norm_rotate_fwd(q, k, wq=None, wk=None, cos=None, sin=None, eps: float = 
     if stream is not None:
         return _on(qk_norm_rotate_fwd, locals())
     import torch
-    B, T, Hq, Hk, D, R, rows, ptrs = _norm_sizes(q, k, wq, wk, cos, sin, positions, pairs)
+    B, T, Hq, Hk, D, R, rows, ptrs = _norm_sizes(q, k, wq, wk, cos, sin, positions, pairs, first)
     if out is None:
         out = q.new_empty((B, T, Hq, D)), q.new_empty((B, T, Hk, D))
     yq, yk = out
@@ -164,7 +176,7 @@ def qk_norm_rotate_bwd(q, k, wq, wk, dyq, dyk, cos=None, sin=None, eps: float = 
     if stream is not None:
         return _on(qk_norm_rotate_bwd, locals())
     import torch
-    B, T, Hq, Hk, D, R, rows, ptrs = _norm_sizes(q, k, wq, wk, cos, sin, positions, pairs)
+    B, T, Hq, Hk, D, R, rows, ptrs = _norm_sizes(q, k, wq, wk, cos, sin, positions, pairs, first)
     if out is None:
         kw = dict(dtype=q.dtype, device=q.device)
         out = (torch.empty((B, T, Hq, D), **kw), torch.empty((B, T, Hk, D), **kw),
@@ -189,8 +201,10 @@ def qk_norm_rotate_bwd(q, k, wq, wk, dyq, dyk, cos=None, sin=None, eps: float = 
 # attention with a sliding window and sinks
 # ---------------------------------------------------------------------------
 
-def _attn_sizes(q, k, v, lens):
+def _attn_sizes(q, k, v, lens, left, right, sinks, offset):
     import torch
+    if not (-_MOST <= left <= _MOST and -_MOST <= right <= _MOST and -_MOST <= sinks <= _MOST and -_MOST <= offset <= _MOST):
+        _ints(left=left, right=right, sinks=sinks, offset=offset)
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q, k and v must be [B, T, H, D]")
     B, Tq, Hq, D = q.shape
@@ -214,7 +228,7 @@ def window_attn_fwd(q, k, v, left: int = -1, right: int = -1, sinks: int = 0, le
     if stream is not None:
         return _on(window_attn_fwd, locals())
     import torch
-    B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens)
+    B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens, left, right, sinks, offset)
     if o is None:
         o = q.new_empty((B, Tq, Hq, D))
     if lse is None:
@@ -240,7 +254,7 @@ def window_attn_bwd(q, k, v, o, lse, do, left: int = -1, right: int = -1, sinks:
     if stream is not None:
         return _on(window_attn_bwd, locals())
     import torch
-    B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens)
+    B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens, left, right, sinks, offset)
     if out is None:
         kw = dict(dtype=q.dtype, device=q.device)
         out = (torch.empty((B, Tq, Hq, D), **kw), torch.empty((B, Tk, Hkv, D), **kw),
@@ -270,7 +284,7 @@ def window_attn_decode(q, k, v, lens=None, left: int = -1, sinks: int = 0, scale
     if stream is not None:
         return _on(window_attn_decode, locals())
     import torch
-    B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens)
+    B, Tq, Tk, Hq, Hkv, D, lens_p = _attn_sizes(q, k, v, lens, left, 0, sinks, 0)
     if o is None:
         o = q.new_empty((B, Tq, Hq, D))
     _heads(q, (q, (B, Tq, Hq, D), "q"), (k, (B, Tk, Hkv, D), "k"), (v, (B, Tk, Hkv, D), "v"),
