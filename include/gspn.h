@@ -391,10 +391,12 @@ int gspn_latent_params(const void *xc, const void *l_u, const void *l_lam,
  * fused projection or of a cache.  Strides of dimensions of size 1 are not
  * read.  Heads tensors have one storage type (fp32 or bf16), base pointers and
  * strides that are multiples of 16 bytes, token strides up to 2^23, and D a
- * multiple of 8 (GSPN_ERR_ALIGN, GSPN_ERR_UNSUPPORTED).  int32 and fp32 arrays (lens, lse,
- * positions) are contiguous and need their own alignment only.  Outputs may be
- * slices of one buffer (dq, dk and dv of one fused gradient), by tokens, by heads
- * or within heads; they must not overlap anything otherwise (GSPN_ERR_ALIAS).  Arithmetic is fp32;
+ * multiple of 8 (GSPN_ERR_ALIGN, GSPN_ERR_UNSUPPORTED).  Everything else is
+ * contiguous: weights, tables, states, workspaces and reserves 16-byte aligned;
+ * lens, lse, positions, gates and their gradients to their elements.  Inputs may
+ * share memory (strides of 0, windows that overlap).  Outputs may be slices of one
+ * buffer (dq, dk and dv of one fused gradient), by tokens, by heads or within heads;
+ * they must not overlap anything otherwise (GSPN_ERR_ALIAS).  Arithmetic is fp32;
  * with bf16 storage the operands of matrix products are bf16 (softmax weights
  * and their gradients are rounded to nearest even for the products that take
  * them, to twice the bits in decoding, in forwards that split their keys (few
@@ -442,14 +444,18 @@ int gspn_qk_norm_rotate_bwd(const void *q, const void *k, const void *wq, const 
  *   o = sum_j softmax_j(scale q k_j) v_j,  lse = log sum_j exp(scale q k_j)
  * A query that sees no key has o = 0, lse = -infinity and no part in any
  * gradient.  Keys, values and queries at and past len may hold anything, NaN
- * included; those before it must be finite.
+ * included; those before it must be finite (a NaN there is not hidden: rows that it
+ * counts in have o and lse of NaN).
  * q, o [B][Tq][Hq][D]; k, v [B][Tk][Hkv][D], Hq a multiple of Hkv: query head h
  * reads key head h / (Hq / Hkv); D up to 128; lse fp32 [B][Hq][Tq] (NULL: not
  * wanted, forward only); scale > 0.
  * gspn_window_attn_bwd takes the forward's inputs, o and lse, and the gradient
  * dout of o.  gspn_window_attn_decode is the form for the last Tq tokens of
  * each sequence over a cache of Tk: p = len - Tq + t, causal, no lse; its time
- * goes by the keys seen.  A cache that holds only the sinks and the window (in
+ * goes by the keys seen, once for every 16 rows (queries times the heads that share
+ * a key head).  It is meant for few of them: whole prompts of some hundred tokens
+ * (of 64 for 8 sequences at 16 heads on 4) are faster as gspn_window_attn_fwd with an
+ * offset, where the sequences have one length.  A cache that holds only the sinks and the window (in
  * any order) is read with left = -1, all its tokens being visible.
  * strides: forward and decode q, k, v, o; backward q, k, v, o, dout, dq, dk, dv.
  * gspn_window_attn_workspace_size: op one of GSPN_ATTN_*; right and offset are
@@ -484,14 +490,15 @@ int gspn_window_attn_decode(const void *q, const void *k, const void *v, const i
  *   o_t = scale S_t^T q_t
  * q, k [B][T][Hq][Dk]; v, o [B][T][Hv][Dv], Hv a multiple of Hq: value head h
  * reads query and key head h / (Hv / Hq); g, beta [B][T][Hv], contiguous, in the
- * storage type, finite, g <= 0 (values below -100 count as -100, where exp(g)
- * is 0 to fp32) and keys of a length of about 1 (|I - beta k k^T| <= 1, or the
+ * storage type, finite (a NaN stays one, in all that follows), g <= 0 (values below
+ * -100 count as -100, where exp(g) is 0 to fp32) and keys of a length of about 1 (|I - beta k k^T| <= 1, or the
  * recurrence itself grows).  state, state_out: fp32 [B][Hv][Dk][Dv], the state
  * ahead of the first token (NULL: zeros) and behind the last (NULL: not wanted);
  * they may be the same buffer.  Dk and Dv up to 128.  lens as for the
  * attention: tokens at and past it write nothing, leave the state as it is, may
- * hold anything, and have o = 0 and gradients 0.  States and what they are
- * formed from are fp32 for either storage type.
+ * hold anything, and have o = 0 and gradients 0.  States are carried in fp32 for
+ * either storage type; with bf16 storage the outputs and gradients of a chunk take
+ * them, and what the recurrence writes into them, with 16 bits.
  * Up to 8 tokens run the recurrence itself, more run in chunks of 64 (results
  * agree within the rounding of fp32).
  * Training: gspn_delta_rule_fwd_train also fills a caller buffer, the reserve

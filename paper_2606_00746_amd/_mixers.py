@@ -280,7 +280,10 @@ def window_attn_decode(q, k, v, lens=None, left: int = -1, sinks: int = 0, scale
     """o for the last Tq tokens of each sequence, q [B, Tq, Hq, D], over a cache
     k, v [B, Tk, Hkv, D] of which lens[b] tokens (None: all) are there, the
     queries' own among them: query t stands at position lens[b] - Tq + t and
-    sees the `left` keys before it (-1: all), itself and the first `sinks`."""
+    sees the `left` keys before it (-1: all), itself and the first `sinks`.  For
+    few tokens: every 16 rows (queries times heads that share a key head) read
+    the keys again, and prompts of some hundred tokens are faster in
+    window_attn_fwd with an offset, where sequences have one length."""
     if stream is not None:
         return _on(window_attn_decode, locals())
     import torch

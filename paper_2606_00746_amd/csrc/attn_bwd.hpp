@@ -17,10 +17,11 @@
 // queries split over several workgroups, whose fp32 shares are added up, in
 // order, by attn_dkv_sum_kernel.
 //
-// Bound, as the forward, by the matrix instructions and their power: 8 x 4100 tokens of
-// 12 heads of 64, bf16, a window of 448 to either side: 212 us for dq (607 TFLOP/s of its
-// three products) and 312 for dk and dv (550 of its four); heads of 128, 2 x 8192 tokens
-// of 16 heads on 4, a causal window of 1023: 273 and 384.
+// 8 x 4100 tokens of 12 heads of 64, bf16, a window of 448 to either side: 211 us for dq
+// (609 TFLOP/s of its three products) and 311 for dk and dv (551 of its four); heads of
+// 128, 2 x 8192 tokens of 16 heads on 4, a causal window of 1023: 273 and 391.  As in the
+// forward the matrix cores are busy 27 to 32% of the cycles, at 2.1 GHz of 2.4; a wave waits
+// 30 to 40% of its time, for LDS and the other waves, and 20 to 30% for its turn to issue.
 //
 // bf16: p and ds are rounded to 8 significant bits for their products, and d_i comes
 // from the rounded o_i.  The first costs an error of the size of the results' own

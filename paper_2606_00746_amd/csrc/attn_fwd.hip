@@ -6,19 +6,24 @@
 // One pass over the keys with a running maximum and sum.  A workgroup owns 128
 // queries of one head, a wave 32 of them; tiles of 64 keys and values are staged
 // in LDS for all four waves, double buffered: the next tile is on its way while one
-// is multiplied, bf16 straight into LDS (through registers: 1.40M cycles at the size
-// below, this way 0.98M), fp32 through registers, whose order in LDS differs.  The
-// tiles are those of the sinks, then those of the window; a wave passes over
-// tiles that none of its queries sees and masks only those that not all see.
+// is multiplied, bf16 straight into LDS (0.7 of the cycles that it takes through
+// registers), fp32 through registers, whose order in LDS differs.  The tiles are those
+// of the sinks, then those of the window; a wave passes over tiles that none of its
+// queries sees and masks only those that not all see.
 // S^T = K Q^T is formed, so that a query's scores are one lane's (and its
 // neighbour's, 32 lanes on) and their exponentials, as they stand in registers, are
 // an operand of O^T += V^T P^T.
 //
-// The bound is the matrix instructions, and the power they draw: 34229 tokens, 18
-// heads of 64, bf16, a window of 1110 to either side and 4 sinks, in 560 us = 630
-// TFLOP/s, at a clock that falls from 2.4 to about 1.7 GHz while it lasts (a large
-// matrix product reaches 1250 on the same card).  64 queries a wave take the LDS
-// reads that a product needs to half, but leave one wave a SIMD: slower.
+// 34229 tokens, 18 heads of 64, bf16, a window of 1110 to either side and 4 sinks, take
+// 467 to 485 us = 710 to 740 TFLOP/s (a large matrix product reaches 1250 on the same
+// card).  The matrix cores are busy a third of the cycles, vector instructions
+// (exponentials, maxima, sums, roundings) a quarter; a wave waits another third, for LDS
+// and the other waves; and the clock is 2.0 GHz of 2.4 while it lasts.  64 queries a wave
+// take the LDS reads that a product needs to half, but leave one wave a SIMD: slower.
+// Softmax weights of 16 bits instead of 8 (a second product with what the rounding
+// leaves) would take the error of o from 2.3e-3 to 1.7e-3, that of its own rounding,
+// and the time from 467 to 625 us: not done here, unlike where memory is the bound
+// (attn_split.hip).
 #include "attn.hpp"
 
 namespace gspn {

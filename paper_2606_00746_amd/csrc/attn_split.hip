@@ -12,8 +12,12 @@
 // joined in LDS, and those of several workgroups by attn_join_kernel, in order.
 //
 // Bound by memory where there is work: one token each of 64 sequences over caches of
-// up to 8192, 16 heads of 128 on 4, bf16, in 166 us, 4.9 TB/s, and 4 for the join; a
-// token of one sequence with a window of 4096 takes 8 us, both launches.
+// up to 8192, 16 heads of 128 on 4, bf16, in 166 to 173 us, 4.8 TB/s, and 5 for the join;
+// for a token of one sequence with a window of 4096 a trace has 10.4 and 3.9 us.
+// Made for few rows: every 16 of them read the keys again.  One sequence of 8192 keys, 16
+// heads of 128 on 4, whole prompts at the end (us, here and by the forward proper): 256
+// tokens 101 and 138, 512 170 and 137, 2048 564 and 174; 8 sequences: 32 tokens 98 and 136,
+// 128 320 and 138, 2048 4098 and 999.
 #include <algorithm>
 
 #include "attn.hpp"
@@ -405,6 +409,9 @@ hipError_t run(const AttnProblem &p, hipStream_t s)
 // (us; here and there): 64 queries of 8 heads of 64, 8192 keys 17 and 97, 512 keys 8.2
 // and 10.2; 512 queries 49 and 97, 1024 queries 84 and 98; 16 x 32 queries, 1024 keys 19
 // and 16; 16 heads of 128 on 4, 256 queries, 8192 keys 94 and 138, 512 queries 162 and 138.
+// fp32 goes by the same figures, though its forward proper takes some 5 times as long a
+// key: between the two lines it is up to 1.3 times slower than it could be (the same heads
+// and keys, 512 queries 757 there, 622 here; 8 sequences of 64 queries 766 and 627).
 bool attn_split_preferred(const AttnProblem &p)
 {
     const double rows = (double)p.B * p.Hq * p.Tq, keys = (double)keys_of(p);

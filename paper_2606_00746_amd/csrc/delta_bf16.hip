@@ -103,7 +103,7 @@ __device__ __forceinline__ constexpr int turned_unit(int tb, int g) { return tb 
 __device__ __forceinline__ int index_of(int tb, int m) { return 32 * (tb / 2) + 8 * (m / 4) + 4 * (tb & 1) + m % 4; }
 
 // Gates, and (I + b M)^-1 by forward substitution, a wave a chunk, a lane a column.
-// 8 x 4096 tokens of 12 heads of 64: 89 us, most of it the substitution's 64 dependent
+// 8 x 4096 tokens of 12 heads of 64: 96 us, most of it the substitution's 64 dependent
 // rows, broadcast from LDS.
 template <int DKP>
 __global__ __launch_bounds__(kThreads) void delta16_inverse_kernel(DeltaProblem p, Kept16 kept, int nc)
@@ -305,8 +305,8 @@ __device__ __forceinline__ int own_block(int w, int j)
 // U and the states of 16 columns, all chunks in turn.  Wave w holds the rows
 // 32 w .. 32 w + 31 of the state, forms their share of K S, and takes the
 // blocks own_block of the tokens through X and U: the three exchanges are the
-// chain's length, its work is shared.  64 chunks of heads of 64 (8 x 12 of them) in 190
-// us, 128 chunks of heads of 128 (2 x 16) in 256: 2 to 3 us a chunk, of which loads that
+// chain's length, its work is shared.  64 chunks of heads of 64 (8 x 12 of them) in 195
+// us, 128 chunks of heads of 128 (2 x 16) in 265: 2 to 3 us a chunk, of which loads that
 // all hit would leave 2; 16 columns a workgroup give the card 384 and 256 of them.
 template <int DKP>
 __global__ __launch_bounds__(DKP * 2) void delta16_state_kernel(DeltaProblem p, Kept16 kept, int nc, int nv)
@@ -466,7 +466,7 @@ __device__ __forceinline__ Terms<N> row_terms(const char *lds, int row, int piec
 }
 
 // O of a chunk, transposed: a lane holds four columns of one token.  8 x 4096 tokens
-// of 12 heads of 64: 122 us, 290 MB moved; forming Q K^T and its decays for a chunk's
+// of 12 heads of 64: 112 us, 341 MB moved; forming Q K^T and its decays for a chunk's
 // four waves bounds it, not memory.
 template <int DKP>
 __global__ __launch_bounds__(kThreads) void delta16_out_kernel(DeltaProblem p, Kept16 kept, int nc, int nv)
@@ -575,7 +575,7 @@ struct Grads16 {
     uint4 *r = nullptr, *ds = nullptr;
 };
 
-// scale A^T dO of a chunk (8 x 4096 tokens of 12 heads of 64: 62 us).
+// scale A^T dO of a chunk (8 x 4096 tokens of 12 heads of 64: 63 us).
 template <int DKP, int DVP>
 __global__ __launch_bounds__(kThreads) void delta16_du_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv)
 {
@@ -656,7 +656,7 @@ __global__ __launch_bounds__(kThreads) void delta16_du_kernel(DeltaProblem p, Ke
 
 // R, dV and the gradients of the states of 16 columns, the chunks from the last
 // on; shared among the waves like delta16_state_kernel (8 x 4096 tokens of 12 heads of
-// 64: 255 us, 4 us a chunk: it has dO's share of the state's gradient beside).
+// 64: 263 us, 4 us a chunk: it has dO's share of the state's gradient beside).
 template <int DKP>
 __global__ __launch_bounds__(DKP * 2) void delta16_dstate_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv)
 {
@@ -871,9 +871,9 @@ __device__ __forceinline__ Terms<kKeep> turned_terms(const char *lds, int blk, i
 
 // dQ, dK, dg and dbeta of a chunk, with the value heads that share its queries
 // and keys in turn.  Wave w holds the rows 64 j + 16 w .. of dQ^T and dK^T.  8 x 4096
-// tokens of 12 heads of 64: 281 us, two workgroups a CU (with dO in registers instead of
-// LDS and the loads where they are used 315); waits 70% of its time, on LDS reads of operands
-// in two terms and the barriers between its phases.
+// tokens of 12 heads of 64: 286 us, two workgroups a CU (with dO in registers instead of
+// LDS and the loads where they are used 12% longer); waits 68% of its time, on LDS reads of
+// operands in two terms and the barriers between its phases.
 template <int DKP, int DVP>
 __global__ __launch_bounds__(kThreads, (DKP + DVP <= 128 ? 2 : 1))
 void delta16_grad_kernel(DeltaProblem p, Kept16 kept, Grads16 gr, int nc, int nv)

@@ -13,9 +13,9 @@
 // owns both runs of its pairs and nothing is exchanged; adjacent pairs lie in
 // one run; other pairings go through LDS.  A group of the forward takes several
 // heads of one token, whose rows are in flight together and share the token's
-// angles (32 x 5476 tokens of 18 + 18 heads of 64, bf16, slices of a fused buffer: 350 to
-// 380 us, 4.3 to 4.6 TB/s, where a large copy reaches 4.9); of the backward one, which
-// leaves registers for more waves (8 x 4096 tokens of 12 + 12 heads of 64: 68 us, 4.5
+// angles (32 x 5476 tokens of 18 + 18 heads of 64, bf16, slices of a fused buffer: 348 to
+// 365 us, 4.4 to 4.6 TB/s, where a large copy reaches 4.9); of the backward one, which
+// leaves registers for more waves (8 x 4096 tokens of 12 + 12 heads of 64: 66 us, 4.6
 // TB/s, and 5 for the weights' shares; two heads at once 80).
 #include <algorithm>
 
