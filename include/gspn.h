@@ -533,6 +533,119 @@ int gspn_delta_rule_bwd_reserve(const void *q, const void *k, const void *v, con
                                 void *reserve, int64_t reserve_bytes, void *workspace,
                                 int64_t workspace_bytes, void *stream);
 
+/*
+ * The state space sublayer: a short causal convolution, the selective state space scan
+ * (the scan's nearest relative over a sequence of tokens, a diagonal recurrence for every
+ * channel), and what joins one sublayer to the next.
+ *
+ * Layouts.  Tensors are [B][T][C] with C contiguous and a multiple of 8, and B and C of the
+ * scan [B][T][G][N] with N contiguous; `strides` holds three int64 a strided tensor, in the
+ * order given (batch, token and head strides in elements; NULL: all contiguous), of which
+ * [B][T][C] tensors leave the third unread.  Optional tensors have their place in it all the
+ * same.  Base pointers and strides are multiples of 16 bytes (of the scan's B and C and their
+ * gradients: of an element), vectors and states 16-byte aligned and contiguous.  Everything
+ * else is as for the token mixers: token strides up to 2^23, inputs that may share memory,
+ * outputs that may be slices of one buffer, fp32 arithmetic, results that repeat bit for bit,
+ * asynchronous on `stream`, no allocation.  lens: int32 [B] (limited to 0..T), or NULL for T;
+ * tokens at and past it may hold anything, leave the states as they are, and have outputs
+ * and gradients 0.
+ *
+ * Short convolution of every channel with its own K taps along the tokens, 2 to 8 of them:
+ *   u_t = bias + sum_j w_j x_{t-K+1+j},  y = u (GSPN_ACT_NONE) or u sigmoid(u) (GSPN_ACT_SILU)
+ * w [C][K], bias [C] or NULL, in the storage type.  state, state_out [B][K-1][C], in the storage
+ * type: the inputs ahead of the first token, oldest first (NULL: zeros), and the last K-1 behind
+ * the last (NULL: not wanted); they may be the same buffer.  One token at a time is the
+ * serving form.  The backward takes the gradients dy of y and dstate_out of state_out (NULL:
+ * zeros) and writes dx, dw, dbias (with a bias) and, unless NULL, dstate, the gradient of state.
+ * strides: forward x, y; backward x, dy, dx.
+ */
+#define GSPN_ACT_NONE 0
+#define GSPN_ACT_SILU 1
+int gspn_short_conv_fwd(const void *x, const void *w, const void *bias, const void *state,
+                        const int32_t *lens, void *y, void *state_out, const int64_t *strides,
+                        int B, int T, int C, int K, int act, int dtype, void *stream);
+int gspn_short_conv_workspace_size(int B, int T, int C, int K, int dtype, int64_t *bytes);
+int gspn_short_conv_bwd(const void *x, const void *w, const void *bias, const void *dy,
+                        const void *dstate_out, const void *state, const int32_t *lens, void *dx,
+                        void *dw, void *dbias, void *dstate, const int64_t *strides, int B, int T,
+                        int C, int K, int act, int dtype, void *workspace, int64_t workspace_bytes,
+                        void *stream);
+
+/*
+ * The selective state space scan: N states for every channel,
+ *   d = softplus(dt + dt_bias)  (or dt + dt_bias where softplus is 0)
+ *   h_t = exp(d A) h_{t-1} + d x_t B_t,  y_t = (C_t . h_t + D x_t) z sigmoid(z)
+ * x, dt, z, y [B][T][C]; Bm, Cm [B][T][G][N]: channel c reads group c / (C / G), C / G a multiple
+ * of 8; N up to 64; A [C][N], D and dt_bias [C] fp32 (D, dt_bias NULL: zeros; z NULL: no gate).
+ * d A <= 0 is what keeps the recurrence bounded and is not checked.  state, state_out: fp32
+ * [B][C][N], ahead of the first token (NULL: zeros) and behind the last (NULL: not wanted); they
+ * may be the same buffer.  Up to 8 tokens run token by token, more in chunks that are joined by
+ * their states (results agree within the rounding of fp32).
+ * Training: gspn_selective_scan_fwd_train also fills a caller buffer, the reserve
+ * (gspn_selective_scan_reserve_size bytes: the states of every eighth token), which
+ * gspn_selective_scan_bwd_reserve reads, with the forward's inputs (the state is in the
+ * reserve).  It writes the gradients of what was given: dx, ddt, dA, dBm, dCm, dD (with D), dz
+ * (with z), ddt_bias (with dt_bias) and, unless NULL, dstate, that of state; dstate_out (NULL:
+ * zeros) is the gradient of state_out.
+ * strides: forward x, dt, Bm, Cm, z, y; backward x, dt, Bm, Cm, z, dy, dx, ddt, dBm, dCm, dz.
+ */
+#define GSPN_SELECTIVE_FWD 0
+#define GSPN_SELECTIVE_FWD_TRAIN 1
+#define GSPN_SELECTIVE_BWD_RESERVE 2
+int gspn_selective_scan_workspace_size(int op, int B, int T, int C, int G, int N, int dtype,
+                                       int64_t *bytes);
+int gspn_selective_scan_reserve_size(int B, int T, int C, int G, int N, int dtype, int64_t *bytes);
+int gspn_selective_scan_fwd(const void *x, const void *dt, const float *A, const void *Bm,
+                            const void *Cm, const float *D, const void *z, const float *dt_bias,
+                            const float *state, const int32_t *lens, void *y, float *state_out,
+                            const int64_t *strides, int B, int T, int C, int G, int N,
+                            int softplus, int dtype, void *workspace, int64_t workspace_bytes,
+                            void *stream);
+int gspn_selective_scan_fwd_train(const void *x, const void *dt, const float *A, const void *Bm,
+                                  const void *Cm, const float *D, const void *z,
+                                  const float *dt_bias, const float *state, const int32_t *lens,
+                                  void *y, float *state_out, const int64_t *strides, int B, int T,
+                                  int C, int G, int N, int softplus, int dtype, void *reserve,
+                                  int64_t reserve_bytes, void *workspace, int64_t workspace_bytes,
+                                  void *stream);
+int gspn_selective_scan_bwd_reserve(const void *x, const void *dt, const float *A, const void *Bm,
+                                    const void *Cm, const float *D, const void *z,
+                                    const float *dt_bias, const void *dy, const float *dstate_out,
+                                    const int32_t *lens, void *dx, void *ddt, float *dA, void *dBm,
+                                    void *dCm, float *dD, void *dz, float *ddt_bias, float *dstate,
+                                    const int64_t *strides, int B, int T, int C, int G, int N,
+                                    int softplus, int dtype, void *reserve, int64_t reserve_bytes,
+                                    void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * What joins two sublayers: the block's output f is normed (with w_post), gated a sequence and
+ * scaled a channel, added to the residual stream r, and the sum normed for the next block,
+ *   p = w_post f / sqrt(mean(f^2) + eps)  (without w_post: p = f),  r_out = r + scale gate p
+ *   y = w r_out / sqrt(mean(r_out^2) + eps)
+ * r, f, y, r_out [B][T][C], C up to 16384; w, w_post, scale [C], gate [B][C] (w, scale, gate NULL:
+ * ones).  r, r_out and their gradients are of residual_dtype, `dtype` or fp32; all else is of
+ * `dtype`.  y is formed from the sum before it is rounded.  r_out may be r, with the same strides.
+ * f NULL: y is the norm of r alone; r_out is not written, and w_post, scale and gate must be NULL.
+ * The backward takes r_out as it was stored, the gradients dy of y and dr_out of r_out from what
+ * else reads it (NULL: none), and writes dr, df (with f) and, for each vector given, its
+ * gradient.  dr may be dr_out, with the same strides.
+ * strides: forward r, f, y, r_out; backward r_out, f, dy, dr_out, dr, df.
+ * gspn_residual_norm_workspace_size: of the backward; gated: 1 with a gate, of up to 65535
+ * sequences then, else 0.
+ */
+int gspn_residual_norm_fwd(const void *r, const void *f, const void *w, const void *w_post,
+                           const void *scale, const void *gate, void *y, void *r_out,
+                           const int64_t *strides, int B, int T, int C, float eps, int dtype,
+                           int residual_dtype, void *stream);
+int gspn_residual_norm_workspace_size(int B, int T, int C, int gated, int dtype,
+                                      int residual_dtype, int64_t *bytes);
+int gspn_residual_norm_bwd(const void *r_out, const void *f, const void *w, const void *w_post,
+                           const void *scale, const void *gate, const void *dy, const void *dr_out,
+                           void *dr, void *df, void *dw, void *dw_post, void *dscale, void *dgate,
+                           const int64_t *strides, int B, int T, int C, float eps, int dtype,
+                           int residual_dtype, void *workspace, int64_t workspace_bytes,
+                           void *stream);
+
 /* Static description of a status code (never NULL). */
 const char *gspn_strerror(int status);
 

@@ -40,6 +40,11 @@ EXPORTED = ("gspn_workspace_size", "gspn_scan_fwd", "gspn_scan_bwd", "gspn_scan_
             "gspn_window_attn_bwd", "gspn_window_attn_decode",
             "gspn_delta_rule_workspace_size", "gspn_delta_rule_reserve_size",
             "gspn_delta_rule_fwd", "gspn_delta_rule_fwd_train", "gspn_delta_rule_bwd_reserve",
+            "gspn_short_conv_fwd", "gspn_short_conv_workspace_size", "gspn_short_conv_bwd",
+            "gspn_selective_scan_workspace_size", "gspn_selective_scan_reserve_size",
+            "gspn_selective_scan_fwd", "gspn_selective_scan_fwd_train",
+            "gspn_selective_scan_bwd_reserve", "gspn_residual_norm_fwd",
+            "gspn_residual_norm_workspace_size", "gspn_residual_norm_bwd",
             "gspn_strerror", "gspn_last_hip_error", "gspn_version")
 
 _lib = None
@@ -99,6 +104,17 @@ def load() -> ctypes.CDLL:
         lib.gspn_delta_rule_fwd.argtypes = [vp] * 10 + [i] * 6 + [f, i] + ws
         lib.gspn_delta_rule_fwd_train.argtypes = [vp] * 10 + [i] * 6 + [f, i, vp, i64] + ws
         lib.gspn_delta_rule_bwd_reserve.argtypes = [vp] * 15 + [i] * 6 + [f, i, vp, i64] + ws
+        lib.gspn_short_conv_fwd.argtypes = [vp] * 8 + [i] * 6 + [vp]
+        lib.gspn_short_conv_workspace_size.argtypes = [i] * 5 + [pi64]
+        lib.gspn_short_conv_bwd.argtypes = [vp] * 12 + [i] * 6 + ws
+        lib.gspn_selective_scan_workspace_size.argtypes = [i] * 7 + [pi64]
+        lib.gspn_selective_scan_reserve_size.argtypes = [i] * 6 + [pi64]
+        lib.gspn_selective_scan_fwd.argtypes = [vp] * 13 + [i] * 7 + ws
+        lib.gspn_selective_scan_fwd_train.argtypes = [vp] * 13 + [i] * 7 + [vp, i64] + ws
+        lib.gspn_selective_scan_bwd_reserve.argtypes = [vp] * 21 + [i] * 7 + [vp, i64] + ws
+        lib.gspn_residual_norm_fwd.argtypes = [vp] * 9 + [i] * 3 + [f, i, i, vp]
+        lib.gspn_residual_norm_workspace_size.argtypes = [i] * 6 + [pi64]
+        lib.gspn_residual_norm_bwd.argtypes = [vp] * 15 + [i] * 3 + [f, i, i] + ws
         for name in EXPORTED:
             getattr(lib, name).restype = i
         lib.gspn_strerror.argtypes = [i]

@@ -14,7 +14,8 @@ SOURCES = ["api.cpp", "scan_tiny.hip", "scan_small.hip", "scan_med_64.hip", "sca
            "scan_med_48.hip", "scan_med_40_32_24.hip", "scan_med.hip", "scan_pm.hip",
            "scan_wide.hip", "scan_norm.hip", "scan_plane.hip", "scan_line.hip", "scan_general.hip", "latent.hip",
            "mixers_api.cpp", "qk_norm.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_bwd_f32.hip", "attn_split.hip",
-           "delta_fwd.hip", "delta_bwd.hip", "delta_bf16.hip"]
+           "delta_fwd.hip", "delta_bwd.hip", "delta_bf16.hip",
+           "sublayer_api.cpp", "short_conv.hip", "selective_fwd.hip", "selective_bwd.hip", "residual_norm.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

@@ -1,0 +1,65 @@
+// The selective state space scan (internal).
+//
+//   d = softplus(dt + dt_bias),  h_t = exp(d A) h_{t-1} + d x B_t,  y = (C_t . h_t + D x) silu(z)
+//
+// for every channel with its own N states.  The tokens are cut into chunks where the
+// channels alone do not fill the card: what a chunk adds to its states from zeros, and the
+// sum of its steps, whose exponentials are the chunk's whole decay; a chain over the
+// chunks; and the chunks again from the states they begin with.
+#pragma once
+
+#include "attn.hpp"
+
+namespace gspn {
+
+struct SelectiveProblem {
+    Heads x, dt, z, y;                    // [B][T][C], strides of b and t; z.p may be null
+    Heads Bm, Cm;                         // [B][T][G][N]
+    const float *A;                       // [C][N]
+    const float *D, *dt_bias;             // [C] or null
+    const float *state;                   // [B][C][N], or null: zeros
+    float *state_out;                     // the same, or null: not wanted
+    Heads dy, dx, ddt, dz, dBm, dCm;      // backward
+    const float *dstate;                  // gradient of state_out, or null: zeros
+    float *dA, *dD, *ddt_bias, *dstate_in;
+    const int32_t *lens;                  // [B], or null: T
+    int B, T, C, G, N;
+    bool softplus;
+    int dtype;
+    Workspace *ws;
+    Workspace *rs = nullptr;              // the training pair's reserve
+};
+
+constexpr int kSelMaxStates = 64;
+
+// Tokens between the states that a training forward keeps for its backward.
+constexpr int kSelKeep = 8;
+
+// States as the kernels hold them: N rounded up to a power of two, at least the four that
+// the backward's quads of lanes share out in training; entries past N are 0.
+inline int sel_states(const SelectiveProblem &p)
+{
+    int n = p.rs ? 4 : 1;
+    while (n < p.N)
+        n *= 2;
+    return n;
+}
+
+// The states ahead of every kSelKeep-th token, [B][ceil(T / kSelKeep)][states][C].
+inline hipError_t take_sel_kept(const SelectiveProblem &p, Workspace *rs, void **kept)
+{
+    return rs->take(kept, (size_t)p.B * ((p.T + kSelKeep - 1) / kSelKeep) * sel_states(p) * p.C * 4);
+}
+
+hipError_t launch_selective_fwd(const SelectiveProblem &p, hipStream_t s);
+hipError_t launch_selective_bwd(const SelectiveProblem &p, hipStream_t s);
+
+#ifdef __HIPCC__
+
+// B and C of every token as fp32, [B][T][G][B, C][states], entries past N and tokens past a
+// sequence's end 0: the kernels read them as scalars.  bc has 2 B T G states floats.
+hipError_t launch_sel_pack(const SelectiveProblem &p, float *bc, hipStream_t s);
+
+#endif
+
+}  // namespace gspn

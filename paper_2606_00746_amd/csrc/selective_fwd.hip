@@ -1,0 +1,346 @@
+// The selective state space scan, forward (gspn_selective_scan_fwd, _fwd_train).
+//
+// A lane holds a channel with all its states: h_t = 2^(d A log2 e) h_{t-1} + d x B_t and
+// y = C_t . h need nothing of another lane, and B and C of a token, the same for all
+// channels of a group, are scalars.  A state and token take a product, an exponential, a
+// product, two multiply-adds: bound by the vector units, not by memory.
+#include <algorithm>
+
+#include "selective_dev.hpp"
+
+namespace gspn {
+namespace {
+
+using namespace sel;
+
+constexpr int kBlk = 256;
+
+// ---------------------------------------------------------------------------
+// B and C as fp32
+// ---------------------------------------------------------------------------
+
+template <typename T>
+__global__ __launch_bounds__(kBlk) void pack_kernel(SelectiveProblem p, int np, float *bc)
+{
+    const int64_t n = (int64_t)p.B * p.T * p.G * 2 * np;
+    for (int64_t i = (int64_t)blockIdx.x * kBlk + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlk) {
+        const int s = (int)(i % np);
+        int64_t at = i / np;
+        const bool second = at & 1;
+        at >>= 1;
+        const int g = (int)(at % p.G);
+        at /= p.G;
+        const int t = (int)(at % p.T), b = (int)(at / p.T);
+        const Heads &m = second ? p.Cm : p.Bm;
+        bc[i] = s < p.N && t < length_of(p, b) ? load_f(static_cast<const T *>(m.p) + b * m.sb + t * m.st + g * m.sh + s) : 0.f;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// chunks of tokens
+// ---------------------------------------------------------------------------
+
+struct Chunks {
+    int n, len;     // how many, tokens of each (a multiple of kSelKeep)
+    int blocks;     // waves that a group's channels take
+};
+
+// OUT: the outputs, from `starts`, or from the sequence's state where there is one chunk.
+// Otherwise what the chunk adds to its states from zeros, into `starts`, and the sum of
+// its steps.
+template <typename T, int NP, bool OUT>
+__global__ __launch_bounds__(64) void chunk_kernel(SelectiveProblem p, Chunks ch, const float *bc, float *starts, float *steps, float *kept)
+{
+    constexpr int U = kSelKeep;
+    int64_t at = blockIdx.x;
+    const int per = p.G * ch.blocks, nch = OUT ? ch.n : ch.n - 1;
+    const int gb = (int)(at % per);
+    at /= per;
+    const int k = (int)(at % nch), b = (int)(at / nch), g = gb / ch.blocks;
+    const int cpg = p.C / p.G, ci = gb % ch.blocks * 64 + threadIdx.x;
+    const bool on = ci < cpg;
+    const int c = g * cpg + min(ci, cpg - 1);
+    const int t0 = k * ch.len, t1 = min(t0 + ch.len, p.T), te = min(t1, length_of(p, b));
+
+    const T *x = static_cast<const T *>(p.x.p) + b * p.x.sb + c;
+    const T *dt = static_cast<const T *>(p.dt.p) + b * p.dt.sb + c;
+    const T *z = p.z.p ? static_cast<const T *>(p.z.p) + b * p.z.sb + c : nullptr;
+    T *y = OUT ? static_cast<T *>(p.y.p) + b * p.y.sb + c : nullptr;
+    const float bias = p.dt_bias ? p.dt_bias[c] : 0.f, skip = OUT && p.D ? p.D[c] : 0.f;
+    float A2[NP], h[NP], sum = 0.f;
+    const int64_t slot = (((int64_t)b * ch.n + k) * NP) * p.C + c;
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
+        A2[n] = n < p.N ? p.A[(int64_t)c * p.N + n] * kLog2e : 0.f;
+        if (!OUT)
+            h[n] = 0.f;
+        else if (ch.n > 1)
+            h[n] = starts[slot + (int64_t)n * p.C];
+        else
+            h[n] = p.state && n < p.N ? p.state[((int64_t)b * p.C + c) * p.N + n] : 0.f;
+    }
+
+    Raw<T, 1> xr[U], dr[U], zr[U];
+    const auto fetch = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const bool live = t + i < te;
+            xr[i] = live ? load_raw<T, 1>(x + (int64_t)(t + i) * p.x.st) : zero_raw<T, 1>();
+            dr[i] = live ? load_raw<T, 1>(dt + (int64_t)(t + i) * p.dt.st) : zero_raw<T, 1>();
+            if (OUT)
+                zr[i] = live && z ? load_raw<T, 1>(z + (int64_t)(t + i) * p.z.st) : zero_raw<T, 1>();
+        }
+    };
+    fetch(t0);
+    cfloat *m = constant(bc) + (((int64_t)b * p.T + t0) * p.G + g) * 2 * NP;
+    int t = t0;
+    for (; t < te; t += U) {
+        if (OUT && kept && on) {
+            float *to = kept + (((int64_t)b * ((p.T + U - 1) / U) + t / U) * NP) * p.C + c;
+#pragma unroll
+            for (int n = 0; n < NP; ++n)
+                to[(int64_t)n * p.C] = h[n];
+        }
+        Raw<T, 1> xc[U], dc[U], zc[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            xc[i] = xr[i], dc[i] = dr[i];
+            if (OUT)
+                zc[i] = zr[i];
+        }
+        fetch(t + U);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (t + i >= te)
+                break;
+            const float xv = get(xc[i], 0), raw = get(dc[i], 0) + bias;
+            const float d = p.softplus ? softplus(raw) : raw, u = d * xv;
+            float out = skip * xv;
+            if (!OUT)
+                sum += d;
+#pragma unroll
+            for (int n = 0; n < NP; ++n) {
+                h[n] = fmaf(exp2_hw(d * A2[n]), h[n], u * m[n]);
+                if (OUT)
+                    out = fmaf(m[NP + n], h[n], out);
+            }
+            m += p.G * 2 * NP;
+            if (OUT) {
+                if (z)
+                    out *= silu(get(zc[i], 0));
+                if (on)
+                    store_f(y + (int64_t)(t + i) * p.y.st, out);
+            }
+        }
+    }
+    if (OUT) {
+        if (on)
+            for (t = max(te, t0); t < t1; ++t)
+                store_f(y + (int64_t)t * p.y.st, 0.f);
+        if (k == ch.n - 1 && p.state_out && on)
+#pragma unroll
+            for (int n = 0; n < NP; ++n)
+                if (n < p.N)
+                    p.state_out[((int64_t)b * p.C + c) * p.N + n] = h[n];
+    } else if (on) {
+#pragma unroll
+        for (int n = 0; n < NP; ++n)
+            starts[slot + (int64_t)n * p.C] = h[n];
+        steps[((int64_t)b * ch.n + k) * p.C + c] = sum;
+    }
+}
+
+// From what each chunk adds to the states that it begins with, in the same place.
+template <int NP>
+__global__ __launch_bounds__(kBlk) void chain_kernel(SelectiveProblem p, Chunks ch, float *starts, const float *steps)
+{
+    const int64_t i = (int64_t)blockIdx.x * kBlk + threadIdx.x;
+    if (i >= (int64_t)p.B * NP * p.C)
+        return;
+    const int c = (int)(i % p.C), n = (int)(i / p.C % NP), b = (int)(i / p.C / NP);
+    const float a2 = n < p.N ? p.A[(int64_t)c * p.N + n] * kLog2e : 0.f;
+    float h = p.state && n < p.N ? p.state[((int64_t)b * p.C + c) * p.N + n] : 0.f;
+    const int64_t step = (int64_t)NP * p.C;
+    float *at = starts + (int64_t)b * ch.n * step + (int64_t)n * p.C + c;
+    const float *s = steps + (int64_t)b * ch.n * p.C + c;
+    constexpr int U = 8;
+    for (int k = 0; k < ch.n; k += U) {
+        float add[U], sum[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const bool in = k + j < ch.n - 1;
+            add[j] = in ? at[(k + j) * step] : 0.f;
+            sum[j] = in ? s[(int64_t)(k + j) * p.C] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            if (k + j < ch.n) {
+                at[(k + j) * step] = h;
+                h = fmaf(exp2_hw(a2 * sum[j]), h, add[j]);
+            }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// a few tokens: four lanes a channel, B and C as they lie
+// ---------------------------------------------------------------------------
+
+constexpr int kFewTokens = 8;
+
+template <typename T, int NP>
+__global__ __launch_bounds__(kBlk) void token_kernel(SelectiveProblem p)
+{
+    constexpr int NS = NP >= 4 ? NP / 4 : 1;   // states of a lane
+    const int64_t i = ((int64_t)blockIdx.x * kBlk + threadIdx.x) / 4;
+    if (i >= (int64_t)p.B * p.C)
+        return;
+    const int s = threadIdx.x % 4, c = (int)(i % p.C), b = (int)(i / p.C), g = c / (p.C / p.G), n0 = s * NS;
+    const int te = length_of(p, b);
+    const T *x = static_cast<const T *>(p.x.p) + b * p.x.sb + c;
+    const T *dt = static_cast<const T *>(p.dt.p) + b * p.dt.sb + c;
+    const T *z = p.z.p ? static_cast<const T *>(p.z.p) + b * p.z.sb + c : nullptr;
+    const T *Bm = static_cast<const T *>(p.Bm.p) + b * p.Bm.sb + g * p.Bm.sh + n0;
+    const T *Cm = static_cast<const T *>(p.Cm.p) + b * p.Cm.sb + g * p.Cm.sh + n0;
+    T *y = static_cast<T *>(p.y.p) + b * p.y.sb + c;
+    const float bias = p.dt_bias ? p.dt_bias[c] : 0.f, skip = p.D ? p.D[c] : 0.f;
+    const float *A = p.A + (int64_t)c * p.N + n0, *from = p.state ? p.state + i * p.N + n0 : nullptr;
+    float A2[NS], h[NS];
+    if (NS % 4 == 0 && p.N == NP) {
+        load_all<float, NS>(A, A2);
+        widen_all(from ? load_raw<float, NS>(from) : zero_raw<float, NS>(), h);
+    } else {
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            A2[n] = n0 + n < p.N ? A[n] : 0.f;
+            h[n] = from && n0 + n < p.N ? from[n] : 0.f;
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+        A2[n] *= kLog2e;
+    for (int t = 0; t < p.T; ++t) {
+        float out = 0.f, xv = 0.f;
+        if (t < te) {
+            xv = load_f(x + (int64_t)t * p.x.st);
+            const float raw = load_f(dt + (int64_t)t * p.dt.st) + bias;
+            const float d = p.softplus ? softplus(raw) : raw, u = d * xv;
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+                if (n0 + n < p.N) {
+                    h[n] = fmaf(exp2_hw(d * A2[n]), h[n], u * load_f(Bm + (int64_t)t * p.Bm.st + n));
+                    out = fmaf(load_f(Cm + (int64_t)t * p.Cm.st + n), h[n], out);
+                }
+        }
+        out += dpp<kXor1>(out);
+        out += dpp<kXor2>(out);
+        if (t < te) {
+            out = fmaf(skip, xv, out);
+            if (z)
+                out *= silu(load_f(z + (int64_t)t * p.z.st));
+        }
+        if (s == 0)
+            store_f(y + (int64_t)t * p.y.st, out);
+    }
+    if (p.state_out) {
+        float *to = p.state_out + i * p.N + n0;
+        if (NS % 4 == 0 && p.N == NP)
+            store_all(to, h);
+        else
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+                if (n0 + n < p.N)
+                    to[n] = h[n];
+    }
+}
+
+// Waves that the chunks of a call are cut for, and a chunk's fewest tokens.
+constexpr int64_t kWaves = 4096;
+constexpr int kLeast = 32;
+
+Chunks chunks_of(const SelectiveProblem &p)
+{
+    Chunks c;
+    c.blocks = (p.C / p.G + 63) / 64;
+    const int64_t waves = (int64_t)p.B * p.G * c.blocks, want = std::max<int64_t>(1, kWaves / waves);
+    const int64_t len = std::max<int64_t>(kLeast, (p.T + want - 1) / want);
+    c.len = (int)((len + kSelKeep - 1) / kSelKeep * kSelKeep);
+    c.n = (p.T + c.len - 1) / c.len;
+    return c;
+}
+
+template <typename T, int NP>
+hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
+{
+    if (p.T <= kFewTokens && !p.rs) {
+        const int64_t n = ((int64_t)p.B * p.C * 4 + kBlk - 1) / kBlk;
+        if (n * kBlk > kMaxThreads)
+            return hipErrorInvalidConfiguration;
+        if (p.ws->counting)
+            return hipSuccess;
+        token_kernel<T, NP><<<dim3((unsigned)n), kBlk, 0, s>>>(p);
+        return hipGetLastError();
+    }
+    const Chunks ch = chunks_of(p);
+    const int64_t waves = (int64_t)p.B * p.G * ch.blocks * ch.n, joins = ((int64_t)p.B * NP * p.C + kBlk - 1) / kBlk;
+    if (waves * 64 > kMaxThreads || joins * kBlk > kMaxThreads)
+        return hipErrorInvalidConfiguration;
+    void *bc = nullptr, *starts = nullptr, *steps = nullptr, *kept = nullptr;
+    hipError_t e = p.ws->take(&bc, (size_t)p.B * p.T * p.G * 2 * NP * 4);
+    if (e == hipSuccess && ch.n > 1)
+        e = p.ws->take(&starts, (size_t)p.B * ch.n * NP * p.C * 4);
+    if (e == hipSuccess && ch.n > 1)
+        e = p.ws->take(&steps, (size_t)p.B * ch.n * p.C * 4);
+    if (e == hipSuccess && p.rs)
+        e = take_sel_kept(p, p.rs, &kept);
+    if (e != hipSuccess || p.ws->counting)
+        return e;
+    float *const m = static_cast<float *>(bc), *const st = static_cast<float *>(starts), *const sm = static_cast<float *>(steps);
+    e = launch_sel_pack(p, m, s);
+    if (e == hipSuccess && ch.n > 1) {
+        chunk_kernel<T, NP, false><<<dim3((unsigned)(waves / ch.n * (ch.n - 1))), 64, 0, s>>>(p, ch, m, st, sm, nullptr);
+        e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+        chain_kernel<NP><<<dim3((unsigned)joins), kBlk, 0, s>>>(p, ch, st, sm);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess)
+        return e;
+    chunk_kernel<T, NP, true><<<dim3((unsigned)waves), 64, 0, s>>>(p, ch, m, st, sm, static_cast<float *>(kept));
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t pick(const SelectiveProblem &p, hipStream_t s)
+{
+    switch (sel_states(p)) {
+    case 1: return fwd<T, 1>(p, s);
+    case 2: return fwd<T, 2>(p, s);
+    case 4: return fwd<T, 4>(p, s);
+    case 8: return fwd<T, 8>(p, s);
+    case 16: return fwd<T, 16>(p, s);
+    case 32: return fwd<T, 32>(p, s);
+    default: return fwd<T, 64>(p, s);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_sel_pack(const SelectiveProblem &p, float *bc, hipStream_t s)
+{
+    const int np = sel_states(p);
+    const int64_t n = ((int64_t)p.B * p.T * p.G * 2 * np + kBlk - 1) / kBlk;
+    const unsigned grid = (unsigned)std::min<int64_t>(n, 65536);
+    if (p.dtype == 0)
+        pack_kernel<float><<<grid, kBlk, 0, s>>>(p, np, bc);
+    else
+        pack_kernel<bf16_t><<<grid, kBlk, 0, s>>>(p, np, bc);
+    return hipGetLastError();
+}
+
+hipError_t launch_selective_fwd(const SelectiveProblem &p, hipStream_t s)
+{
+    return p.dtype == 0 ? pick<float>(p, s) : pick<bf16_t>(p, s);
+}
+
+}  // namespace gspn
