@@ -57,7 +57,11 @@ hipError_t launch_selective_bwd(const SelectiveProblem &p, hipStream_t s);
 #ifdef __HIPCC__
 
 // B and C of every token as fp32, [B][T][G][B, C][states], entries past N and tokens past a
-// sequence's end 0: the kernels read them as scalars.  bc has 2 B T G states floats.
+// sequence's end 0: the kernels read them as scalars, one token ahead, and there is room for
+// a token's before the first and behind the last.
+constexpr int kPackTokens = 16;   // of a workgroup
+inline int64_t sel_pack_groups(const SelectiveProblem &p) { return (int64_t)p.B * ((p.T + kPackTokens - 1) / kPackTokens); }
+inline size_t sel_packed(const SelectiveProblem &p) { return ((size_t)p.B * p.T + 2) * p.G * 2 * sel_states(p) * 4; }
 hipError_t launch_sel_pack(const SelectiveProblem &p, float *bc, hipStream_t s);
 
 #endif

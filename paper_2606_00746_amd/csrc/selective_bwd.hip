@@ -33,68 +33,93 @@ struct Chunks {
 // ---------------------------------------------------------------------------
 
 // A lane a channel: g from 0 behind the chunk's last token to ahead of its first.  Chunks 1 ..
-template <typename T, int NP>
+// Addresses and loads ahead as in the forward.
+template <typename T, int NP, bool Z>
 __global__ __launch_bounds__(64) void back_kernel(SelectiveProblem p, Chunks ch, const float *bc, float *ends, float *steps)
 {
-    int64_t at = blockIdx.x;
+    constexpr int U = K;
     const int per = p.G * ch.waves;
-    const int gb = (int)(at % per);
-    at /= per;
-    const int k = 1 + (int)(at % (ch.n - 1)), b = (int)(at / (ch.n - 1)), g = gb / ch.waves;
-    const int cpg = p.C / p.G, ci = gb % ch.waves * 64 + threadIdx.x;
-    const bool on = ci < cpg;
-    const int c = g * cpg + min(ci, cpg - 1);
-    const int t0 = k * ch.len, te = min(min(t0 + ch.len, p.T), length_of(p, b));
-
-    const T *dt = static_cast<const T *>(p.dt.p) + b * p.dt.sb + c;
-    const T *z = p.z.p ? static_cast<const T *>(p.z.p) + b * p.z.sb + c : nullptr;
-    const T *dy = static_cast<const T *>(p.dy.p) + b * p.dy.sb + c;
-    const float bias = p.dt_bias ? p.dt_bias[c] : 0.f;
+    const int gb = (int)(blockIdx.x % per), kb = (int)(blockIdx.x / per);
+    const int k = 1 + kb % (ch.n - 1), b = kb / (ch.n - 1), g = gb / ch.waves;
+    const int cpg = p.C / p.G, c0 = gb % ch.waves * 64;
+    const bool on = c0 + (int)threadIdx.x < cpg;
+    const uint32_t l = g * cpg + (on ? c0 + threadIdx.x : 0), off = l * (uint32_t)sizeof(T);
+    const int t0 = k * ch.len, te = max(t0, min(min(t0 + ch.len, p.T), length_of(p, b)));
+    const bool soft = p.softplus;
+    const float bias = p.dt_bias ? p.dt_bias[l] : 0.f;
     float A2[NP], G[NP], sum = 0.f;
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
-        A2[n] = n < p.N ? p.A[(int64_t)c * p.N + n] * kLog2e : 0.f;
+        A2[n] = n < p.N ? p.A[(int64_t)l * p.N + n] * kLog2e : 0.f;
         G[n] = 0.f;
     }
-    Raw<T, 1> dr[K], zr[K], yr[K];
-    const auto fetch = [&](int t) {   // tokens t, t - 1, ..
+    // C of a token, from the last on; the one ahead of the first is read too
+    const int mstep = p.G * 2 * NP;
+    cfloat *m = constant(bc) + ((((int64_t)b * p.T + te) * p.G + g) * 2 + 1) * NP;
+    float Ct[NP];
 #pragma unroll
-        for (int i = 0; i < K; ++i) {
-            const bool live = t - i >= t0;
-            dr[i] = live ? load_raw<T, 1>(dt + (int64_t)(t - i) * p.dt.st) : zero_raw<T, 1>();
-            yr[i] = live ? load_raw<T, 1>(dy + (int64_t)(t - i) * p.dy.st) : zero_raw<T, 1>();
-            zr[i] = live && z ? load_raw<T, 1>(z + (int64_t)(t - i) * p.z.st) : zero_raw<T, 1>();
+    for (int n = 0; n < NP; ++n)
+        Ct[n] = m[n];
+    const auto token = [&](uint32_t dr, uint32_t zr, uint32_t yr) {
+        float next[NP];
+        m -= mstep;
+#pragma unroll
+        for (int n = 0; n < NP; ++n)
+            next[n] = m[n];
+        step_fence();
+        const float raw = widened<T>(dr) + bias, sp = softplus(raw), d = soft ? sp : raw;
+        float up = widened<T>(yr);
+        if (Z)
+            up *= silu(widened<T>(zr));
+        sum += d;
+#pragma unroll
+        for (int n = 0; n < NP; ++n)
+            G[n] = exp2_hw(d * A2[n]) * fmaf(Ct[n], up, G[n]);
+        step_fence();
+#pragma unroll
+        for (int n = 0; n < NP; ++n)
+            Ct[n] = next[n];
+    };
+    const int last = max(te - 1, t0);
+    RowAt<T> dt(p.dt, b, last), z(Z ? p.z : p.dt, b, last), dy(p.dy, b, last);
+    dt.step = -dt.step, z.step = -z.step, dy.step = -dy.step;
+    uint32_t dr[U], zr[U], yr[U];
+    const auto fetch = [&]() {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            dr[i] = dt.load(off), yr[i] = dy.load(off), zr[i] = Z ? z.load(off) : 0;
+            dt.next(), dy.next();
+            if (Z)
+                z.next();
         }
     };
-    fetch(te - 1);
-    for (int t = te - 1; t >= t0; t -= K) {
-        Raw<T, 1> dc[K], zc[K], yc[K];
+    const int full = (te - t0) / U;
+    if (full > 0)
+        fetch();
+    for (int blk = 0; blk < full; ++blk) {
+        uint32_t dc[U], zc[U], yc[U];
 #pragma unroll
-        for (int i = 0; i < K; ++i)
+        for (int i = 0; i < U; ++i)
             dc[i] = dr[i], zc[i] = zr[i], yc[i] = yr[i];
-        fetch(t - K);
+        if (blk + 1 < full)
+            fetch();
 #pragma unroll
-        for (int i = 0; i < K; ++i) {
-            if (t - i < t0)
-                break;
-            cfloat *m = constant(bc) + ((((int64_t)b * p.T + t - i) * p.G + g) * 2 + 1) * NP;
-            const float raw = get(dc[i], 0) + bias, d = p.softplus ? softplus(raw) : raw;
-            float up = get(yc[i], 0);
-            if (z)
-                up *= silu(get(zc[i], 0));
-            sum += d;
-#pragma unroll
-            for (int n = 0; n < NP; ++n)
-                G[n] = exp2_hw(d * A2[n]) * fmaf(m[n], up, G[n]);
-        }
+        for (int i = 0; i < U; ++i)
+            token(dc[i], zc[i], yc[i]);
+    }
+    for (int t = te - full * U; t > t0; --t) {
+        token(dt.load(off), Z ? z.load(off) : 0, dy.load(off));
+        dt.next(), dy.next();
+        if (Z)
+            z.next();
     }
     if (!on)
         return;
-    const int64_t slot = (((int64_t)b * ch.n + k) * NP) * p.C + c;
+    const int64_t slot = (((int64_t)b * ch.n + k) * NP) * p.C;
 #pragma unroll
     for (int n = 0; n < NP; ++n)
-        ends[slot + (int64_t)n * p.C] = G[n];
-    steps[((int64_t)b * ch.n + k) * p.C + c] = sum;
+        (ends + slot + (int64_t)n * p.C)[l] = G[n];
+    steps[((int64_t)b * ch.n + k) * p.C + l] = sum;
 }
 
 // From what each chunk passes on to the gradient that arrives behind it, in the same place.
@@ -110,7 +135,7 @@ __global__ __launch_bounds__(kBlk) void back_chain_kernel(SelectiveProblem p, Ch
     const int64_t step = (int64_t)NP * p.C;
     float *at = ends + (int64_t)b * ch.n * step + (int64_t)n * p.C + c;
     const float *s = steps + (int64_t)b * ch.n * p.C + c;
-    constexpr int U = 8;
+    constexpr int U = 32;   // chunks in flight
     for (int k = ch.n - 1; k >= 0; k -= U) {
         float add[U], sum[U];
 #pragma unroll
@@ -169,11 +194,12 @@ struct Parts {
 };
 
 // Lane 4 q + s: channels CH q .. of its wave's 16 CH, states NS s .. of 4 NS.
-template <typename T, int NS, int CH>
+// Z: with a gate.
+template <typename T, int NS, int CH, bool Z>
 __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks ch, const float *bc, const float *kept, const float *ends, Parts parts)
 {
     constexpr int NP = 4 * NS, CW = 16 * CH, V = 2 * CH;   // states; channels of a wave; a lane's, of a token, at the ends
-    constexpr int TR = NS >= 16 ? 1 : NS <= 2 ? 8 : 16 / NS;   // tokens whose sums are formed at once
+    constexpr int TR = NS <= 4 ? 8 : 32 / NS;                // tokens whose sums are formed at once
     __shared__ float4 tok_[4][3][K][CW / 4];                // d, u, dy' of a wave's tokens; then C . h, du, dd
     __shared__ float4 mat_[K][2][NS];                       // B and C of the tokens
     __shared__ float4 red_[4][TR][2][NS][16];               // a wave's terms of dB and dC: float4 over s
@@ -212,73 +238,104 @@ __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks c
     const int tl = lane / 8, cl = lane % 8 * V;
     const bool von = w0 + cl < cpg;
     const int cv = g * cpg + (von ? w0 + cl : 0);
-    float bias[V], skip[V], dD[V], db[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        bias[e] = p.dt_bias ? p.dt_bias[cv + e] : 0.f;
-        skip[e] = p.D ? p.D[cv + e] : 0.f;
-        dD[e] = db[e] = 0.f;
-    }
+    float dD[V] = {}, db[V] = {};
+    const bool soft = p.softplus;
     const T *x = static_cast<const T *>(p.x.p) + b * p.x.sb + cv;
     const T *dt = static_cast<const T *>(p.dt.p) + b * p.dt.sb + cv;
-    const T *z = p.z.p ? static_cast<const T *>(p.z.p) + b * p.z.sb + cv : nullptr;
+    const T *z = Z ? static_cast<const T *>(p.z.p) + b * p.z.sb + cv : nullptr;
     const T *dy = static_cast<const T *>(p.dy.p) + b * p.dy.sb + cv;
     const int nkept = (p.T + K - 1) / K;
 
-    for (int tb = t0 + (t1 - 1 - t0) / K * K; tb >= t0; tb -= K) {
+    // a block of tokens past the sequence: gradients of 0
+    int tb = t0 + (t1 - 1 - t0) / K * K;
+    const int64_t out_step = (int64_t)p.G * ch.blocks * 2 * NP;
+    const auto sums_at = [&](int t) { return parts.bc + ((((int64_t)b * p.T + t) * p.G + g) * ch.blocks + blk) * 2 * NP; };
+    for (; tb >= t0 && tb >= len; tb -= K) {
+        const int t = tb + tl;
+        const float none[V] = {};
+        if (von && t < t1) {
+            store_all(static_cast<T *>(p.dx.p) + b * p.dx.sb + t * p.dx.st + cv, none);
+            store_all(static_cast<T *>(p.ddt.p) + b * p.ddt.sb + t * p.ddt.st + cv, none);
+            if (Z)
+                store_all(static_cast<T *>(p.dz.p) + b * p.dz.sb + t * p.dz.st + cv, none);
+        }
+        for (int i = threadIdx.x; i < K * 2 * NP; i += kBlk)
+            if (tb + i / (2 * NP) < t1)
+                sums_at(tb)[i / (2 * NP) * out_step + i % (2 * NP)] = 0.f;
+    }
+    // what a block reads, asked for while the one behind it is worked on
+    constexpr int MR = (K * 2 * NP + kBlk - 1) / kBlk;
+    Raw<T, V> xn, dn, yn, zn;
+    Raw<float, CH> hn[NS];
+    float mn[MR];
+    const auto fetch = [&](int at) {
+        const int t = at + tl;
+        const bool live = von && t < len;
+        xn = live ? load_raw<T, V>(x + t * p.x.st) : zero_raw<T, V>();
+        dn = live ? load_raw<T, V>(dt + t * p.dt.st) : zero_raw<T, V>();
+        yn = live ? load_raw<T, V>(dy + t * p.dy.st) : zero_raw<T, V>();
+        zn = Z && live ? load_raw<T, V>(z + t * p.z.st) : zero_raw<T, V>();
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+            hn[i] = load_raw<float, CH>(kept + ((int64_t)(b * (int64_t)nkept + at / K) * NP + n0 + i) * p.C + cq);
+#pragma unroll
+        for (int j = 0; j < MR; ++j) {
+            const int i = threadIdx.x + j * kBlk, ti = at + i / (2 * NP);
+            mn[j] = i < K * 2 * NP && ti < p.T ? bc[(((int64_t)b * p.T + ti + 1) * p.G + g) * 2 * NP + i % (2 * NP)] : 0.f;
+        }
+    };
+    if (tb >= t0)
+        fetch(tb);
+    for (; tb >= t0; tb -= K) {
         const int t = tb + tl;
         const bool live = von && t < len;
-        float *const out_bc = parts.bc + ((((int64_t)b * p.T + tb) * p.G + g) * ch.blocks + blk) * 2 * NP;
-        const int64_t out_step = (int64_t)p.G * ch.blocks * 2 * NP;
-        if (tb >= len) {   // past the sequence: gradients of 0
-            const float none[V] = {};
-            if (von && t < t1) {
-                store_all(static_cast<T *>(p.dx.p) + b * p.dx.sb + t * p.dx.st + cv, none);
-                store_all(static_cast<T *>(p.ddt.p) + b * p.ddt.sb + t * p.ddt.st + cv, none);
-                if (z)
-                    store_all(static_cast<T *>(p.dz.p) + b * p.dz.sb + t * p.dz.st + cv, none);
-            }
-            for (int i = threadIdx.x; i < K * 2 * NP; i += kBlk)
-                if (tb + i / (2 * NP) < t1)
-                    out_bc[i / (2 * NP) * out_step + i % (2 * NP)] = 0.f;
-            continue;
-        }
-        const Raw<T, V> xr = live ? load_raw<T, V>(x + t * p.x.st) : zero_raw<T, V>();
-        const Raw<T, V> dr = live ? load_raw<T, V>(dt + t * p.dt.st) : zero_raw<T, V>();
-        const Raw<T, V> yr = live ? load_raw<T, V>(dy + t * p.dy.st) : zero_raw<T, V>();
-        const Raw<T, V> zr = live && z ? load_raw<T, V>(z + t * p.z.st) : zero_raw<T, V>();
+        float *const out_bc = sums_at(tb);
+        const Raw<T, V> xr = xn, dr = dn, yr = yn, zr = zn;
         float first[CH][NS];
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            float f[CH];
-            load_all<float, CH>(kept + ((int64_t)(b * (int64_t)nkept + tb / K) * NP + n0 + i) * p.C + cq, f);
+        for (int i = 0; i < NS; ++i)
 #pragma unroll
             for (int e = 0; e < CH; ++e)
-                first[e][i] = qon ? f[e] : 0.f;
-        }
-        for (int i = threadIdx.x; i < K * 2 * NP; i += kBlk) {
-            const int ti = tb + i / (2 * NP);
-            mat[i] = ti < p.T ? bc[(((int64_t)b * p.T + ti) * p.G + g) * 2 * NP + i % (2 * NP)] : 0.f;
-        }
-        float d[V], u[V], up[V];
+                first[e][i] = qon ? get(hn[i], e) : 0.f;
+#pragma unroll
+        for (int j = 0; j < MR; ++j)
+            if ((int)threadIdx.x + j * kBlk < K * 2 * NP)
+                mat[threadIdx.x + j * kBlk] = mn[j];
+        float bias[V] = {}, skip[V] = {};
+        if (p.dt_bias)
+            load_all<float, V>(p.dt_bias + cv, bias);
+        // of dd and C . h + D x: what ddt and dz are of them; 0 where there is no token
+        float d[V], u[V], up[V], fd[V], fz[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const float raw = get(dr, e) + bias[e], v = p.softplus ? softplus(raw) : raw;
-            d[e] = live ? v : 0.f;
+            const float raw = get(dr, e) + bias[e];
+            float grad;
+            const float v = softplus(raw, grad);
+            d[e] = live ? (soft ? v : raw) : 0.f;
+            fd[e] = live ? (soft ? grad : 1.f) : 0.f;
             u[e] = d[e] * get(xr, e);
             up[e] = get(yr, e);
-            if (z)
-                up[e] *= silu(get(zr, e));
+            if (Z) {
+                fz[e] = up[e];
+                up[e] *= silu(get(zr, e), grad);
+                fz[e] *= grad;
+            }
         }
         put_lds(&dts[tl][cl], d);
         put_lds(&us[tl][cl], u);
         put_lds(&ups[tl][cl], up);
-        __syncthreads();
+        if (p.D)
+            load_all<float, V>(p.D + cv, skip);
+        lds_barrier();
+        if (tb > t0)
+            fetch(tb - K);
 
         float h[K][CH][NS];
 #pragma unroll
         for (int j = 0; j < K; ++j) {
             float dv[CH], uv[CH], Bv[NS];
+            step_fence();
+            asm volatile("" ::: "memory");   // read again for each token: kept, they take the registers of more waves
             get_lds(&dts[j][q * CH], dv);
             get_lds(&us[j][q * CH], uv);
             get_lds(mat + j * 2 * NP + n0, Bv);
@@ -294,6 +351,8 @@ __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks c
             for (int jj = TR - 1; jj >= 0; --jj) {
                 const int j = jr + jj;
                 float dv[CH], uv[CH], gv[CH], Bv[NS], Cv[NS];
+                step_fence();
+                asm volatile("" ::: "memory");
                 get_lds(&dts[j][q * CH], dv);
                 get_lds(&us[j][q * CH], uv);
                 get_lds(&ups[j][q * CH], gv);
@@ -306,7 +365,8 @@ __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks c
 #pragma unroll
                     for (int i = 0; i < NS; ++i) {
                         const float gt = fmaf(Cv[i], gv[e], G[e][i]);
-                        yh = fmaf(Cv[i], h[j][e][i], yh);
+                        if (Z)
+                            yh = fmaf(Cv[i], h[j][e][i], yh);
                         du = fmaf(gt, Bv[i], du);
                         tB[i] = fmaf(gt, uv[e], tB[i]);
                         tC[i] = fmaf(h[j][e][i], gv[e], tC[i]);
@@ -314,13 +374,19 @@ __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks c
                         const float w = G[e][i] * (j ? h[j - 1][e][i] : first[e][i]);
                         dd = fmaf(w, A2[e][i], dd);
                         dA[e][i] = fmaf(w, dv[e], dA[e][i]);
+                        asm volatile("" : "+v"(dA[e][i]));   // here, not behind the block with every w kept
                     }
-                    yh += dpp<kXor1>(yh), du += dpp<kXor1>(du), dd += dpp<kXor1>(dd);
-                    yh += dpp<kXor2>(yh), du += dpp<kXor2>(du), dd += dpp<kXor2>(dd);
-                    res[e] = s == 0 ? yh : s == 1 ? du : dd;
+                    // over the quad: du's sum to lane 0, dd's to lane 1, C . h's to lane 2
+                    const float own = in_lanes(du, dd, kOddLanes) + dpp<kXor1>(in_lanes(dd, du, kOddLanes));
+                    if (Z) {
+                        yh += dpp<kXor1>(yh);
+                        res[e] = in_lanes(own, yh, kOddPairs) + dpp<kXor2>(in_lanes(yh, own, kOddPairs));
+                    } else {
+                        res[e] = own + dpp<kXor2>(own);
+                    }
                 }
                 // over d, u and dy' of the token, which have been read
-                if (s < 3)
+                if (s < 2 + Z)
                     put_lds(&dts[s * K + j][q * CH], res);
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
@@ -328,7 +394,7 @@ __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks c
                     reinterpret_cast<float *>(&red_[wave][jj][1][i][0])[lane] = tC[i];
                 }
             }
-            __syncthreads();
+            lds_barrier();
             // a row of 16 float4 a token, matrix and i: float4 (over s) q of all waves; RT threads a row
             constexpr int rows = TR * 2 * NS, RT = kBlk / rows >= 16 ? 16 : kBlk / rows;
             if ((int)threadIdx.x < rows * RT) {
@@ -349,30 +415,30 @@ __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks c
                 }
             }
             if (jr > 0)
-                __syncthreads();
+                lds_barrier();
         }
 
-        float yh[V], du[V], dd[V];
-        get_lds(&dts[tl][cl], yh);
-        get_lds(&dts[K + tl][cl], du);
-        get_lds(&dts[2 * K + tl][cl], dd);
+        float du[V], dd[V], yh[V];
+        get_lds(&dts[tl][cl], du);
+        get_lds(&dts[K + tl][cl], dd);
+        if (Z)
+            get_lds(&dts[2 * K + tl][cl], yh);
         float odx[V], odt[V], odz[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float xv = get(xr, e);
-            odx[e] = live ? fmaf(du[e], d[e], skip[e] * up[e]) : 0.f;
-            float v = fmaf(dd[e], kLn2, du[e] * xv);
-            if (p.softplus)
-                v *= logistic(get(dr, e) + bias[e]);
-            odt[e] = live ? v : 0.f;
-            odz[e] = z && live ? get(yr, e) * fmaf(skip[e], xv, yh[e]) * silu_grad(get(zr, e)) : 0.f;
+            odx[e] = fmaf(du[e], d[e], skip[e] * up[e]);
+            odt[e] = fmaf(dd[e], kLn2, du[e] * xv) * fd[e];
+            if (Z)
+                odz[e] = fmaf(skip[e], xv, yh[e]) * fz[e];
             dD[e] = fmaf(up[e], xv, dD[e]);
             db[e] += odt[e];
+            asm volatile("" : "+v"(dD[e]), "+v"(db[e]));
         }
         if (von && t < t1) {
             store_all(static_cast<T *>(p.dx.p) + b * p.dx.sb + t * p.dx.st + cv, odx);
             store_all(static_cast<T *>(p.ddt.p) + b * p.ddt.sb + t * p.ddt.st + cv, odt);
-            if (z)
+            if (Z)
                 store_all(static_cast<T *>(p.dz.p) + b * p.dz.sb + t * p.dz.st + cv, odz);
         }
     }
@@ -411,25 +477,22 @@ __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks c
 // ---------------------------------------------------------------------------
 
 template <typename T>
-__global__ __launch_bounds__(kBlk) void sum_bc_kernel(SelectiveProblem p, int np, int blocks, const float *part)
+__global__ __launch_bounds__(kBlk) void sum_bc_kernel(SelectiveProblem p, int np, int parts, int blocks, const float *part)
 {
-    const int64_t n = (int64_t)p.B * p.T * p.G * 2 * np;
-    for (int64_t i = (int64_t)blockIdx.x * kBlk + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlk) {
-        const int s = (int)(i % np);
-        int64_t at = i / np;
-        const int second = (int)(at & 1);
-        at >>= 1;
-        if (s >= p.N)
+    const int b = (int)(blockIdx.x / (unsigned)parts), t0 = (int)(blockIdx.x % (unsigned)parts) * kPackTokens, row = p.G * 2 * np;
+    const int n = min(kPackTokens, p.T - t0) * row;
+    const float *const from = part + ((int64_t)b * p.T + t0) * row * blocks;
+    for (int i = threadIdx.x; i < n; i += kBlk) {
+        const int s = i % (2 * np), gt = i / (2 * np), g = gt % p.G, t = t0 + gt / p.G;
+        if (s % np >= p.N)
             continue;
-        const float *in = part + at * blocks * 2 * np + second * np + s;
+        const float *in = from + (int64_t)gt * blocks * 2 * np + s;
         float a = 0.f;
+#pragma unroll 4
         for (int k = 0; k < blocks; ++k)
             a += in[(int64_t)k * 2 * np];
-        const int g = (int)(at % p.G);
-        at /= p.G;
-        const int t = (int)(at % p.T), b = (int)(at / p.T);
-        const Heads &m = second ? p.dCm : p.dBm;
-        store_f(static_cast<T *>(m.p) + b * m.sb + t * m.st + g * m.sh + s, a);
+        const Heads &m = s < np ? p.dBm : p.dCm;
+        store_f(static_cast<T *>(m.p) + b * m.sb + t * m.st + g * m.sh + s % np, a);
     }
 }
 
@@ -470,8 +533,8 @@ __global__ __launch_bounds__(16 * kSumRows) void sum_channels_kernel(SelectivePr
     }
 }
 
-constexpr int64_t kWaves = 4096;
-constexpr int kLeast = 32;
+constexpr int64_t kWaves = 6144;
+constexpr int kLeast = 16;
 
 template <typename T, int NP>
 hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
@@ -481,17 +544,18 @@ hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
     const int cpg = p.C / p.G;
     ch.waves = (cpg + 63) / 64;
     ch.blocks = (cpg + 64 * CH - 1) / (64 * CH);
-    const int64_t waves = (int64_t)p.B * p.G * ch.blocks * 4, want = std::max<int64_t>(1, kWaves / waves);
+    const int64_t waves = (int64_t)p.B * p.G * ch.waves, want = std::max<int64_t>(1, kWaves / waves);
     const int64_t len = std::max<int64_t>(kLeast, (p.T + want - 1) / want);
     ch.len = (int)((len + K - 1) / K * K);
     ch.n = (p.T + ch.len - 1) / ch.len;
     const int64_t groups = (int64_t)p.B * p.G * ch.blocks * ch.n, passes = (int64_t)p.B * p.G * ch.waves * (ch.n - 1);
     const int64_t joins = ((int64_t)p.B * NP * p.C + kBlk - 1) / kBlk;
-    if (groups * kBlk > kMaxThreads || passes * 64 > kMaxThreads || joins * kBlk > kMaxThreads)
+    if (groups * kBlk > kMaxThreads || passes * 64 > kMaxThreads || joins * kBlk > kMaxThreads ||
+        sel_pack_groups(p) * kBlk > kMaxThreads)
         return hipErrorInvalidConfiguration;
     void *bc = nullptr, *ends = nullptr, *steps = nullptr, *kept = nullptr, *pbc = nullptr, *pa = nullptr, *pd = nullptr;
     const int64_t slots = (int64_t)p.B * ch.n, tokens = (int64_t)p.B * p.T * p.G;
-    hipError_t e = p.ws->take(&bc, (size_t)tokens * 2 * NP * 4);
+    hipError_t e = p.ws->take(&bc, sel_packed(p));
     if (e == hipSuccess && ch.n > 1)
         e = p.ws->take(&ends, (size_t)slots * NP * p.C * 4);
     if (e == hipSuccess && ch.n > 1)
@@ -510,7 +574,10 @@ hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
     const Parts parts{static_cast<float *>(pbc), static_cast<float *>(pa), static_cast<float *>(pd)};
     e = launch_sel_pack(p, m, s);
     if (e == hipSuccess && ch.n > 1) {
-        back_kernel<T, NP><<<dim3((unsigned)passes), 64, 0, s>>>(p, ch, m, en, sm);
+        if (p.z.p)
+            back_kernel<T, NP, true><<<dim3((unsigned)passes), 64, 0, s>>>(p, ch, m, en, sm);
+        else
+            back_kernel<T, NP, false><<<dim3((unsigned)passes), 64, 0, s>>>(p, ch, m, en, sm);
         e = hipGetLastError();
         if (e != hipSuccess)
             return e;
@@ -519,12 +586,14 @@ hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
     }
     if (e != hipSuccess)
         return e;
-    grad_kernel<T, NS, CH><<<dim3((unsigned)groups), kBlk, 0, s>>>(p, ch, m, static_cast<const float *>(kept), en, parts);
+    if (p.z.p)
+        grad_kernel<T, NS, CH, true><<<dim3((unsigned)groups), kBlk, 0, s>>>(p, ch, m, static_cast<const float *>(kept), en, parts);
+    else
+        grad_kernel<T, NS, CH, false><<<dim3((unsigned)groups), kBlk, 0, s>>>(p, ch, m, static_cast<const float *>(kept), en, parts);
     e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    const int64_t sums = (tokens * 2 * NP + kBlk - 1) / kBlk;
-    sum_bc_kernel<T><<<dim3((unsigned)std::min<int64_t>(sums, 65536)), kBlk, 0, s>>>(p, NP, ch.blocks, parts.bc);
+    sum_bc_kernel<T><<<dim3((unsigned)sel_pack_groups(p)), kBlk, 0, s>>>(p, NP, (p.T + kPackTokens - 1) / kPackTokens, ch.blocks, parts.bc);
     e = hipGetLastError();
     if (e != hipSuccess)
         return e;

@@ -22,8 +22,13 @@ __device__ __forceinline__ float softplus(float x)
     return fmaxf(x, 0.f) + (__builtin_amdgcn_logf(w) * kLn2 + (e - (w - 1.f)));
 }
 
-// Step of a token from its entry of dt.
-__device__ __forceinline__ float step_of(float raw, bool soft) { return soft ? softplus(raw) : raw; }
+// The same with its derivative, 1 / (1 + e^-x), which shares e and w.
+__device__ __forceinline__ float softplus(float x, float &grad)
+{
+    const float e = exp2_hw(-fabsf(x) * kLog2e), w = 1.f + e, i = __builtin_amdgcn_rcpf(w);
+    grad = x < 0.f ? e * i : i;
+    return fmaxf(x, 0.f) + (__builtin_amdgcn_logf(w) * kLn2 + (e - (w - 1.f)));
+}
 
 __device__ __forceinline__ int length_of(const SelectiveProblem &p, int b)
 {
@@ -36,6 +41,33 @@ typedef const float __attribute__((address_space(4))) cfloat;
 __device__ __forceinline__ cfloat *constant(const float *p)
 {
     return (cfloat *)(uintptr_t)p;
+}
+
+// A row of a [B][T][C] tensor: a scalar address and a scalar step from token to token in
+// bytes (strides are up to 2^23 elements); a lane adds the offset of its channel, in bytes
+// too, so that an access takes the address as it is.
+template <typename T>
+struct RowAt {
+    const char *p;
+    int step;
+    __device__ __forceinline__ RowAt(const Heads &h, int b, int t)
+        : p(static_cast<const char *>(h.p) + (b * h.sb + t * h.st) * (int64_t)sizeof(T)), step((int)(h.st * (int64_t)sizeof(T)))
+    {
+    }
+    __device__ __forceinline__ void next() { p += step; }
+    __device__ __forceinline__ uint32_t load(uint32_t off) const
+    {
+        if constexpr (sizeof(T) == 2)
+            return *reinterpret_cast<const uint16_t *>(p + off);
+        else
+            return *reinterpret_cast<const uint32_t *>(p + off);
+    }
+    __device__ __forceinline__ void store(uint32_t off, float v) const { store_f(reinterpret_cast<T *>(const_cast<char *>(p) + off), v); }
+};
+template <typename T>
+__device__ __forceinline__ float widened(uint32_t raw)
+{
+    return sizeof(T) == 2 ? bf_lo(raw) : __uint_as_float(raw);
 }
 
 }  // namespace sel

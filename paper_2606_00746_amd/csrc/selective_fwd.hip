@@ -20,19 +20,15 @@ constexpr int kBlk = 256;
 // ---------------------------------------------------------------------------
 
 template <typename T>
-__global__ __launch_bounds__(kBlk) void pack_kernel(SelectiveProblem p, int np, float *bc)
+__global__ __launch_bounds__(kBlk) void pack_kernel(SelectiveProblem p, int np, int parts, float *bc)
 {
-    const int64_t n = (int64_t)p.B * p.T * p.G * 2 * np;
-    for (int64_t i = (int64_t)blockIdx.x * kBlk + threadIdx.x; i < n; i += (int64_t)gridDim.x * kBlk) {
-        const int s = (int)(i % np);
-        int64_t at = i / np;
-        const bool second = at & 1;
-        at >>= 1;
-        const int g = (int)(at % p.G);
-        at /= p.G;
-        const int t = (int)(at % p.T), b = (int)(at / p.T);
-        const Heads &m = second ? p.Cm : p.Bm;
-        bc[i] = s < p.N && t < length_of(p, b) ? load_f(static_cast<const T *>(m.p) + b * m.sb + t * m.st + g * m.sh + s) : 0.f;
+    const int b = (int)(blockIdx.x / (unsigned)parts), t0 = (int)(blockIdx.x % (unsigned)parts) * kPackTokens, row = p.G * 2 * np;
+    const int len = length_of(p, b), n = min(kPackTokens, p.T - t0) * row;
+    float *const to = bc + ((int64_t)b * p.T + t0 + 1) * row;
+    for (int i = threadIdx.x; i < n; i += kBlk) {
+        const int s = i % np, gs = i / np, g = gs % (2 * p.G) / 2, t = t0 + gs / (2 * p.G);
+        const Heads &m = gs & 1 ? p.Cm : p.Bm;
+        to[i] = s < p.N && t < len ? load_f(static_cast<const T *>(m.p) + b * m.sb + t * m.st + g * m.sh + s) : 0.f;
     }
 }
 
@@ -47,106 +43,148 @@ struct Chunks {
 
 // OUT: the outputs, from `starts`, or from the sequence's state where there is one chunk.
 // Otherwise what the chunk adds to its states from zeros, into `starts`, and the sum of
-// its steps.
-template <typename T, int NP, bool OUT>
+// its steps.  Z: with a gate.
+//
+// Rows' addresses are a scalar and the lane's channel; eight tokens are in flight ahead of
+// the eight that are worked on, B of a token one token ahead, and its C from its beginning.
+template <typename T, int NP, bool OUT, bool Z>
 __global__ __launch_bounds__(64) void chunk_kernel(SelectiveProblem p, Chunks ch, const float *bc, float *starts, float *steps, float *kept)
 {
     constexpr int U = kSelKeep;
-    int64_t at = blockIdx.x;
     const int per = p.G * ch.blocks, nch = OUT ? ch.n : ch.n - 1;
-    const int gb = (int)(at % per);
-    at /= per;
-    const int k = (int)(at % nch), b = (int)(at / nch), g = gb / ch.blocks;
-    const int cpg = p.C / p.G, ci = gb % ch.blocks * 64 + threadIdx.x;
-    const bool on = ci < cpg;
-    const int c = g * cpg + min(ci, cpg - 1);
-    const int t0 = k * ch.len, t1 = min(t0 + ch.len, p.T), te = min(t1, length_of(p, b));
-
-    const T *x = static_cast<const T *>(p.x.p) + b * p.x.sb + c;
-    const T *dt = static_cast<const T *>(p.dt.p) + b * p.dt.sb + c;
-    const T *z = p.z.p ? static_cast<const T *>(p.z.p) + b * p.z.sb + c : nullptr;
-    T *y = OUT ? static_cast<T *>(p.y.p) + b * p.y.sb + c : nullptr;
-    const float bias = p.dt_bias ? p.dt_bias[c] : 0.f, skip = OUT && p.D ? p.D[c] : 0.f;
+    const int gb = (int)(blockIdx.x % per), kb = (int)(blockIdx.x / per);
+    const int k = kb % nch, b = kb / nch, g = gb / ch.blocks;
+    const int cpg = p.C / p.G, c0 = gb % ch.blocks * 64;
+    const bool on = c0 + (int)threadIdx.x < cpg;
+    const uint32_t l = g * cpg + (on ? c0 + threadIdx.x : 0), off = l * (uint32_t)sizeof(T);
+    const int t0 = k * ch.len, te = max(t0, min(min(t0 + ch.len, p.T), length_of(p, b)));
+    const bool soft = p.softplus;
+    const float bias = p.dt_bias ? p.dt_bias[l] : 0.f, skip = OUT && p.D ? p.D[l] : 0.f;
     float A2[NP], h[NP], sum = 0.f;
-    const int64_t slot = (((int64_t)b * ch.n + k) * NP) * p.C + c;
+    const int64_t slot = (((int64_t)b * ch.n + k) * NP) * p.C;
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
-        A2[n] = n < p.N ? p.A[(int64_t)c * p.N + n] * kLog2e : 0.f;
+        A2[n] = n < p.N ? p.A[(int64_t)l * p.N + n] * kLog2e : 0.f;
         if (!OUT)
             h[n] = 0.f;
         else if (ch.n > 1)
-            h[n] = starts[slot + (int64_t)n * p.C];
+            h[n] = (starts + slot + (int64_t)n * p.C)[l];
         else
-            h[n] = p.state && n < p.N ? p.state[((int64_t)b * p.C + c) * p.N + n] : 0.f;
+            h[n] = p.state && n < p.N ? p.state[((int64_t)b * p.C + l) * p.N + n] : 0.f;
     }
 
-    Raw<T, 1> xr[U], dr[U], zr[U];
-    const auto fetch = [&](int t) {
+    // the B behind the last token is read too (the buffer has room)
+    cfloat *m = constant(bc) + (((int64_t)b * p.T + t0 + 1) * p.G + g) * 2 * NP;
+    const int mstep = p.G * 2 * NP;
+    float Bt[NP];
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const bool live = t + i < te;
-            xr[i] = live ? load_raw<T, 1>(x + (int64_t)(t + i) * p.x.st) : zero_raw<T, 1>();
-            dr[i] = live ? load_raw<T, 1>(dt + (int64_t)(t + i) * p.dt.st) : zero_raw<T, 1>();
-            if (OUT)
-                zr[i] = live && z ? load_raw<T, 1>(z + (int64_t)(t + i) * p.z.st) : zero_raw<T, 1>();
-        }
-    };
-    fetch(t0);
-    cfloat *m = constant(bc) + (((int64_t)b * p.T + t0) * p.G + g) * 2 * NP;
-    int t = t0;
-    for (; t < te; t += U) {
-        if (OUT && kept && on) {
-            float *to = kept + (((int64_t)b * ((p.T + U - 1) / U) + t / U) * NP) * p.C + c;
+    for (int n = 0; n < NP; ++n)
+        Bt[n] = m[n];
+    const auto token = [&](uint32_t xr, uint32_t dr, uint32_t zr, const RowAt<T> &to) {
+        float next[NP], Ct[NP];
+        if (OUT)
 #pragma unroll
             for (int n = 0; n < NP; ++n)
-                to[(int64_t)n * p.C] = h[n];
-        }
-        Raw<T, 1> xc[U], dc[U], zc[U];
+                Ct[n] = m[NP + n];
+        m += mstep;
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            xc[i] = xr[i], dc[i] = dr[i];
-            if (OUT)
-                zc[i] = zr[i];
-        }
-        fetch(t + U);
+        for (int n = 0; n < NP; ++n)
+            next[n] = m[n];
+        step_fence();
+        const float xv = widened<T>(xr), raw = widened<T>(dr) + bias, sp = softplus(raw), d = soft ? sp : raw, u = d * xv;
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            if (t + i >= te)
-                break;
-            const float xv = get(xc[i], 0), raw = get(dc[i], 0) + bias;
-            const float d = p.softplus ? softplus(raw) : raw, u = d * xv;
+        for (int n = 0; n < NP; ++n)
+            h[n] = fmaf(exp2_hw(d * A2[n]), h[n], u * Bt[n]);
+        if (OUT) {
+            float gate = 1.f;
+            if (Z)
+                gate = silu(widened<T>(zr));
+            step_fence();
             float out = skip * xv;
-            if (!OUT)
-                sum += d;
 #pragma unroll
-            for (int n = 0; n < NP; ++n) {
-                h[n] = fmaf(exp2_hw(d * A2[n]), h[n], u * m[n]);
-                if (OUT)
-                    out = fmaf(m[NP + n], h[n], out);
-            }
-            m += p.G * 2 * NP;
-            if (OUT) {
-                if (z)
-                    out *= silu(get(zc[i], 0));
-                if (on)
-                    store_f(y + (int64_t)(t + i) * p.y.st, out);
-            }
+            for (int n = 0; n < NP; ++n)
+                out = fmaf(Ct[n], h[n], out);
+            if (Z)
+                out *= gate;
+            if (on)
+                to.store(off, out);
+        } else {
+            sum += d;
+        }
+        step_fence();
+#pragma unroll
+        for (int n = 0; n < NP; ++n)
+            Bt[n] = next[n];
+    };
+
+    RowAt<T> x(p.x, b, t0), dt(p.dt, b, t0), z(Z ? p.z : p.x, b, t0), y(OUT ? p.y : p.x, b, t0);
+    const int64_t keep_step = (int64_t)NP * p.C;
+    float *keep = kept;
+    if (OUT && kept)
+        keep += ((int64_t)b * ((p.T + U - 1) / U) + t0 / U) * keep_step;
+    const auto put_states = [&]() {
+        if (OUT && kept) {
+            if (on)
+#pragma unroll
+                for (int n = 0; n < NP; ++n)
+                    (keep + (int64_t)n * p.C)[l] = h[n];
+            keep += keep_step;
+        }
+    };
+    const int full = (te - t0) / U;
+    uint32_t xr[U], dr[U], zr[U];
+    const auto fetch = [&]() {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            xr[i] = x.load(off), dr[i] = dt.load(off), zr[i] = OUT && Z ? z.load(off) : 0;
+            x.next(), dt.next();
+            if (OUT && Z)
+                z.next();
+        }
+    };
+    if (full > 0)
+        fetch();
+    for (int blk = 0; blk < full; ++blk) {
+        uint32_t xc[U], dc[U], zc[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            xc[i] = xr[i], dc[i] = dr[i], zc[i] = zr[i];
+        if (blk + 1 < full)
+            fetch();
+        put_states();   // behind the loads, whose waits are not for these stores then
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            token(xc[i], dc[i], zc[i], y);
+            if (OUT)
+                y.next();
         }
     }
+    int t = t0 + full * U;
+    if (t < te)
+        put_states();
+    for (; t < te; ++t) {
+        token(x.load(off), dt.load(off), OUT && Z ? z.load(off) : 0, y);
+        x.next(), dt.next();
+        if (OUT && Z)
+            z.next();
+        if (OUT)
+            y.next();
+    }
+    if (!on)
+        return;
     if (OUT) {
-        if (on)
-            for (t = max(te, t0); t < t1; ++t)
-                store_f(y + (int64_t)t * p.y.st, 0.f);
-        if (k == ch.n - 1 && p.state_out && on)
+        for (; t < min(t0 + ch.len, p.T); ++t, y.next())
+            y.store(off, 0.f);
+        if (k == ch.n - 1 && p.state_out)
 #pragma unroll
             for (int n = 0; n < NP; ++n)
                 if (n < p.N)
-                    p.state_out[((int64_t)b * p.C + c) * p.N + n] = h[n];
-    } else if (on) {
+                    p.state_out[((int64_t)b * p.C + l) * p.N + n] = h[n];
+    } else {
 #pragma unroll
         for (int n = 0; n < NP; ++n)
-            starts[slot + (int64_t)n * p.C] = h[n];
-        steps[((int64_t)b * ch.n + k) * p.C + c] = sum;
+            (starts + slot + (int64_t)n * p.C)[l] = h[n];
+        steps[((int64_t)b * ch.n + k) * p.C + l] = sum;
     }
 }
 
@@ -163,7 +201,7 @@ __global__ __launch_bounds__(kBlk) void chain_kernel(SelectiveProblem p, Chunks 
     const int64_t step = (int64_t)NP * p.C;
     float *at = starts + (int64_t)b * ch.n * step + (int64_t)n * p.C + c;
     const float *s = steps + (int64_t)b * ch.n * p.C + c;
-    constexpr int U = 8;
+    constexpr int U = 32;   // chunks in flight
     for (int k = 0; k < ch.n; k += U) {
         float add[U], sum[U];
 #pragma unroll
@@ -254,8 +292,8 @@ __global__ __launch_bounds__(kBlk) void token_kernel(SelectiveProblem p)
 }
 
 // Waves that the chunks of a call are cut for, and a chunk's fewest tokens.
-constexpr int64_t kWaves = 4096;
-constexpr int kLeast = 32;
+constexpr int64_t kWaves = 8192;
+constexpr int kLeast = 16;
 
 Chunks chunks_of(const SelectiveProblem &p)
 {
@@ -282,10 +320,10 @@ hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
     }
     const Chunks ch = chunks_of(p);
     const int64_t waves = (int64_t)p.B * p.G * ch.blocks * ch.n, joins = ((int64_t)p.B * NP * p.C + kBlk - 1) / kBlk;
-    if (waves * 64 > kMaxThreads || joins * kBlk > kMaxThreads)
+    if (waves * 64 > kMaxThreads || joins * kBlk > kMaxThreads || sel_pack_groups(p) * kBlk > kMaxThreads)
         return hipErrorInvalidConfiguration;
     void *bc = nullptr, *starts = nullptr, *steps = nullptr, *kept = nullptr;
-    hipError_t e = p.ws->take(&bc, (size_t)p.B * p.T * p.G * 2 * NP * 4);
+    hipError_t e = p.ws->take(&bc, sel_packed(p));
     if (e == hipSuccess && ch.n > 1)
         e = p.ws->take(&starts, (size_t)p.B * ch.n * NP * p.C * 4);
     if (e == hipSuccess && ch.n > 1)
@@ -297,7 +335,7 @@ hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
     float *const m = static_cast<float *>(bc), *const st = static_cast<float *>(starts), *const sm = static_cast<float *>(steps);
     e = launch_sel_pack(p, m, s);
     if (e == hipSuccess && ch.n > 1) {
-        chunk_kernel<T, NP, false><<<dim3((unsigned)(waves / ch.n * (ch.n - 1))), 64, 0, s>>>(p, ch, m, st, sm, nullptr);
+        chunk_kernel<T, NP, false, false><<<dim3((unsigned)(waves / ch.n * (ch.n - 1))), 64, 0, s>>>(p, ch, m, st, sm, nullptr);
         e = hipGetLastError();
         if (e != hipSuccess)
             return e;
@@ -306,7 +344,10 @@ hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
     }
     if (e != hipSuccess)
         return e;
-    chunk_kernel<T, NP, true><<<dim3((unsigned)waves), 64, 0, s>>>(p, ch, m, st, sm, static_cast<float *>(kept));
+    if (p.z.p)
+        chunk_kernel<T, NP, true, true><<<dim3((unsigned)waves), 64, 0, s>>>(p, ch, m, st, sm, static_cast<float *>(kept));
+    else
+        chunk_kernel<T, NP, true, false><<<dim3((unsigned)waves), 64, 0, s>>>(p, ch, m, st, sm, static_cast<float *>(kept));
     return hipGetLastError();
 }
 
@@ -328,13 +369,12 @@ hipError_t pick(const SelectiveProblem &p, hipStream_t s)
 
 hipError_t launch_sel_pack(const SelectiveProblem &p, float *bc, hipStream_t s)
 {
-    const int np = sel_states(p);
-    const int64_t n = ((int64_t)p.B * p.T * p.G * 2 * np + kBlk - 1) / kBlk;
-    const unsigned grid = (unsigned)std::min<int64_t>(n, 65536);
+    const int np = sel_states(p), parts = (p.T + kPackTokens - 1) / kPackTokens;
+    const unsigned grid = (unsigned)sel_pack_groups(p);
     if (p.dtype == 0)
-        pack_kernel<float><<<grid, kBlk, 0, s>>>(p, np, bc);
+        pack_kernel<float><<<grid, kBlk, 0, s>>>(p, np, parts, bc);
     else
-        pack_kernel<bf16_t><<<grid, kBlk, 0, s>>>(p, np, bc);
+        pack_kernel<bf16_t><<<grid, kBlk, 0, s>>>(p, np, parts, bc);
     return hipGetLastError();
 }
 

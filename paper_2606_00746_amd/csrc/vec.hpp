@@ -126,10 +126,12 @@ __device__ __forceinline__ void store_all(bf16_t *p, const float (&f)[V])
     }
 }
 
+// x of another lane of the same 16, all of which are there (with bound_ctrl the compiler
+// makes it part of the addition that takes it).
 template <int CTRL>
 __device__ __forceinline__ float dpp(float x)
 {
-    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, false));
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
 }
 constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
 
@@ -152,6 +154,15 @@ __device__ __forceinline__ float lanes_sum(float v, int n)
     return v;
 }
 
+// b in the lanes of a mask, a in the others (a branch around what forms b costs more).
+__device__ __forceinline__ float in_lanes(float a, float b, uint64_t mask)
+{
+    float r;
+    asm("v_cndmask_b32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(mask));
+    return r;
+}
+constexpr uint64_t kOddLanes = 0xAAAAAAAAAAAAAAAAull, kOddPairs = 0xCCCCCCCCCCCCCCCCull;
+
 // x sigmoid(x) and its derivative; -inf gives 0 (not NaN) in both.
 __device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
 __device__ __forceinline__ float silu(float x)
@@ -163,6 +174,13 @@ __device__ __forceinline__ float silu_grad(float x)
 {
     const float s = logistic(x), m = s * (1.f - s);
     return m == 0.f ? s : fmaf(x, m, s);
+}
+// Both.
+__device__ __forceinline__ float silu(float x, float &grad)
+{
+    const float s = logistic(x), m = s * (1.f - s);
+    grad = m == 0.f ? s : fmaf(x, m, s);
+    return s == 0.f ? 0.f : x * s;
 }
 
 }  // namespace vec
