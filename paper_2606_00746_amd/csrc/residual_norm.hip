@@ -27,6 +27,19 @@ using namespace vec;
 struct Shape {
     int lanes, per;        // per: rows that a workgroup has at once
     int runs;              // 16-byte (bf16) runs of a row
+    int step_b, step_t;    // from a group's row to its next
+};
+
+// A row of a group: its sequence and token.
+struct At {
+    int b, t;
+    __device__ __forceinline__ At(int64_t row, int T) : b((int)(row / T)), t((int)(row % T)) {}
+    __device__ __forceinline__ void next(const Shape &s, int T)
+    {
+        b += s.step_b, t += s.step_t;
+        if (t >= T)
+            t -= T, ++b;
+    }
 };
 
 // Sum over the group's lanes.  WIDE: the group is the workgroup, whose waves exchange
@@ -58,6 +71,15 @@ __device__ __forceinline__ void load_row(const T *p, int lane, int lanes, int ru
     for (int k = 0; k < P; ++k) {
         const int at = lane + k * lanes;
         widen_all(p && at < runs ? load_raw<T, 8>(p + 8 * at) : zero_raw<T, 8>(), v[k]);
+    }
+}
+template <typename T, int P>
+__device__ __forceinline__ void load_raws(const T *p, int lane, int lanes, int runs, Raw<T, 8> (&v)[P])
+{
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+        const int at = lane + k * lanes;
+        v[k] = p && at < runs ? load_raw<T, 8>(p + 8 * at) : zero_raw<T, 8>();
     }
 }
 template <typename T, int P>
@@ -121,9 +143,8 @@ __global__ __launch_bounds__(BLK) void join_fwd_kernel(JoinProblem p, Shape s)
     __shared__ float cell[2][16];
     int turn = 0;
     const int lane = threadIdx.x % s.lanes, grp = threadIdx.x / s.lanes;
-    const int64_t rows = (int64_t)p.B * p.T;
-    for (int64_t row = (int64_t)blockIdx.x * s.per + grp; row < rows; row += (int64_t)gridDim.x * s.per) {
-        const int b = (int)(row / p.T), t = (int)(row % p.T);
+    for (At at((int64_t)blockIdx.x * s.per + grp, p.T); at.b < p.B; at.next(s, p.T)) {
+        const int b = at.b, t = at.t;
         float r[P][8], f[P][8];
         load_row<R, P>(static_cast<const R *>(p.r.p) + b * p.r.sb + t * p.r.st, lane, s.lanes, s.runs, r);
         if (p.f.p) {
@@ -157,61 +178,78 @@ __global__ __launch_bounds__(BLK) void join_bwd_kernel(JoinProblem p, Shape s, f
     __shared__ float cell[2][16];
     __shared__ float sums[WIDE ? 1 : 256 * 8];
     int turn = 0;
-    const int lane = threadIdx.x % s.lanes, grp = threadIdx.x / s.lanes;
-    const int64_t rows = p.gate ? p.T : (int64_t)p.B * p.T, first = p.gate ? (int64_t)blockIdx.y * p.T : 0;
-    float q[P][8] = {}, dw[P][8] = {};
-    for (int64_t at = (int64_t)blockIdx.x * s.per + grp; at < rows; at += (int64_t)gridDim.x * s.per) {
-        const int64_t row = first + at;
-        const int b = (int)(row / p.T), t = (int)(row % p.T);
-        float r[P][8], g[P][8], f[P][8];
-        load_row<R, P>(static_cast<const R *>(p.r.p) + b * p.r.sb + t * p.r.st, lane, s.lanes, s.runs, r);
-        load_row<T, P>(static_cast<const T *>(p.dy.p) + b * p.dy.sb + t * p.dy.st, lane, s.lanes, s.runs, g);
-        load_row<T, P>(p.f.p ? static_cast<const T *>(p.f.p) + b * p.f.sb + t * p.f.st : nullptr, lane, s.lanes, s.runs, f);
+    const int lane = threadIdx.x % s.lanes, grp = threadIdx.x / s.lanes, end = p.gate ? blockIdx.y + 1 : p.B;
+    float q[P][8] = {}, dw[P][8] = {}, k[P][8];
+    // what takes g to the gradient of n_f (or f), the same for all of the workgroup's rows
+#pragma unroll
+    for (int j = 0; j < P; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            k[j][e] = 1.f;
+    times<T, P>(p.gate, (int64_t)blockIdx.y * p.C, lane, s.lanes, s.runs, k);
+    times<T, P>(p.scale, 0, lane, s.lanes, s.runs, k);
+    times<T, P>(p.w_post, 0, lane, s.lanes, s.runs, k);
+    Raw<T, 8> w[P];
+    load_raws<T, P>(static_cast<const T *>(p.w), lane, s.lanes, s.runs, w);
+    for (At at((int64_t)blockIdx.x * s.per + grp + (p.gate ? (int64_t)blockIdx.y * p.T : 0), p.T); at.b < end; at.next(s, p.T)) {
+        const int b = at.b, t = at.t;
+        // all of a row's loads ahead of its sums
+        Raw<R, 8> rr[P], ro[P];
+        Raw<T, 8> ry[P], rf[P];
+        load_raws<R, P>(static_cast<const R *>(p.r.p) + b * p.r.sb + t * p.r.st, lane, s.lanes, s.runs, rr);
+        load_raws<T, P>(static_cast<const T *>(p.dy.p) + b * p.dy.sb + t * p.dy.st, lane, s.lanes, s.runs, ry);
+        load_raws<T, P>(p.f.p ? static_cast<const T *>(p.f.p) + b * p.f.sb + t * p.f.st : nullptr, lane, s.lanes, s.runs, rf);
+        load_raws<R, P>(p.dro.p ? static_cast<const R *>(p.dro.p) + b * p.dro.sb + t * p.dro.st : nullptr, lane, s.lanes, s.runs, ro);
+        step_fence();
+        float r[P][8], g[P][8];
+#pragma unroll
+        for (int j = 0; j < P; ++j)
+            widen_all(rr[j], r[j]), widen_all(ry[j], g[j]);
         const float ir = inverse_rms(row_sum<WIDE>(dot(r, r), s.lanes, cell, turn), p);
-        scaled(r, ir);
 #pragma unroll
-        for (int k = 0; k < P; ++k)
+        for (int j = 0; j < P; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                dw[k][e] = fmaf(g[k][e], r[k][e], dw[k][e]);
-        times<T, P>(p.w, 0, lane, s.lanes, s.runs, g);
+            for (int e = 0; e < 8; ++e) {
+                r[j][e] *= ir;
+                dw[j][e] = fmaf(g[j][e], r[j][e], dw[j][e]);
+                if (p.w)
+                    g[j][e] *= get(w[j], e);
+            }
         const float mr = row_sum<WIDE>(dot(g, r), s.lanes, cell, turn) / (float)p.C;
 #pragma unroll
-        for (int k = 0; k < P; ++k)
+        for (int j = 0; j < P; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                g[k][e] = ir * (g[k][e] - r[k][e] * mr);
-        if (p.dro.p) {
-            load_row<R, P>(static_cast<const R *>(p.dro.p) + b * p.dro.sb + t * p.dro.st, lane, s.lanes, s.runs, r);
-#pragma unroll
-            for (int k = 0; k < P; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    g[k][e] += r[k][e];
-        }
+            for (int e = 0; e < 8; ++e) {
+                g[j][e] = ir * (g[j][e] - r[j][e] * mr);
+                if (p.dro.p)
+                    g[j][e] += get(ro[j], e);
+            }
         store_row<R, P>(static_cast<R *>(p.dr.p) + b * p.dr.sb + t * p.dr.st, lane, s.lanes, s.runs, g);
         if (!p.f.p)
             continue;
+        float(&f)[P][8] = r;
+#pragma unroll
+        for (int j = 0; j < P; ++j)
+            widen_all(rf[j], f[j]);
         float i = 0.f;
         if (p.w_post) {
             i = inverse_rms(row_sum<WIDE>(dot(f, f), s.lanes, cell, turn), p);
             scaled(f, i);
         }
 #pragma unroll
-        for (int k = 0; k < P; ++k)
+        for (int j = 0; j < P; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                q[k][e] = fmaf(g[k][e], f[k][e], q[k][e]);
-        times<T, P>(p.gate, (int64_t)b * p.C, lane, s.lanes, s.runs, g);
-        times<T, P>(p.scale, 0, lane, s.lanes, s.runs, g);
+            for (int e = 0; e < 8; ++e) {
+                q[j][e] = fmaf(g[j][e], f[j][e], q[j][e]);
+                g[j][e] *= k[j][e];
+            }
         if (p.w_post) {
-            times<T, P>(p.w_post, 0, lane, s.lanes, s.runs, g);
             const float m = row_sum<WIDE>(dot(g, f), s.lanes, cell, turn) / (float)p.C;
 #pragma unroll
-            for (int k = 0; k < P; ++k)
+            for (int j = 0; j < P; ++j)
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    g[k][e] = i * (g[k][e] - f[k][e] * m);
+                    g[j][e] = i * (g[j][e] - f[j][e] * m);
         }
         store_row<T, P>(static_cast<T *>(p.df.p) + b * p.df.sb + t * p.df.st, lane, s.lanes, s.runs, g);
     }
@@ -345,6 +383,14 @@ Shape shape_of(const JoinProblem &p, int most)
     while (s.lanes < 1024 && s.runs > s.lanes * most)
         s.lanes *= 4;
     s.per = std::max(256, s.lanes) / s.lanes;
+    s.step_b = s.step_t = 0;
+    return s;
+}
+
+Shape stepping(Shape s, int64_t groups, int T)
+{
+    s.step_b = (int)(groups * s.per / T);
+    s.step_t = (int)(groups * s.per % T);
     return s;
 }
 
@@ -357,7 +403,7 @@ hipError_t fwd(const JoinProblem &p, const Shape &s, hipStream_t st)
     if (p.ws->counting)
         return hipSuccess;
     const int64_t n = std::min(((int64_t)p.B * p.T + s.per - 1) / s.per, kFwdBlocks);
-    join_fwd_kernel<T, R, P, BLK, WIDE><<<dim3((unsigned)n), BLK, 0, st>>>(p, s);
+    join_fwd_kernel<T, R, P, BLK, WIDE><<<dim3((unsigned)n), BLK, 0, st>>>(p, stepping(s, n, p.T));
     return hipGetLastError();
 }
 
@@ -375,7 +421,7 @@ hipError_t bwd(const JoinProblem &p, const Shape &s, hipStream_t st)
         e = p.ws->take(&each, (size_t)(seqs * 2 * p.C * 4));
     if (e != hipSuccess || p.ws->counting)
         return e;
-    join_bwd_kernel<T, R, P, BLK, WIDE><<<dim3((unsigned)n, (unsigned)seqs), BLK, 0, st>>>(p, s, static_cast<float *>(part));
+    join_bwd_kernel<T, R, P, BLK, WIDE><<<dim3((unsigned)n, (unsigned)seqs), BLK, 0, st>>>(p, stepping(s, n, p.T), static_cast<float *>(part));
     e = hipGetLastError();
     if (e != hipSuccess || !sums)
         return e;
@@ -391,8 +437,9 @@ hipError_t bwd(const JoinProblem &p, const Shape &s, hipStream_t st)
 template <typename T, typename R, bool BWD, int P>
 hipError_t pick(const JoinProblem &p, const Shape &s, hipStream_t st)
 {
-    if (s.lanes > 256)
-        return BWD ? bwd<T, R, P, 1024, true>(p, s, st) : fwd<T, R, P, 1024, true>(p, s, st);
+    if constexpr (P * 8 * 1024 <= kJoinMaxRow)   // what rows of more than 256 lanes can take
+        if (s.lanes > 256)
+            return BWD ? bwd<T, R, P, 1024, true>(p, s, st) : fwd<T, R, P, 1024, true>(p, s, st);
     if (s.lanes > 64)
         return BWD ? bwd<T, R, P, 256, true>(p, s, st) : fwd<T, R, P, 256, true>(p, s, st);
     return BWD ? bwd<T, R, P, 256, false>(p, s, st) : fwd<T, R, P, 256, false>(p, s, st);

@@ -21,8 +21,9 @@ using namespace vec;
 
 constexpr int kBlk = 256;
 
-// How a call's channels and tokens lie on threads: PB runs of V channels by SB segments
-// of L tokens a workgroup.
+// How a call's channels and tokens lie on threads.  Forward: run after run of V channels,
+// segment after segment.  Backward, whose workgroups add up the shares of a channel: pb runs
+// by sb segments a workgroup.
 struct Shape {
     int runs, pb, sb, segs;   // runs of a row; of a workgroup; segments of a workgroup, of a sequence
     int len;                  // tokens of a segment
@@ -30,15 +31,22 @@ struct Shape {
     bool fits;
 };
 
-Shape shape_of(const ConvProblem &p, int V, int len)
+Shape shape_of(const ConvProblem &p, int V, int len, bool bwd)
 {
     Shape s;
     s.runs = p.C / V;
+    s.segs = (p.T + len - 1) / len;
+    s.len = len;
+    if (!bwd) {
+        const int64_t n = ((int64_t)p.B * s.segs * s.runs + kBlk - 1) / kBlk;
+        s.pb = s.sb = 0;
+        s.fits = n * kBlk <= kMaxThreads;
+        s.grid = dim3((unsigned)n);
+        return s;
+    }
     const int cols = (s.runs + 63) / 64;
     s.pb = (s.runs + cols - 1) / cols;
     s.sb = kBlk / s.pb;
-    s.len = len;
-    s.segs = (p.T + len - 1) / len;
     const int64_t rows = ((int64_t)p.B * s.segs + s.sb - 1) / s.sb;
     // rows vary along x, whose limit is the larger one
     s.fits = rows * cols * kBlk <= kMaxThreads && cols <= 65535;
@@ -95,13 +103,11 @@ constexpr int kAhead = 8;
 template <typename T, int V, int K>
 __global__ __launch_bounds__(kBlk) void conv_fwd_kernel(ConvProblem p, Shape s)
 {
-    const int pc = threadIdx.x % s.pb, sl = threadIdx.x / s.pb;
-    const int run = blockIdx.y * s.pb + pc;
-    const int64_t seg = (int64_t)blockIdx.x * s.sb + sl;
-    if (sl >= s.sb || run >= s.runs || seg >= (int64_t)p.B * s.segs)
+    const unsigned item = blockIdx.x * (unsigned)kBlk + threadIdx.x, seg = item / (unsigned)s.runs;
+    if (seg >= (uint64_t)p.B * s.segs)
         return;
-    const int b = (int)(seg / s.segs), t0 = (int)(seg % s.segs) * s.len, t1 = min(t0 + s.len, p.T), c = run * V;
-    const int n = length_of(p, b);
+    const int b = (int)(seg / (unsigned)s.segs), t0 = (int)(seg % (unsigned)s.segs) * s.len, t1 = min(t0 + s.len, p.T);
+    const int n = length_of(p, b), c = (int)(item % (unsigned)s.runs) * V;
     const T *x = static_cast<const T *>(p.x.p) + b * p.x.sb + c;
     T *y = static_cast<T *>(p.y.p) + b * p.y.sb + c;
 
@@ -301,6 +307,9 @@ __global__ __launch_bounds__(16 * kSumRows) void conv_dw_kernel(ConvProblem p, c
     }
 }
 
+// Channels of a thread: forward 8 where the taps leave registers for them (8 x 4096 tokens of
+// 1536 channels, bf16, us: 41 and 44 with 4; 32 x 5476 of 1152 176 and 235), backward 4 (97
+// with 8, 75 with 4, for the waves that fewer registers allow).
 // Tokens of a thread's segment: many, so that few are read twice, but fewer where that
 // leaves the card with few threads.
 constexpr int64_t kFewThreads = 128 * 1024;
@@ -316,7 +325,7 @@ template <typename T, int K>
 hipError_t fwd(const ConvProblem &p, hipStream_t s)
 {
     constexpr int V = K <= 4 ? 8 : 4;
-    const Shape sh = shape_of(p, V, segment(p, V, 64));
+    const Shape sh = shape_of(p, V, segment(p, V, 32), false);
     if (!sh.fits)
         return hipErrorInvalidConfiguration;
     if (p.ws->counting)
@@ -328,8 +337,8 @@ hipError_t fwd(const ConvProblem &p, hipStream_t s)
 template <typename T, int K>
 hipError_t bwd(const ConvProblem &p, hipStream_t s)
 {
-    constexpr int V = K <= 4 ? 8 : 4;
-    const Shape sh = shape_of(p, V, segment(p, V, 64));
+    constexpr int V = 4;
+    const Shape sh = shape_of(p, V, segment(p, V, 64), true);
     if (!sh.fits)
         return hipErrorInvalidConfiguration;
     void *part = nullptr;
