@@ -21,7 +21,8 @@ SELECTIVE_FWD, SELECTIVE_FWD_TRAIN, SELECTIVE_BWD_RESERVE = 0, 1, 2
 
 def _elsewhere(t):
     """Whether t is on another GPU than the current one, which a call then has to be for."""
-    return t.get_device() not in (-1, _current_device())
+    dev = t.get_device()
+    return dev >= 0 and dev != _current_device()
 
 
 def _on(call, args, first):
