@@ -53,32 +53,38 @@ __global__ __launch_bounds__(64) void back_kernel(SelectiveProblem p, Chunks ch,
         A2[n] = n < p.N ? p.A[(int64_t)l * p.N + n] * kLog2e : 0.f;
         G[n] = 0.f;
     }
-    // C of a token, from the last on; the one ahead of the first is read too
+    // C from the last token on, a part of the states at a time, as B and C in the forward; a
+    // token's ahead of the first is read too
+    constexpr int P = NP < 16 ? NP : 16;
     const int mstep = p.G * 2 * NP;
     cfloat *m = constant(bc) + ((((int64_t)b * p.T + te) * p.G + g) * 2 + 1) * NP;
-    float Ct[NP];
+    float Ct[P];
 #pragma unroll
-    for (int n = 0; n < NP; ++n)
+    for (int n = 0; n < P; ++n)
         Ct[n] = m[n];
     const auto token = [&](uint32_t dr, uint32_t zr, uint32_t yr) {
-        float next[NP];
-        m -= mstep;
-#pragma unroll
-        for (int n = 0; n < NP; ++n)
-            next[n] = m[n];
-        step_fence();
         const float raw = widened<T>(dr) + bias, sp = softplus(raw), d = soft ? sp : raw;
         float up = widened<T>(yr);
         if (Z)
             up *= silu(widened<T>(zr));
         sum += d;
 #pragma unroll
-        for (int n = 0; n < NP; ++n)
-            G[n] = exp2_hw(d * A2[n]) * fmaf(Ct[n], up, G[n]);
-        step_fence();
+        for (int q = 0; q < NP; q += P) {
+            float nC[P];
+            cfloat *const next = q + P < NP ? m + q + P : m - mstep;
 #pragma unroll
-        for (int n = 0; n < NP; ++n)
-            Ct[n] = next[n];
+            for (int n = 0; n < P; ++n)
+                nC[n] = next[n];
+            step_fence();
+#pragma unroll
+            for (int n = 0; n < P; ++n)
+                G[q + n] = exp2_hw(d * A2[q + n]) * fmaf(Ct[n], up, G[q + n]);
+            step_fence();
+#pragma unroll
+            for (int n = 0; n < P; ++n)
+                Ct[n] = nC[n];
+        }
+        m -= mstep;
     };
     const int last = max(te - 1, t0);
     RowAt<T> dt(p.dt, b, last), z(Z ? p.z : p.dt, b, last), dy(p.dy, b, last);

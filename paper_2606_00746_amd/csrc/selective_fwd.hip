@@ -43,11 +43,13 @@ struct Chunks {
 
 // OUT: the outputs, from `starts`, or from the sequence's state where there is one chunk.
 // Otherwise what the chunk adds to its states from zeros, into `starts`, and the sum of
-// its steps.  Z: with a gate.
+// its steps.  Z: with a gate.  KEEP: with the states of every kSelKeep-th token.
 //
 // Rows' addresses are a scalar and the lane's channel; eight tokens are in flight ahead of
-// the eight that are worked on, B of a token one token ahead, and its C from its beginning.
-template <typename T, int NP, bool OUT, bool Z>
+// the eight that are worked on, B and C of a token one token ahead: they are what the scalar
+// registers hold, and loads from its beginning come too late (64 x 64, us: C from the token's
+// beginning 281, a token ahead 255).
+template <typename T, int NP, bool OUT, bool Z, bool KEEP>
 __global__ __launch_bounds__(64) void chunk_kernel(SelectiveProblem p, Chunks ch, const float *bc, float *starts, float *steps, float *kept)
 {
     constexpr int U = kSelKeep;
@@ -73,57 +75,56 @@ __global__ __launch_bounds__(64) void chunk_kernel(SelectiveProblem p, Chunks ch
             h[n] = p.state && n < p.N ? p.state[((int64_t)b * p.C + l) * p.N + n] : 0.f;
     }
 
-    // the B behind the last token is read too (the buffer has room)
+    // B and C of the states of a part, the next part's asked for ahead of it: 16 states are what
+    // the scalar registers hold twice.  A token's behind the last is read too (the buffer has
+    // room).
+    constexpr int P = NP < 16 ? NP : 16;
     cfloat *m = constant(bc) + (((int64_t)b * p.T + t0 + 1) * p.G + g) * 2 * NP;
     const int mstep = p.G * 2 * NP;
-    float Bt[NP];
+    float Bt[P], Ct[P];
 #pragma unroll
-    for (int n = 0; n < NP; ++n)
-        Bt[n] = m[n];
+    for (int n = 0; n < P; ++n)
+        Bt[n] = m[n], Ct[n] = OUT ? m[NP + n] : 0.f;
     const auto token = [&](uint32_t xr, uint32_t dr, uint32_t zr, const RowAt<T> &to) {
-        float next[NP], Ct[NP];
-        if (OUT)
-#pragma unroll
-            for (int n = 0; n < NP; ++n)
-                Ct[n] = m[NP + n];
-        m += mstep;
-#pragma unroll
-        for (int n = 0; n < NP; ++n)
-            next[n] = m[n];
-        step_fence();
         const float xv = widened<T>(xr), raw = widened<T>(dr) + bias, sp = softplus(raw), d = soft ? sp : raw, u = d * xv;
-#pragma unroll
-        for (int n = 0; n < NP; ++n)
-            h[n] = fmaf(exp2_hw(d * A2[n]), h[n], u * Bt[n]);
-        if (OUT) {
-            float gate = 1.f;
-            if (Z)
-                gate = silu(widened<T>(zr));
-            step_fence();
-            float out = skip * xv;
-#pragma unroll
-            for (int n = 0; n < NP; ++n)
-                out = fmaf(Ct[n], h[n], out);
-            if (Z)
-                out *= gate;
-            if (on)
-                to.store(off, out);
-        } else {
+        float out = skip * xv;
+        if (!OUT)
             sum += d;
-        }
-        step_fence();
 #pragma unroll
-        for (int n = 0; n < NP; ++n)
-            Bt[n] = next[n];
+        for (int q = 0; q < NP; q += P) {
+            float nB[P], nC[P];
+            cfloat *const next = q + P < NP ? m + q + P : m + mstep;
+#pragma unroll
+            for (int n = 0; n < P; ++n)
+                nB[n] = next[n], nC[n] = OUT ? next[NP + n] : 0.f;
+            step_fence();
+#pragma unroll
+            for (int n = 0; n < P; ++n) {
+                h[q + n] = fmaf(exp2_hw(d * A2[q + n]), h[q + n], u * Bt[n]);
+                if (OUT)
+                    out = fmaf(Ct[n], h[q + n], out);
+            }
+            if (OUT && q + P == NP) {
+                if (Z)
+                    out *= silu(widened<T>(zr));
+                if (on)
+                    to.store(off, out);
+            }
+            step_fence();
+#pragma unroll
+            for (int n = 0; n < P; ++n)
+                Bt[n] = nB[n], Ct[n] = nC[n];
+        }
+        m += mstep;
     };
 
     RowAt<T> x(p.x, b, t0), dt(p.dt, b, t0), z(Z ? p.z : p.x, b, t0), y(OUT ? p.y : p.x, b, t0);
     const int64_t keep_step = (int64_t)NP * p.C;
     float *keep = kept;
-    if (OUT && kept)
+    if (KEEP)
         keep += ((int64_t)b * ((p.T + U - 1) / U) + t0 / U) * keep_step;
     const auto put_states = [&]() {
-        if (OUT && kept) {
+        if (KEEP) {
             if (on)
 #pragma unroll
                 for (int n = 0; n < NP; ++n)
@@ -335,7 +336,7 @@ hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
     float *const m = static_cast<float *>(bc), *const st = static_cast<float *>(starts), *const sm = static_cast<float *>(steps);
     e = launch_sel_pack(p, m, s);
     if (e == hipSuccess && ch.n > 1) {
-        chunk_kernel<T, NP, false, false><<<dim3((unsigned)(waves / ch.n * (ch.n - 1))), 64, 0, s>>>(p, ch, m, st, sm, nullptr);
+        chunk_kernel<T, NP, false, false, false><<<dim3((unsigned)(waves / ch.n * (ch.n - 1))), 64, 0, s>>>(p, ch, m, st, sm, nullptr);
         e = hipGetLastError();
         if (e != hipSuccess)
             return e;
@@ -344,10 +345,20 @@ hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
     }
     if (e != hipSuccess)
         return e;
+    const dim3 grid((unsigned)waves);
+    float *const kp = static_cast<float *>(kept);
+    if constexpr (NP >= 4)
+        if (kp) {
+            if (p.z.p)
+                chunk_kernel<T, NP, true, true, true><<<grid, 64, 0, s>>>(p, ch, m, st, sm, kp);
+            else
+                chunk_kernel<T, NP, true, false, true><<<grid, 64, 0, s>>>(p, ch, m, st, sm, kp);
+            return hipGetLastError();
+        }
     if (p.z.p)
-        chunk_kernel<T, NP, true, true><<<dim3((unsigned)waves), 64, 0, s>>>(p, ch, m, st, sm, static_cast<float *>(kept));
+        chunk_kernel<T, NP, true, true, false><<<grid, 64, 0, s>>>(p, ch, m, st, sm, nullptr);
     else
-        chunk_kernel<T, NP, true, false><<<dim3((unsigned)waves), 64, 0, s>>>(p, ch, m, st, sm, static_cast<float *>(kept));
+        chunk_kernel<T, NP, true, false, false><<<grid, 64, 0, s>>>(p, ch, m, st, sm, nullptr);
     return hipGetLastError();
 }
 
