@@ -545,7 +545,7 @@ constexpr int kLeast = 16;
 template <typename T, int NP>
 hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
 {
-    constexpr int NS = NP / 4, CH = NS <= 2 ? 4 : NS <= 4 ? 2 : 1;
+    constexpr int NS = NP / 4, CH = NS <= 4 ? 2 : 1;
     Chunks ch;
     const int cpg = p.C / p.G;
     ch.waves = (cpg + 63) / 64;
