@@ -626,10 +626,11 @@ int gspn_selective_scan_bwd_reserve(const void *x, const void *dt, const float *
  * ones).  r, r_out and their gradients are of residual_dtype, `dtype` or fp32; all else is of
  * `dtype`.  y is formed from the sum before it is rounded.  r_out may be r, with the same strides.
  * f NULL: y is the norm of r alone; r_out is not written, and w_post, scale and gate must be NULL.
- * The backward takes r_out as it was stored, the gradients dy of y and dr_out of r_out from what
- * else reads it (NULL: none), and writes dr, df (with f) and, for each vector given, its
- * gradient.  dr may be dr_out, with the same strides.
- * strides: forward r, f, y, r_out; backward r_out, f, dy, dr_out, dr, df.
+ * The backward takes the forward's r and f (the sum is formed again from them, not read
+ * rounded), the gradients dy of y and dr_out of r_out from what else reads it (NULL: none), and
+ * writes dr, df (with f) and, for each vector given, its gradient.  dr may be dr_out, with the
+ * same strides.
+ * strides: forward r, f, y, r_out; backward r, f, dy, dr_out, dr, df.
  * gspn_residual_norm_workspace_size: of the backward; gated: 1 with a gate, of up to 65535
  * sequences then, else 0.
  */
@@ -639,7 +640,7 @@ int gspn_residual_norm_fwd(const void *r, const void *f, const void *w, const vo
                            int residual_dtype, void *stream);
 int gspn_residual_norm_workspace_size(int B, int T, int C, int gated, int dtype,
                                       int residual_dtype, int64_t *bytes);
-int gspn_residual_norm_bwd(const void *r_out, const void *f, const void *w, const void *w_post,
+int gspn_residual_norm_bwd(const void *r, const void *f, const void *w, const void *w_post,
                            const void *scale, const void *gate, const void *dy, const void *dr_out,
                            void *dr, void *df, void *dw, void *dw_post, void *dscale, void *dgate,
                            const int64_t *strides, int B, int T, int C, float eps, int dtype,

@@ -311,35 +311,35 @@ def residual_norm_fwd(r, f=None, w=None, w_post=None, scale=None, gate=None, eps
     return y, ro
 
 
-def residual_norm_bwd(r_out, f, w, w_post, scale, gate, dy, dr_out=None, eps: float = 1e-6,
+def residual_norm_bwd(r, f, w, w_post, scale, gate, dy, dr_out=None, eps: float = 1e-6,
                       out=None, stream=None, workspace=None):
     """(dr, df, dw, dw_post, dscale, dgate) from the gradients dy of y and dr_out of r_out, from
-    what else reads it (None: nothing); r_out is residual_norm_fwd's (without f: its r), the other
-    arguments those it was called with.  A gradient is None where what it is of is.  `out`: the
-    six, where dr may be dr_out."""
-    if stream is not None or _elsewhere(r_out):
-        return _on(residual_norm_bwd, locals(), "r_out")
+    what else reads it (None: nothing); the other arguments are those residual_norm_fwd was called
+    with (r too: the sum is formed again).  A gradient is None where what it is of is.  `out`:
+    the six, where dr may be dr_out."""
+    if stream is not None or _elsewhere(r):
+        return _on(residual_norm_bwd, locals(), "r")
     import torch
-    sizes, like, ptrs = _join_sizes(r_out, dy, None, w, w_post, scale, gate)
+    sizes, like, ptrs = _join_sizes(r, dy, None, w, w_post, scale, gate)
     B, T, C = sizes
     if out is None:
-        kw = dict(dtype=like.dtype, device=r_out.device)
-        out = (torch.empty(sizes, dtype=r_out.dtype, device=r_out.device),
+        kw = dict(dtype=like.dtype, device=r.device)
+        out = (torch.empty(sizes, dtype=r.dtype, device=r.device),
                None if f is None else torch.empty(sizes, **kw),
                *(None if t is None else torch.empty(C, **kw) for t in (w, w_post, scale)),
                None if gate is None else torch.empty((B, C), **kw))
     dr, df, *grads, dgate = out
-    _same_gpu(r_out, like)
-    _rows(r_out, (r_out, sizes, "r_out"), (dr, sizes, "dr"),
+    _same_gpu(r, like)
+    _rows(r, (r, sizes, "r"), (dr, sizes, "dr"),
           *(((dr_out, sizes, "dr_out"),) if dr_out is not None else ()))
     _rows(like, (dy, sizes, "dy"), *(((f, sizes, "f"), (df, sizes, "df")) if f is not None else ()))
-    codes = _dtype_code(like), _dtype_code(r_out)
+    codes = _dtype_code(like), _dtype_code(r)
     n = _sized("gspn_residual_norm_workspace_size", (*sizes, int(gate is not None), *codes),
                _current_device())
-    ws, held = _take(n, workspace, r_out.device)
+    ws, held = _take(n, workspace, r.device)
     _check_raise(load().gspn_residual_norm_bwd(
-        r_out.data_ptr(), _ptr(f), *ptrs, dy.data_ptr(), _ptr(dr_out), dr.data_ptr(), _ptr(df),
-        *(_plain(name, t, (C,), like.dtype, r_out) for name, t in zip(("dw", "dw_post", "dscale"), grads)),
-        _plain("dgate", dgate, (B, C), like.dtype, r_out), _strides(r_out, f, dy, dr_out, dr, df),
-        *sizes, eps, *codes, *ws, _stream_handle(r_out, None)))
+        r.data_ptr(), _ptr(f), *ptrs, dy.data_ptr(), _ptr(dr_out), dr.data_ptr(), _ptr(df),
+        *(_plain(name, t, (C,), like.dtype, r) for name, t in zip(("dw", "dw_post", "dscale"), grads)),
+        _plain("dgate", dgate, (B, C), like.dtype, r), _strides(r, f, dy, dr_out, dr, df),
+        *sizes, eps, *codes, *ws, _stream_handle(r, None)))
     return out

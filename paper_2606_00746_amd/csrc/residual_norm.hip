@@ -8,8 +8,8 @@
 //   Q_b = sum_t g n_f (or g f):  dgate_b = scale w_post Q_b, dscale = sum_b gate_b w_post Q_b,
 //   dw_post = sum_b gate_b scale Q_b;  dw = sum dy n
 //
-// Bound by memory: r and f read once, r' and y written once (r', f, dy and dr' read, dr and
-// df written).  A row lies in the registers of a group of lanes, part of a wave to a whole
+// Bound by memory: r and f read once, r' and y written once (r, f, dy and dr' read, dr and
+// df written; r' is formed again from r and f, as r' itself may have been rounded to 16 bits).  A row lies in the registers of a group of lanes, part of a wave to a whole
 // workgroup, as runs of 8 entries; its sums are exchanged inside the group.  Backwards a
 // group keeps its columns' shares of Q and dw over all its rows; they are added up in a
 // fixed order by one or two small launches.
@@ -201,10 +201,21 @@ __global__ __launch_bounds__(BLK) void join_bwd_kernel(JoinProblem p, Shape s, f
         load_raws<T, P>(p.f.p ? static_cast<const T *>(p.f.p) + b * p.f.sb + t * p.f.st : nullptr, lane, s.lanes, s.runs, rf);
         load_raws<R, P>(p.dro.p ? static_cast<const R *>(p.dro.p) + b * p.dro.sb + t * p.dro.st : nullptr, lane, s.lanes, s.runs, ro);
         step_fence();
-        float r[P][8], g[P][8];
+        float r[P][8], g[P][8], f[P][8], i = 0.f;   // r', which is formed again; g; n_f (or f)
 #pragma unroll
         for (int j = 0; j < P; ++j)
-            widen_all(rr[j], r[j]), widen_all(ry[j], g[j]);
+            widen_all(rr[j], r[j]), widen_all(ry[j], g[j]), widen_all(rf[j], f[j]);
+        if (p.f.p) {
+            if (p.w_post) {
+                i = inverse_rms(row_sum<WIDE>(dot(f, f), s.lanes, cell, turn), p);
+                scaled(f, i);
+            }
+#pragma unroll
+            for (int j = 0; j < P; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    r[j][e] = fmaf(k[j][e], f[j][e], r[j][e]);
+        }
         const float ir = inverse_rms(row_sum<WIDE>(dot(r, r), s.lanes, cell, turn), p);
 #pragma unroll
         for (int j = 0; j < P; ++j)
@@ -227,15 +238,6 @@ __global__ __launch_bounds__(BLK) void join_bwd_kernel(JoinProblem p, Shape s, f
         store_row<R, P>(static_cast<R *>(p.dr.p) + b * p.dr.sb + t * p.dr.st, lane, s.lanes, s.runs, g);
         if (!p.f.p)
             continue;
-        float(&f)[P][8] = r;
-#pragma unroll
-        for (int j = 0; j < P; ++j)
-            widen_all(rf[j], f[j]);
-        float i = 0.f;
-        if (p.w_post) {
-            i = inverse_rms(row_sum<WIDE>(dot(f, f), s.lanes, cell, turn), p);
-            scaled(f, i);
-        }
 #pragma unroll
         for (int j = 0; j < P; ++j)
 #pragma unroll

@@ -8,7 +8,7 @@ namespace gspn {
 
 struct JoinProblem {
     Heads r, f, y, ro;                   // [B][T][C], strides of b and t; f.p and ro.p may be null
-    Heads dy, dro, dr, df;               // backward (r: r'); dro.p and df.p may be null
+    Heads dy, dro, dr, df;               // backward; dro.p and df.p may be null
     const void *w, *w_post, *scale;      // [C] or null
     const void *gate;                    // [B][C] or null
     void *dw, *dw_post, *dscale, *dgate; // null where not wanted

@@ -417,7 +417,12 @@ __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks c
                 const int i = row % NS, m = row / NS % 2, j = jr + row / NS / 2;
                 if (part == 0 && tb + j < t1) {
                     float *to = out_bc + j * out_step + m * NP + i;
-                    to[0] = a.x, to[NS] = a.y, to[2 * NS] = a.z, to[3 * NS] = a.w;
+                    if constexpr (NS == 1) {   // neighbours: one store, with its wait states
+                        const float row[4] = {a.x, a.y, a.z, a.w};
+                        store_all(to, row);
+                    } else {
+                        to[0] = a.x, to[NS] = a.y, to[2 * NS] = a.z, to[3 * NS] = a.w;
+                    }
                 }
             }
             if (jr > 0)

@@ -380,7 +380,7 @@ extern "C" int gspn_residual_norm_workspace_size(int B, int T, int C, int gated,
     return count(p, launch_join_bwd, bytes);
 }
 
-extern "C" int gspn_residual_norm_bwd(const void *r_out, const void *f, const void *w, const void *w_post, const void *scale,
+extern "C" int gspn_residual_norm_bwd(const void *r, const void *f, const void *w, const void *w_post, const void *scale,
                                       const void *gate, const void *dy, const void *dr_out, void *dr, void *df, void *dw,
                                       void *dw_post, void *dscale, void *dgate, const int64_t *strides, int B, int T, int C,
                                       float eps, int dtype, int residual_dtype, void *workspace, int64_t workspace_bytes,
@@ -393,7 +393,7 @@ extern "C" int gspn_residual_norm_bwd(const void *r_out, const void *f, const vo
     const int64_t es = storage(dtype);
     Buffers bufs;
     int sum = -1;   // the buffer that dr may be
-    p.r = bufs.rows(r_out, at(strides, 0), B, T, C, residual_dtype, false);
+    p.r = bufs.rows(r, at(strides, 0), B, T, C, residual_dtype, false);
     if (f)
         p.f = bufs.rows(f, at(strides, 1), B, T, C, dtype, false);
     join_vectors(p, bufs, w, w_post, scale, gate);

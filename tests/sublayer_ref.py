@@ -134,9 +134,8 @@ def scan(x, dt, A, B, C, D, z, bias, h, n, soft, dy=None, dend=None, depth_t=0, 
     return out
 
 
-def join(r, f, w, w_post, scale, gate, eps, dy=None, dro=None, r_kept=None, depth=0):
-    """r, f [B][T][C], gate [B][C] (any vector may be None).  r_kept: r_out as it was stored, which
-    the gradient takes.  A sum of squares of C terms is off by C u of itself at most, its inverse
+def join(r, f, w, w_post, scale, gate, eps, dy=None, dro=None, depth=0):
+    """r, f [B][T][C], gate [B][C] (any vector may be None).  A sum of squares of C terms is off by C u of itself at most, its inverse
     root by half of that and three roundings."""
     C = r.shape[-1]
     ri = (C / 2 + 4) * U
@@ -163,14 +162,12 @@ def join(r, f, w, w_post, scale, gate, eps, dy=None, dro=None, r_kept=None, dept
     out["y"], out["e_y"] = n * ww, np.abs(ww) * (en + U * np.abs(n))
     if dy is None:
         return out
-    if r_kept is not None:
-        i = 1 / np.sqrt((r_kept * r_kept).mean(-1, keepdims=True) + eps)
-        n = r_kept * i
-    en = np.abs(n) * (ri + U)
     t = dy * ww
     m, am = (t * n).mean(-1, keepdims=True), np.abs(t * n).mean(-1, keepdims=True)
+    em = (np.abs(t) * en).mean(-1, keepdims=True) + am * (C + 4) * U
     g = i * (t - n * m)
-    eg = i * (np.abs(t) * (ri + 3 * U) + np.abs(n) * am * ((C + 4) * U + 3 * ri))
+    rr = ri + 3 * U + i * np.sqrt((ero * ero).mean(-1, keepdims=True))      # of the inverse root, relative
+    eg = i * (np.abs(t) * rr + en * am + np.abs(n) * (em + am * rr))
     if dro is not None:
         g, eg = g + dro, eg + U * np.abs(g + dro)
     ax = (0, 1)

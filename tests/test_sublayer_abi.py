@@ -37,7 +37,7 @@ CALLS = {
     "selective_scan_bwd_reserve": (pointers("x dt A Bm Cm D z dt_bias dy dstate_out lens dx ddt dA dBm dCm dD dz ddt_bias dstate"),
                                    dict(SCAN, **RS)),
     "residual_norm_fwd": (pointers("r f w w_post scale gate y r_out"), dict(JOIN, stream=None)),
-    "residual_norm_bwd": (pointers("r_out f w w_post scale gate dy dr_out dr df dw dw_post dscale dgate"), dict(JOIN, **WS)),
+    "residual_norm_bwd": (pointers("r f w w_post scale gate dy dr_out dr df dw dw_post dscale dgate"), dict(JOIN, **WS)),
 }
 # NULL for these is a meaning of its own; without f its vectors may not be there
 OPTIONAL = {"bias", "state", "lens", "state_out", "dstate_out", "dstate", "D", "z", "dt_bias", "w_post", "scale", "gate", "dr_out"}
@@ -45,7 +45,7 @@ OPTIONAL = {"bias", "state", "lens", "state_out", "dstate_out", "dstate", "D", "
 SMALL = {"lens", "Bm", "Cm", "dBm", "dCm"}
 STRIDED = {"short_conv_fwd": "x y", "short_conv_bwd": "x dy dx", "selective_scan_fwd": "x dt Bm Cm z y",
            "selective_scan_fwd_train": "x dt Bm Cm z y", "selective_scan_bwd_reserve": "x dt Bm Cm z dy dx ddt dBm dCm dz",
-           "residual_norm_fwd": "r f y r_out", "residual_norm_bwd": "r_out f dy dr_out dr df"}
+           "residual_norm_fwd": "r f y r_out", "residual_norm_bwd": "r f dy dr_out dr df"}
 OUTPUTS = {"short_conv_fwd": "y state_out", "short_conv_bwd": "dx dw dbias dstate", "selective_scan_fwd": "y state_out",
            "selective_scan_fwd_train": "y state_out", "selective_scan_bwd_reserve": "dx ddt dA dBm dCm dD dz ddt_bias dstate",
            "residual_norm_fwd": "y r_out", "residual_norm_bwd": "dr df dw dw_post dscale dgate"}

@@ -46,10 +46,10 @@ def everything(x, **kw):
     s2, _ = gspn.selective_scan_fwd(*sel, state=x["state"], lens=x["lens"], **kw)
     f = s @ x["out"]
     y2, r2 = gspn.residual_norm_fwd(r, f, x["w"], **kw)
-    dj = gspn.residual_norm_bwd(r2, f, x["w"], None, None, None, x["dy"], x["r"], **kw)
+    dj = gspn.residual_norm_bwd(r, f, x["w"], None, None, None, x["dy"], x["r"], **kw)
     ds = gspn.selective_scan_bwd_reserve(*sel, dj[1] @ x["out"].T.contiguous(), reserve, dstate=x["dend"], state=x["state"], lens=x["lens"], **kw)
     dc = gspn.short_conv_bwd(xz[..., :C], x["taps"], x["bias"], ds[0], dstate=x["ends"], state=x["ends"], lens=x["lens"], **kw)
-    d0 = gspn.residual_norm_bwd(r, x["f"], x["w"], x["wp"], x["scale"], x["gate"], dc[0], dj[0], **kw)
+    d0 = gspn.residual_norm_bwd(x["r"], x["f"], x["w"], x["wp"], x["scale"], x["gate"], dc[0], dj[0], **kw)
     # the next token
     t1, e1 = gspn.short_conv_fwd(xz[:, :1, :C], x["taps"], x["bias"], state=ends, **kw)
     o1, end1 = gspn.selective_scan_fwd(t1, small[:, :1, :C], x["A"], *(m[:, :1] for m in mats), x["D"], xz[:, :1, C:], x["dtb"], state=end, **kw)
@@ -217,10 +217,10 @@ def test_offsets_past_32_bits():
         assert torch.equal(a, c)
     v = (x["w"], x["wp"], x["scale"], x["gate"])
     want = [*gspn.residual_norm_fwd(near["x"], near["dt"], *v)]
-    want += gspn.residual_norm_bwd(want[1], near["dt"], *v, near["z"])
+    want += gspn.residual_norm_bwd(near["x"], near["dt"], *v, near["z"])
     got = [*gspn.residual_norm_fwd(far["x"], far["dt"], *v, out=(o[0], o[1]))]
     got = [t.clone() for t in got]
-    got += gspn.residual_norm_bwd(o[1], far["dt"], *v, far["z"], out=(o[0], o[6], *(torch.empty_like(t) for t in v)))
+    got += gspn.residual_norm_bwd(far["x"], far["dt"], *v, far["z"], out=(o[0], o[6], *(torch.empty_like(t) for t in v)))
     for i, (a, c) in enumerate(zip(want, got)):
         assert torch.equal(a, c), i
 
@@ -304,13 +304,13 @@ def test_under_autograd():
         @staticmethod
         def forward(ctx, r, f, w):
             y, ro = gspn.residual_norm_fwd(r, f, w)
-            ctx.save_for_backward(ro, f, w)
+            ctx.save_for_backward(r, f, w)
             return y, ro
 
         @staticmethod
         def backward(ctx, dy, dro):
-            ro, f, w = ctx.saved_tensors
-            return gspn.residual_norm_bwd(ro, f, w, None, None, None, dy.contiguous(), dro.contiguous())[:3]
+            r, f, w = ctx.saved_tensors
+            return gspn.residual_norm_bwd(r, f, w, None, None, None, dy.contiguous(), dro.contiguous())[:3]
 
     leaves = {n: x[n].clone().requires_grad_() for n in ("r", "f", "w", "taps", "bias", "A", "D", "dtb")}
 
