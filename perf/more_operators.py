@@ -190,7 +190,7 @@ def _run_own(c, s):
         y, r = gspn.residual_norm_fwd(s["r"], s["f"], *weights, eps=EPS)
         if c["op"] == "residual_fwd":
             return y, r
-        return (y, r, *gspn.residual_norm_bwd(r, s["f"], *weights, s["dy"], s["dr"], eps=EPS))
+        return (y, r, *gspn.residual_norm_bwd(s["r"], s["f"], *weights, s["dy"], s["dr"], eps=EPS))
     if c["op"].startswith("conv"):
         y, end = gspn.short_conv_fwd(s["x"], s["w"], s["bias"], state=s["state"], lens=s["lens"])
         if c["op"] == "conv_fwd":
