@@ -87,6 +87,9 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+# What a call makes itself is not looked over (a small call's time is this binding's).
+
+
 # ---------------------------------------------------------------------------
 # short causal convolution
 # ---------------------------------------------------------------------------
@@ -109,16 +112,21 @@ def short_conv_fwd(x, w, bias=None, state=None, lens=None, silu: bool = True, y=
     if stream is not None or _elsewhere(x):
         return _on(short_conv_fwd, locals(), "x")
     (B, T, C, K), weights, lens_p = _conv_sizes(x, w, bias, lens)
+    rows, ends = (B, T, C), (B, K - 1, C)
     if y is None:
-        y = x.new_empty((B, T, C))
+        _rows(x, (x, rows, "x"))
+        y = x.new_empty(rows)
+    else:
+        _rows(x, (x, rows, "x"), (y, rows, "y"))
     if state_out is None:
-        state_out = x.new_empty((B, K - 1, C))
-    _rows(x, (x, (B, T, C), "x"), (y, (B, T, C), "y"))
-    ends = (B, K - 1, C)
+        state_out = x.new_empty(ends)
+        out_p = state_out.data_ptr()
+    else:
+        out_p = _plain("state_out", state_out, ends, x.dtype, x)
     _check_raise(load().gspn_short_conv_fwd(
         x.data_ptr(), *weights, _plain("state", state, ends, x.dtype, x), lens_p, y.data_ptr(),
-        _plain("state_out", state_out, ends, x.dtype, x), _strides(x, y), B, T, C, K,
-        ACT_SILU if silu else ACT_NONE, _dtype_code(x), _stream_handle(x, None)))
+        out_p, _strides(x, y), B, T, C, K, ACT_SILU if silu else ACT_NONE, _dtype_code(x),
+        _stream_handle(x, None)))
     return y, state_out
 
 
@@ -180,16 +188,20 @@ def _selective_fwd(op, x, dt, A, B, C, D, z, dt_bias, state, lens, softplus, y, 
     import torch
     sizes, ptrs, lens_p = _selective_sizes(x, dt, A, B, C, D, z, dt_bias, lens)
     b, T, ch, G, N = sizes
+    ss = (b, ch, N)
     if y is None:
         y = x.new_empty((b, T, ch))
+    else:
+        _rows(x, (y, (b, T, ch), "y"))
     if state_out is None:
-        state_out = torch.empty((b, ch, N), dtype=torch.float32, device=x.device)
-    _rows(x, (y, (b, T, ch), "y"))
+        state_out = A.new_empty(ss)
+        out_p = state_out.data_ptr()
+    else:
+        out_p = _plain("state_out", state_out, ss, torch.float32, x)
     code = _dtype_code(x)
     n = _sized("gspn_selective_scan_workspace_size", (op, *sizes, code), _current_device())
     ws, held = _take(n, workspace, x.device)
-    args = (*ptrs, _plain("state", state, (b, ch, N), torch.float32, x), lens_p, y.data_ptr(),
-            _plain("state_out", state_out, (b, ch, N), torch.float32, x),
+    args = (*ptrs, _plain("state", state, ss, torch.float32, x), lens_p, y.data_ptr(), out_p,
             _strides(x, dt, B, C, z, y), *sizes, int(bool(softplus)), code)
     if op == SELECTIVE_FWD:
         _check_raise(load().gspn_selective_scan_fwd(*args, *ws, _stream_handle(x, None)))
@@ -275,10 +287,9 @@ def _join_sizes(r, f, y, w, w_post, scale, gate):
     """Sizes, the tensor whose dtype the block has, and the vectors' pointers."""
     B, T, C = _sizes("r", r, 3)
     like = f if f is not None else y if y is not None else w if w is not None else r
-    v = (C,)
-    return (B, T, C), like, tuple(
-        _plain(name, t, shape, like.dtype, r)
-        for name, t, shape in (("w", w, v), ("w_post", w_post, v), ("scale", scale, v), ("gate", gate, (B, C))))
+    v, dt = (C,), like.dtype
+    return (B, T, C), like, (_plain("w", w, v, dt, r), _plain("w_post", w_post, v, dt, r),
+                             _plain("scale", scale, v, dt, r), _plain("gate", gate, (B, C), dt, r))
 
 
 def _same_gpu(r, like):
@@ -295,15 +306,20 @@ def residual_norm_fwd(r, f=None, w=None, w_post=None, scale=None, gate=None, eps
     r.  `out`: (y, r_out), where r_out may be r."""
     if stream is not None or _elsewhere(r):
         return _on(residual_norm_fwd, locals(), "r")
-    import torch
     sizes, like, ptrs = _join_sizes(r, f, None if out is None else out[0], w, w_post, scale, gate)
-    if out is None:
-        out = (torch.empty(sizes, dtype=like.dtype, device=r.device),
-               r if f is None else r.new_empty(sizes))
-    y, ro = out
     _same_gpu(r, like)
-    _rows(r, (r, sizes, "r"), *(((ro, sizes, "r_out"),) if f is not None else ()))
-    _rows(like, (y, sizes, "y"), *(((f, sizes, "f"),) if f is not None else ()))
+    _rows(r, (r, sizes, "r"))
+    if f is not None:
+        _rows(like, (f, sizes, "f"))
+    if out is None:
+        y = like.new_empty(sizes)
+        ro = r if f is None else r.new_empty(sizes)
+        out = y, ro
+    else:
+        y, ro = out
+        _rows(like, (y, sizes, "y"))
+        if f is not None:
+            _rows(r, (ro, sizes, "r_out"))
     _check_raise(load().gspn_residual_norm_fwd(
         r.data_ptr(), _ptr(f), *ptrs, y.data_ptr(), None if f is None else ro.data_ptr(),
         _strides(r, f, y, ro), *sizes, eps, _dtype_code(like), _dtype_code(r),

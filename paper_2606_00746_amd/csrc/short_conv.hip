@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kBlk) void conv_bwd_kernel(ConvProblem p, Shape s, 
         load_taps<T, V, K>(p.w, c, w);
         widen_all(p.bias ? load_raw<T, V>(static_cast<const T *>(p.bias) + c) : zero_raw<T, V>(), bias);
         load_window<T, V, K>(p, x, b, c, t0, n, win);
-        constexpr int kStep = V * (int)sizeof(T) > 16 ? kAhead / 4 : kAhead / 2;
+        constexpr int kStep = kAhead / 2;
         for (int t = t0; t < t1 + K - 1; t += kStep) {
             Raw<T, V> in[kStep], up[kStep];
 #pragma unroll

@@ -76,7 +76,7 @@ CASES = [
     (1, 33, 64, 1, 16, None),
     (2, 100, 136, 1, 16, [100, 65]),
     (1, 257, 48, 2, 8, [250]),
-    (3, 70, 144, 3, 16, [0, 1, 70]),
+    (3, 70, 144, 3, 16, [-1, 1, 99]),
     (1, 130, 16, 2, 5, None),
     (1, 90, 72, 1, 33, [81]),
     (2, 41, 40, 1, 64, None),
@@ -129,7 +129,7 @@ def test_steps_as_they_are():
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("case", [(2, 1, 40, 1, 16, None), (3, 1, 16, 2, 5, [1, 0, 1]), (1, 5, 72, 1, 64, [3]), (2, 8, 24, 3, 1, None),
-                                  (1, 2, 8, 1, 2, None), (5, 3, 264, 1, 32, [3, 3, 2, 0, 1])],
+                                  (1, 2, 8, 1, 2, None), (5, 3, 264, 1, 32, [3, 9, 2, -7, 1])],
                          ids=lambda c: "x".join(map(str, c[:5])))
 def test_single_tokens(case, dtype):
     torch = require_gpu()

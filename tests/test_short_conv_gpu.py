@@ -55,7 +55,7 @@ CASES = [
     (1, 77, 104, 5, [76]),
     (2, 70, 136, 7, None),
     (1, 200, 32, 8, [190]),
-    (4, 515, 16, 6, [515, 0, 8, 512]),
+    (4, 515, 16, 6, [600, -1, 8, 512]),
 ]
 
 
