@@ -582,9 +582,9 @@ int gspn_short_conv_bwd(const void *x, const void *w, const void *bias, const vo
  * may be the same buffer.  Up to 8 tokens run token by token, more in chunks that are joined by
  * their states (results agree within the rounding of fp32).
  * Training: gspn_selective_scan_fwd_train also fills a caller buffer, the reserve
- * (gspn_selective_scan_reserve_size bytes: the states of every eighth token), which
- * gspn_selective_scan_bwd_reserve reads, with the forward's inputs (the state is in the
- * reserve).  It writes the gradients of what was given: dx, ddt, dA, dBm, dCm, dD (with D), dz
+ * (gspn_selective_scan_reserve_size bytes: the states of every eighth token, and B and C in
+ * fp32), which gspn_selective_scan_bwd_reserve reads, with the forward's inputs (the state is
+ * in the reserve).  It writes the gradients of what was given: dx, ddt, dA, dBm, dCm, dD (with D), dz
  * (with z), ddt_bias (with dt_bias) and, unless NULL, dstate, that of state; dstate_out (NULL:
  * zeros) is the gradient of state_out.
  * strides: forward x, dt, Bm, Cm, z, y; backward x, dt, Bm, Cm, z, dy, dx, ddt, dBm, dCm, dz.

@@ -45,25 +45,23 @@ inline int sel_states(const SelectiveProblem &p)
     return n;
 }
 
-// The states ahead of every kSelKeep-th token, [B][ceil(T / kSelKeep)][states][C].
-inline hipError_t take_sel_kept(const SelectiveProblem &p, Workspace *rs, void **kept)
-{
-    return rs->take(kept, (size_t)p.B * ((p.T + kSelKeep - 1) / kSelKeep) * sel_states(p) * p.C * 4);
-}
-
-hipError_t launch_selective_fwd(const SelectiveProblem &p, hipStream_t s);
-hipError_t launch_selective_bwd(const SelectiveProblem &p, hipStream_t s);
-
-#ifdef __HIPCC__
-
 // B and C of every token as fp32, [B][T][G][B, C][states], entries past N and tokens past a
 // sequence's end 0: the kernels read them as scalars, one token ahead, and there is room for
 // a token's before the first and behind the last.
 constexpr int kPackTokens = 16;   // of a workgroup
 inline int64_t sel_pack_groups(const SelectiveProblem &p) { return (int64_t)p.B * ((p.T + kPackTokens - 1) / kPackTokens); }
 inline size_t sel_packed(const SelectiveProblem &p) { return ((size_t)p.B * p.T + 2) * p.G * 2 * sel_states(p) * 4; }
-hipError_t launch_sel_pack(const SelectiveProblem &p, float *bc, hipStream_t s);
 
-#endif
+// The reserve: the states ahead of every kSelKeep-th token, [B][ceil(T / kSelKeep)][states][C],
+// and B and C as they are packed.
+inline hipError_t take_sel_kept(const SelectiveProblem &p, Workspace *rs, void **kept, void **bc)
+{
+    const hipError_t e = rs->take(kept, (size_t)p.B * ((p.T + kSelKeep - 1) / kSelKeep) * sel_states(p) * p.C * 4);
+    return e == hipSuccess ? rs->take(bc, sel_packed(p)) : e;
+}
+
+hipError_t launch_selective_fwd(const SelectiveProblem &p, hipStream_t s);
+hipError_t launch_selective_bwd(const SelectiveProblem &p, hipStream_t s);
+hipError_t launch_sel_pack(const SelectiveProblem &p, float *bc, hipStream_t s);
 
 }  // namespace gspn

@@ -566,7 +566,7 @@ hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
         return hipErrorInvalidConfiguration;
     void *bc = nullptr, *ends = nullptr, *steps = nullptr, *kept = nullptr, *pbc = nullptr, *pa = nullptr, *pd = nullptr;
     const int64_t slots = (int64_t)p.B * ch.n, tokens = (int64_t)p.B * p.T * p.G;
-    hipError_t e = p.ws->take(&bc, sel_packed(p));
+    hipError_t e = take_sel_kept(p, p.rs, &kept, &bc);
     if (e == hipSuccess && ch.n > 1)
         e = p.ws->take(&ends, (size_t)slots * NP * p.C * 4);
     if (e == hipSuccess && ch.n > 1)
@@ -577,14 +577,12 @@ hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
         e = p.ws->take(&pa, (size_t)slots * NP * p.C * 4);
     if (e == hipSuccess)
         e = p.ws->take(&pd, (size_t)slots * 2 * p.C * 4);
-    if (e == hipSuccess)
-        e = take_sel_kept(p, p.rs, &kept);
     if (e != hipSuccess || p.ws->counting)
         return e;
-    float *const m = static_cast<float *>(bc), *const en = static_cast<float *>(ends), *const sm = static_cast<float *>(steps);
+    const float *const m = static_cast<const float *>(bc);
+    float *const en = static_cast<float *>(ends), *const sm = static_cast<float *>(steps);
     const Parts parts{static_cast<float *>(pbc), static_cast<float *>(pa), static_cast<float *>(pd)};
-    e = launch_sel_pack(p, m, s);
-    if (e == hipSuccess && ch.n > 1) {
+    if (ch.n > 1) {
         if (p.z.p)
             back_kernel<T, NP, true><<<dim3((unsigned)passes), 64, 0, s>>>(p, ch, m, en, sm);
         else

@@ -324,13 +324,11 @@ hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
     if (waves * 64 > kMaxThreads || joins * kBlk > kMaxThreads || sel_pack_groups(p) * kBlk > kMaxThreads)
         return hipErrorInvalidConfiguration;
     void *bc = nullptr, *starts = nullptr, *steps = nullptr, *kept = nullptr;
-    hipError_t e = p.ws->take(&bc, sel_packed(p));
+    hipError_t e = p.rs ? take_sel_kept(p, p.rs, &kept, &bc) : p.ws->take(&bc, sel_packed(p));
     if (e == hipSuccess && ch.n > 1)
         e = p.ws->take(&starts, (size_t)p.B * ch.n * NP * p.C * 4);
     if (e == hipSuccess && ch.n > 1)
         e = p.ws->take(&steps, (size_t)p.B * ch.n * p.C * 4);
-    if (e == hipSuccess && p.rs)
-        e = take_sel_kept(p, p.rs, &kept);
     if (e != hipSuccess || p.ws->counting)
         return e;
     float *const m = static_cast<float *>(bc), *const st = static_cast<float *>(starts), *const sm = static_cast<float *>(steps);

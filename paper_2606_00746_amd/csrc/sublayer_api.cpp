@@ -83,8 +83,8 @@ int64_t selective_reserve(const SelectiveProblem &p)
     rs.counting = true;
     SelectiveProblem q = p;
     q.rs = &rs;
-    void *kept;
-    (void)take_sel_kept(q, &rs, &kept);
+    void *kept, *bc;
+    (void)take_sel_kept(q, &rs, &kept, &bc);
     return (int64_t)rs.used;
 }
 

@@ -171,7 +171,7 @@ def test_workspaces():
         assert call(name, ws=first) == n.ERR_ALIAS, name
     assert size("gspn_selective_scan_workspace_size", SELECTIVE_FWD, 2, 8, 64, 2, 16, g.BF16) == (n.OK, 0)    # token by token
     st, need = size("gspn_selective_scan_reserve_size", 2, 70, 64, 2, 16, g.BF16)
-    assert st == n.OK and need == 2 * 9 * 16 * 64 * 4     # every eighth token's states
+    assert st == n.OK and need >= 2 * 9 * 16 * 64 * 4 + 2 * 70 * 2 * 2 * 16 * 4     # every eighth token's states, B and C
     for name, out in (("selective_scan_fwd_train", "y"), ("selective_scan_bwd_reserve", "dx")):
         assert call(name, reserve_bytes=need - 1) == n.ERR_WORKSPACE
         assert call(name, reserve=None) == n.ERR_WORKSPACE
