@@ -128,37 +128,6 @@ __global__ __launch_bounds__(64) void back_kernel(SelectiveProblem p, Chunks ch,
     steps[((int64_t)b * ch.n + k) * p.C + l] = sum;
 }
 
-// From what each chunk passes on to the gradient that arrives behind it, in the same place.
-template <int NP>
-__global__ __launch_bounds__(kBlk) void back_chain_kernel(SelectiveProblem p, Chunks ch, float *ends, const float *steps)
-{
-    const int64_t i = (int64_t)blockIdx.x * kBlk + threadIdx.x;
-    if (i >= (int64_t)p.B * NP * p.C)
-        return;
-    const int c = (int)(i % p.C), n = (int)(i / p.C % NP), b = (int)(i / p.C / NP);
-    const float a2 = n < p.N ? p.A[(int64_t)c * p.N + n] * kLog2e : 0.f;
-    float h = p.dstate && n < p.N ? p.dstate[((int64_t)b * p.C + c) * p.N + n] : 0.f;
-    const int64_t step = (int64_t)NP * p.C;
-    float *at = ends + (int64_t)b * ch.n * step + (int64_t)n * p.C + c;
-    const float *s = steps + (int64_t)b * ch.n * p.C + c;
-    constexpr int U = 32;   // chunks in flight
-    for (int k = ch.n - 1; k >= 0; k -= U) {
-        float add[U], sum[U];
-#pragma unroll
-        for (int j = 0; j < U; ++j) {
-            const bool in = k - j > 0;
-            add[j] = in ? at[(k - j) * step] : 0.f;
-            sum[j] = in ? s[(int64_t)(k - j) * p.C] : 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < U; ++j)
-            if (k - j >= 0) {
-                at[(k - j) * step] = h;
-                h = fmaf(exp2_hw(a2 * sum[j]), h, add[j]);
-            }
-    }
-}
-
 // ---------------------------------------------------------------------------
 // the gradients
 // ---------------------------------------------------------------------------
@@ -544,8 +513,9 @@ __global__ __launch_bounds__(16 * kSumRows) void sum_channels_kernel(SelectivePr
     }
 }
 
+// Waves of the first pass that the chunks are cut for (8 x 4096 tokens of 1536 channels, us,
+// 4096, 6144 and 8192: that pass 189, 183 and 192, the gradients 737, 728 and 748).
 constexpr int64_t kWaves = 6144;
-constexpr int kLeast = 16;
 
 template <typename T, int NP>
 hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
@@ -556,12 +526,11 @@ hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
     ch.waves = (cpg + 63) / 64;
     ch.blocks = (cpg + 64 * CH - 1) / (64 * CH);
     const int64_t waves = (int64_t)p.B * p.G * ch.waves, want = std::max<int64_t>(1, kWaves / waves);
-    const int64_t len = std::max<int64_t>(kLeast, (p.T + want - 1) / want);
+    const int64_t len = std::max(least_tokens(p.T), (p.T + want - 1) / want);
     ch.len = (int)((len + K - 1) / K * K);
     ch.n = (p.T + ch.len - 1) / ch.len;
     const int64_t groups = (int64_t)p.B * p.G * ch.blocks * ch.n, passes = (int64_t)p.B * p.G * ch.waves * (ch.n - 1);
-    const int64_t joins = ((int64_t)p.B * NP * p.C + kBlk - 1) / kBlk;
-    if (groups * kBlk > kMaxThreads || passes * 64 > kMaxThreads || joins * kBlk > kMaxThreads ||
+    if (groups * kBlk > kMaxThreads || passes * 64 > kMaxThreads || (ch.n > 1 && p.B > 65535) ||
         sel_pack_groups(p) * kBlk > kMaxThreads)
         return hipErrorInvalidConfiguration;
     void *bc = nullptr, *ends = nullptr, *steps = nullptr, *kept = nullptr, *pbc = nullptr, *pa = nullptr, *pd = nullptr;
@@ -590,8 +559,7 @@ hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
         e = hipGetLastError();
         if (e != hipSuccess)
             return e;
-        back_chain_kernel<NP><<<dim3((unsigned)joins), kBlk, 0, s>>>(p, ch, en, sm);
-        e = hipGetLastError();
+        e = join_chunks<NP, true>(p, ch.n, en, sm, p.dstate, s);
     }
     if (e != hipSuccess)
         return e;

@@ -1,6 +1,8 @@
 // Device code that both passes of the selective scan share (internal).
 #pragma once
 
+#include <algorithm>
+
 #include "selective.hpp"
 #include "vec.hpp"
 
@@ -68,6 +70,84 @@ template <typename T>
 __device__ __forceinline__ float widened(uint32_t raw)
 {
     return sizeof(T) == 2 ? bf_lo(raw) : __uint_as_float(raw);
+}
+
+// The chain over n chunks: from what each adds to the states (or gradients, BACK: from the
+// last chunk on) that it begins with, to these, in the same place; `from` is what the first
+// begins with, null for zeros.  The last adds to nothing.  A workgroup takes 64 columns (a
+// state of a channel), up to 16 runs of chunks side by side: each run from zeros with its
+// whole decay, then, from what the runs ahead of it come to, its chunks one by one.  Where
+// chunks are many and channels few that is what the chain's time goes by (34225 tokens of 16
+// channels: the call 201 us with one run, 84 with 16); runs of fewer chunks than are loaded at
+// once cost more than they save (43 chunks of 196608 columns: 37 us in 16 runs, 18 in three).
+constexpr int kJoinRuns = 16, kJoinColumns = 64, kJoinAhead = 16;
+
+template <int NP, bool BACK>
+__global__ __launch_bounds__(kJoinRuns *kJoinColumns) void join_chunks_kernel(SelectiveProblem p, int n, float *ends, const float *steps, const float *from)
+{
+    constexpr int U = kJoinAhead;
+    __shared__ float h_[kJoinRuns][kJoinColumns], s_[kJoinRuns][kJoinColumns];
+    const int col = threadIdx.x % kJoinColumns, run = threadIdx.x / kJoinColumns, b = blockIdx.y;
+    const int64_t i = (int64_t)blockIdx.x * kJoinColumns + col, step = (int64_t)NP * p.C;
+    const bool on = i < step;
+    const int c = (int)(i % p.C), st = on ? (int)(i / p.C) : NP;
+    const int runs = blockDim.x / kJoinColumns, per = (n + runs - 1) / runs, k0 = run * per, k1 = min(k0 + per, n);
+    const float a2 = st < p.N ? p.A[(int64_t)c * p.N + st] * kLog2e : 0.f;
+    float *const at = ends + (int64_t)b * n * step + i;
+    const float *const s = steps + (int64_t)b * n * p.C + c;
+    const auto chunk = [&](int k) { return (int64_t)(BACK ? n - 1 - k : k); };
+    float add[U], sum[U];
+    const auto fetch = [&](int k) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const bool in = on && k + j < min(k1, n - 1);
+            add[j] = in ? at[chunk(k + j) * step] : 0.f;
+            sum[j] = in ? s[chunk(k + j) * p.C] : 0.f;
+        }
+    };
+    float h = 0.f, total = 0.f;
+    for (int k = k0; k < k1; k += U) {
+        fetch(k);
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            h = fmaf(exp2_hw(a2 * sum[j]), h, add[j]);
+            total += sum[j];
+        }
+    }
+    h_[run][col] = h, s_[run][col] = total;
+    __syncthreads();
+    h = from && st < p.N ? from[((int64_t)b * p.C + c) * p.N + st] : 0.f;
+    for (int r = 0; r < run; ++r)
+        h = fmaf(exp2_hw(a2 * s_[r][col]), h, h_[r][col]);
+    for (int k = k0; k < k1; k += U) {
+        if (per > U)   // else they are still here
+            fetch(k);
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            if (on && k + j < k1) {
+                at[chunk(k + j) * step] = h;
+                h = fmaf(exp2_hw(a2 * sum[j]), h, add[j]);
+            }
+    }
+}
+
+template <int NP, bool BACK>
+hipError_t join_chunks(const SelectiveProblem &p, int n, float *ends, const float *steps, const float *from, hipStream_t s)
+{
+    const int64_t groups = ((int64_t)NP * p.C + kJoinColumns - 1) / kJoinColumns;
+    const int runs = std::min(kJoinRuns, (n + kJoinAhead - 1) / kJoinAhead);
+    join_chunks_kernel<NP, BACK><<<dim3((unsigned)groups, (unsigned)p.B), runs * kJoinColumns, 0, s>>>(p, n, ends, steps, from);
+    return hipGetLastError();
+}
+
+// Tokens of a chunk, at least: few, where waves are few, but as many chunks as these take a
+// chain (a channel's 34225 tokens of one sequence: chunks of 16 are 2140).
+inline int64_t least_tokens(int T)
+{
+    int64_t n = 16;
+    while (16 * n * n < T)
+        n += 8;
+    return n;
 }
 
 }  // namespace sel

@@ -189,37 +189,6 @@ __global__ __launch_bounds__(64) void chunk_kernel(SelectiveProblem p, Chunks ch
     }
 }
 
-// From what each chunk adds to the states that it begins with, in the same place.
-template <int NP>
-__global__ __launch_bounds__(kBlk) void chain_kernel(SelectiveProblem p, Chunks ch, float *starts, const float *steps)
-{
-    const int64_t i = (int64_t)blockIdx.x * kBlk + threadIdx.x;
-    if (i >= (int64_t)p.B * NP * p.C)
-        return;
-    const int c = (int)(i % p.C), n = (int)(i / p.C % NP), b = (int)(i / p.C / NP);
-    const float a2 = n < p.N ? p.A[(int64_t)c * p.N + n] * kLog2e : 0.f;
-    float h = p.state && n < p.N ? p.state[((int64_t)b * p.C + c) * p.N + n] : 0.f;
-    const int64_t step = (int64_t)NP * p.C;
-    float *at = starts + (int64_t)b * ch.n * step + (int64_t)n * p.C + c;
-    const float *s = steps + (int64_t)b * ch.n * p.C + c;
-    constexpr int U = 32;   // chunks in flight
-    for (int k = 0; k < ch.n; k += U) {
-        float add[U], sum[U];
-#pragma unroll
-        for (int j = 0; j < U; ++j) {
-            const bool in = k + j < ch.n - 1;
-            add[j] = in ? at[(k + j) * step] : 0.f;
-            sum[j] = in ? s[(int64_t)(k + j) * p.C] : 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < U; ++j)
-            if (k + j < ch.n) {
-                at[(k + j) * step] = h;
-                h = fmaf(exp2_hw(a2 * sum[j]), h, add[j]);
-            }
-    }
-}
-
 // ---------------------------------------------------------------------------
 // a few tokens: four lanes a channel, B and C as they lie
 // ---------------------------------------------------------------------------
@@ -292,16 +261,16 @@ __global__ __launch_bounds__(kBlk) void token_kernel(SelectiveProblem p)
     }
 }
 
-// Waves that the chunks of a call are cut for, and a chunk's fewest tokens.
+// Waves that the chunks of a call are cut for (us, 4096, 6144, 8192 and 12288: 34225 tokens of
+// 2304 channels 681, 634, 603 and 616; 8 x 4096 of 1536 468, 460, 457 and 446).
 constexpr int64_t kWaves = 8192;
-constexpr int kLeast = 16;
 
 Chunks chunks_of(const SelectiveProblem &p)
 {
     Chunks c;
     c.blocks = (p.C / p.G + 63) / 64;
     const int64_t waves = (int64_t)p.B * p.G * c.blocks, want = std::max<int64_t>(1, kWaves / waves);
-    const int64_t len = std::max<int64_t>(kLeast, (p.T + want - 1) / want);
+    const int64_t len = std::max(least_tokens(p.T), (p.T + want - 1) / want);
     c.len = (int)((len + kSelKeep - 1) / kSelKeep * kSelKeep);
     c.n = (p.T + c.len - 1) / c.len;
     return c;
@@ -320,8 +289,8 @@ hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
         return hipGetLastError();
     }
     const Chunks ch = chunks_of(p);
-    const int64_t waves = (int64_t)p.B * p.G * ch.blocks * ch.n, joins = ((int64_t)p.B * NP * p.C + kBlk - 1) / kBlk;
-    if (waves * 64 > kMaxThreads || joins * kBlk > kMaxThreads || sel_pack_groups(p) * kBlk > kMaxThreads)
+    const int64_t waves = (int64_t)p.B * p.G * ch.blocks * ch.n;
+    if (waves * 64 > kMaxThreads || (ch.n > 1 && p.B > 65535) || sel_pack_groups(p) * kBlk > kMaxThreads)
         return hipErrorInvalidConfiguration;
     void *bc = nullptr, *starts = nullptr, *steps = nullptr, *kept = nullptr;
     hipError_t e = p.rs ? take_sel_kept(p, p.rs, &kept, &bc) : p.ws->take(&bc, sel_packed(p));
@@ -338,8 +307,7 @@ hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
         e = hipGetLastError();
         if (e != hipSuccess)
             return e;
-        chain_kernel<NP><<<dim3((unsigned)joins), kBlk, 0, s>>>(p, ch, st, sm);
-        e = hipGetLastError();
+        e = join_chunks<NP, false>(p, ch.n, st, sm, p.state, s);
     }
     if (e != hipSuccess)
         return e;
