@@ -379,7 +379,8 @@ __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks c
                 for (int w = 0; w < 4; ++w)
 #pragma unroll
                     for (int i = 0; i < 16 / RT; ++i) {
-                        const float4 f = (&red_[w][0][0][0][0])[row * 16 + i * RT + part];
+                        // rows begin at different q, so that neighbouring rows lie in different banks
+                        const float4 f = (&red_[w][0][0][0][0])[row * 16 + (i * RT + part + RT * row) % 16];
                         a.x += f.x, a.y += f.y, a.z += f.z, a.w += f.w;
                     }
                 a.x = lanes_sum(a.x, RT), a.y = lanes_sum(a.y, RT), a.z = lanes_sum(a.z, RT), a.w = lanes_sum(a.w, RT);
