@@ -579,8 +579,9 @@ int gspn_short_conv_bwd(const void *x, const void *w, const void *bias, const vo
  * of 8; N up to 64; A [C][N], D and dt_bias [C] fp32 (D, dt_bias NULL: zeros; z NULL: no gate).
  * d A <= 0 is what keeps the recurrence bounded and is not checked.  state, state_out: fp32
  * [B][C][N], ahead of the first token (NULL: zeros) and behind the last (NULL: not wanted); they
- * may be the same buffer.  Up to 8 tokens run token by token, more in chunks that are joined by
- * their states (results agree within the rounding of fp32).
+ * may be the same buffer.  Whole sequences run in one pass or, where channels are few for their
+ * length, in chunks that are joined by their states (results agree within the rounding of
+ * fp32); so do gspn_selective_scan_fwd and _fwd_train, each by its own times.
  * Training: gspn_selective_scan_fwd_train also fills a caller buffer, the reserve
  * (gspn_selective_scan_reserve_size bytes: the states of every eighth token, and B and C in
  * fp32), which gspn_selective_scan_bwd_reserve reads, with the forward's inputs (the state is

@@ -35,11 +35,36 @@ constexpr int kSelMaxStates = 64;
 // Tokens between the states that a training forward keeps for its backward.
 constexpr int kSelKeep = 8;
 
+// Whether a forward goes along whole sequences in one pass, four lanes a channel (16 of them a
+// wave), instead of in chunks that it goes through twice: by what either takes.  One pass:
+// 17 us and, a token, `first` ns with up to one wave a SIMD and `more` for each further one.
+// Chunks: 30 us and, a token and wave's worth of channels, `chunks` ps.  Measured (us, one pass
+// and chunks, 1024 tokens of 1536 channels, with the states kept): 4 states batch 1 152 and
+// 39, 64 420 and 360; 8 states batch 32 307 and 268, 64 477 and 488; 16 states batch 1 125
+// and 48, 8 130 and 138, 32 364 and 402; 32 states batch 1 199 and 74, 8 210 and 264, 32 579
+// and 846; 64 states batch 1 319 and 131, 8 334 and 575, 32 981 and 1830; 64 tokens, 16
+// states, batch 1 30 and 37, 32 32 and 65.
+inline bool sel_one_pass(const SelectiveProblem &p)
+{
+    struct Cost {
+        int first, more, chunks;
+    };
+    constexpr Cost cost[2][5] = {{{158, 40, 53}, {162, 42, 75}, {108, 68, 111}, {180, 102, 225}, {292, 170, 495}},
+                                 {{165, 50, 57}, {165, 55, 82}, {120, 105, 115}, {186, 185, 260}, {310, 300, 585}}};
+    int i = 0;
+    while (4 << i < p.N)
+        ++i;
+    const Cost &c = cost[p.rs ? 1 : 0][i];
+    const int64_t waves = (int64_t)p.B * p.G * ((p.C / p.G + 15) / 16), simds = 1024;
+    const double one = 17000. + (double)p.T * (c.first + c.more * (double)((waves - 1) / simds));
+    return one < 30000. + (double)p.T * (double)waves * c.chunks / 1000.;
+}
+
 // States as the kernels hold them: N rounded up to a power of two, at least the four that
-// the backward's quads of lanes share out in training; entries past N are 0.
+// quads of lanes share out (in one pass, and in the backward); entries past N are 0.
 inline int sel_states(const SelectiveProblem &p)
 {
-    int n = p.rs ? 4 : 1;
+    int n = p.rs || sel_one_pass(p) ? 4 : 1;
     while (n < p.N)
         n *= 2;
     return n;

@@ -132,36 +132,6 @@ __global__ __launch_bounds__(64) void back_kernel(SelectiveProblem p, Chunks ch,
 // the gradients
 // ---------------------------------------------------------------------------
 
-// V neighbouring floats in LDS.
-template <int V>
-__device__ __forceinline__ void get_lds(const float *p, float (&f)[V])
-{
-    if constexpr (V == 1) {
-        f[0] = p[0];
-    } else if constexpr (V == 2) {
-        const float2 u = *reinterpret_cast<const float2 *>(p);
-        f[0] = u.x, f[1] = u.y;
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; i += 4) {
-            const float4 u = *reinterpret_cast<const float4 *>(p + i);
-            f[i] = u.x, f[i + 1] = u.y, f[i + 2] = u.z, f[i + 3] = u.w;
-        }
-    }
-}
-template <int V>
-__device__ __forceinline__ void put_lds(float *p, const float (&f)[V])
-{
-    if constexpr (V == 1)
-        p[0] = f[0];
-    else if constexpr (V == 2)
-        *reinterpret_cast<float2 *>(p) = make_float2(f[0], f[1]);
-    else
-#pragma unroll
-        for (int i = 0; i < V; i += 4)
-            *reinterpret_cast<float4 *>(p + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
-}
-
 // Shares of a workgroup: part_bc[b][t][g][block][B, C][states], part_a[b][chunk][states][C],
 // part_d[b][chunk][D, bias][C].
 struct Parts {

@@ -72,6 +72,36 @@ __device__ __forceinline__ float widened(uint32_t raw)
     return sizeof(T) == 2 ? bf_lo(raw) : __uint_as_float(raw);
 }
 
+// V neighbouring floats in LDS.
+template <int V>
+__device__ __forceinline__ void get_lds(const float *p, float (&f)[V])
+{
+    if constexpr (V == 1) {
+        f[0] = p[0];
+    } else if constexpr (V == 2) {
+        const float2 u = *reinterpret_cast<const float2 *>(p);
+        f[0] = u.x, f[1] = u.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            const float4 u = *reinterpret_cast<const float4 *>(p + i);
+            f[i] = u.x, f[i + 1] = u.y, f[i + 2] = u.z, f[i + 3] = u.w;
+        }
+    }
+}
+template <int V>
+__device__ __forceinline__ void put_lds(float *p, const float (&f)[V])
+{
+    if constexpr (V == 1)
+        p[0] = f[0];
+    else if constexpr (V == 2)
+        *reinterpret_cast<float2 *>(p) = make_float2(f[0], f[1]);
+    else
+#pragma unroll
+        for (int i = 0; i < V; i += 4)
+            *reinterpret_cast<float4 *>(p + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+}
+
 // The chain over n chunks: from what each adds to the states (or gradients, BACK: from the
 // last chunk on) that it begins with, to these, in the same place; `from` is what the first
 // begins with, null for zeros.  The last adds to nothing.  A workgroup takes 64 columns (a

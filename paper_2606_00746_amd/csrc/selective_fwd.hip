@@ -190,6 +190,147 @@ __global__ __launch_bounds__(64) void chunk_kernel(SelectiveProblem p, Chunks ch
 }
 
 // ---------------------------------------------------------------------------
+// whole sequences in one pass: four lanes a channel
+// ---------------------------------------------------------------------------
+
+// A quad of lanes holds a channel, a quarter of its states each, and goes along the whole
+// sequence: no chunk is gone through twice.  Of four tokens lane s has token s's entries of x,
+// dt and z, whose step it forms for the quad (one exchange inside the multiplication that
+// takes it), and is left with token s's sum over the states.  B and C of eight tokens come
+// through the wave's own piece of LDS, one wide load a lane.
+template <typename T, int NP, bool Z, bool KEEP>
+__global__ __launch_bounds__(kBlk) void quad_kernel(SelectiveProblem p, int blocks, const float *bc, float *kept)
+{
+    constexpr int NS = NP / 4, U = kSelKeep, TB = NS <= 4 ? 4 : 16 / NS;   // TB: tokens whose B and C are read at once
+    const int item = blockIdx.x * (kBlk / 64) + (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int per = p.G * blocks, gb = item % per, b = item / per, g = gb / blocks;
+    if (b >= p.B)
+        return;
+    const int lane = threadIdx.x % 64, s = lane % 4, cpg = p.C / p.G, ci = gb % blocks * 16 + lane / 4;
+    const bool on = ci < cpg, soft = p.softplus;
+    const int c = g * cpg + (on ? ci : 0), n0 = s * NS, te = length_of(p, b);
+    const float bias = p.dt_bias ? p.dt_bias[c] : 0.f, skip = p.D ? p.D[c] : 0.f;
+    const int64_t st = ((int64_t)b * p.C + c) * p.N + n0;
+    float A2[NS], h[NS];
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+        const bool in = n0 + n < p.N;
+        A2[n] = in ? p.A[(int64_t)c * p.N + n0 + n] * kLog2e : 0.f;
+        h[n] = in && p.state ? p.state[st + n] : 0.f;
+    }
+    const T *x = static_cast<const T *>(p.x.p) + b * p.x.sb + s * p.x.st + c;
+    const T *dt = static_cast<const T *>(p.dt.p) + b * p.dt.sb + s * p.dt.st + c;
+    const T *z = Z ? static_cast<const T *>(p.z.p) + b * p.z.sb + s * p.z.st + c : nullptr;
+    T *y = static_cast<T *>(p.y.p) + b * p.y.sb + s * p.y.st + c;
+    constexpr int MR = (U * NP / 2 + 63) / 64;   // float4s of B and C of U tokens, a lane
+    __shared__ float4 mat_[kBlk / 64][U][NP / 2];
+    float(*const mat)[2 * NP] = reinterpret_cast<float(*)[2 * NP]>(&mat_[threadIdx.x / 64][0][0]);
+    const float *const mats = bc + (((int64_t)b * p.T + 1) * p.G + g) * 2 * NP;
+    float *keep = KEEP ? kept + ((int64_t)b * ((p.T + U - 1) / U) * NP + n0) * p.C + c : nullptr;
+
+    uint32_t xn[U / 4], dn[U / 4], zn[U / 4];
+    const auto fetch = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < U / 4; ++i) {
+            const bool live = t + 4 * i + s < te;
+            xn[i] = live ? load_raw<T, 1>(x + (int64_t)(t + 4 * i) * p.x.st).w[0] : 0;
+            dn[i] = live ? load_raw<T, 1>(dt + (int64_t)(t + 4 * i) * p.dt.st).w[0] : 0;
+            zn[i] = Z && live ? load_raw<T, 1>(z + (int64_t)(t + 4 * i) * p.z.st).w[0] : 0;
+        }
+    };
+    Raw<float, 4> mn[MR];
+    const auto fetch_mats = [&](int t) {   // of tokens past the last: the last's again
+#pragma unroll
+        for (int j = 0; j < MR; ++j) {
+            const int i = lane + 64 * j, at = min(t + i / (NP / 2), p.T - 1);
+            if (NP >= 16 || i < U * NP / 2)
+                mn[j] = load_raw<float, 4>(mats + (int64_t)at * p.G * 2 * NP + i % (NP / 2) * 4);
+        }
+    };
+    fetch(0);
+    fetch_mats(0);
+    for (int t = 0; t < te; t += U) {
+        if (KEEP) {
+            if (on)
+#pragma unroll
+                for (int n = 0; n < NS; ++n)
+                    keep[(int64_t)n * p.C] = h[n];
+            keep += (int64_t)NP * p.C;
+        }
+        float xv[U / 4], d[U / 4], u[U / 4], gate[U / 4];
+#pragma unroll
+        for (int i = 0; i < U / 4; ++i) {
+            const bool live = t + 4 * i + s < te;
+            xv[i] = widened<T>(xn[i]);
+            const float raw = widened<T>(dn[i]) + bias, sp = softplus(raw);
+            d[i] = live ? (soft ? sp : raw) : 0.f;
+            u[i] = d[i] * xv[i];
+            gate[i] = Z ? silu(widened<T>(zn[i])) : 1.f;
+        }
+#pragma unroll
+        for (int j = 0; j < MR; ++j)
+            if (NP >= 16 || lane + 64 * j < U * NP / 2) {
+                float f[4];
+                widen_all(mn[j], f);
+                put_lds(&mat[0][0] + 4 * (lane + 64 * j), f);
+            }
+        fetch(t + U);
+        fetch_mats(t + U);
+#pragma unroll
+        for (int i = 0; i < U / 4; ++i) {
+            float sum[4];
+#pragma unroll
+            for (int k0 = 0; k0 < 4; k0 += TB) {
+                float Bt[TB][NS], Ct[TB][NS];
+#pragma unroll
+                for (int j = 0; j < TB; ++j) {
+                    get_lds(&mat[4 * i + k0 + j][n0], Bt[j]);
+                    get_lds(&mat[4 * i + k0 + j][NP + n0], Ct[j]);
+                }
+                const auto token = [&](auto kc) {
+                    constexpr int k = decltype(kc)::value, j = k % TB;
+                    const float dk = dpp<k * 0x55>(d[i]), uk = dpp<k * 0x55>(u[i]);
+                    sum[k] = 0.f;
+#pragma unroll
+                    for (int n = 0; n < NS; ++n) {
+                        h[n] = fmaf(exp2_hw(dk * A2[n]), h[n], uk * Bt[j][n]);
+                        sum[k] = fmaf(Ct[j][n], h[n], sum[k]);
+                    }
+                };
+                if (k0 == 0)
+                    token(std::integral_constant<int, 0>{});
+                if (k0 <= 1 && 1 < k0 + TB)
+                    token(std::integral_constant<int, 1>{});
+                if (k0 <= 2 && 2 < k0 + TB)
+                    token(std::integral_constant<int, 2>{});
+                if (k0 <= 3 && 3 < k0 + TB)
+                    token(std::integral_constant<int, 3>{});
+            }
+            // lane s: token s over the quad
+            const float a = in_lanes(sum[0], sum[1], kOddLanes) + dpp<kXor1>(in_lanes(sum[1], sum[0], kOddLanes));
+            const float e = in_lanes(sum[2], sum[3], kOddLanes) + dpp<kXor1>(in_lanes(sum[3], sum[2], kOddLanes));
+            float out = in_lanes(a, e, kOddPairs) + dpp<kXor2>(in_lanes(e, a, kOddPairs));
+            out = fmaf(skip, xv[i], out);
+            if (Z)
+                out *= gate[i];
+            const int at = t + 4 * i + s;
+            if (on && at < p.T)
+                store_f(y + (int64_t)(t + 4 * i) * p.y.st, at < te ? out : 0.f);
+            step_fence();
+        }
+    }
+    if (!on)
+        return;
+    for (int t = (te + U - 1) / U * U; t + s < p.T; t += 4)
+        store_f(y + (int64_t)t * p.y.st, 0.f);
+    if (p.state_out)
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+            if (n0 + n < p.N)
+                p.state_out[st + n] = h[n];
+}
+
+// ---------------------------------------------------------------------------
 // a few tokens: four lanes a channel, B and C as they lie
 // ---------------------------------------------------------------------------
 
@@ -198,7 +339,7 @@ constexpr int kFewTokens = 8;
 template <typename T, int NP>
 __global__ __launch_bounds__(kBlk) void token_kernel(SelectiveProblem p)
 {
-    constexpr int NS = NP >= 4 ? NP / 4 : 1;   // states of a lane
+    constexpr int NS = NP / 4;   // states of a lane
     const int64_t i = ((int64_t)blockIdx.x * kBlk + threadIdx.x) / 4;
     if (i >= (int64_t)p.B * p.C)
         return;
@@ -277,16 +418,47 @@ Chunks chunks_of(const SelectiveProblem &p)
 }
 
 template <typename T, int NP>
+hipError_t one_pass(const SelectiveProblem &p, hipStream_t s)
+{
+    const int blocks = (p.C / p.G + 15) / 16;
+    const int64_t groups = ((int64_t)p.B * p.G * blocks + 3) / 4;
+    if (groups * kBlk > kMaxThreads || sel_pack_groups(p) * kBlk > kMaxThreads)
+        return hipErrorInvalidConfiguration;
+    void *bc = nullptr, *kept = nullptr;
+    hipError_t e = p.rs ? take_sel_kept(p, p.rs, &kept, &bc) : p.ws->take(&bc, sel_packed(p));
+    if (e != hipSuccess || p.ws->counting)
+        return e;
+    float *const m = static_cast<float *>(bc), *const k = static_cast<float *>(kept);
+    e = launch_sel_pack(p, m, s);
+    if (e != hipSuccess)
+        return e;
+    const dim3 grid((unsigned)groups);
+    if (k && p.z.p)
+        quad_kernel<T, NP, true, true><<<grid, kBlk, 0, s>>>(p, blocks, m, k);
+    else if (k)
+        quad_kernel<T, NP, false, true><<<grid, kBlk, 0, s>>>(p, blocks, m, k);
+    else if (p.z.p)
+        quad_kernel<T, NP, true, false><<<grid, kBlk, 0, s>>>(p, blocks, m, nullptr);
+    else
+        quad_kernel<T, NP, false, false><<<grid, kBlk, 0, s>>>(p, blocks, m, nullptr);
+    return hipGetLastError();
+}
+
+template <typename T, int NP>
 hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
 {
-    if (p.T <= kFewTokens && !p.rs) {
-        const int64_t n = ((int64_t)p.B * p.C * 4 + kBlk - 1) / kBlk;
-        if (n * kBlk > kMaxThreads)
-            return hipErrorInvalidConfiguration;
-        if (p.ws->counting)
-            return hipSuccess;
-        token_kernel<T, NP><<<dim3((unsigned)n), kBlk, 0, s>>>(p);
-        return hipGetLastError();
+    if constexpr (NP >= 4) {   // fewer states are held as four there
+        if (p.T <= kFewTokens && !p.rs) {
+            const int64_t n = ((int64_t)p.B * p.C * 4 + kBlk - 1) / kBlk;
+            if (n * kBlk > kMaxThreads)
+                return hipErrorInvalidConfiguration;
+            if (p.ws->counting)
+                return hipSuccess;
+            token_kernel<T, NP><<<dim3((unsigned)n), kBlk, 0, s>>>(p);
+            return hipGetLastError();
+        }
+        if (sel_one_pass(p))
+            return one_pass<T, NP>(p, s);
     }
     const Chunks ch = chunks_of(p);
     const int64_t waves = (int64_t)p.B * p.G * ch.blocks * ch.n;

@@ -2,8 +2,8 @@
 the recurrence in 64 bits, token by token, on inputs that are exact in the storage type.  An
 output is one rounding (2^-8 of itself for bf16, 2^-24 for fp32, states and the gradients of
 A, D and dt_bias) of what fp32 arithmetic gives, which is off by at most what sublayer_ref
-counts.  Sums over channels: up to 4 in a lane, 8 and 3 of lanes and waves, the workgroups'
-of a group (up to 3 here): a depth of 18.  Sums over tokens: a lane's own (T), 3 of lanes,
+counts.  Sums over channels: up to 2 in a lane, 16 rows of lanes of 4 waves by up to 16, the
+workgroups' of a group (up to 3 here): a depth of 25 at most.  Sums over tokens: a lane's own (T), 3 of lanes,
 64 rows of shares with 8 each: T + 75."""
 import numpy as np
 import pytest
@@ -41,7 +41,7 @@ def expect(x, lens, without=(), soft=True, grads=True):
         wide = [x[k][i].repeat(C // G, 1) for k in "BC"]
         r = ref.scan(x["x"][i], x["dt"][i], x["A"], *wide, x["D"], None if "z" in without else x["z"][i], x["bias"], x["state"][i],
                      T if lens is None else min(max(lens[i], 0), T), soft, x["dy"][i] if grads else None, x["dend"][i],
-                     T + 75, 18)
+                     T + 75, 25)
         for k, v in r.items():
             if k.replace("e_", "") in ("dB", "dC"):
                 v = v.reshape(T, G, C // G, -1).sum(2)
@@ -83,6 +83,13 @@ CASES = [
     (1, 64, 272, 1, 2, None),
     (1, 200, 32, 4, 24, [199]),
     (1, 600, 8, 1, 3, [555]),
+    (2, 40, 40, 1, 24, [33, 40]),
+    (2, 30, 24, 1, 8, [7, 30]),
+    (1, 300, 40, 1, 4, None),
+    (1, 333, 88, 1, 16, [300]),
+    (2, 64, 48, 1, 1, [64, 50]),
+    (9, 75, 256, 32, 16, [75, 1, 0, 40, 75, 75, 8, 9, 64]),
+    (8, 100, 512, 64, 64, [100, 99, 3, 0, 100, 57, 8, 1]),
 ]
 
 
@@ -99,8 +106,6 @@ def test_training_pair(case, dtype):
     # the same without a reserve
     a, b = gspn.selective_scan_fwd(*args(t), state=t["state"], lens=ln)
     check(dict(y=a, end=b), expect(x, lens, grads=False), dtype)
-    if sizes[1] > 8 and sizes[4] > 2:   # the same kernels then
-        assert torch.equal(a, y) and torch.equal(b, end)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -18,7 +18,7 @@ def P(i, off=0):
 
 
 CONV = dict(B=2, T=70, C=64, K=4, act=1, dtype=g.BF16)
-SCAN = dict(B=2, T=70, C=64, G=2, N=16, softplus=1, dtype=g.BF16)
+SCAN = dict(B=2, T=300, C=64, G=2, N=16, softplus=1, dtype=g.BF16)
 JOIN = dict(B=2, T=70, C=64, eps=1e-6, dtype=g.BF16, rdtype=g.F32)
 WS = dict(ws=P(40), ws_bytes=1 << 25, stream=None)
 RS = dict(reserve=P(30), reserve_bytes=1 << 25, **WS)
@@ -157,9 +157,9 @@ def size(name, *args):
 def test_workspaces():
     for name, query, args in (
         ("short_conv_bwd", "gspn_short_conv_workspace_size", (2, 70, 64, 4, g.BF16)),
-        ("selective_scan_fwd", "gspn_selective_scan_workspace_size", (SELECTIVE_FWD, 2, 70, 64, 2, 16, g.BF16)),
-        ("selective_scan_fwd_train", "gspn_selective_scan_workspace_size", (SELECTIVE_FWD_TRAIN, 2, 70, 64, 2, 16, g.BF16)),
-        ("selective_scan_bwd_reserve", "gspn_selective_scan_workspace_size", (SELECTIVE_BWD_RESERVE, 2, 70, 64, 2, 16, g.BF16)),
+        ("selective_scan_fwd", "gspn_selective_scan_workspace_size", (SELECTIVE_FWD, 2, 300, 64, 2, 16, g.BF16)),
+        ("selective_scan_fwd_train", "gspn_selective_scan_workspace_size", (SELECTIVE_FWD_TRAIN, 2, 300, 64, 2, 16, g.BF16)),
+        ("selective_scan_bwd_reserve", "gspn_selective_scan_workspace_size", (SELECTIVE_BWD_RESERVE, 2, 300, 64, 2, 16, g.BF16)),
         ("residual_norm_bwd", "gspn_residual_norm_workspace_size", (2, 70, 64, 1, g.BF16, g.F32)),
     ):
         st, need = size(query, *args)
@@ -170,8 +170,8 @@ def test_workspaces():
         assert call(name, ws=P(40, 8)) == n.ERR_ALIGN, name
         assert call(name, ws=first) == n.ERR_ALIAS, name
     assert size("gspn_selective_scan_workspace_size", SELECTIVE_FWD, 2, 8, 64, 2, 16, g.BF16) == (n.OK, 0)    # token by token
-    st, need = size("gspn_selective_scan_reserve_size", 2, 70, 64, 2, 16, g.BF16)
-    assert st == n.OK and need >= 2 * 9 * 16 * 64 * 4 + 2 * 70 * 2 * 2 * 16 * 4     # every eighth token's states, B and C
+    st, need = size("gspn_selective_scan_reserve_size", 2, 300, 64, 2, 16, g.BF16)
+    assert st == n.OK and need >= 2 * 38 * 16 * 64 * 4 + 2 * 300 * 2 * 2 * 16 * 4     # every eighth token's states, B and C
     for name, out in (("selective_scan_fwd_train", "y"), ("selective_scan_bwd_reserve", "dx")):
         assert call(name, reserve_bytes=need - 1) == n.ERR_WORKSPACE
         assert call(name, reserve=None) == n.ERR_WORKSPACE
