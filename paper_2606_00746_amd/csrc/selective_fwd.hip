@@ -3,7 +3,9 @@
 // A lane holds a channel with all its states: h_t = 2^(d A log2 e) h_{t-1} + d x B_t and
 // y = C_t . h need nothing of another lane, and B and C of a token, the same for all
 // channels of a group, are scalars.  A state and token take a product, an exponential, a
-// product, two multiply-adds: bound by the vector units, not by memory.
+// product, two multiply-adds: bound by the vector units, not by memory (34225 tokens of 2304
+// channels, 16 states, bf16: first pass 249 us, outputs 317, vector units active 88 and 92%
+// of the cycles; their bytes alone would take 125).
 #include <algorithm>
 
 #include "selective_dev.hpp"
