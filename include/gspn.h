@@ -577,7 +577,8 @@ int gspn_short_conv_bwd(const void *x, const void *w, const void *bias, const vo
  *   h_t = exp(d A) h_{t-1} + d x_t B_t,  y_t = (C_t . h_t + D x_t) z sigmoid(z)
  * x, dt, z, y [B][T][C]; Bm, Cm [B][T][G][N]: channel c reads group c / (C / G), C / G a multiple
  * of 8; N up to 64; A [C][N], D and dt_bias [C] fp32 (D, dt_bias NULL: zeros; z NULL: no gate).
- * d A <= 0 is what keeps the recurrence bounded and is not checked.  state, state_out: fp32
+ * d A <= 0 is what keeps the recurrence bounded and is not checked; rates A down to -inf are
+ * taken (-inf as the lowest finite rate).  state, state_out: fp32
  * [B][C][N], ahead of the first token (NULL: zeros) and behind the last (NULL: not wanted); they
  * may be the same buffer.  Whole sequences run in one pass or, where channels are few for their
  * length, in chunks that are joined by their states (results agree within the rounding of

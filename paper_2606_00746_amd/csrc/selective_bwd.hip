@@ -52,7 +52,7 @@ __global__ __launch_bounds__(64) void back_kernel(SelectiveProblem p, Chunks ch,
     float A2[NP], G[NP], sum = 0.f;
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
-        A2[n] = n < p.N ? p.A[(int64_t)l * p.N + n] * kLog2e : 0.f;
+        A2[n] = n < p.N ? rate(p.A[(int64_t)l * p.N + n]) : 0.f;
         G[n] = 0.f;
     }
     // C from the last token on, a part of the states at a time, as B and C in the forward; a
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks c
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
             const bool in = qon && n0 + i < p.N;
-            A2[e][i] = in ? p.A[(int64_t)(cq + e) * p.N + n0 + i] * kLog2e : 0.f;
+            A2[e][i] = in ? rate(p.A[(int64_t)(cq + e) * p.N + n0 + i]) : 0.f;
             dA[e][i] = 0.f;
             if (ch.n > 1)
                 G[e][i] = in ? ends[(((int64_t)b * ch.n + k) * NP + n0 + i) * p.C + cq + e] : 0.f;
@@ -381,9 +381,10 @@ __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks c
         for (int e = 0; e < V; ++e) {
             const float xv = get(xr, e);
             odx[e] = fmaf(du[e], d[e], skip[e] * up[e]);
-            odt[e] = fmaf(dd[e], kLn2, du[e] * xv) * fd[e];
+            // 0 where there is no token, also where what it is taken times is not finite
+            odt[e] = fd[e] != 0.f ? fmaf(dd[e], kLn2, du[e] * xv) * fd[e] : 0.f;
             if (Z)
-                odz[e] = fmaf(skip[e], xv, yh[e]) * fz[e];
+                odz[e] = live ? fmaf(skip[e], xv, yh[e]) * fz[e] : 0.f;
             dD[e] = fmaf(up[e], xv, dD[e]);
             db[e] += odt[e];
             asm volatile("" : "+v"(dD[e]), "+v"(db[e]));

@@ -16,6 +16,14 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // 2^x, one instruction (relative error 2^-23; below 2^-126: 0)
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A log2 e, kept finite: a step of 0 (a token past a sequence's end) leaves a state as it is
+// at any rate, where 0 times an infinite one is NaN, and 2^(d A) is 0 as soon as d > 2^-120.
+__device__ __forceinline__ float rate(float A)
+{
+    const float a = A * kLog2e;
+    return a < -3.402823466e38f ? -3.402823466e38f : a;
+}
+
 // log(1 + e^x) = max(x, 0) + log(1 + e), e = exp(-|x|) <= 1: with w = 1 + e rounded, log(1 + e)
 // is log w plus what the rounding lost, e - (w - 1), as small e would otherwise be.
 __device__ __forceinline__ float softplus(float x)
@@ -122,7 +130,7 @@ __global__ __launch_bounds__(kJoinRuns *kJoinColumns) void join_chunks_kernel(Se
     const bool on = i < step;
     const int c = (int)(i % p.C), st = on ? (int)(i / p.C) : NP;
     const int runs = blockDim.x / kJoinColumns, per = (n + runs - 1) / runs, k0 = run * per, k1 = min(k0 + per, n);
-    const float a2 = st < p.N ? p.A[(int64_t)c * p.N + st] * kLog2e : 0.f;
+    const float a2 = st < p.N ? rate(p.A[(int64_t)c * p.N + st]) : 0.f;
     float *const at = ends + (int64_t)b * n * step + i;
     const float *const s = steps + (int64_t)b * n * p.C + c;
     const auto chunk = [&](int k) { return (int64_t)(BACK ? n - 1 - k : k); };

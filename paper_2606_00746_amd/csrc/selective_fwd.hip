@@ -68,7 +68,7 @@ __global__ __launch_bounds__(64) void chunk_kernel(SelectiveProblem p, Chunks ch
     const int64_t slot = (((int64_t)b * ch.n + k) * NP) * p.C;
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
-        A2[n] = n < p.N ? p.A[(int64_t)l * p.N + n] * kLog2e : 0.f;
+        A2[n] = n < p.N ? rate(p.A[(int64_t)l * p.N + n]) : 0.f;
         if (!OUT)
             h[n] = 0.f;
         else if (ch.n > 1)
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(kBlk) void quad_kernel(SelectiveProblem p, int bloc
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
         const bool in = n0 + n < p.N;
-        A2[n] = in ? p.A[(int64_t)c * p.N + n0 + n] * kLog2e : 0.f;
+        A2[n] = in ? rate(p.A[(int64_t)c * p.N + n0 + n]) : 0.f;
         h[n] = in && p.state ? p.state[st + n] : 0.f;
     }
     const T *x = static_cast<const T *>(p.x.p) + b * p.x.sb + s * p.x.st + c;
@@ -241,12 +241,12 @@ __global__ __launch_bounds__(kBlk) void quad_kernel(SelectiveProblem p, int bloc
         }
     };
     Raw<float, 4> mn[MR];
-    const auto fetch_mats = [&](int t) {   // of tokens past the last: the last's again
+    const auto fetch_mats = [&](int t) {   // of tokens past the last: zeros
 #pragma unroll
         for (int j = 0; j < MR; ++j) {
-            const int i = lane + 64 * j, at = min(t + i / (NP / 2), p.T - 1);
-            if (NP >= 16 || i < U * NP / 2)
-                mn[j] = load_raw<float, 4>(mats + (int64_t)at * p.G * 2 * NP + i % (NP / 2) * 4);
+            const int i = lane + 64 * j, at = t + i / (NP / 2);
+            mn[j] = at < p.T && (NP >= 16 || i < U * NP / 2) ? load_raw<float, 4>(mats + (int64_t)at * p.G * 2 * NP + i % (NP / 2) * 4)
+                                                             : zero_raw<float, 4>();
         }
     };
     fetch(0);
@@ -368,7 +368,7 @@ __global__ __launch_bounds__(kBlk) void token_kernel(SelectiveProblem p)
     }
 #pragma unroll
     for (int n = 0; n < NS; ++n)
-        A2[n] *= kLog2e;
+        A2[n] = rate(A2[n]);
     for (int t = 0; t < p.T; ++t) {
         float out = 0.f, xv = 0.f;
         if (t < te) {

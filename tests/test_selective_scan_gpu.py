@@ -242,3 +242,55 @@ def test_gradient_against_differences():
             sums.append(float((y.double() * t["dy"].double()).sum() + (end.double() * t["dend"].double()).sum()))
         num, ana = (sums[0] - sums[1]) / (2 * h), float((grads[i].double() * d.double()).sum())
         assert abs(num - ana) <= 2e-2 * float(grads[i].double().norm()) + 1e-2, (n, num, ana)
+
+
+ENDS = [(9, 75, 256, 32, 16, [75, 1, 0, 40, 75, 75, 8, 9, 64]), (1, 333, 88, 1, 16, [300]), (1, 600, 8, 1, 3, [555]),
+        (2, 41, 40, 1, 64, None), (1, 30, 24, 1, 4, [27]), (2, 5, 24, 1, 16, [5, 3])]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", ENDS, ids=lambda c: "x".join(map(str, c[:5])))
+def test_rates_down_to_the_lowest(case, dtype):
+    """States that forget at once: exp(d A) is 0 at any of these rates, so that results are the
+    same bits, also where tokens and whole chunks lie past a sequence's end."""
+    torch = require_gpu()
+    *sizes, lens = case
+    x = make(*sizes, dtype, seed=21)
+    ln, got = lengths(lens), []
+    for rate in (-1e30, np.finfo(np.float32).min, -np.inf):
+        x["A"][:, 1::2], x["A"][3] = rate, rate
+        t = tensors(x, dtype)
+        y, end, reserve = gspn.selective_scan_fwd_train(*args(t), state=t["state"], lens=ln)
+        grads = gspn.selective_scan_bwd_reserve(*args(t), t["dy"], reserve, dstate=t["dend"], state=t["state"], lens=ln)
+        a, b = gspn.selective_scan_fwd(*args(t), state=t["state"], lens=ln)
+        got.append(dict(y=y, end=end, **dict(zip(GRADS, grads)), a=a, b=b))
+        if rate == -1e30:
+            want = expect(x, lens)
+            check({k: v for k, v in got[0].items() if k not in "ab"}, want, dtype)
+            check(dict(y=a, end=b), want, dtype)
+    for other in got[1:]:
+        for n, v in other.items():
+            assert torch.equal(got[0][n], v), n
+
+
+@pytest.mark.parametrize("case", ENDS, ids=lambda c: "x".join(map(str, c[:5])))
+def test_an_infinite_last_token(case):
+    """What a sequence's last token makes infinite stays so, its sign kept, and nothing else changes."""
+    torch = require_gpu()
+    *sizes, lens = case
+    b, T = sizes[:2]
+    lens = [T] * b if lens is None else lens
+    x = make(*sizes, "f32", seed=22)
+    t, ln = tensors(x, "f32"), lengths(lens)
+    base = gspn.selective_scan_fwd(*args(t), state=t["state"], lens=ln)
+    for i, n in enumerate(lens):
+        if n > 0:
+            t["B"][i, n - 1, :, 0] = float("inf")
+    for y, end, *_ in (gspn.selective_scan_fwd(*args(t), state=t["state"], lens=ln),
+                       gspn.selective_scan_fwd_train(*args(t), state=t["state"], lens=ln)):
+        for i, n in enumerate(lens):
+            if n > 0:
+                assert torch.equal(end[i, :, 0], torch.sign(t["x"][i, n - 1]) * float("inf")), i
+                torch.testing.assert_close(y[i, :n - 1], base[0][i, :n - 1], rtol=1e-4, atol=1e-4)
+            torch.testing.assert_close(end[i, :, 1:], base[1][i, :, 1:], rtol=1e-4, atol=1e-4)
+            assert (y[i, max(n, 0):] == 0).all()
