@@ -208,7 +208,7 @@ __global__ __launch_bounds__(kBlk) void conv_bwd_kernel(ConvProblem p, Shape s, 
                         du[K - 1][e] *= silu_grad(u);
                     if (at >= n)   // also where u is not a number
                         du[K - 1][e] = 0.f;
-                    if (at < t1) {
+                    if (at < min(t1, n)) {
                         db[e] += du[K - 1][e];
 #pragma unroll
                         for (int j = 0; j < K; ++j)

@@ -179,3 +179,18 @@ def test_gradient_against_differences():
         num, ana = (sums[0] - sums[1]) / (2 * h), float((grads[i].double() * d.double()).sum())
         # the difference's own error, h^2 times a third derivative, and roundings over h
         assert abs(num - ana) <= 1e-2 * float(grads[i].double().norm()) + 1e-2, (n, num, ana)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [2, 4, 8])
+def test_an_infinite_last_input(K, dtype):
+    """It reaches the last tap's gradient alone: the other taps' pair it with tokens past the end."""
+    torch = require_gpu()
+    t = {n: dev(a, dtype) for n, a in make(2, 70, 40, K, dtype, seed=4).items()}
+    lens, got = torch.tensor([50, 70], dtype=torch.int32, device="cuda"), []
+    for _ in range(2):
+        got.append(gspn.short_conv_bwd(t["x"], t["w"], t["bias"], t["dy"], lens=lens, silu=False))
+        t["x"][0, 49] = float("inf")
+    (dx, dw, db, _), (dx2, dw2, db2, _) = got
+    assert torch.isinf(dw2[:, -1]).all()
+    assert torch.equal(dx, dx2) and torch.equal(dw[:, :-1], dw2[:, :-1]) and torch.equal(db, db2)
