@@ -359,6 +359,8 @@ __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks c
                 const int i = row % NS, m = row / NS % 2, j = jr + row / NS / 2;
                 if (part == 0 && tb + j < t1) {
                     float *to = out_bc + j * out_step + m * NP + i;
+                    if (tb + j >= len)   // also where a state is not finite
+                        a = make_float4(0.f, 0.f, 0.f, 0.f);
                     if constexpr (NS == 1) {   // neighbours: one store, with its wait states
                         const float row[4] = {a.x, a.y, a.z, a.w};
                         store_all(to, row);

@@ -294,3 +294,19 @@ def test_an_infinite_last_token(case):
                 torch.testing.assert_close(y[i, :n - 1], base[0][i, :n - 1], rtol=1e-4, atol=1e-4)
             torch.testing.assert_close(end[i, :, 1:], base[1][i, :, 1:], rtol=1e-4, atol=1e-4)
             assert (y[i, max(n, 0):] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", [c for c in ENDS if c[5]], ids=lambda c: "x".join(map(str, c[:5])))
+def test_gradients_past_the_end_of_infinite_states(case, dtype):
+    torch = require_gpu()
+    *sizes, lens = case
+    t, ln = tensors(make(*sizes, dtype, seed=23), dtype), lengths(lens)
+    for i, n in enumerate(lens):
+        if n > 0:
+            t["B"][i, n - 1, :, 0] = float("inf")
+    y, end, reserve = gspn.selective_scan_fwd_train(*args(t), state=t["state"], lens=ln)
+    grads = dict(zip(GRADS, gspn.selective_scan_bwd_reserve(*args(t), t["dy"], reserve, dstate=t["dend"], state=t["state"], lens=ln)))
+    for n in ("dx", "ddt", "dB", "dC", "dz"):
+        for i, k in enumerate(lens):
+            assert (grads[n][i, k:] == 0).all(), (n, i)
