@@ -14,8 +14,8 @@
 // workgroup, as runs of 8 entries; its sums are exchanged inside the group.  Backwards a
 // group keeps its columns' shares of Q and dw over all its rows; they are added up in a
 // fixed order by one or two small launches.  bf16: forward 290 us for 32 x 5476 tokens of
-// 1152 channels (5.6 TB/s); with an fp32 stream, 8 x 4096 tokens of 768 channels, 60 us (5.0)
-// and the gradient 101 (4.5).
+// 1152 channels (5.6 TB/s); with an fp32 stream, 8 x 4096 tokens of 768 channels, 61 us (5.0)
+// and the gradient 100 (4.5).
 #include <algorithm>
 
 #include "residual_norm.hpp"

@@ -11,8 +11,8 @@
 // and the sums over channels begin inside a lane; these are formed in LDS for several tokens
 // at once, over the channels of a workgroup.  The states come from the forward's reserve for
 // every kSelKeep-th token, and from there again into registers.  8 x 4096 tokens of 1536
-// channels, 16 states, bf16: what chunks pass on 191 us, the gradients 726; these are bound by
-// the vector units, 23 instructions a state and token and 82% of the cycles.
+// channels, 16 states, bf16: what chunks pass on 188 us, the gradients 727; these are bound by
+// the vector units, 23 instructions a state and token and 83% of the cycles.
 #include <algorithm>
 
 #include "selective_dev.hpp"

@@ -9,7 +9,7 @@
 // last K - 1 inputs (and gradients) in registers; the tokens ahead of a segment are read
 // again, from the caches.  The weights' gradients are shares per workgroup, added up in
 // a fixed order by a second launch.  bf16, 4 taps: forward 169 us for 32 x 5476 tokens of
-// 1152 channels (4.8 TB/s); 8 x 4096 tokens of 1536 channels 41 us (4.9), gradient 74 (4.1).
+// 1152 channels (4.8 TB/s); 8 x 4096 tokens of 1536 channels 41 us (4.9), gradient 75 (4.0).
 #include <algorithm>
 
 #include "short_conv.hpp"
