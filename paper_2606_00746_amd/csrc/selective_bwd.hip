@@ -143,7 +143,7 @@ struct Parts {
 // Lane 4 q + s: channels CH q .. of its wave's 16 CH, states NS s .. of 4 NS.
 // Z: with a gate.
 template <typename T, int NS, int CH, bool Z>
-__global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks ch, const float *bc, const float *kept, const float *ends, Parts parts)
+__global__ __launch_bounds__(kBlk) void selective_grad_kernel(SelectiveProblem p, Chunks ch, const float *bc, const float *kept, const float *ends, Parts parts)
 {
     constexpr int NP = 4 * NS, CW = 16 * CH, V = 2 * CH;   // states; channels of a wave; a lane's, of a token, at the ends
     constexpr int TR = NS <= 4 ? 8 : 32 / NS;                // tokens whose sums are formed at once
@@ -433,7 +433,7 @@ __global__ __launch_bounds__(kBlk) void grad_kernel(SelectiveProblem p, Chunks c
 // ---------------------------------------------------------------------------
 
 template <typename T>
-__global__ __launch_bounds__(kBlk) void sum_bc_kernel(SelectiveProblem p, int np, int parts, int blocks, const float *part)
+__global__ __launch_bounds__(kBlk) void selective_sum_bc_kernel(SelectiveProblem p, int np, int parts, int blocks, const float *part)
 {
     const int b = (int)(blockIdx.x / (unsigned)parts), t0 = (int)(blockIdx.x % (unsigned)parts) * kPackTokens, row = p.G * 2 * np;
     const int n = min(kPackTokens, p.T - t0) * row;
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(kBlk) void sum_bc_kernel(SelectiveProblem p, int np
 // Rows 0 .. states - 1 of shares: dA; the next two dD and ddt_bias.  16 channels a workgroup,
 // whose rows of threads add every 64th share, eight in flight, then their sums in order.
 constexpr int kSumRows = 64;
-__global__ __launch_bounds__(16 * kSumRows) void sum_channels_kernel(SelectiveProblem p, int np, int shares, Parts parts)
+__global__ __launch_bounds__(16 * kSumRows) void selective_sum_channels_kernel(SelectiveProblem p, int np, int shares, Parts parts)
 {
     __shared__ float sums[kSumRows][17];
     const int r = blockIdx.y, c = blockIdx.x * 16 + threadIdx.x % 16, i0 = threadIdx.x / 16;
@@ -540,17 +540,17 @@ hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
     if (e != hipSuccess)
         return e;
     if (p.z.p)
-        grad_kernel<T, NS, CH, true><<<dim3((unsigned)groups), kBlk, 0, s>>>(p, ch, m, static_cast<const float *>(kept), en, parts);
+        selective_grad_kernel<T, NS, CH, true><<<dim3((unsigned)groups), kBlk, 0, s>>>(p, ch, m, static_cast<const float *>(kept), en, parts);
     else
-        grad_kernel<T, NS, CH, false><<<dim3((unsigned)groups), kBlk, 0, s>>>(p, ch, m, static_cast<const float *>(kept), en, parts);
+        selective_grad_kernel<T, NS, CH, false><<<dim3((unsigned)groups), kBlk, 0, s>>>(p, ch, m, static_cast<const float *>(kept), en, parts);
     e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    sum_bc_kernel<T><<<dim3((unsigned)sel_pack_groups(p)), kBlk, 0, s>>>(p, NP, (p.T + kPackTokens - 1) / kPackTokens, ch.blocks, parts.bc);
+    selective_sum_bc_kernel<T><<<dim3((unsigned)sel_pack_groups(p)), kBlk, 0, s>>>(p, NP, (p.T + kPackTokens - 1) / kPackTokens, ch.blocks, parts.bc);
     e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    sum_channels_kernel<<<dim3((unsigned)((p.C + 15) / 16), (unsigned)(p.N + 2)), 16 * kSumRows, 0, s>>>(p, NP, (int)slots, parts);
+    selective_sum_channels_kernel<<<dim3((unsigned)((p.C + 15) / 16), (unsigned)(p.N + 2)), 16 * kSumRows, 0, s>>>(p, NP, (int)slots, parts);
     return hipGetLastError();
 }
 

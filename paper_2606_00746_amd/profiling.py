@@ -30,6 +30,7 @@ import csv
 import hashlib
 import json
 import os
+import re
 import subprocess
 import sys
 import tempfile
@@ -39,7 +40,8 @@ _ROOT = os.path.dirname(_HERE)
 COPY_KERNEL = "__amd_rocclr_copyBuffer"
 
 
-# the source files of each kernel family, by a part of the kernel's name
+# the source files of each kernel family, by a part of the kernel's name, or by the whole of
+# it where that ends in "kernel" (other operators' kernels have such names as parts)
 _MED = ("scan_med.hpp", "scan_med.hip", "scan_med_64.hip", "scan_med_56.hip", "scan_med_48.hip",
         "scan_med_40_32_24.hip")
 _FAMILY_SOURCES = (("_med_", _MED), ("dw_sum", _MED), ("_pm_", ("scan_pm.hip",)),
@@ -51,7 +53,8 @@ _FAMILY_SOURCES = (("_med_", _MED), ("dw_sum", _MED), ("_pm_", ("scan_pm.hip",))
                                                        "merge_kernel", "transpose_kernel",
                                                        "rows_kernel", "dw_parts_kernel")),
                    *((k, ("latent.hip",)) for k in ("proj_", "params_blocks", "zero_margin")),
-                   ("norm", ("scan_norm.hip",)))
+                   *((k, ("scan_norm.hip",)) for k in ("norm_kernel", "norm_pm_kernel",
+                                                       "norm_to_blocked_kernel")))
 # kernels that run at the start of a call (re-layouts into the blocked order or
 # into rows, and the line family's sweeps): they belong to the call whose scan
 # kernel follows them
@@ -72,7 +75,9 @@ def source_files(kernels=None) -> list:
     every = sorted(f for f in os.listdir(csrc) if f.endswith((".hip", ".hpp", ".cpp")))
     names = set(_COMMON_SOURCES)
     for k in kernels or ():
-        hit = [f for part, fs in _FAMILY_SOURCES if part in k for f in fs]
+        whole = re.match(r"\w*", k).group()
+        hit = [f for part, fs in _FAMILY_SOURCES
+               if (part == whole if part.endswith("kernel") else part in k) for f in fs]
         if not hit:
             return [os.path.join(csrc, f) for f in every] + [os.path.join(_HERE, "build.py")]
         names.update(hit)
