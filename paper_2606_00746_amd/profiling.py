@@ -14,8 +14,8 @@ making CALLS calls of the forward and of the backward (``--warmup 1 --steps 2``:
 
 Each counter is scaled by what it reads for the plain copy of known size that
 the same run makes, so the record holds bytes.  The record carries a hash of
-the kernel sources: the benchmark reports the figure only while the sources
-are unchanged.
+the kernel sources and their build flags: the benchmark reports the figure only
+while these are unchanged.
 
 Where the waves' time goes, from one counter run collecting the SQ_ counters
 in ``WAVE_COUNTERS`` (wave-cycles waiting, issuing, and by instruction kind)::
@@ -34,6 +34,8 @@ import re
 import subprocess
 import sys
 import tempfile
+
+from . import build
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
@@ -64,7 +66,6 @@ _PREPASS = ("to_blocked_kernel", "norm_to_blocked_kernel", "pieces_kernel", "tra
 # start of a call, or the logits' gradient at the end of a backward
 _NORM = ("norm_kernel", "norm_pm_kernel")
 # shared by every family: device helpers, launch declarations, the dispatch
-# and the build flags
 _COMMON_SOURCES = ("cdna.hpp", "device.hpp", "launch.hpp", "api.cpp")
 
 
@@ -79,21 +80,26 @@ def source_files(kernels=None) -> list:
         hit = [f for part, fs in _FAMILY_SOURCES
                if (part == whole if part.endswith("kernel") else part in k) for f in fs]
         if not hit:
-            return [os.path.join(csrc, f) for f in every] + [os.path.join(_HERE, "build.py")]
+            return [os.path.join(csrc, f) for f in every]
         names.update(hit)
     if not kernels:
         names = set(every)
-    return [os.path.join(csrc, f) for f in sorted(names)] + [os.path.join(_HERE, "build.py")]
+    return [os.path.join(csrc, f) for f in sorted(names)]
 
 
 def source_hash(kernels=None) -> str:
     """sha256 over the sources of the named kernels (all sources if None) and
-    the build flags."""
+    the flags that these are built with (where the tree lies is no part of it)."""
     h = hashlib.sha256()
+    flags = {"": [f for f in build.HIPCC_FLAGS if not os.path.isabs(f)]}
     for f in source_files(kernels):
-        h.update(os.path.basename(f).encode())
+        name = os.path.basename(f)
+        h.update(name.encode())
         with open(f, "rb") as fh:
             h.update(fh.read())
+        if name in build.SOURCE_FLAGS:
+            flags[name] = build.SOURCE_FLAGS[name]
+    h.update(json.dumps(flags, sort_keys=True).encode())
     return h.hexdigest()
 
 
