@@ -382,8 +382,8 @@ __global__ __launch_bounds__(kBlk) void selective_grad_kernel(SelectiveProblem p
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float xv = get(xr, e);
-            odx[e] = fmaf(du[e], d[e], skip[e] * up[e]);
             // 0 where there is no token, also where what it is taken times is not finite
+            odx[e] = live ? fmaf(du[e], d[e], skip[e] * up[e]) : 0.f;
             odt[e] = fd[e] != 0.f ? fmaf(dd[e], kLn2, du[e] * xv) * fd[e] : 0.f;
             if (Z)
                 odz[e] = live ? fmaf(skip[e], xv, yh[e]) * fz[e] : 0.f;

@@ -1,0 +1,75 @@
+"""Infinite inputs of the selective scan: what its formula leaves finite stays as it was, bit
+for bit, what it makes infinite is so with its sign, and what lies past a sequence's end
+is 0.  Signs are chosen so that no sum of the formula adds infinities of both signs."""
+import pytest
+
+import paper_2606_00746_amd as gspn
+from gpu_util import require_gpu
+from test_selective_scan_gpu import GRADS, args, lengths, make, tensors
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+# b, T, C, G, N, lens: token by token, whole sequences in one pass, chunks; numbers of states that
+# are held as they are and with room; groups that do and do not fill a wave; ends in a block of 8
+CASES = [
+    (2, 5, 24, 1, 5, [5, 3]), (1, 7, 16, 1, 16, None),
+    (9, 75, 256, 32, 5, [75, 1, 0, 40, 75, 75, 8, 9, 64]), (2, 41, 40, 1, 33, None), (1, 30, 24, 1, 4, [27]),
+    (1, 333, 88, 1, 13, [300]), (1, 600, 8, 1, 3, [555]), (1, 333, 128, 1, 16, [301]), (1, 260, 136, 1, 24, None),
+    (2, 150, 64, 1, 64, [131, 150]), (1, 270, 128, 2, 7, [266]),
+]
+TYPES = ["bf16", "f32"]
+ids = lambda c: "x".join(map(str, c[:5]))  # noqa: E731
+
+
+def prepared(case, dtype, seed):
+    *sizes, lens = case
+    x = make(*sizes, dtype, seed=seed)
+    return tensors(x, dtype), lengths(lens), [sizes[1]] * sizes[0] if lens is None else lens
+
+
+def forwards(t, ln):
+    return gspn.selective_scan_fwd(*args(t), state=t["state"], lens=ln)
+
+
+def both(t, ln):
+    y, end, reserve = gspn.selective_scan_fwd_train(*args(t), state=t["state"], lens=ln)
+    grads = gspn.selective_scan_bwd_reserve(*args(t), t["dy"], reserve, dstate=t["dend"], state=t["state"], lens=ln)
+    return dict(zip(("y", "end", *GRADS), (y, end, *grads)))
+
+
+def past_the_end_is_zero(got, lens):
+    for n in ("y", "dx", "ddt", "dB", "dC", "dz"):
+        for i, k in enumerate(lens):
+            assert (got[n][i, k:] == 0).all(), (n, i)
+
+
+def same(got, base, names, lens=(), but=None):
+    """Names' values are the base's; `but`(length): a token that is left out."""
+    torch = require_gpu()
+    for n in names:
+        a, b = got[n].clone(), base[n].clone()
+        for i, k in enumerate(lens):
+            if k > 0:
+                a[i, but(k)], b[i, but(k)] = 0, 0
+        assert torch.equal(a, b), n
+
+
+def last(k):
+    return k - 1
+
+
+def first(k):
+    return 0
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("name", ["dend", "D"])
+@pytest.mark.parametrize("case", [c for c in CASES if c[5]], ids=ids)
+def test_past_the_end_of_infinite_gradients(case, name, dtype):
+    t, ln, lens = prepared(case, dtype, 42)
+    if name == "dend":
+        t["dend"][..., 0] = INF
+    else:
+        t["D"][:] = INF
+    past_the_end_is_zero(both(t, ln), lens)
