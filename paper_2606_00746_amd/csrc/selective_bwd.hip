@@ -297,6 +297,8 @@ __global__ __launch_bounds__(kBlk) void selective_grad_kernel(SelectiveProblem p
 #pragma unroll
             for (int jj = TR - 1; jj >= 0; --jj) {
                 const int j = jr + jj;
+                if (tb + j >= len)   // no token: a state that is not finite would reach dA
+                    continue;
                 float dv[CH], uv[CH], gv[CH], Bv[NS], Cv[NS];
                 step_fence();
                 asm volatile("" ::: "memory");

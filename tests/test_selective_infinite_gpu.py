@@ -64,6 +64,21 @@ def first(k):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", CASES, ids=ids)
+def test_an_infinite_last_state(case, dtype):
+    """B of the last token: no gradient of A, D, the first state or another token takes it up."""
+    t, ln, lens = prepared(case, dtype, 41)
+    base = both(t, ln)
+    for i, k in enumerate(lens):
+        if k > 0:
+            t["B"][i, k - 1, :, 0] = INF
+    got = both(t, ln)
+    same(got, base, ("dA", "dD", "dB", "dstate"))
+    same(got, base, ("y", "dx", "ddt", "dC", "dz"), lens, last)
+    past_the_end_is_zero(got, lens)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("name", ["dend", "D"])
 @pytest.mark.parametrize("case", [c for c in CASES if c[5]], ids=ids)
 def test_past_the_end_of_infinite_gradients(case, name, dtype):
