@@ -148,7 +148,7 @@ __global__ __launch_bounds__(kBlk) void selective_grad_kernel(SelectiveProblem p
     constexpr int NP = 4 * NS, CW = 16 * CH, V = 2 * CH;   // states; channels of a wave; a lane's, of a token, at the ends
     constexpr int TR = NS <= 4 ? 8 : 32 / NS;                // tokens whose sums are formed at once
     __shared__ float4 tok_[4][3][K][CW / 4];                // d, u, dy' of a wave's tokens; then C . h, du, dd
-    __shared__ float4 mat_[K][2][NS];                       // B and C of the tokens
+    __shared__ float4 mat_[2][K][2][NS];                    // B and C of the tokens; zeros
     __shared__ float4 red_[4][TR][2][NS][16];               // a wave's terms of dB and dC: float4 over s
 
     int64_t at = blockIdx.x;
@@ -180,6 +180,11 @@ __global__ __launch_bounds__(kBlk) void selective_grad_kernel(SelectiveProblem p
             else
                 G[e][i] = in && p.dstate ? p.dstate[((int64_t)b * p.C + cq + e) * p.N + n0 + i] : 0.f;
         }
+    // lanes without a channel have B and C of 0: what they add to the sums over channels is 0 then,
+    // which with its own 0s it is not where B or C is infinite
+    for (int i = threadIdx.x; i < K * 2 * NP; i += kBlk)
+        mat[K * 2 * NP + i] = 0.f;
+    const float *const mine = mat + (qon ? 0 : K * 2 * NP) + n0;
 
     // ahead of the scan and behind it: token lane / 8, channels cv ..
     const int tl = lane / 8, cl = lane % 8 * V;
@@ -285,7 +290,7 @@ __global__ __launch_bounds__(kBlk) void selective_grad_kernel(SelectiveProblem p
             asm volatile("" ::: "memory");   // read again for each token: kept, they take the registers of more waves
             get_lds(&dts[j][q * CH], dv);
             get_lds(&us[j][q * CH], uv);
-            get_lds(mat + j * 2 * NP + n0, Bv);
+            get_lds(mine + j * 2 * NP, Bv);
 #pragma unroll
             for (int e = 0; e < CH; ++e)
 #pragma unroll
@@ -305,8 +310,8 @@ __global__ __launch_bounds__(kBlk) void selective_grad_kernel(SelectiveProblem p
                 get_lds(&dts[j][q * CH], dv);
                 get_lds(&us[j][q * CH], uv);
                 get_lds(&ups[j][q * CH], gv);
-                get_lds(mat + j * 2 * NP + n0, Bv);
-                get_lds(mat + j * 2 * NP + NP + n0, Cv);
+                get_lds(mine + j * 2 * NP, Bv);
+                get_lds(mine + j * 2 * NP + NP, Cv);
                 float tB[NS] = {}, tC[NS] = {}, res[CH];
 #pragma unroll
                 for (int e = 0; e < CH; ++e) {

@@ -88,3 +88,29 @@ def test_past_the_end_of_infinite_gradients(case, name, dtype):
     else:
         t["D"][:] = INF
     past_the_end_is_zero(both(t, ln), lens)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", CASES, ids=ids)
+def test_sums_over_channels_of_infinite_states(case, dtype):
+    """C of the first token and B of the last, of one state: dB and dC there are sums over a
+    group's channels alone, also where it does not fill the lanes."""
+    torch = require_gpu()
+    t, ln, lens = prepared(case, dtype, 46)
+    for i, k in enumerate(lens):
+        if k > 0:
+            for n in ("x", "z", "dy"):
+                for j, sign in ((0, -1 if n == "x" else 1), (k - 1, 1)):
+                    t[n][i, j] = sign * (t[n][i, j].abs() + 0.1)
+    base = both(t, ln)
+    C0, B1 = t["C"].clone(), t["B"].clone()
+    for i, k in enumerate(lens):
+        if k > 1:
+            C0[i, 0, :, 0], B1[i, k - 1, :, 0] = INF, INF
+    up, down = both({**t, "C": C0}, ln), both({**t, "B": B1}, ln)
+    for i, k in enumerate(lens):
+        if k > 1:
+            assert (up["dB"][i, 0, :, 0] == -INF).all(), i
+            assert torch.equal(up["dB"][i, 0, :, 1:], base["dB"][i, 0, :, 1:]), i
+            assert (down["dC"][i, k - 1, :, 0] == INF).all(), i
+            assert torch.equal(down["dC"][i, k - 1, :, 1:], base["dC"][i, k - 1, :, 1:]), i
