@@ -141,8 +141,8 @@ struct Parts {
 };
 
 // Lane 4 q + s: channels CH q .. of its wave's 16 CH, states NS s .. of 4 NS.
-// Z: with a gate.
-template <typename T, int NS, int CH, bool Z>
+// Z: with a gate.  PAD: fewer states than 4 NS; those past N stay 0.
+template <typename T, int NS, int CH, bool Z, bool PAD>
 __global__ __launch_bounds__(kBlk) void selective_grad_kernel(SelectiveProblem p, Chunks ch, const float *bc, const float *kept, const float *ends, Parts parts)
 {
     constexpr int NP = 4 * NS, CW = 16 * CH, V = 2 * CH;   // states; channels of a wave; a lane's, of a token, at the ends
@@ -258,6 +258,7 @@ __global__ __launch_bounds__(kBlk) void selective_grad_kernel(SelectiveProblem p
             load_all<float, V>(p.dt_bias + cv, bias);
         // of dd and C . h + D x: what ddt and dz are of them; 0 where there is no token
         float d[V], u[V], up[V], fd[V], fz[V];
+        float most = 0.f;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float raw = get(dr, e) + bias[e];
@@ -272,7 +273,10 @@ __global__ __launch_bounds__(kBlk) void selective_grad_kernel(SelectiveProblem p
                 up[e] *= silu(get(zr, e), grad);
                 fz[e] *= grad;
             }
+            if (PAD)
+                most = fmaxf(fmaxf(most, fabsf(d[e])), fmaxf(fabsf(u[e]), fabsf(up[e])));
         }
+        const bool odd = PAD && any_infinite(most);
         put_lds(&dts[tl][cl], d);
         put_lds(&us[tl][cl], u);
         put_lds(&ups[tl][cl], up);
@@ -282,23 +286,31 @@ __global__ __launch_bounds__(kBlk) void selective_grad_kernel(SelectiveProblem p
         if (tb > t0)
             fetch(tb - K);
 
+        // the block's states, and their terms, TR tokens at a time; odd: where inputs are infinite
         float h[K][CH][NS];
+        const auto states = [&](auto odd_block) {
 #pragma unroll
-        for (int j = 0; j < K; ++j) {
-            float dv[CH], uv[CH], Bv[NS];
-            step_fence();
-            asm volatile("" ::: "memory");   // read again for each token: kept, they take the registers of more waves
-            get_lds(&dts[j][q * CH], dv);
-            get_lds(&us[j][q * CH], uv);
-            get_lds(mine + j * 2 * NP, Bv);
+            for (int j = 0; j < K; ++j) {
+                float dv[CH], uv[CH], Bv[NS];
+                step_fence();
+                asm volatile("" ::: "memory");   // read again for each token: kept, they take the registers of more waves
+                get_lds(&dts[j][q * CH], dv);
+                get_lds(&us[j][q * CH], uv);
+                get_lds(mine + j * 2 * NP, Bv);
 #pragma unroll
-            for (int e = 0; e < CH; ++e)
+                for (int e = 0; e < CH; ++e)
 #pragma unroll
-                for (int i = 0; i < NS; ++i)
-                    h[j][e][i] = fmaf(exp2_hw(dv[e] * A2[e][i]), j ? h[j - 1][e][i] : first[e][i], uv[e] * Bv[i]);
-        }
-#pragma unroll
-        for (int jr = K - TR; jr >= 0; jr -= TR) {
+                    for (int i = 0; i < NS; ++i) {
+                        const float v = fmaf(exp2_hw(dv[e] * A2[e][i]), j ? h[j - 1][e][i] : first[e][i], uv[e] * Bv[i]);
+                        h[j][e][i] = !odd_block || n0 + i < p.N ? v : 0.f;
+                    }
+            }
+        };
+        if (PAD && odd)
+            states(std::true_type{});
+        else
+            states(std::false_type{});
+        const auto terms = [&](auto odd_block, int jr) {
 #pragma unroll
             for (int jj = TR - 1; jj >= 0; --jj) {
                 const int j = jr + jj;
@@ -318,13 +330,14 @@ __global__ __launch_bounds__(kBlk) void selective_grad_kernel(SelectiveProblem p
                     float yh = 0.f, du = 0.f, dd = 0.f;
 #pragma unroll
                     for (int i = 0; i < NS; ++i) {
-                        const float gt = fmaf(Cv[i], gv[e], G[e][i]);
+                        const bool in = !odd_block || n0 + i < p.N;
+                        const float gt = in ? fmaf(Cv[i], gv[e], G[e][i]) : 0.f;
                         if (Z)
                             yh = fmaf(Cv[i], h[j][e][i], yh);
                         du = fmaf(gt, Bv[i], du);
                         tB[i] = fmaf(gt, uv[e], tB[i]);
                         tC[i] = fmaf(h[j][e][i], gv[e], tC[i]);
-                        G[e][i] = exp2_hw(dv[e] * A2[e][i]) * gt;
+                        G[e][i] = in ? exp2_hw(dv[e] * A2[e][i]) * gt : 0.f;
                         const float w = G[e][i] * (j ? h[j - 1][e][i] : first[e][i]);
                         dd = fmaf(w, A2[e][i], dd);
                         dA[e][i] = fmaf(w, dv[e], dA[e][i]);
@@ -348,6 +361,13 @@ __global__ __launch_bounds__(kBlk) void selective_grad_kernel(SelectiveProblem p
                     reinterpret_cast<float *>(&red_[wave][jj][1][i][0])[lane] = tC[i];
                 }
             }
+        };
+#pragma unroll
+        for (int jr = K - TR; jr >= 0; jr -= TR) {
+            if (PAD && odd)
+                terms(std::true_type{}, jr);
+            else
+                terms(std::false_type{}, jr);
             lds_barrier();
             // a row of 16 float4 a token, matrix and i: float4 (over s) q of all waves; RT threads a row
             constexpr int rows = TR * 2 * NS, RT = kBlk / rows >= 16 ? 16 : kBlk / rows;
@@ -500,7 +520,7 @@ __global__ __launch_bounds__(16 * kSumRows) void selective_sum_channels_kernel(S
 // 4096, 6144 and 8192: that pass 189, 183 and 192, the gradients 737, 728 and 748).
 constexpr int64_t kWaves = 6144;
 
-template <typename T, int NP>
+template <typename T, int NP, bool PAD>
 hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
 {
     constexpr int NS = NP / 4, CH = NS <= 4 ? 2 : 1;
@@ -547,9 +567,9 @@ hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
     if (e != hipSuccess)
         return e;
     if (p.z.p)
-        selective_grad_kernel<T, NS, CH, true><<<dim3((unsigned)groups), kBlk, 0, s>>>(p, ch, m, static_cast<const float *>(kept), en, parts);
+        selective_grad_kernel<T, NS, CH, true, PAD><<<dim3((unsigned)groups), kBlk, 0, s>>>(p, ch, m, static_cast<const float *>(kept), en, parts);
     else
-        selective_grad_kernel<T, NS, CH, false><<<dim3((unsigned)groups), kBlk, 0, s>>>(p, ch, m, static_cast<const float *>(kept), en, parts);
+        selective_grad_kernel<T, NS, CH, false, PAD><<<dim3((unsigned)groups), kBlk, 0, s>>>(p, ch, m, static_cast<const float *>(kept), en, parts);
     e = hipGetLastError();
     if (e != hipSuccess)
         return e;
@@ -564,12 +584,14 @@ hipError_t bwd(const SelectiveProblem &p, hipStream_t s)
 template <typename T>
 hipError_t pick(const SelectiveProblem &p, hipStream_t s)
 {
-    switch (sel_states(p)) {
-    case 4: return bwd<T, 4>(p, s);
-    case 8: return bwd<T, 8>(p, s);
-    case 16: return bwd<T, 16>(p, s);
-    case 32: return bwd<T, 32>(p, s);
-    default: return bwd<T, 64>(p, s);
+    const int np = sel_states(p);
+    const bool pad = p.N < np;
+    switch (np) {
+    case 4: return pad ? bwd<T, 4, true>(p, s) : bwd<T, 4, false>(p, s);
+    case 8: return pad ? bwd<T, 8, true>(p, s) : bwd<T, 8, false>(p, s);
+    case 16: return pad ? bwd<T, 16, true>(p, s) : bwd<T, 16, false>(p, s);
+    case 32: return pad ? bwd<T, 32, true>(p, s) : bwd<T, 32, false>(p, s);
+    default: return pad ? bwd<T, 64, true>(p, s) : bwd<T, 64, false>(p, s);
     }
 }
 

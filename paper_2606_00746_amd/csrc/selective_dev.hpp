@@ -80,6 +80,11 @@ __device__ __forceinline__ float widened(uint32_t raw)
     return sizeof(T) == 2 ? bf_lo(raw) : __uint_as_float(raw);
 }
 
+// Whether v is infinite in any lane.  States past N, where the kernels hold more, have B and C
+// of 0 and stay 0, but for products with infinite inputs: these are looked for a token (or more)
+// at once, so that what puts the states right costs nothing else.  (NaN reaches all states.)
+__device__ __forceinline__ bool any_infinite(float v) { return __any(fabsf(v) == __builtin_inff()); }
+
 // V neighbouring floats in LDS.
 template <int V>
 __device__ __forceinline__ void get_lds(const float *p, float (&f)[V])

@@ -45,13 +45,14 @@ struct Chunks {
 
 // OUT: the outputs, from `starts`, or from the sequence's state where there is one chunk.
 // Otherwise what the chunk adds to its states from zeros, into `starts`, and the sum of
-// its steps.  Z: with a gate.  KEEP: with the states of every kSelKeep-th token.
+// its steps.  Z: with a gate.  KEEP: with the states of every kSelKeep-th token.  PAD: fewer
+// states than NP, of which those past N stay 0.
 //
 // Rows' addresses are a scalar and the lane's channel; eight tokens are in flight ahead of
 // the eight that are worked on, B and C of a token one token ahead: they are what the scalar
 // registers hold, and loads from its beginning come too late (64 x 64, us: C from the token's
 // beginning 281, a token ahead 255).
-template <typename T, int NP, bool OUT, bool Z, bool KEEP>
+template <typename T, int NP, bool OUT, bool Z, bool KEEP, bool PAD>
 __global__ __launch_bounds__(64) void chunk_kernel(SelectiveProblem p, Chunks ch, const float *bc, float *starts, float *steps, float *kept)
 {
     constexpr int U = kSelKeep;
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(64) void chunk_kernel(SelectiveProblem p, Chunks ch
         if (!OUT)
             h[n] = 0.f;
         else if (ch.n > 1)
-            h[n] = (starts + slot + (int64_t)n * p.C)[l];
+            h[n] = PAD && n >= p.N ? 0.f : (starts + slot + (int64_t)n * p.C)[l];
         else
             h[n] = p.state && n < p.N ? p.state[((int64_t)b * p.C + l) * p.N + n] : 0.f;
     }
@@ -103,7 +104,16 @@ __global__ __launch_bounds__(64) void chunk_kernel(SelectiveProblem p, Chunks ch
 #pragma unroll
             for (int n = 0; n < P; ++n) {
                 h[q + n] = fmaf(exp2_hw(d * A2[q + n]), h[q + n], u * Bt[n]);
-                if (OUT)
+                if (OUT && !PAD)
+                    out = fmaf(Ct[n], h[q + n], out);
+            }
+            if (PAD) {
+                if (any_infinite(u))
+#pragma unroll
+                    for (int n = 0; n < P; ++n)
+                        h[q + n] = q + n < p.N ? h[q + n] : 0.f;
+#pragma unroll
+                for (int n = 0; n < P; ++n)
                     out = fmaf(Ct[n], h[q + n], out);
             }
             if (OUT && q + P == NP) {
@@ -200,7 +210,7 @@ __global__ __launch_bounds__(64) void chunk_kernel(SelectiveProblem p, Chunks ch
 // dt and z, whose step it forms for the quad (one exchange inside the multiplication that
 // takes it), and is left with token s's sum over the states.  B and C of eight tokens come
 // through the wave's own piece of LDS, one wide load a lane.
-template <typename T, int NP, bool Z, bool KEEP>
+template <typename T, int NP, bool Z, bool KEEP, bool PAD>
 __global__ __launch_bounds__(kBlk) void quad_kernel(SelectiveProblem p, int blocks, const float *bc, float *kept)
 {
     constexpr int NS = NP / 4, U = kSelKeep, TB = NS <= 4 ? 4 : 16 / NS;   // TB: tokens whose B and C are read at once
@@ -280,6 +290,7 @@ __global__ __launch_bounds__(kBlk) void quad_kernel(SelectiveProblem p, int bloc
         fetch_mats(t + U);
 #pragma unroll
         for (int i = 0; i < U / 4; ++i) {
+            const bool odd = PAD && any_infinite(u[i]);
             float sum[4];
 #pragma unroll
             for (int k0 = 0; k0 < 4; k0 += TB) {
@@ -296,7 +307,17 @@ __global__ __launch_bounds__(kBlk) void quad_kernel(SelectiveProblem p, int bloc
 #pragma unroll
                     for (int n = 0; n < NS; ++n) {
                         h[n] = fmaf(exp2_hw(dk * A2[n]), h[n], uk * Bt[j][n]);
-                        sum[k] = fmaf(Ct[j][n], h[n], sum[k]);
+                        if (!PAD)
+                            sum[k] = fmaf(Ct[j][n], h[n], sum[k]);
+                    }
+                    if (PAD) {
+                        if (odd)
+#pragma unroll
+                            for (int n = 0; n < NS; ++n)
+                                h[n] = n0 + n < p.N ? h[n] : 0.f;
+#pragma unroll
+                        for (int n = 0; n < NS; ++n)
+                            sum[k] = fmaf(Ct[j][n], h[n], sum[k]);
                     }
                 };
                 if (k0 == 0)
@@ -419,7 +440,7 @@ Chunks chunks_of(const SelectiveProblem &p)
     return c;
 }
 
-template <typename T, int NP>
+template <typename T, int NP, bool PAD>
 hipError_t one_pass(const SelectiveProblem &p, hipStream_t s)
 {
     const int blocks = (p.C / p.G + 15) / 16;
@@ -436,17 +457,17 @@ hipError_t one_pass(const SelectiveProblem &p, hipStream_t s)
         return e;
     const dim3 grid((unsigned)groups);
     if (k && p.z.p)
-        quad_kernel<T, NP, true, true><<<grid, kBlk, 0, s>>>(p, blocks, m, k);
+        quad_kernel<T, NP, true, true, PAD><<<grid, kBlk, 0, s>>>(p, blocks, m, k);
     else if (k)
-        quad_kernel<T, NP, false, true><<<grid, kBlk, 0, s>>>(p, blocks, m, k);
+        quad_kernel<T, NP, false, true, PAD><<<grid, kBlk, 0, s>>>(p, blocks, m, k);
     else if (p.z.p)
-        quad_kernel<T, NP, true, false><<<grid, kBlk, 0, s>>>(p, blocks, m, nullptr);
+        quad_kernel<T, NP, true, false, PAD><<<grid, kBlk, 0, s>>>(p, blocks, m, nullptr);
     else
-        quad_kernel<T, NP, false, false><<<grid, kBlk, 0, s>>>(p, blocks, m, nullptr);
+        quad_kernel<T, NP, false, false, PAD><<<grid, kBlk, 0, s>>>(p, blocks, m, nullptr);
     return hipGetLastError();
 }
 
-template <typename T, int NP>
+template <typename T, int NP, bool PAD>
 hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
 {
     if constexpr (NP >= 4) {   // fewer states are held as four there
@@ -460,7 +481,7 @@ hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
             return hipGetLastError();
         }
         if (sel_one_pass(p))
-            return one_pass<T, NP>(p, s);
+            return one_pass<T, NP, PAD>(p, s);
     }
     const Chunks ch = chunks_of(p);
     const int64_t waves = (int64_t)p.B * p.G * ch.blocks * ch.n;
@@ -477,7 +498,7 @@ hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
     float *const m = static_cast<float *>(bc), *const st = static_cast<float *>(starts), *const sm = static_cast<float *>(steps);
     e = launch_sel_pack(p, m, s);
     if (e == hipSuccess && ch.n > 1) {
-        chunk_kernel<T, NP, false, false, false><<<dim3((unsigned)(waves / ch.n * (ch.n - 1))), 64, 0, s>>>(p, ch, m, st, sm, nullptr);
+        chunk_kernel<T, NP, false, false, false, false><<<dim3((unsigned)(waves / ch.n * (ch.n - 1))), 64, 0, s>>>(p, ch, m, st, sm, nullptr);
         e = hipGetLastError();
         if (e != hipSuccess)
             return e;
@@ -490,29 +511,31 @@ hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
     if constexpr (NP >= 4)
         if (kp) {
             if (p.z.p)
-                chunk_kernel<T, NP, true, true, true><<<grid, 64, 0, s>>>(p, ch, m, st, sm, kp);
+                chunk_kernel<T, NP, true, true, true, PAD><<<grid, 64, 0, s>>>(p, ch, m, st, sm, kp);
             else
-                chunk_kernel<T, NP, true, false, true><<<grid, 64, 0, s>>>(p, ch, m, st, sm, kp);
+                chunk_kernel<T, NP, true, false, true, PAD><<<grid, 64, 0, s>>>(p, ch, m, st, sm, kp);
             return hipGetLastError();
         }
     if (p.z.p)
-        chunk_kernel<T, NP, true, true, false><<<grid, 64, 0, s>>>(p, ch, m, st, sm, nullptr);
+        chunk_kernel<T, NP, true, true, false, PAD><<<grid, 64, 0, s>>>(p, ch, m, st, sm, nullptr);
     else
-        chunk_kernel<T, NP, true, false, false><<<grid, 64, 0, s>>>(p, ch, m, st, sm, nullptr);
+        chunk_kernel<T, NP, true, false, false, PAD><<<grid, 64, 0, s>>>(p, ch, m, st, sm, nullptr);
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t pick(const SelectiveProblem &p, hipStream_t s)
 {
-    switch (sel_states(p)) {
-    case 1: return fwd<T, 1>(p, s);
-    case 2: return fwd<T, 2>(p, s);
-    case 4: return fwd<T, 4>(p, s);
-    case 8: return fwd<T, 8>(p, s);
-    case 16: return fwd<T, 16>(p, s);
-    case 32: return fwd<T, 32>(p, s);
-    default: return fwd<T, 64>(p, s);
+    const int np = sel_states(p);
+    const bool pad = p.N < np;
+    switch (np) {
+    case 1: return fwd<T, 1, false>(p, s);
+    case 2: return fwd<T, 2, false>(p, s);
+    case 4: return pad ? fwd<T, 4, true>(p, s) : fwd<T, 4, false>(p, s);
+    case 8: return pad ? fwd<T, 8, true>(p, s) : fwd<T, 8, false>(p, s);
+    case 16: return pad ? fwd<T, 16, true>(p, s) : fwd<T, 16, false>(p, s);
+    case 32: return pad ? fwd<T, 32, true>(p, s) : fwd<T, 32, false>(p, s);
+    default: return pad ? fwd<T, 64, true>(p, s) : fwd<T, 64, false>(p, s);
     }
 }
 

@@ -92,6 +92,108 @@ def test_past_the_end_of_infinite_gradients(case, name, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("case", CASES, ids=ids)
+def test_an_infinite_last_input(case, dtype):
+    """x of the last token, with B, C and D above 0: states and y are infinite with x's sign (and
+    the gate's), whatever room there is beside the states."""
+    torch = require_gpu()
+    t, ln, lens = prepared(case, dtype, 43)
+    t["D"] = t["D"].abs() + 0.1
+    for i, k in enumerate(lens):
+        if k > 0:
+            for n in ("B", "C"):
+                t[n][i, k - 1] = t[n][i, k - 1].abs() + 0.1
+    few, base = forwards(t, ln), both(t, ln)
+    for i, k in enumerate(lens):
+        if k > 0:
+            t["x"][i, k - 1] = torch.sign(t["x"][i, k - 1]) * INF
+    got = both(t, ln)
+    for (y, end), (y0, end0) in ((forwards(t, ln), few), ((got["y"], got["end"]), (base["y"], base["end"]))):
+        for i, k in enumerate(lens):
+            if k > 0:
+                assert torch.equal(y[i, k - 1], t["x"][i, k - 1] * torch.sign(t["z"][i, k - 1])), i
+                assert torch.equal(end[i], t["x"][i, k - 1].float()[:, None].expand_as(end[i])), i
+                assert torch.equal(y[i, :k - 1], y0[i, :k - 1])
+            else:
+                assert torch.equal(end[i], end0[i])
+    same(got, base, ("dx", "dA", "dstate"))
+    same(got, base, ("ddt", "dB", "dC", "dz"), lens, last)
+    for i, k in enumerate(lens):
+        if k > 0:
+            assert torch.isinf(got["ddt"][i, k - 1]).all() and torch.isinf(got["dz"][i, k - 1]).all(), i
+    past_the_end_is_zero(got, lens)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", CASES, ids=ids)
+def test_an_infinite_last_step(case, dtype):
+    """dt of the last token: all that was is forgotten, what it writes is infinite."""
+    torch = require_gpu()
+    t, ln, lens = prepared(case, dtype, 44)
+    t["D"] = t["D"].abs() + 0.1
+    for i, k in enumerate(lens):
+        if k > 0:
+            for n in ("B", "C", "x"):
+                t[n][i, k - 1] = t[n][i, k - 1].abs() + 0.1
+            t["dt"][i, k - 1] = INF
+    for y, end, *_ in (forwards(t, ln), gspn.selective_scan_fwd_train(*args(t), state=t["state"], lens=ln)):
+        for i, k in enumerate(lens):
+            if k > 0:
+                assert (end[i] == INF).all(), i
+                assert torch.equal(y[i, k - 1], torch.sign(t["z"][i, k - 1]) * INF), i
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", CASES, ids=ids)
+def test_an_infinite_step_in_the_middle(case, dtype):
+    """Its decay is 0, as that of a step of 200 with these rates: what stands ahead of it does not
+    tell them apart, forward or back (an input of 0 there makes NaN of what stands behind)."""
+    torch = require_gpu()
+    t, ln, lens = prepared(case, dtype, 47)
+    t["A"] = -t["A"].abs().clamp(min=1)
+    got = []
+    for step in (200.0, INF):
+        for i, k in enumerate(lens):
+            if k > 1:
+                t["dt"][i, k // 2], t["x"][i, k // 2] = step, 0
+        got.append(both(t, ln))
+    for n in ("y", "dx", "ddt", "dB", "dC", "dz"):
+        for i, k in enumerate(lens):
+            m = k // 2 if k > 1 else k
+            assert torch.equal(got[0][n][i, :m], got[1][n][i, :m]), (n, i)
+    assert torch.equal(got[0]["dstate"], got[1]["dstate"])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", CASES, ids=ids)
+def test_an_infinite_first_gradient(case, dtype):
+    """dy of the first token: what goes back from it is infinite, the tokens behind it know
+    nothing of it.  A decay exp(d A) below 2^-120 may be 0 in fp32 (whose normal numbers end at
+    2^-126; d A log2 e is off by less than a hundredth there), and 0 times an infinite gradient is
+    not a number: states that decay so, and sums that take them, are left out."""
+    torch = require_gpu()
+    t, ln, lens = prepared(case, dtype, 45)
+    t["state"], t["D"] = t["state"].abs() + 0.1, t["D"].abs() + 0.1
+    for n in ("B", "C", "z"):
+        t[n][:, 0] = t[n][:, 0].abs() + 0.1
+    t["x"][:, 0] = -t["x"][:, 0].abs() - 0.1
+    base = both(t, ln)
+    t["dy"][:, 0] = INF
+    got = both(t, ln)
+    same(got, base, ("dx", "ddt", "dB", "dC", "dz"), lens, first)
+    d = torch.nn.functional.softplus(t["dt"][:, 0].double() + t["bias"].double())
+    lasts = d[..., None] * t["A"].double() > -120 * 0.6931471805599453     # [b, C, N]
+    assert lasts.double().mean() > 0.9
+    for i, k in enumerate(lens):
+        if k > 0:
+            assert (got["dx"][i, 0] == INF).all() and (got["dB"][i, 0] == -INF).all(), i
+            assert (got["ddt"][i, 0] == -INF)[lasts[i].all(-1)].all() and (got["dstate"][i] == INF)[lasts[i]].all(), i
+            assert torch.isinf(got["dz"][i, 0]).all(), i
+    assert (got["dA"] == INF)[lasts.all(0)].all() and (got["dD"] == -INF).all()
+    past_the_end_is_zero(got, lens)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", CASES, ids=ids)
 def test_sums_over_channels_of_infinite_states(case, dtype):
     """C of the first token and B of the last, of one state: dB and dC there are sums over a
     group's channels alone, also where it does not fill the lanes."""
