@@ -87,6 +87,14 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _gradients(*pairs):
+    """(name, tensor, input's name, input) each: what a call was given to write a gradient to has
+    an input that it is of (else it would be left as it is)."""
+    for name, t, of, given in pairs:
+        if t is not None and given is None:
+            raise ValueError(f"{name} is the gradient of {of}, which is not given")
+
+
 # What a call makes itself is not looked over (a small call's time is this binding's).
 
 
@@ -145,6 +153,8 @@ def short_conv_bwd(x, w, bias, dy, dstate=None, state=None, lens=None, silu: boo
         out = (torch.empty((B, T, C), **kw), torch.empty((C, K), **kw),
                None if bias is None else torch.empty(C, **kw),
                None if state is None else torch.empty(ends, **kw))
+    else:
+        _gradients(("dbias", out[2], "bias", bias))
     dx, dw, dbias, din = out
     _rows(x, (x, (B, T, C), "x"), (dy, (B, T, C), "dy"), (dx, (B, T, C), "dx"))
     dt = _dtype_code(x)
@@ -251,6 +261,8 @@ def selective_scan_bwd_reserve(x, dt, A, B, C, D, z, dt_bias, dy, reserve, dstat
     if stream is not None or _elsewhere(x):
         return _on(selective_scan_bwd_reserve, locals(), "x")
     import torch
+    if out is not None:
+        _gradients(("dD", out[5], "D", D), ("dz", out[6], "z", z), ("ddt_bias", out[7], "dt_bias", dt_bias))
     sizes, ptrs, lens_p = _selective_sizes(x, dt, A, B, C, D, z, dt_bias, lens)
     b, T, ch, G, N = sizes
     rows, shared, ss, f32 = (b, T, ch), (b, T, G, N), (b, ch, N), torch.float32
@@ -344,6 +356,9 @@ def residual_norm_bwd(r, f, w, w_post, scale, gate, dy, dr_out=None, eps: float 
                None if f is None else torch.empty(sizes, **kw),
                *(None if t is None else torch.empty(C, **kw) for t in (w, w_post, scale)),
                None if gate is None else torch.empty((B, C), **kw))
+    else:
+        _gradients(("df", out[1], "f", f), ("dw", out[2], "w", w), ("dw_post", out[3], "w_post", w_post),
+                   ("dscale", out[4], "scale", scale), ("dgate", out[5], "gate", gate))
     dr, df, *grads, dgate = out
     _same_gpu(r, like)
     _rows(r, (r, sizes, "r"), (dr, sizes, "dr"),
