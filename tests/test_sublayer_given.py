@@ -25,3 +25,9 @@ reserve = torch.zeros(8, dtype=torch.uint8)
 def test_a_gradient_of_what_is_not_there(what, call):
     with pytest.raises(ValueError, match=f"{what} is the gradient of"):
         call()
+
+
+def test_a_stream_of_its_own_without_a_sum():
+    """Without f the stream is r; another tensor would be left as it is."""
+    with pytest.raises(ValueError, match="r_out"):
+        gspn.residual_norm_fwd(x, None, v, out=(x.clone(), x.clone()))
