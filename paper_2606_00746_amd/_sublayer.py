@@ -34,6 +34,8 @@ def _on(call, args, first):
         s = torch.cuda.current_stream(dev)
     elif not hasattr(s, "cuda_stream"):
         s = torch.cuda.ExternalStream(int(s), device=dev) if s else torch.cuda.default_stream(dev)
+    elif s.device != dev:   # the call would go to its own device's current stream instead
+        raise ValueError(f"stream must be of {dev}, not of {s.device}")
     with torch.cuda.stream(s):
         return call(**args)
 

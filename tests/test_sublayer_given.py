@@ -1,5 +1,7 @@
-"""What a call of the sublayer could not fill is refused (the front end's
+"""What a call of the sublayer could not fill or could not run on is refused (the front end's
 own checks, ahead of any GPU)."""
+import types
+
 import pytest
 import torch
 
@@ -31,3 +33,13 @@ def test_a_stream_of_its_own_without_a_sum():
     """Without f the stream is r; another tensor would be left as it is."""
     with pytest.raises(ValueError, match="r_out"):
         gspn.residual_norm_fwd(x, None, v, out=(x.clone(), x.clone()))
+
+
+@pytest.mark.parametrize("call", [lambda s: gspn.short_conv_fwd(x, w, stream=s), lambda s: gspn.short_conv_bwd(*conv, x, stream=s),
+                                  lambda s: gspn.selective_scan_fwd(*sel, stream=s), lambda s: gspn.selective_scan_fwd_train(*sel, stream=s),
+                                  lambda s: gspn.selective_scan_bwd_reserve(*sel, x, reserve, stream=s), lambda s: gspn.residual_norm_fwd(x, stream=s),
+                                  lambda s: gspn.residual_norm_bwd(x, None, None, None, None, None, x, stream=s)])
+def test_a_stream_of_another_device(call):
+    """It would run on the current stream of the tensors' device."""
+    with pytest.raises(ValueError, match="stream must be of"):
+        call(types.SimpleNamespace(cuda_stream=0, device=torch.device("cuda", 1)))
