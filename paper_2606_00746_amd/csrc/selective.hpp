@@ -87,6 +87,5 @@ inline hipError_t take_sel_kept(const SelectiveProblem &p, Workspace *rs, void *
 
 hipError_t launch_selective_fwd(const SelectiveProblem &p, hipStream_t s);
 hipError_t launch_selective_bwd(const SelectiveProblem &p, hipStream_t s);
-hipError_t launch_sel_pack(const SelectiveProblem &p, float *bc, hipStream_t s);
 
 }  // namespace gspn

@@ -34,6 +34,17 @@ __global__ __launch_bounds__(kBlk) void pack_kernel(SelectiveProblem p, int np, 
     }
 }
 
+hipError_t launch_pack(const SelectiveProblem &p, float *bc, hipStream_t s)
+{
+    const int np = sel_states(p), parts = (p.T + kPackTokens - 1) / kPackTokens;
+    const unsigned grid = (unsigned)sel_pack_groups(p);
+    if (p.dtype == 0)
+        pack_kernel<float><<<grid, kBlk, 0, s>>>(p, np, parts, bc);
+    else
+        pack_kernel<bf16_t><<<grid, kBlk, 0, s>>>(p, np, parts, bc);
+    return hipGetLastError();
+}
+
 // ---------------------------------------------------------------------------
 // chunks of tokens
 // ---------------------------------------------------------------------------
@@ -452,7 +463,7 @@ hipError_t one_pass(const SelectiveProblem &p, hipStream_t s)
     if (e != hipSuccess || p.ws->counting)
         return e;
     float *const m = static_cast<float *>(bc), *const k = static_cast<float *>(kept);
-    e = launch_sel_pack(p, m, s);
+    e = launch_pack(p, m, s);
     if (e != hipSuccess)
         return e;
     const dim3 grid((unsigned)groups);
@@ -496,7 +507,7 @@ hipError_t fwd(const SelectiveProblem &p, hipStream_t s)
     if (e != hipSuccess || p.ws->counting)
         return e;
     float *const m = static_cast<float *>(bc), *const st = static_cast<float *>(starts), *const sm = static_cast<float *>(steps);
-    e = launch_sel_pack(p, m, s);
+    e = launch_pack(p, m, s);
     if (e == hipSuccess && ch.n > 1) {
         chunk_kernel<T, NP, false, false, false, false><<<dim3((unsigned)(waves / ch.n * (ch.n - 1))), 64, 0, s>>>(p, ch, m, st, sm, nullptr);
         e = hipGetLastError();
@@ -540,17 +551,6 @@ hipError_t pick(const SelectiveProblem &p, hipStream_t s)
 }
 
 }  // namespace
-
-hipError_t launch_sel_pack(const SelectiveProblem &p, float *bc, hipStream_t s)
-{
-    const int np = sel_states(p), parts = (p.T + kPackTokens - 1) / kPackTokens;
-    const unsigned grid = (unsigned)sel_pack_groups(p);
-    if (p.dtype == 0)
-        pack_kernel<float><<<grid, kBlk, 0, s>>>(p, np, parts, bc);
-    else
-        pack_kernel<bf16_t><<<grid, kBlk, 0, s>>>(p, np, parts, bc);
-    return hipGetLastError();
-}
 
 hipError_t launch_selective_fwd(const SelectiveProblem &p, hipStream_t s)
 {
