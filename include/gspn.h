@@ -578,7 +578,9 @@ int gspn_short_conv_bwd(const void *x, const void *w, const void *bias, const vo
  * x, dt, z, y [B][T][C]; Bm, Cm [B][T][G][N]: channel c reads group c / (C / G), C / G a multiple
  * of 8; N up to 64; A [C][N], D and dt_bias [C] fp32 (D, dt_bias NULL: zeros; z NULL: no gate).
  * d A <= 0 is what keeps the recurrence bounded and is not checked; rates A down to -inf are
- * taken (-inf as the lowest finite rate).  state, state_out: fp32
+ * taken (-inf as the lowest finite rate).  Infinite inputs and states go through as in the
+ * formula, but that exp(d A) below 2^-126 is 0, and 0 times an infinite state not a number (in
+ * chunks: of the whole decay over a chunk).  state, state_out: fp32
  * [B][C][N], ahead of the first token (NULL: zeros) and behind the last (NULL: not wanted); they
  * may be the same buffer.  Whole sequences run in one pass or, where channels are few for their
  * length, in chunks that are joined by their states (results agree within the rounding of

@@ -15,7 +15,10 @@
 // group keeps its columns' shares of Q and dw over all its rows; they are added up in a
 // fixed order by one or two small launches.  bf16: forward 290 us for 32 x 5476 tokens of
 // 1152 channels (5.6 TB/s); with an fp32 stream, 8 x 4096 tokens of 768 channels, 61 us (5.0)
-// and the gradient 100 (4.5).
+// and the gradient 100 (4.5).  Rows above 8192 channels take 1024 threads, which leaves 128
+// registers to each: their gradient does not hold a row without scratch memory (107 to 124
+// registers spilled; 2 x 4096 rows of 8200 and 16384, bf16: 782 and 928 us, 1.0 and 1.7 TB/s;
+// of 8192 225, 3.6).
 #include <algorithm>
 
 #include "residual_norm.hpp"

@@ -39,11 +39,13 @@ constexpr int kSelKeep = 8;
 // wave), instead of in chunks that it goes through twice: by what either takes.  One pass:
 // 17 us and, a token, `first` ns with up to one wave a SIMD and `more` for each further one.
 // Chunks: 30 us and, a token and wave's worth of channels, `chunks` ps.  Measured (us, one pass
-// and chunks, 1024 tokens of 1536 channels, with the states kept): 4 states batch 1 152 and
-// 39, 64 420 and 360; 8 states batch 32 307 and 268, 64 477 and 488; 16 states batch 1 125
-// and 48, 8 130 and 138, 32 364 and 402; 32 states batch 1 199 and 74, 8 210 and 264, 32 579
-// and 846; 64 states batch 1 319 and 131, 8 334 and 575, 32 981 and 1830; 64 tokens, 16
-// states, batch 1 30 and 37, 32 32 and 65.
+// and chunks, 1024 tokens of 1536 channels, with the states kept): 4 states batch 1 120 and
+// 34, 64 412 and 351; 8 states batch 32 360 and 259, 64 476 and 481; 16 states batch 1 138
+// and 44, 8 140 and 135, 32 381 and 397, 64 753 and 706; 32 states batch 1 231 and 73, 8 295
+// and 259, 32 562 and 842; 64 states batch 1 371 and 128, 8 447 and 573, 32 1160 and 1834;
+// 64 tokens, 16 states, batch 1 23 and 34, 32 28 and 65.  Without: 16 states batch 8 120 and
+// 127, 32 250 and 366, 64 463 and 655; 32 states batch 8 219 and 230.  It errs at 16 states
+// batch 64 and 32 states batch 8 with the states kept, and at 16 batch 8 without (5 to 14%).
 inline bool sel_one_pass(const SelectiveProblem &p)
 {
     struct Cost {

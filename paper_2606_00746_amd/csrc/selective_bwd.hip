@@ -11,7 +11,7 @@
 // and the sums over channels begin inside a lane; these are formed in LDS for several tokens
 // at once, over the channels of a workgroup.  The states come from the forward's reserve for
 // every kSelKeep-th token, and from there again into registers.  8 x 4096 tokens of 1536
-// channels, 16 states, bf16: what chunks pass on 188 us, the gradients 727; these are bound by
+// channels, 16 states, bf16: what chunks pass on 170 us, the gradients 637; these are bound by
 // the vector units, 23 instructions a state and token and 83% of the cycles.
 #include <algorithm>
 
@@ -516,8 +516,8 @@ __global__ __launch_bounds__(16 * kSumRows) void selective_sum_channels_kernel(S
     }
 }
 
-// Waves of the first pass that the chunks are cut for (8 x 4096 tokens of 1536 channels, us,
-// 4096, 6144 and 8192: that pass 189, 183 and 192, the gradients 737, 728 and 748).
+// Waves of the first pass that the chunks are cut for (8 x 4096 tokens of 1536 channels, the
+// whole call, us, 4096, 6144 and 8192: 867, 842 and 883).
 constexpr int64_t kWaves = 6144;
 
 template <typename T, int NP, bool PAD>

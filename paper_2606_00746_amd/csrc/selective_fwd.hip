@@ -4,8 +4,8 @@
 // y = C_t . h need nothing of another lane, and B and C of a token, the same for all
 // channels of a group, are scalars.  A state and token take a product, an exponential, a
 // product, two multiply-adds: bound by the vector units, not by memory (34225 tokens of 2304
-// channels, 16 states, bf16: first pass 249 us, outputs 317, vector units active 88 and 92%
-// of the cycles; their bytes alone would take 125).
+// channels, 16 states, bf16: first pass 225 us, outputs 287, vector units active 88 and 92%
+// of the cycles; their bytes alone would take 113).
 #include <algorithm>
 
 #include "selective_dev.hpp"
@@ -437,7 +437,8 @@ __global__ __launch_bounds__(kBlk) void token_kernel(SelectiveProblem p)
 }
 
 // Waves that the chunks of a call are cut for (us, 4096, 6144, 8192 and 12288: 34225 tokens of
-// 2304 channels 681, 634, 603 and 616; 8 x 4096 of 1536 468, 460, 457 and 446).
+// 2304 channels 619, 561, 543 and 562; 8 x 4096 of 1536 383, 362, 385 and 359; 4 x 8191 of
+// 768, 8 states, fp32, 152, 162, 157 and 169).
 constexpr int64_t kWaves = 8192;
 
 Chunks chunks_of(const SelectiveProblem &p)

@@ -308,9 +308,10 @@ __global__ __launch_bounds__(16 * kSumRows) void conv_dw_kernel(ConvProblem p, c
     }
 }
 
-// Channels of a thread: forward 8 where the taps leave registers for them (8 x 4096 tokens of
-// 1536 channels, bf16, us: 41 and 44 with 4; 32 x 5476 of 1152 176 and 235), backward 4 (97
-// with 8, 75 with 4, for the waves that fewer registers allow).
+// Channels of a thread: forward 8 where the taps leave registers for them (us with 8 and 4, 8 x
+// 4096 tokens of 1536 channels and 32 x 5476 of 1152: bf16 40 and 40, 175 and 169; fp32 92 and
+// 87, 349 and 323: the 8 are not what carries it), backward 4 (for the waves that fewer
+// registers allow: bf16 97 and 75, 329 and 385; fp32 150 and 140, 549 and 652).
 // Tokens of a thread's segment: many, so that few are read twice, but fewer where that
 // leaves the card with few threads.
 constexpr int64_t kFewThreads = 128 * 1024;
