@@ -10,12 +10,14 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgspn.so")
-SOURCES = ["api.cpp", "scan_tiny.hip", "scan_small.hip", "scan_med_64.hip", "scan_med_56.hip",
-           "scan_med_48.hip", "scan_med_40_32_24.hip", "scan_med.hip", "scan_pm.hip",
-           "scan_wide.hip", "scan_norm.hip", "scan_plane.hip", "scan_line.hip", "scan_general.hip", "latent.hip",
+# the longest to compile first
+SOURCES = ["scan_med_40_32_24.hip", "scan_med_64.hip", "scan_plane.hip", "scan_med_56.hip", "scan_med_48.hip",
+           "selective_fwd.hip", "selective_fwd_f32.hip", "selective_bwd.hip",
+           "api.cpp", "scan_tiny.hip", "scan_small.hip", "scan_med.hip", "scan_pm.hip",
+           "scan_wide.hip", "scan_norm.hip", "scan_line.hip", "scan_general.hip", "latent.hip",
            "mixers_api.cpp", "qk_norm.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_bwd_f32.hip", "attn_split.hip",
            "delta_fwd.hip", "delta_bwd.hip", "delta_bf16.hip",
-           "sublayer_api.cpp", "short_conv.hip", "selective_fwd.hip", "selective_bwd.hip", "residual_norm.hip"]
+           "sublayer_api.cpp", "short_conv.hip", "residual_norm.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

@@ -88,6 +88,7 @@ inline hipError_t take_sel_kept(const SelectiveProblem &p, Workspace *rs, void *
 }
 
 hipError_t launch_selective_fwd(const SelectiveProblem &p, hipStream_t s);
+hipError_t launch_selective_fwd_f32(const SelectiveProblem &p, hipStream_t s);   // of launch_selective_fwd
 hipError_t launch_selective_bwd(const SelectiveProblem &p, hipStream_t s);
 
 }  // namespace gspn
