@@ -320,7 +320,7 @@ def residual_norm_fwd(r, f=None, w=None, w_post=None, scale=None, gate=None, eps
     r.  `out`: (y, r_out), where r_out may be r."""
     if stream is not None or _elsewhere(r):
         return _on(residual_norm_fwd, locals(), "r")
-    if f is None and out is not None and out[1] is not None and out[1] is not r:
+    if f is None and out is not None and out[1] is not None and out[1].data_ptr() != r.data_ptr():
         raise ValueError("r_out is r without f (nothing else is written)")
     sizes, like, ptrs = _join_sizes(r, f, None if out is None else out[0], w, w_post, scale, gate)
     _same_gpu(r, like)
@@ -340,7 +340,7 @@ def residual_norm_fwd(r, f=None, w=None, w_post=None, scale=None, gate=None, eps
         r.data_ptr(), _ptr(f), *ptrs, y.data_ptr(), None if f is None else ro.data_ptr(),
         _strides(r, f, y, ro), *sizes, eps, _dtype_code(like), _dtype_code(r),
         _stream_handle(r, None)))
-    return y, r if f is None else ro
+    return y, r if ro is None else ro
 
 
 def residual_norm_bwd(r, f, w, w_post, scale, gate, dy, dr_out=None, eps: float = 1e-6,

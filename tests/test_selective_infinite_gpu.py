@@ -216,3 +216,30 @@ def test_sums_over_channels_of_infinite_states(case, dtype):
             assert torch.equal(up["dB"][i, 0, :, 1:], base["dB"][i, 0, :, 1:]), i
             assert (down["dC"][i, k - 1, :, 0] == INF).all(), i
             assert torch.equal(down["dC"][i, k - 1, :, 1:], base["dC"][i, k - 1, :, 1:]), i
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("name", ["x", "dy"])
+@pytest.mark.parametrize("case", CASES, ids=ids)
+def test_nan_goes_one_way(case, name, dtype):
+    """NaN of an input goes to its own token's outputs and all behind it, of a gradient to those
+    ahead of it, and to nothing on the other side."""
+    torch = require_gpu()
+    t, ln, lens = prepared(case, dtype, 48)
+    base = both(t, ln)
+    for i, k in enumerate(lens):
+        if k > 0:
+            t[name][i, k // 2] = float("nan")
+    got = both(t, ln)
+    for i, k in enumerate(lens):
+        m = k // 2
+        if name == "x":
+            assert torch.equal(got["y"][i, :m], base["y"][i, :m]) and torch.equal(got["dx"][i], base["dx"][i]), i
+            assert torch.equal(got["ddt"][i, :m], base["ddt"][i, :m]) and torch.equal(got["dstate"][i], base["dstate"][i]), i
+            assert got["y"][i, m:k].isnan().all() and (k == 0 or got["end"][i].isnan().all()), i
+        else:
+            assert torch.equal(got["y"][i], base["y"][i]) and torch.equal(got["end"][i], base["end"][i]), i
+            for n in ("dx", "ddt", "dB", "dC", "dz"):
+                assert torch.equal(got[n][i, m + 1:], base[n][i, m + 1:]), (n, i)
+            assert k == 0 or got["dx"][i, :m + 1].isnan().all() and got["dstate"][i].isnan().all(), i
+    past_the_end_is_zero(got, lens)

@@ -33,6 +33,9 @@ def test_a_stream_of_its_own_without_a_sum():
     """Without f the stream is r; another tensor would be left as it is."""
     with pytest.raises(ValueError, match="r_out"):
         gspn.residual_norm_fwd(x, None, v, out=(x.clone(), x.clone()))
+    for same in (x, x.view_as(x), None):
+        with pytest.raises(ValueError, match="on a GPU"):      # which is all that these lack
+            gspn.residual_norm_fwd(x, None, v, out=(x.clone(), same))
 
 
 @pytest.mark.parametrize("call", [lambda s: gspn.short_conv_fwd(x, w, stream=s), lambda s: gspn.short_conv_bwd(*conv, x, stream=s),
